@@ -271,8 +271,141 @@ rudder_status rudder_rmsnorm(const uint16_t* X, int64_t ldx, int M, int N, const
 rudder_status rudder_add(const uint16_t* A, int64_t lda, const uint16_t* B, int64_t ldb, int M, int N, uint16_t* Y, int64_t ldy,
                          void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Attention over a paged key-value cache, and what stands around it.  (The paper keeps attention, position rotation and the
+ * key-value cache in BF16 outside the quantized path -- Appendix "Quantization"; these are this library's own forms of them for
+ * the steps of a few action / proprioceptive tokens next to a cached context.)
+ *
+ * Data that only the device sees (lengths, page ids, slots, positions) is checked by the kernels: a bad value is
+ * skipped, never used as an index, and recorded for rudder_device_status as RUDDER_ERR_ARG with `where` = 911 page id,
+ * 912 length or row range, 913 position, 914 slot, 915 pages or table columns exhausted, 916 slot map full.
+ */
+typedef enum {
+    RUDDER_CACHE_BF16 = 0,
+    RUDDER_CACHE_E4M3 = 1        /* value = code x scale of the head */
+} rudder_cache_format;
+
+/* Keys and values of all requests: n_pages pages of page_size tokens (a power of two, 1..1024), `heads` key-value heads of head_dim
+ * channels (64, 128 or 256), channels contiguous.  The three strides (elements, multiples of 16 bytes, the same for k and v)
+ * put pages, heads and tokens in any order; offsets are 64-bit.  Slot of a token = page id x page_size + place in the page. */
+typedef struct {
+    void* k;                     /* 16-byte aligned */
+    void* v;
+    rudder_cache_format format;
+    int n_pages, page_size, heads, head_dim;
+    int64_t page_stride, head_stride, token_stride;
+    const float* k_scale;        /* [heads] fp32 > 0, E4M3 only; NULL = ones */
+    const float* v_scale;
+} rudder_paged_cache;
+
+/* rudder_page_tables -- page tables and slot maps on the device from the requests' lengths, one launch.
+ * Request b holds old_lens[b] tokens and gets new_lens[b] more; pages(l) = ceil(l / page_size).  Requests take pages from
+ * free_pages in order:  need_b = pages(old + new) - pages(old),  first_b = sum_{i<b} need_i,
+ *     page_table[b][pages(old_b) + j] = free_pages[first_b + j]            for j < need_b
+ * starts[b] = sum_{i<b} new_i (starts[B] = all new tokens); token starts[b] + i has position old_b + i and its slot; the
+ * capacity - starts[B] rows behind the last token get position and slot -1.  used = sum need_b (above n_free: exhausted -- the
+ * tokens without a page get slot -1).  Other table entries are left as they were; calling again with the same inputs writes the same. */
+typedef struct {
+    const int32_t* old_lens;     /* [B] >= 0 */
+    const int32_t* new_lens;     /* [B] >= 0 */
+    int B;                       /* 1..8192 */
+    int page_size;
+    const int32_t* free_pages;   /* [n_free]; may be NULL when n_free is 0 */
+    int n_free;
+    int32_t* page_table;         /* [B, ld_table], in and out */
+    int64_t ld_table;
+    int max_pages;               /* columns, <= ld_table */
+    int64_t* slots;              /* [capacity] out */
+    int32_t* positions;          /* [capacity] out */
+    int capacity;                /* 1..2^30 - 1 */
+    int32_t* starts;             /* [B + 1] out */
+    int32_t* used;               /* [1] out */
+} rudder_page_table_args;
+rudder_status rudder_page_tables(const rudder_page_table_args* args, void* stream);
+
+/* rudder_qk_norm_rope -- RMS norm of every query and key head, rotation by the row's position, keys and values appended to the
+ * cache: one pass over the QKV linear's output.  Per head of D channels: y = (x r) w, r = 1 / sqrt(mean(x^2) + eps); of
+ * its first `rot` channels the pairs (i, i + rot/2) (RUDDER_ROPE_HALF) or (2i, 2i + 1) (RUDDER_ROPE_PAIRS) become
+ * (y_i c - y_j s, y_j c + y_i s), c and s the entry i of row positions[m] of the tables.  Q = bf16 of the result; K likewise, or in
+ * the cache at slots[m] (bf16, or E4M3 of value x (1 / scale), saturating); V = the values unchanged, cache only.
+ * Bit-defined: fp32, every operation rounded once, sums of squares by lanes of 8 channels combined by the exchange l ^ D/16 .. 1.
+ * A row with positions[m] < 0 is padding and left as it was; one with slots[m] < 0 is not appended.  Slots of one call are
+ * distinct (which of two equal ones stays is not defined).  Q may be X itself (same leading dimension) and K the keys' place in X. */
+typedef enum { RUDDER_ROPE_HALF = 0, RUDDER_ROPE_PAIRS = 1 } rudder_rope_style;
+typedef struct {
+    const uint16_t* X;           /* bf16 [M, ldx]: heads x D query, kv_heads x D key, kv_heads x D value channels */
+    int64_t ldx;
+    int M;
+    int heads, kv_heads, head_dim;   /* head_dim 64, 128 or 256; heads up to 1024 */
+    const float* q_weight;       /* [D] fp32, 16-byte aligned, or NULL = ones */
+    const float* k_weight;
+    float eps;                   /* >= 0 */
+    const float* cos;            /* fp32 [n_pos, rot / 2]; not read when rot is 0 */
+    const float* sin;
+    int n_pos, rot;              /* rot a multiple of 16, 0..D */
+    rudder_rope_style style;
+    const int32_t* positions;    /* [M]; may be NULL when rot is 0 */
+    uint16_t* Q;                 /* bf16 [M, ldq] */
+    int64_t ldq;
+    uint16_t* K;                 /* bf16 [M, ldk], or NULL with cache and slots */
+    int64_t ldk;
+    const rudder_paged_cache* cache;
+    const int64_t* slots;        /* [M] */
+} rudder_qk_args;
+rudder_status rudder_qk_norm_rope(const rudder_qk_args* args, void* stream);
+
+/* rudder_attention_paged -- attention of the new tokens of each request over its cached keys and values:
+ *     s_j = scale q . k_j,  O = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m),  lse = m + ln sum_j exp(s_j - m)
+ * over j < kv_lens[b] (the new tokens' own keys included when they have been appended); with `causal` token t of n sees
+ * j <= kv_lens[b] - n + t.  Query head h uses key-value head h / (heads / cache heads).  A row that sees no key gets zeros and
+ * lse = -infinity.  What the cache holds at and behind kv_lens[b] is never used.
+ * Request b has the rows q_starts[b] .. q_starts[b+1] - 1 (at most max_q), or with q_starts NULL the rows b max_q ..
+ * (b + 1) max_q - 1; all other rows of O and lse are left as they were.  O may be Q.
+ * workspace: rudder_attention_workspace_bytes(args) bytes (from heads, max_q and the cache's shape alone), 256-byte
+ * aligned, contents irrelevant; calls that may overlap on the GPU need one each.  Results do not depend on timing. */
+typedef struct {
+    const uint16_t* Q;           /* bf16 [M, ldq], heads x D */
+    int64_t ldq;
+    int M;
+    int heads;                   /* a multiple of cache->heads */
+    const rudder_paged_cache* cache;
+    const int32_t* page_table;   /* [B, ld_table] */
+    int64_t ld_table;
+    int max_pages;               /* columns that may be read; max_pages x page_size < 2^31 - 2^16 */
+    const int32_t* kv_lens;      /* [B] */
+    const int32_t* q_starts;     /* [B + 1] or NULL */
+    int B, max_q;
+    int causal;
+    float scale;
+    uint16_t* O;                 /* bf16 [M, ldo] */
+    int64_t ldo;
+    float* lse;                  /* fp32 [M, heads] or NULL */
+} rudder_attention_args;
+size_t rudder_attention_workspace_bytes(const rudder_attention_args* args);
+rudder_status rudder_attention_paged(const rudder_attention_args* args, void* workspace, size_t workspace_bytes, void* stream);
+
+/* rudder_linear_a16 -- 1 to 16 rows through a packed weight with the activations kept in 16 bits (a step embedding, a
+ * handful of action tokens): Y_mj = bf16( sum_k (x_mk dinv_k) q_jk Delta_W[j, g(k)] + b_j ), one launch, no workspace, any scheme.
+ * The gains of Eq. 8 cancel without an activation quantiser, so there are no segments, steps or tables.  fp32 sums; x dinv
+ * enters the product with 16 significant bits.  Other shape and alignment rules as in rudder_linear. */
+rudder_status rudder_linear_a16(const rudder_weight* w, const uint16_t* X, int64_t ldx, int M, const float* bias, uint16_t* Y, int64_t ldy,
+                                void* stream);
+
+/* rudder_block_cached -- rudder_block_dit with attention over a paged cache in the place of its stand-in:
+ *     h   = x + O( attention( norm and rotation( QKV( rmsnorm(x; norm1_weight) ) ), cache ) )
+ *     out = h + down( gelu( up( rmsnorm(h; norm2_weight) ) ) )
+ * The M rows are the new tokens of attn->B requests; their keys and values are appended to the cache before attention reads it.
+ * Shapes: QKV H -> (heads + 2 kv heads) D, O heads D -> H, up H -> F, down F -> H.  Of `qk` the members X, ldx, M, Q, ldq, K, ldk and of `attn`
+ * Q, ldq, M, O, ldo are supplied by the block; both name the same cache.  attn->lse [M, heads] or NULL.  A row of padding attends to
+ * nothing (its attention output is zero).  Workspace: rudder_block_cached_workspace_bytes(args, attn, M), 256-byte aligned. */
+size_t rudder_block_cached_workspace_bytes(const rudder_block_args* args, const rudder_attention_args* attn, int M);
+rudder_status rudder_block_cached(const rudder_block_args* args, const rudder_block_glue* glue, const rudder_qk_args* qk,
+                                  const rudder_attention_args* attn, int M, const rudder_segments* seg, int step, void* workspace,
+                                  size_t workspace_bytes, void* stream);
+
 /* Reads and clears the device status word (SYNCHRONISES the device).  *last (HOST) receives
- * RUDDER_OK or RUDDER_ERR_TIMEOUT; *where (HOST, may be NULL) a code naming the wait that gave up. */
+ * RUDDER_OK, RUDDER_ERR_TIMEOUT or RUDDER_ERR_ARG (bad device data, see above); *where (HOST, may be NULL) a code
+ * naming the wait that gave up or what was bad. */
 rudder_status rudder_device_status(int* last, int* where);
 
 /* Self-test of the bounded-wait path (no counterpart in the paper): launches ONE warp that waits, for at

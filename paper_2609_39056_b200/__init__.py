@@ -19,6 +19,10 @@ LIB_PATH = _HERE / "librudder.so"
 OK, ERR_ARG, ERR_SHAPE, ERR_ALIGN, ERR_UNSUPPORTED, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT = range(8)
 W4A8_INT, W4A4_INT, W4A4_NVFP4 = 0, 1, 2
 RANGE_PER_TOKEN, RANGE_STATIC = 0, 1
+CACHE_BF16, CACHE_E4M3 = 0, 1
+ROPE_HALF, ROPE_PAIRS = 0, 1
+# second value of rudder_device_status after ERR_ARG: what a kernel found in the caller's device data
+BAD_PAGE, BAD_LENGTH, BAD_POSITION, BAD_SLOT, NO_PAGES, NO_ROOM = range(911, 917)
 SCHEMES = {"w4a8": W4A8_INT, "w4a4": W4A4_INT, "nvfp4": W4A4_NVFP4}
 
 EXPORTED = [
@@ -29,6 +33,8 @@ EXPORTED = [
     "rudder_quantize_activations", "rudder_linear_dump_acc", "rudder_device_status", "rudder_status_string",
     "rudder_gelu", "rudder_selftest_wait_timeout", "rudder_rmsnorm", "rudder_add",
     "rudder_block_dit", "rudder_block_dit_workspace_bytes", "rudder_gelu_quantize_activations",
+    "rudder_page_tables", "rudder_qk_norm_rope", "rudder_attention_workspace_bytes", "rudder_attention_paged", "rudder_linear_a16",
+    "rudder_block_cached_workspace_bytes", "rudder_block_cached",
 ]
 
 
@@ -57,6 +63,34 @@ class _BlockArgs(ctypes.Structure):
     _fields_ = [("w", ctypes.c_void_p * 4), ("tab", ctypes.POINTER(_ScaleTable) * 4), ("bias", ctypes.c_void_p * 4),
                 ("x", ctypes.c_void_p * 4), ("ldx", ctypes.c_int64 * 4), ("y", ctypes.c_void_p * 4),
                 ("ldy", ctypes.c_int64 * 4)]
+
+
+class _PagedCache(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("format", ctypes.c_int), ("n_pages", ctypes.c_int), ("page_size", ctypes.c_int),
+                ("heads", ctypes.c_int), ("head_dim", ctypes.c_int), ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("token_stride", ctypes.c_int64), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
+
+
+class _PageTableArgs(ctypes.Structure):
+    _fields_ = [("old_lens", ctypes.c_void_p), ("new_lens", ctypes.c_void_p), ("B", ctypes.c_int), ("page_size", ctypes.c_int),
+                ("free_pages", ctypes.c_void_p), ("n_free", ctypes.c_int), ("page_table", ctypes.c_void_p), ("ld_table", ctypes.c_int64),
+                ("max_pages", ctypes.c_int), ("slots", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("capacity", ctypes.c_int),
+                ("starts", ctypes.c_void_p), ("used", ctypes.c_void_p)]
+
+
+class _QkArgs(ctypes.Structure):
+    _fields_ = [("X", ctypes.c_void_p), ("ldx", ctypes.c_int64), ("M", ctypes.c_int), ("heads", ctypes.c_int), ("kv_heads", ctypes.c_int),
+                ("head_dim", ctypes.c_int), ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float),
+                ("cos", ctypes.c_void_p), ("sin", ctypes.c_void_p), ("n_pos", ctypes.c_int), ("rot", ctypes.c_int), ("style", ctypes.c_int),
+                ("positions", ctypes.c_void_p), ("Q", ctypes.c_void_p), ("ldq", ctypes.c_int64), ("K", ctypes.c_void_p), ("ldk", ctypes.c_int64),
+                ("cache", ctypes.POINTER(_PagedCache)), ("slots", ctypes.c_void_p)]
+
+
+class _AttentionArgs(ctypes.Structure):
+    _fields_ = [("Q", ctypes.c_void_p), ("ldq", ctypes.c_int64), ("M", ctypes.c_int), ("heads", ctypes.c_int), ("cache", ctypes.POINTER(_PagedCache)),
+                ("page_table", ctypes.c_void_p), ("ld_table", ctypes.c_int64), ("max_pages", ctypes.c_int), ("kv_lens", ctypes.c_void_p),
+                ("q_starts", ctypes.c_void_p), ("B", ctypes.c_int), ("max_q", ctypes.c_int), ("causal", ctypes.c_int), ("scale", ctypes.c_float),
+                ("O", ctypes.c_void_p), ("ldo", ctypes.c_int64), ("lse", ctypes.c_void_p)]
 
 
 _lib = None
@@ -110,6 +144,16 @@ def lib() -> ctypes.CDLL:
         L.rudder_block_dit_workspace_bytes.restype = sz
         L.rudder_block_dit_workspace_bytes.argtypes = [ctypes.POINTER(_BlockArgs), i32]
         L.rudder_block_dit.argtypes = [ctypes.POINTER(_BlockArgs), ctypes.POINTER(_BlockGlue), i32, ctypes.POINTER(_Segments), i32, vp, sz, vp]
+        L.rudder_page_tables.argtypes = [ctypes.POINTER(_PageTableArgs), vp]
+        L.rudder_qk_norm_rope.argtypes = [ctypes.POINTER(_QkArgs), vp]
+        L.rudder_attention_workspace_bytes.restype = sz
+        L.rudder_attention_workspace_bytes.argtypes = [ctypes.POINTER(_AttentionArgs)]
+        L.rudder_attention_paged.argtypes = [ctypes.POINTER(_AttentionArgs), vp, sz, vp]
+        L.rudder_linear_a16.argtypes = [vp, vp, i64, i32, vp, vp, i64, vp]
+        L.rudder_block_cached_workspace_bytes.restype = sz
+        L.rudder_block_cached_workspace_bytes.argtypes = [ctypes.POINTER(_BlockArgs), ctypes.POINTER(_AttentionArgs), i32]
+        L.rudder_block_cached.argtypes = [ctypes.POINTER(_BlockArgs), ctypes.POINTER(_BlockGlue), ctypes.POINTER(_QkArgs), ctypes.POINTER(_AttentionArgs),
+                                          i32, ctypes.POINTER(_Segments), i32, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -411,3 +455,179 @@ def rudder_gelu_quantize_activations(w: Weight, X, seg, step, tab, stream=None):
                                                   ctypes.byref(tab.c), _ptr(codes), _ptr(r), _stream(stream)),
            "rudder_gelu_quantize_activations")
     return codes, r
+
+
+# ---- attention over a paged key-value cache, and what stands around it ------------------------------------------------------
+# The argument objects hold the C structure and the tensors it points to: build one per set of buffers, call it every step.
+
+def _on_one_device(*tensors) -> int:
+    """The CUDA device index that all given tensors share (None entries are skipped)."""
+    devs = {t.device for t in tensors if t is not None}
+    if len(devs) != 1 or next(iter(devs)).type != "cuda":
+        raise RudderError(ERR_ARG, f"tensors on one CUDA device expected, got {sorted(map(str, devs))}")
+    return next(iter(devs)).index
+
+
+def _launch_stream(device: int, stream):
+    """Raw stream to launch on.  Like every call of the library, the buffers' device must be the current one."""
+    if torch.cuda.current_device() != device:
+        raise RudderError(ERR_ARG, f"buffers are on device {device}, device {torch.cuda.current_device()} is current")
+    if stream is not None:
+        return stream.cuda_stream
+    return torch._C._cuda_getCurrentRawStream(device)
+
+
+def _int32(t, shape=None):
+    assert t.dtype == torch.int32 and t.is_contiguous() and (shape is None or tuple(t.shape) == shape)
+
+
+class PagedCache:
+    """Keys and values of all requests: ``k`` and ``v`` [n_pages, heads, page_size, head_dim], bf16 or float8_e4m3fn, any strides with
+    contiguous channels (a [n_pages, page_size, heads, head_dim] buffer is passed as ``.transpose(1, 2)``); ``k_scale`` / ``v_scale``
+    fp32 [heads] for E4M3 (value = code x scale) or None."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, k_scale: torch.Tensor | None = None, v_scale: torch.Tensor | None = None):
+        assert k.dim() == 4 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype and k.stride(3) == 1
+        assert k.dtype in (torch.bfloat16, torch.float8_e4m3fn)
+        for s in (k_scale, v_scale):
+            assert s is None or (s.dtype == torch.float32 and s.is_contiguous() and s.numel() == k.shape[1])
+        self.keep = (k, v, k_scale, v_scale)
+        self.device = _on_one_device(k, v, k_scale, v_scale)
+        self.n_pages, self.heads, self.page_size, self.head_dim = k.shape
+        self.c = _PagedCache(k.data_ptr(), v.data_ptr(), CACHE_BF16 if k.dtype == torch.bfloat16 else CACHE_E4M3, self.n_pages, self.page_size,
+                             self.heads, self.head_dim, k.stride(0), k.stride(1), k.stride(2),
+                             k_scale.data_ptr() if k_scale is not None else None, v_scale.data_ptr() if v_scale is not None else None)
+
+
+class PageTableArgs:
+    """Arguments of rudder_page_tables: int32 device tensors except ``slots`` (int64); ``page_table`` [B, columns] is updated in place."""
+
+    def __init__(self, old_lens, new_lens, free_pages, page_table, page_size: int, slots, positions, starts, used):
+        B = old_lens.numel()
+        _int32(old_lens, (B,)), _int32(new_lens, (B,)), _int32(free_pages), _int32(starts, (B + 1,)), _int32(used, (1,)), _int32(positions)
+        assert page_table.dtype == torch.int32 and page_table.dim() == 2 and page_table.shape[0] == B and page_table.stride(1) == 1
+        assert slots.dtype == torch.int64 and slots.is_contiguous() and slots.numel() == positions.numel()
+        self.keep = (old_lens, new_lens, free_pages, page_table, slots, positions, starts, used)
+        self.device = _on_one_device(*self.keep)
+        self.c = _PageTableArgs(old_lens.data_ptr(), new_lens.data_ptr(), B, int(page_size), free_pages.data_ptr() if free_pages.numel() else None,
+                                free_pages.numel(), page_table.data_ptr(), page_table.stride(0) if B > 1 else max(page_table.stride(0), page_table.shape[1]),
+                                page_table.shape[1], slots.data_ptr(), positions.data_ptr(), positions.numel(), starts.data_ptr(), used.data_ptr())
+        self.ref = ctypes.byref(self.c)
+
+
+def rudder_page_tables(args: PageTableArgs, stream=None):
+    """Page table, slots, positions and starts of a step from the requests' lengths, written into the tensors of ``args``."""
+    _check(lib().rudder_page_tables(args.ref, _launch_stream(args.device, stream)), "rudder_page_tables")
+
+
+def _rows(t: torch.Tensor) -> int:
+    """Leading dimension of a [M, N] view with contiguous channels (one row has none of its own)."""
+    assert t.dim() == 2 and t.stride(1) == 1
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), -(-t.shape[1] // 8) * 8)
+
+
+class QkArgs:
+    """Arguments of rudder_qk_norm_rope.  ``X`` bf16 [M, (heads + 2 kv_heads) head_dim]; ``q_weight`` / ``k_weight`` fp32 [head_dim] or None;
+    ``cos`` / ``sin`` fp32 [n_pos, rot / 2] or None (no rotation); ``positions`` int32 [M] (negative = row of padding); ``Q`` the output
+    [M, heads head_dim]; keys to ``K`` [M, kv_heads head_dim], or keys and values to ``cache`` at ``slots`` int64 [M].
+    For rudder_block_cached pass X = Q = None: the block supplies the rows."""
+
+    def __init__(self, X, heads: int, kv_heads: int, head_dim: int, q_weight, k_weight, eps: float, cos, sin, style: int, positions, Q, K=None,
+                 cache: PagedCache | None = None, slots=None):
+        for w in (q_weight, k_weight):
+            assert w is None or (w.dtype == torch.float32 and w.is_contiguous() and w.numel() == head_dim)
+        assert (cos is None) == (sin is None)
+        rot = 0
+        if cos is not None:
+            assert cos.dtype == sin.dtype == torch.float32 and cos.dim() == 2 and cos.shape == sin.shape and cos.is_contiguous() and sin.is_contiguous()
+            rot = 2 * cos.shape[1]
+        M = X.shape[0] if X is not None else (positions.numel() if positions is not None else slots.numel())
+        if X is not None:
+            assert X.dtype == Q.dtype == torch.bfloat16 and X.shape[1] == (heads + 2 * kv_heads) * head_dim and Q.shape == (M, heads * head_dim)
+        assert K is None or (K.dtype == torch.bfloat16 and K.shape == (M, kv_heads * head_dim))
+        if positions is not None:
+            _int32(positions, (M,))
+        assert slots is None or (slots.dtype == torch.int64 and slots.is_contiguous() and slots.numel() == M)
+        self.keep = (X, q_weight, k_weight, cos, sin, positions, Q, K, slots)
+        self.cache = cache
+        self.device = _on_one_device(*self.keep, *(cache.keep if cache is not None else ()))
+        p = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
+        self.c = _QkArgs(p(X), _rows(X) if X is not None else 0, M, int(heads), int(kv_heads), int(head_dim), p(q_weight), p(k_weight), float(eps),
+                         p(cos), p(sin), cos.shape[0] if cos is not None else 0, rot, int(style), p(positions), p(Q), _rows(Q) if Q is not None else 0,
+                         p(K), _rows(K) if K is not None else 0, ctypes.pointer(cache.c) if cache is not None else None, p(slots))
+        self.ref = ctypes.byref(self.c)
+
+
+def rudder_qk_norm_rope(args: QkArgs, stream=None):
+    """Query / key norm per head, rotation and append to the cache, written into the tensors of ``args``."""
+    _check(lib().rudder_qk_norm_rope(args.ref, _launch_stream(args.device, stream)), "rudder_qk_norm_rope")
+
+
+class AttentionArgs:
+    """Arguments of rudder_attention_paged.  ``Q`` and ``O`` bf16 [M, heads head_dim] (None for rudder_block_cached); ``page_table`` int32
+    [B, columns]; ``kv_lens`` int32 [B]; ``q_starts`` int32 [B + 1] or None (rows b max_q .. of request b); ``lse`` fp32 [M, heads] or None."""
+
+    def __init__(self, Q, heads: int, cache: PagedCache, page_table, kv_lens, scale: float, O, q_starts=None, max_q: int = 1, causal: bool = False, lse=None):
+        B = kv_lens.numel()
+        _int32(kv_lens, (B,))
+        assert page_table.dtype == torch.int32 and page_table.dim() == 2 and page_table.shape[0] == B and page_table.stride(1) == 1
+        if q_starts is not None:
+            _int32(q_starts, (B + 1,))
+        M = 0
+        if Q is not None:
+            M = Q.shape[0]
+            assert Q.dtype == O.dtype == torch.bfloat16 and Q.shape == O.shape == (M, heads * cache.head_dim)
+        assert lse is None or (lse.dtype == torch.float32 and lse.is_contiguous() and lse.dim() == 2 and lse.shape[1] == heads and (Q is None or lse.shape[0] == M))
+        self.keep = (Q, page_table, kv_lens, O, q_starts, lse)
+        self.cache = cache
+        self.device = _on_one_device(*self.keep, *cache.keep)
+        p = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
+        self.c = _AttentionArgs(p(Q), _rows(Q) if Q is not None else 0, M, int(heads), ctypes.pointer(cache.c), page_table.data_ptr(),
+                                page_table.stride(0) if B > 1 else max(page_table.stride(0), page_table.shape[1]), page_table.shape[1], kv_lens.data_ptr(),
+                                p(q_starts), B, int(max_q), int(bool(causal)), float(scale), p(O), _rows(O) if O is not None else 0, p(lse))
+        self.ref = ctypes.byref(self.c)
+
+
+def rudder_attention_workspace_bytes(args: AttentionArgs) -> int:
+    return int(lib().rudder_attention_workspace_bytes(args.ref))
+
+
+def rudder_attention_paged(args: AttentionArgs, workspace: torch.Tensor | None = None, stream=None):
+    """Attention of the new tokens over the cache, written into ``O`` (and ``lse``) of ``args``."""
+    st = _launch_stream(args.device, stream)
+    if workspace is None:
+        workspace = _workspace(rudder_attention_workspace_bytes(args), args.keep[0].device, stream)
+    p = workspace.data_ptr()
+    off = -p % 256
+    _check(lib().rudder_attention_paged(args.ref, p + off, workspace.numel() - off, st), "rudder_attention_paged")
+
+
+def rudder_linear_a16(w: Weight, X: torch.Tensor, bias=None, Y=None, stream=None) -> torch.Tensor:
+    """One to sixteen rows through a packed weight with 16-bit activations (no activation quantisation)."""
+    assert X.is_cuda and X.dtype == torch.bfloat16 and X.dim() == 2 and X.stride(1) == 1 and X.shape[1] == w.K
+    if Y is None:
+        Y = torch.empty((X.shape[0], w.N), dtype=torch.bfloat16, device=X.device)
+    assert Y.dtype == torch.bfloat16 and Y.stride(1) == 1 and Y.shape == (X.shape[0], w.N)
+    assert bias is None or (bias.dtype == torch.float32 and bias.is_contiguous() and bias.numel() == w.N and bias.device == X.device)
+    assert Y.device == X.device
+    _check(lib().rudder_linear_a16(w.handle, X.data_ptr(), _rows(X), X.shape[0], bias.data_ptr() if bias is not None else None, Y.data_ptr(), _rows(Y),
+                                   _launch_stream(X.device.index, stream)), "rudder_linear_a16")
+    return Y
+
+
+def rudder_block_cached_workspace_bytes(args: BlockArgs, attn: AttentionArgs, M: int) -> int:
+    return int(lib().rudder_block_cached_workspace_bytes(ctypes.byref(args.c), attn.ref, int(M)))
+
+
+def rudder_block_cached(args: BlockArgs, norm1_weight: torch.Tensor, norm2_weight: torch.Tensor, eps: float, out: torch.Tensor, qk: QkArgs, attn: AttentionArgs,
+                        M: int, seg: Segments, step: int, workspace: torch.Tensor, stream=None):
+    """rudder_block_dit with attention over the paged cache that ``qk`` and ``attn`` share in the place of its stand-in."""
+    if qk.cache is not attn.cache:
+        raise RudderError(ERR_ARG, "rudder_block_cached: qk and attn name different caches")
+    qk.c.cache = attn.c.cache                        # one structure: the library compares the pointers
+    glue = _BlockGlue(norm1_weight.data_ptr(), norm2_weight.data_ptr(), float(eps), out.data_ptr(), out.stride(0))
+    wp, wb = _aligned(workspace)
+    assert qk.c.M == M and (attn.keep[5] is None or attn.keep[5].shape[0] >= M)
+    _check(lib().rudder_block_cached(ctypes.byref(args.c), ctypes.byref(glue), qk.ref, attn.ref, int(M), ctypes.byref(seg.c), int(step), wp, wb,
+                                     _launch_stream(qk.device, stream)), "rudder_block_cached")
+    return out

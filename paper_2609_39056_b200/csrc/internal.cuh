@@ -164,4 +164,29 @@ cudaError_t launch_gemm_i8_midrows(const GemmI8FewRowsArgs& a, cudaStream_t st);
 // Either of the two: the prologue then writes int8 codes whatever the weight layout.
 inline bool gemm_i8_register_path(int M, int N, int K, int G, bool signmag) { return gemm_i8_fewrows_applies(M, N, K, G) || gemm_i8_midrows_applies(M, N, K, G, signmag); }
 
+// ---- paged key-value cache: page tables, query / key norm with rotation, attention; products of a few rows with 4-bit weights ----
+constexpr int kMaxRequests = 8192;        // requests of one page-table call (their prefix sums sit in shared memory)
+constexpr int kAttnWholeKeys = 512;       // attention: items of at most this many keys are handed out whole, see attention_paged.cu
+
+struct CacheParams;                       // paged.cuh
+struct PageTablesArgs {
+    const int32_t* old_lens; const int32_t* new_lens; int B;
+    const int32_t* free_pages; int n_free;
+    int32_t* table; int64_t ld_table; int max_pages;
+    int page_shift;
+    int64_t* slots; int32_t* positions; int capacity;
+    int32_t* starts; int32_t* used;
+};
+cudaError_t page_tables_init();
+cudaError_t launch_page_tables(const PageTablesArgs& a, int sm_count, cudaStream_t st);
+struct QkArgs;
+cudaError_t launch_qk_norm_rope(const QkArgs& a, int head_dim, bool e4m3, int sm_count, cudaStream_t st);
+struct AttnArgs;
+cudaError_t attention_paged_init();
+size_t attention_workspace_bytes(int max_rows, int head_dim, int sm_count);
+cudaError_t launch_attention_paged(const AttnArgs& a, void* workspace, int sm_count, cudaStream_t st);
+cudaError_t linear_a16_init();
+cudaError_t launch_linear_a16(const rudder_weight* w, const uint16_t* X, int64_t ldx, int M, const float* bias, uint16_t* Y, int64_t ldy, int sm_count,
+                              cudaStream_t st);
+
 }  // namespace rudder

@@ -1,0 +1,329 @@
+// Products of one to sixteen rows with 4-bit weights, activations kept in 16 bits (no activation quantisation):
+//     y_mj = sum_k (x_mk dinv_k) q_jk Delta_W[j, g(k)] + b_j
+// on the packed weights of rudder_pack_weights (D folded in, Eq. 6; gains cancel without a quantiser between them).
+//
+// Bound by the stream of packed weights (K N / 2 bytes) and, at these sizes (1 to 20 MB), as much by latency.  The
+// multiply-adds run on mma.sync.m16n8k16 with the WEIGHTS as the 16-row operand, taken straight from global memory:
+// 16 output channels x 16 input channels per instruction, the token side only 8 columns wide.  On the CUDA cores
+// the same work is a conversion and an FMA per weight and row, 2 x the issue slots that 6.5 TB/s of nibbles leave.
+//
+// Precision: v = x dinv is an fp32 product (24 bits), the MMA takes bf16.  Each row of v therefore enters as TWO columns,
+// hi = bf16(v) and lo = bf16(v - hi): 16 bits of v, an error of 2^-17 of each product, far below the bf16 step of y; 8
+// columns hold 4 rows and the second column costs nothing up to 4 rows.  The weight operand is exact: integers in
+// [-7, 7], or E2M1 x UE4M3 (2 + 4 significant bits).  Products and sums in fp32.
+//
+// Work split: a CTA owns 16 output channels over all of K, its warps take blocks of 64 input channels in turn and
+// their sums are added in warp order (deterministic), no scratch in global memory.  v is computed once per CTA and
+// staged in shared memory in fragment order (persistent CTAs keep it for all their tiles).  The order of the input channels
+// inside a 64-channel block is free as long as both operands use the same one: each is the order in which the packed
+// layout's nibbles come out of a word by one shift and one mask per pair.
+#include "internal.cuh"
+#include "paged.cuh"
+
+#include <cuda_bf16.h>
+
+#include "fp4.cuh"
+
+namespace rudder {
+
+namespace {
+
+enum A16Layout { A16_INT, A16_SIGNMAG, A16_NVFP4 };
+
+struct LinearA16Params {
+    const uint16_t* X; int64_t ldx;
+    uint16_t* Y; int64_t ldy;
+    const uint8_t* codes;
+    const float* scales_t;          // INT: [K/G][N] Delta_W / 16
+    const uint8_t* scales_c;        // NVFP4: UE4M3 [N][K/16]
+    const float* dinv;
+    const float* tensor_scale;
+    const float* bias;
+    int M, N, K, G;
+    int chunk;                      // 64-channel blocks of v in shared memory at once
+};
+
+__device__ __forceinline__ void mma_bf16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t hsub2_bf16(uint32_t a, uint32_t b) {
+    const __nv_bfloat162 r = __hsub2(*reinterpret_cast<__nv_bfloat162*>(&a), *reinterpret_cast<__nv_bfloat162*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t hmul2_bf16(uint32_t a, uint32_t b) {
+    const __nv_bfloat162 r = __hmul2(*reinterpret_cast<__nv_bfloat162*>(&a), *reinterpret_cast<__nv_bfloat162*>(&b));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+// Pair t (0..3) of a packed word as two bf16 weights.
+//   INT: bits 4 t of both halves of the word; 0x4300 | (n ^ 8) is the bf16 number 128 + 8 + code, minus 136 exact.
+//   SIGNMAG: magnitudes at 4 t of both halves, signs at bits 3 + 8 t and 7 + 8 t; 128 + magnitude, minus 128, then the signs.
+//   NVFP4: the three low bits moved to bit 6 are an E2M1 magnitude in bf16's exponent range from 2^-126 on (subnormals
+//   included); `mul` brings it back times the block scale (exact: 6 significant bits).
+template <int LAYOUT>
+__device__ __forceinline__ uint32_t weight_pair(uint32_t w, int t, uint32_t mul) {
+    if (LAYOUT == A16_INT) return hsub2_bf16(((w >> (4 * t)) & 0x000F000Fu) ^ 0x43084308u, 0x43084308u);
+    if (LAYOUT == A16_SIGNMAG) {
+        const uint32_t mag = hsub2_bf16(((w >> (4 * t)) & 0x00070007u) | 0x43004300u, 0x43004300u);
+        const uint32_t lo = (t < 2 ? (w << (12 - 8 * t)) : (w >> (8 * t - 12))) & 0x00008000u;
+        const uint32_t hi = (w << (24 - 8 * t)) & 0x80000000u;
+        return mag | lo | hi;
+    }
+    const uint32_t n = w >> (4 * t);
+    return hmul2_bf16(((n & 0x00070007u) << 6) | ((n & 0x00080008u) << 12), mul);
+}
+// Offsets (inside the lane's channels of a 64-channel block) of the two channels of pair t of word j.
+//   INT: lane q holds channels base .. base + 7 and base + 16 .. base + 23, base = 32 (q >> 1) + 8 (q & 1): byte b of the
+//   run = channels b (low nibble) and 16 + b.  Word j: pair t = nibbles t and t + 4 = bytes t / 2 and t / 2 + 2.
+//   As an index 0..15 into the 8 + 8 channels: 4 j + (t >> 1) + 8 (t & 1) and that + 2.
+//   SIGNMAG: pair t = channels 4 j + t and 16 + 4 j + t -> indices 4 j + t, 8 + 4 j + t.
+//   NVFP4: channels 16 q + 8 j + t and + 4.
+template <int LAYOUT>
+__device__ __forceinline__ constexpr int pair_index(int j, int t, int half) {
+    if (LAYOUT == A16_INT) return 4 * j + (t >> 1) + 8 * (t & 1) + 2 * half;
+    if (LAYOUT == A16_SIGNMAG) return 4 * j + t + 8 * half;
+    return 8 * j + t + 4 * half;
+}
+__device__ __forceinline__ uint2 ldg_weights(const uint8_t* p) {
+    uint2 v;
+    asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
+    return v;
+}
+// The split of two fp32 values: hi and lo as packed bf16 pairs.
+__device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& lo) {
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(hi) : "f"(b), "f"(a));
+    const float ra = __fsub_rn(a, __uint_as_float(hi << 16)), rb = __fsub_rn(b, __uint_as_float(hi & 0xFFFF0000u));
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(lo) : "f"(rb), "f"(ra));
+}
+
+constexpr int kPrefetch = 4;        // 64-channel blocks of weights a warp holds in registers at once
+
+// NT: tiles of 8 columns (4 rows each).  Shared memory: v fragments, one block of 64 channels =
+// [4 steps][NT tiles][8 columns][4 lanes q][8 bytes], padded by 32 bytes so that the blocks start on different banks.
+template <int LAYOUT, int NT, int WARPS>
+__global__ void __launch_bounds__(32 * WARPS) linear_a16_kernel(const LinearA16Params p)
+{
+    constexpr int THREADS = 32 * WARPS;
+    constexpr int kBlockBytes = 4 * NT * 256 + 32;
+    extern __shared__ __align__(16) uint8_t vfrag[];
+    __shared__ float red[WARPS][4 * NT][17];
+    pdl_launch_dependents();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int g = lane >> 2, q = lane & 3;
+    const int n_blocks = p.K >> 6;
+    const int n_tiles = p.N >> 4;
+    const size_t row_bytes = static_cast<size_t>(p.K >> 1);
+    const uint32_t lane_off = (LAYOUT == A16_NVFP4) ? 8u * q : 16u * (q >> 1) + 8u * (q & 1);
+    // UE4M3 scale x 2^117: together with the 2^-126 of the raw codes the weights come out times 2^-9 (448 x 2^117 is in range)
+    const float out_scale = (LAYOUT == A16_NVFP4) ? 512.0f * __ldg(p.tensor_scale) : 16.0f;
+    bool waited = false;
+
+    for (int tile = blockIdx.x; tile < n_tiles; tile += gridDim.x) {
+        const int n0 = tile * 16;
+        const uint8_t* w0 = p.codes + static_cast<size_t>(n0 + g) * row_bytes + lane_off;
+        const uint8_t* w1 = w0 + 8 * row_bytes;
+        float acc[NT][4];
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[t][0] = acc[t][1] = acc[t][2] = acc[t][3] = 0.0f;
+
+        for (int c0 = 0; c0 < n_blocks; c0 += p.chunk) {
+            const int c1 = min(n_blocks, c0 + p.chunk);
+            // first weights of this chunk: requested before v is staged (and before waiting for the kernel before this one)
+            uint2 wa[kPrefetch], wb[kPrefetch];
+            float sa[kPrefetch], sb[kPrefetch];
+            auto fetch = [&](int first) {
+#pragma unroll
+                for (int i = 0; i < kPrefetch; ++i) {
+                    const int blk = min(first + i * WARPS, n_blocks - 1);       // past the end: a valid address, never used
+                    wa[i] = ldg_weights(w0 + 32 * blk);
+                    wb[i] = ldg_weights(w1 + 32 * blk);
+                    if (LAYOUT == A16_NVFP4) {
+                        const uint8_t* sp = p.scales_c + static_cast<size_t>(n0 + g) * (p.K >> 4) + 4 * blk + q;
+                        sa[i] = __uint_as_float(__ldg(sp));
+                        sb[i] = __uint_as_float(__ldg(sp + 8 * static_cast<size_t>(p.K >> 4)));
+                    } else {
+                        const float* sp = p.scales_t + static_cast<size_t>((blk << 6) / p.G) * p.N + n0 + g;
+                        sa[i] = __ldg(sp);
+                        sb[i] = __ldg(sp + 8);
+                    }
+                }
+            };
+            fetch(c0 + warp);
+            if (!waited) { pdl_wait(); waited = true; }
+            if (p.chunk < n_blocks || tile == static_cast<int>(blockIdx.x)) {
+                // v of this chunk: item = (row, block, lane q): 16 channels -> 4 steps x (hi, lo) x 8 bytes
+                __syncthreads();                                                // readers of the chunk before
+                const int per_row = 4 * (c1 - c0);
+                for (int it = tid; it < p.M * per_row; it += THREADS) {
+                    const int m = it / per_row, r = it - m * per_row;
+                    const int blk = r >> 2, qq = r & 3;
+                    const int ch = 64 * (c0 + blk) + (LAYOUT == A16_NVFP4 ? 16 * qq : 32 * (qq >> 1) + 8 * (qq & 1));
+                    const int second = (LAYOUT == A16_NVFP4) ? 8 : 16;
+                    float v[16];
+#pragma unroll
+                    for (int hh = 0; hh < 2; ++hh) {
+                        const uint4 x4 = *reinterpret_cast<const uint4*>(p.X + static_cast<size_t>(m) * p.ldx + ch + hh * second);
+                        const float4 d0 = __ldg(reinterpret_cast<const float4*>(p.dinv + ch + hh * second));
+                        const float4 d1 = __ldg(reinterpret_cast<const float4*>(p.dinv + ch + hh * second) + 1);
+                        const uint32_t xw[4] = {x4.x, x4.y, x4.z, x4.w};
+                        const float dd[8] = {d0.x, d0.y, d0.z, d0.w, d1.x, d1.y, d1.z, d1.w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            v[8 * hh + 2 * i] = __fmul_rn(__uint_as_float(xw[i] << 16), dd[2 * i]);
+                            v[8 * hh + 2 * i + 1] = __fmul_rn(__uint_as_float(xw[i] & 0xFFFF0000u), dd[2 * i + 1]);
+                        }
+                    }
+                    uint8_t* dst = vfrag + static_cast<size_t>(blk) * kBlockBytes + (m >> 2) * 256 + 2 * (m & 3) * 32 + qq * 8;
+#pragma unroll
+                    for (int st = 0; st < 4; ++st) {                            // step st = pairs 2 (st & 1), + 1 of word st >> 1
+                        uint2 hi, lo;
+                        split2(v[pair_index<LAYOUT>(st >> 1, 2 * (st & 1), 0)], v[pair_index<LAYOUT>(st >> 1, 2 * (st & 1), 1)], hi.x, lo.x);
+                        split2(v[pair_index<LAYOUT>(st >> 1, 2 * (st & 1) + 1, 0)], v[pair_index<LAYOUT>(st >> 1, 2 * (st & 1) + 1, 1)], hi.y, lo.y);
+                        *reinterpret_cast<uint2*>(dst + st * NT * 256) = hi;
+                        *reinterpret_cast<uint2*>(dst + st * NT * 256 + 32) = lo;
+                    }
+                }
+                __syncthreads();
+            }
+            for (int first = c0 + warp; first < c1; first += kPrefetch * WARPS) {
+                if (first != c0 + warp) fetch(first);
+#pragma unroll
+                for (int i = 0; i < kPrefetch; ++i) {
+                    const int blk = first + i * WARPS;
+                    if (blk < c1) {
+                        uint32_t ma = 0, mb = 0;
+                        if (LAYOUT == A16_NVFP4) {
+                            const float fa = ue4m3_to_f32(__float_as_uint(sa[i])) * 0x1p117f, fb = ue4m3_to_f32(__float_as_uint(sb[i])) * 0x1p117f;
+                            ma = __float_as_uint(fa) >> 16; ma |= ma << 16;      // 4 significant bits: exact in bf16
+                            mb = __float_as_uint(fb) >> 16; mb |= mb << 16;
+                        }
+                        float c[NT][4];
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) c[t][0] = c[t][1] = c[t][2] = c[t][3] = 0.0f;
+                        const uint8_t* vb = vfrag + static_cast<size_t>(blk - c0) * kBlockBytes + lane * 8;
+#pragma unroll
+                        for (int st = 0; st < 4; ++st) {
+                            const uint32_t wx = st < 2 ? wa[i].x : wa[i].y, wy = st < 2 ? wb[i].x : wb[i].y;
+                            const int t0 = 2 * (st & 1);
+                            const uint32_t a0 = weight_pair<LAYOUT>(wx, t0, ma), a2 = weight_pair<LAYOUT>(wx, t0 + 1, ma);
+                            const uint32_t a1 = weight_pair<LAYOUT>(wy, t0, mb), a3 = weight_pair<LAYOUT>(wy, t0 + 1, mb);
+#pragma unroll
+                            for (int t = 0; t < NT; ++t) {
+                                const uint2 b = *reinterpret_cast<const uint2*>(vb + (st * NT + t) * 256);
+                                mma_bf16(c[t], a0, a1, a2, a3, b.x, b.y);
+                            }
+                        }
+                        const float ga = (LAYOUT == A16_NVFP4) ? 1.0f : sa[i], gb = (LAYOUT == A16_NVFP4) ? 1.0f : sb[i];
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) {
+                            acc[t][0] = fmaf(c[t][0], ga, acc[t][0]);
+                            acc[t][1] = fmaf(c[t][1], ga, acc[t][1]);
+                            acc[t][2] = fmaf(c[t][2], gb, acc[t][2]);
+                            acc[t][3] = fmaf(c[t][3], gb, acc[t][3]);
+                        }
+                    }
+                }
+            }
+        }
+        // hi and lo of row 4 t + q are the two columns this lane holds; the warps' sums in warp order
+        __syncthreads();                                                        // readers of `red` of the tile before
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            red[warp][4 * t + q][g] = acc[t][0] + acc[t][1];
+            red[warp][4 * t + q][g + 8] = acc[t][2] + acc[t][3];
+        }
+        __syncthreads();
+        for (int o = tid; o < 16 * p.M; o += THREADS) {
+            const int m = o >> 4, n = o & 15;
+            float sum = 0.0f;
+#pragma unroll
+            for (int w = 0; w < WARPS; ++w) sum += red[w][m][n];
+            const float b = p.bias != nullptr ? __ldg(p.bias + n0 + n) : 0.0f;
+            p.Y[static_cast<size_t>(m) * p.ldy + n0 + n] = __bfloat16_as_ushort(__float2bfloat16_rn(fmaf(sum, out_scale, b)));
+        }
+    }
+}
+
+constexpr int kMaxSmem = 200 * 1024;
+
+template <int LAYOUT, int NT, int WARPS>
+cudaError_t launch_one(LinearA16Params p, int sm_count, cudaStream_t st)
+{
+    constexpr int kBlockBytes = 4 * NT * 256 + 32;
+    const int n_blocks = p.K >> 6;
+    // all of v when it fits, else equal chunks
+    int chunk = kMaxSmem / kBlockBytes;
+    if (n_blocks <= chunk) chunk = n_blocks;
+    else chunk = (n_blocks + (n_blocks + chunk - 1) / chunk - 1) / ((n_blocks + chunk - 1) / chunk);
+    p.chunk = chunk;
+    const int smem = chunk * kBlockBytes;
+    int per_sm = 220 * 1024 / (smem + WARPS * 4 * NT * 17 * 4 + 1024);
+    const int by_threads = 2048 / (32 * WARPS) / 2;                               // half of the register file's threads at 64 registers each
+    if (per_sm > by_threads) per_sm = by_threads;
+    if (per_sm < 1) per_sm = 1;
+    const int tiles = p.N >> 4;
+    int blocks = tiles < sm_count * per_sm ? tiles : sm_count * per_sm;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(blocks), 1, 1);
+    cfg.blockDim = dim3(32 * WARPS, 1, 1);
+    cfg.dynamicSmemBytes = static_cast<size_t>(smem);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, linear_a16_kernel<LAYOUT, NT, WARPS>, p);
+}
+template <int LAYOUT, int NT>
+cudaError_t launch_warps(const LinearA16Params& p, int sm_count, cudaStream_t st)
+{
+    return p.K >= 4096 ? launch_one<LAYOUT, NT, 16>(p, sm_count, st) : launch_one<LAYOUT, NT, 8>(p, sm_count, st);
+}
+template <int LAYOUT>
+cudaError_t launch_layout(const LinearA16Params& p, int sm_count, cudaStream_t st)
+{
+    if (p.M <= 4) return launch_warps<LAYOUT, 1>(p, sm_count, st);
+    if (p.M <= 8) return launch_warps<LAYOUT, 2>(p, sm_count, st);
+    return launch_warps<LAYOUT, 4>(p, sm_count, st);
+}
+template <int LAYOUT, int NT>
+cudaError_t init_one()
+{
+    cudaError_t e = cudaFuncSetAttribute(linear_a16_kernel<LAYOUT, NT, 8>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
+    if (e != cudaSuccess) return e;
+    return cudaFuncSetAttribute(linear_a16_kernel<LAYOUT, NT, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
+}
+template <int LAYOUT>
+cudaError_t init_layout()
+{
+    cudaError_t e = init_one<LAYOUT, 1>();
+    if (e == cudaSuccess) e = init_one<LAYOUT, 2>();
+    if (e == cudaSuccess) e = init_one<LAYOUT, 4>();
+    return e;
+}
+
+}  // namespace
+
+cudaError_t linear_a16_init()
+{
+    cudaError_t e = init_layout<A16_INT>();
+    if (e == cudaSuccess) e = init_layout<A16_SIGNMAG>();
+    if (e == cudaSuccess) e = init_layout<A16_NVFP4>();
+    return e;
+}
+
+cudaError_t launch_linear_a16(const rudder_weight* w, const uint16_t* X, int64_t ldx, int M, const float* bias, uint16_t* Y, int64_t ldy, int sm_count,
+                              cudaStream_t st)
+{
+    LinearA16Params p;
+    p.X = X; p.ldx = ldx; p.Y = Y; p.ldy = ldy;
+    p.codes = w->codes; p.scales_t = w->scales_t; p.scales_c = static_cast<const uint8_t*>(w->scales_c);
+    p.dinv = w->dinv; p.tensor_scale = w->tensor_scale; p.bias = bias;
+    p.M = M; p.N = w->N; p.K = w->K; p.G = w->G; p.chunk = 0;
+    if (w->scheme == RUDDER_W4A4_NVFP4) return launch_layout<A16_NVFP4>(p, sm_count, st);
+    return w->f8 ? launch_layout<A16_SIGNMAG>(p, sm_count, st) : launch_layout<A16_INT>(p, sm_count, st);
+}
+
+}  // namespace rudder
