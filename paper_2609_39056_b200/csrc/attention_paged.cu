@@ -71,11 +71,17 @@ __device__ __forceinline__ void ldsm_x4_t(uint32_t (&r)[4], uint32_t addr) {
 template <bool F16>
 __device__ __forceinline__ void mma16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
     if (F16)
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
     else
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// An 8 x 8 block of 16-bit numbers, a row per 4 lanes: transposed.
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
 }
 __device__ __forceinline__ float exp2_approx(float x) {
     float y;
@@ -122,10 +128,18 @@ __device__ __forceinline__ Req load_request(const AttnParams& p, int b) {
     return r;
 }
 
-// A place in the sequence of units: request, kv head, row tile, unit inside the item.
+// A place in the sequence of units: request, kv head, row tile, unit inside the item, and what is left of the run from there on.
+// What starting and ending an item costs, in units (queries, merge of the warp groups, output): an item counts as its units + kItemCost,
+// the cost in front.  A cut inside the cost leaves the item whole to the run behind.
+#ifndef ITEM_COST
+#define ITEM_COST 3
+#endif
+constexpr int kItemCost = ITEM_COST;
+
 template <int ROWS, int UK>
 struct Cursor {
     int b, h, rt, j, nt, n_rt;
+    long long left;
     Req rq;
     __device__ __forceinline__ void set_request(const AttnParams& p, int bb) {
         b = bb;
@@ -147,7 +161,10 @@ struct Cursor {
         }
     }
     __device__ __forceinline__ void advance(const AttnParams& p) {
-        if (++j == nt) next_item(p);
+        ++j;
+        if (--left <= 0 || j < nt) return;
+        left -= kItemCost;
+        if (left > 0) next_item(p);
     }
 };
 
@@ -157,31 +174,43 @@ __device__ __forceinline__ uint32_t swz(int r, int c) {
     return static_cast<uint32_t>(r) * RB + (static_cast<uint32_t>(RB >= 128 ? (c ^ (r & 7)) : (c ^ ((r >> 1) & 3))) << 4);
 }
 
-// PL: 0 = probabilities once (f16, or bf16), 1 = at most 8 rows: the low parts ride in the unused rows 8..15 of the product (free),
-// 2 = hi and lo as two products.
-template <int D_, bool E4M3_, int RW_, int KW_, int KT_, int NST_, int PL_>
+// LO: 0 = probabilities once (f16, or bf16), 1 = at most 4 rows: columns 4..7 repeat the queries of 0..3 and carry the
+// low parts of the probabilities (free), 2 = hi and lo as two products.
+template <int D_, bool E4M3_, int NB_, int RW_, int KW_, int KT_, int NST_, int LO_>
 struct AttnCfg {
-    static constexpr int D = D_, RW = RW_, KW = KW_, KT = KT_, NST = NST_, PL = PL_;
+    static constexpr int D = D_, NB = NB_, RW = RW_, KW = KW_, KT = KT_, NST = NST_, LO = LO_;
     static constexpr bool E4M3 = E4M3_;
     static constexpr int THREADS = 32 * RW * KW;
-    static constexpr int ROWS = 16 * RW;
+    static constexpr int ROWS = 8 * NB * RW;               // rows of a tile
     static constexpr int UK = KW * KT;                     // keys of a unit
     static constexpr int RB = D * (E4M3 ? 1 : 2);          // bytes of a row of a tile
     static constexpr int STAGE = 2 * KT * RB;              // K tile, V tile
     static constexpr int RING = KW * NST * STAGE;
-    static constexpr int MERGE = (KW / 2) * RW * 32 * (D / 8) * 16 + (KW / 2) * RW * 32 * 16;
-    static constexpr int SMEM = RING + MERGE;
+    // the box in which the warp groups' outputs are added, [KW][ROWS][channels of a round + 4]: as many rounds as make it fit behind the ring
+    static constexpr int ML = KW * ROWS * 8;
+    static constexpr int box_bytes(int rounds) { return KW * ROWS * (D / rounds + 4) * 4; }
+    static constexpr int rounds() {
+        int r = 1;
+        while (r < D / 32 && (RING + ML + box_bytes(r) > 226 * 1024 || box_bytes(r) > 36 * 1024)) r *= 2;
+        return r;
+    }
+    static constexpr int ROUNDS = rounds();
+    static constexpr int DC = D / ROUNDS;
+    static constexpr int BOX = box_bytes(ROUNDS);
+    static constexpr int SMEM = RING + BOX + ML;
+    static_assert(DC % 16 == 0 && DC >= 32, "a round is whole channel tiles");
+    static_assert(SMEM <= 226 * 1024, "shared memory of an SM");
 };
 
 template <class C>
 __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const AttnParams p)
 {
-    constexpr int D = C::D, RW = C::RW, KW = C::KW, KT = C::KT, NST = C::NST, PL = C::PL, RB = C::RB, UK = C::UK, ROWS = C::ROWS;
+    constexpr int D = C::D, NB = C::NB, RW = C::RW, KW = C::KW, KT = C::KT, NST = C::NST, LO = C::LO, RB = C::RB, UK = C::UK, ROWS = C::ROWS, DC = C::DC;
     constexpr bool E4M3 = C::E4M3;
     constexpr int CH = RB / 16;                            // 16-byte chunks of a row
     constexpr int KS = D / 16;                             // steps of the first product
-    constexpr int NT = KT / 8;                             // key tiles of the first product
-    constexpr int DT = D / 8;                              // channel tiles of the second
+    constexpr int MT = KT / 16;                            // key tiles of the first product
+    constexpr int DT = D / 16;                             // channel tiles of the second
     constexpr int GT = 32 * RW;                            // threads of a warp group
     static_assert(KT == 16 || KT == 32, "a lane holds the place of one key of the tile");
     static_assert(GT % CH == 0 || CH % GT == 0, "rows are copied by whole groups of lanes");
@@ -206,7 +235,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
     for (int b = rb0; b < rb1; ++b) {
         const Req r = load_request(p, b);
         const int n_rt = (r.qlen * p.group + ROWS - 1) / ROWS, nt = max(1, (r.len + UK - 1) / UK);
-        t_units += static_cast<long long>(n_rt) * p.kv_heads * nt;
+        t_units += static_cast<long long>(n_rt) * p.kv_heads * (nt + kItemCost);
         t_items += n_rt * p.kv_heads;
         if (n_rt > 0) t_max = max(t_max, nt);
     }
@@ -243,7 +272,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
             long long at = mine0;
             for (int b = rb0; b < rb1; ++b) {
                 const Req r = load_request(p, b);
-                const int n_rt = (r.qlen * p.group + ROWS - 1) / ROWS, nt = whole ? 1 : max(1, (r.len + UK - 1) / UK);
+                const int n_rt = (r.qlen * p.group + ROWS - 1) / ROWS, nt = whole ? 1 : max(1, (r.len + UK - 1) / UK) + kItemCost;
                 const long long here = static_cast<long long>(n_rt) * p.kv_heads * nt;
                 if (u_begin < at + here) {
                     const long long off = u_begin - at;
@@ -251,7 +280,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
                     s_place[0] = b;
                     s_place[1] = item / n_rt;
                     s_place[2] = item % n_rt;
-                    s_place[3] = static_cast<int>(off % nt);
+                    s_place[3] = static_cast<int>(off % nt);      // place inside the item, its cost included
                     break;
                 }
                 at += here;
@@ -261,16 +290,23 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
     __syncthreads();
     Cursor<ROWS, UK> cur;
     cur.set_request(p, s_place[0]);
-    cur.h = s_place[1]; cur.rt = s_place[2]; cur.j = s_place[3];
-    const int n_units = whole ? cur.nt : static_cast<int>(u_end - u_begin);
+    cur.h = s_place[1]; cur.rt = s_place[2];
+    const int place = whole ? kItemCost : s_place[3];
+    cur.j = max(0, place - kItemCost);
+    cur.left = whole ? cur.nt : (u_end - u_begin) - max(0, kItemCost - place);      // of this run, from unit cur.j on
+    if (cur.left <= 0) {                                       // nothing but a part of an item's cost
+        if (tid == 0) p.desc[8 * blockIdx.x] = 0;
+        return;
+    }
     if (tid == 0) {
         // the join of the item that this run starts inside belongs to its first cut, i.e. to the run behind its first owner
         int* d = p.desc + 8 * blockIdx.x;
-        const long long item0 = u_begin - cur.j;
-        const bool first_cut = !whole && cur.j > 0 && item0 >= share * (static_cast<long long>(blockIdx.x) - 1);
+        const long long unit0 = u_begin - cur.j;           // place of the item's first unit
+        const long long before = share * (static_cast<long long>(blockIdx.x) - 1);
+        const bool first_cut = !whole && cur.j > 0 && unit0 >= before;
         d[1] = cur.h; d[2] = cur.rt; d[3] = cur.rq.row0; d[4] = cur.rq.qlen;
-        d[5] = static_cast<int>((item0 + cur.nt - 1) / share);                   // last owner
-        d[6] = item0 == share * (static_cast<long long>(blockIdx.x) - 1) ? 0 : 1;   // slot of the first owner's part
+        d[5] = static_cast<int>((unit0 + cur.nt - 1) / share);                   // last owner
+        d[6] = unit0 <= before + kItemCost ? 0 : 1;        // slot of the first owner's part: its run starts with this item (or inside its cost)
         d[0] = first_cut ? 1 : 0;
     }
 
@@ -304,301 +340,322 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
     };
 #pragma unroll
     for (int s = 0; s < NST - 1; ++s) {
-        if (s < n_units) {
+        if (ld.left > 0) {
             issue(ld, page_of_lane(ld), s);
             ld.advance(p);
         }
         cp_async_commit();
     }
 
-    uint32_t qf[KS][4];
-    float acc[DT][4];
-    float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.0f, l1 = 0.0f;
-    float f0 = p.scale_log2, f1 = p.scale_log2;            // score factors of rows g and g + 8
-    int lim0 = 0, lim1 = 0;                                // keys that rows g and g + 8 see
-    bool fresh = true;
+    uint32_t qf[KS][NB][2];
+    float acc[DT][NB][4];                                  // output, transposed: channels on the 16-row side, rows on the 8 columns
+    float mx[NB][2], sum[NB][2], fac[NB][2];               // of rows 2 q and 2 q + 1 of every 8: running maximum and sum, score factor
+    int lim[NB][2];                                        // keys the rows see
+    int lim_min = 0;
+    bool fresh = true, first_part = true;
+    int part_j = 0;                                        // the unit of the item this run starts it with
+    int stage = 0;
 
-    for (int i = 0; i < n_units; ++i) {
-        const int stage = i % NST;
+    while (cur.left > 0) {
         if (fresh) {
             // ---- a new item (or the rest of one): queries, limits, empty sums
             fresh = false;
+            part_j = cur.j;
 #pragma unroll
-            for (int t = 0; t < DT; ++t) acc[t][0] = acc[t][1] = acc[t][2] = acc[t][3] = 0.0f;
-            m0 = m1 = -INFINITY;
-            l0 = l1 = 0.0f;
-            const int R = cur.rq.qlen * p.group;
-            const int r0 = cur.rt * ROWS + rw * 16 + g, r1 = r0 + 8;
-            const uint16_t* q0 = p.Q;
-            const uint16_t* q1 = p.Q;
-            lim0 = lim1 = cur.rq.len;                      // rows that do not exist: zeros, no limit of their own
-            if (r0 < R) {
-                const int t = r0 / p.group, hh = cur.h * p.group + r0 % p.group;
-                q0 = p.Q + static_cast<size_t>(cur.rq.row0 + t) * p.ldq + static_cast<size_t>(hh) * D;
-                if (p.causal) lim0 = cur.rq.len - cur.rq.qlen + t + 1;
-            }
-            if (r1 < R) {
-                const int t = r1 / p.group, hh = cur.h * p.group + r1 % p.group;
-                q1 = p.Q + static_cast<size_t>(cur.rq.row0 + t) * p.ldq + static_cast<size_t>(hh) * D;
-                if (p.causal) lim1 = cur.rq.len - cur.rq.qlen + t + 1;
-            }
-            if (!E4M3) {
+            for (int t = 0; t < DT; ++t)
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    qf[ks][0] = r0 < R ? *reinterpret_cast<const uint32_t*>(q0 + 16 * ks + 2 * q) : 0u;
-                    qf[ks][1] = r1 < R ? *reinterpret_cast<const uint32_t*>(q1 + 16 * ks + 2 * q) : 0u;
-                    qf[ks][2] = r0 < R ? *reinterpret_cast<const uint32_t*>(q0 + 16 * ks + 2 * q + 8) : 0u;
-                    qf[ks][3] = r1 < R ? *reinterpret_cast<const uint32_t*>(q1 + 16 * ks + 2 * q + 8) : 0u;
+                for (int n = 0; n < NB; ++n) acc[t][n][0] = acc[t][n][1] = acc[t][n][2] = acc[t][n][3] = 0.0f;
+            const int R = cur.rq.qlen * p.group, first_row = cur.rt * ROWS + rw * 8 * NB;
+            lim_min = cur.rq.len;
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+                mx[n][0] = mx[n][1] = -INFINITY;
+                sum[n][0] = sum[n][1] = 0.0f;
+                // rows that do not exist: zeros, no limit of their own
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int r = first_row + 8 * n + (LO == 1 ? (2 * q + e) & 3 : 2 * q + e);
+                    lim[n][e] = (p.causal && r < R) ? cur.rq.len - cur.rq.qlen + r / p.group + 1 : cur.rq.len;
+                    lim_min = min(lim_min, lim[n][e]);
+                    fac[n][e] = p.scale_log2;
                 }
-            } else {
-                // channels 4 q .. 4 q + 3 of every 16 (the K bytes of a lane): pairs (0, 2) and (1, 3); f16 times a power of two per row
-                float x0 = 0.0f, x1 = 0.0f;
+                const int r = first_row + 8 * n + (LO == 1 ? g & 3 : g);
+                const bool live = r < R;
+                const uint16_t* qr = p.Q;
+                if (live) qr += static_cast<size_t>(cur.rq.row0 + r / p.group) * p.ldq + static_cast<size_t>(cur.h * p.group + r % p.group) * D;
+                if (!E4M3) {
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    const uint2 a = r0 < R ? *reinterpret_cast<const uint2*>(q0 + 16 * ks + 4 * q) : make_uint2(0, 0);
-                    const uint2 b = r1 < R ? *reinterpret_cast<const uint2*>(q1 + 16 * ks + 4 * q) : make_uint2(0, 0);
-                    qf[ks][0] = a.x; qf[ks][2] = a.y; qf[ks][1] = b.x; qf[ks][3] = b.y;
-                    x0 = fmaxf(x0, fmaxf(fmaxf(fabsf(bf16_lo(a.x)), fabsf(bf16_hi(a.x))), fmaxf(fabsf(bf16_lo(a.y)), fabsf(bf16_hi(a.y)))));
-                    x1 = fmaxf(x1, fmaxf(fmaxf(fabsf(bf16_lo(b.x)), fabsf(bf16_hi(b.x))), fmaxf(fabsf(bf16_lo(b.y)), fabsf(bf16_hi(b.y)))));
-                }
+                    for (int ks = 0; ks < KS; ++ks) {
+                        qf[ks][n][0] = live ? *reinterpret_cast<const uint32_t*>(qr + 16 * ks + 2 * q) : 0u;
+                        qf[ks][n][1] = live ? *reinterpret_cast<const uint32_t*>(qr + 16 * ks + 2 * q + 8) : 0u;
+                    }
+                } else {
+                    // channels 4 q .. 4 q + 3 of every 16 (the K bytes of a lane): pairs (0, 2) and (1, 3); f16 times a power of two per row
+                    float x = 0.0f;
 #pragma unroll
-                for (int o = 1; o < 4; o <<= 1) {
-                    x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, o));
-                    x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, o));
-                }
-                // the row's largest magnitude lands in [2^14, 2^15); exponent fields outside bf16's normal range give factors of 2^+-126
-                const int e0 = min(126, max(-126, 14 - (static_cast<int>((__float_as_uint(x0) >> 23) & 255u) - 127)));
-                const int e1 = min(126, max(-126, 14 - (static_cast<int>((__float_as_uint(x1) >> 23) & 255u) - 127)));
-                const float s0 = __uint_as_float(static_cast<uint32_t>(e0 + 127) << 23), s1 = __uint_as_float(static_cast<uint32_t>(e1 + 127) << 23);
+                    for (int ks = 0; ks < KS; ++ks) {
+                        const uint2 a = live ? *reinterpret_cast<const uint2*>(qr + 16 * ks + 4 * q) : make_uint2(0, 0);
+                        qf[ks][n][0] = a.x; qf[ks][n][1] = a.y;
+                        x = fmaxf(x, fmaxf(fmaxf(fabsf(bf16_lo(a.x)), fabsf(bf16_hi(a.x))), fmaxf(fabsf(bf16_lo(a.y)), fabsf(bf16_hi(a.y)))));
+                    }
+                    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
+                    x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
+                    // the row's largest magnitude lands in [2^14, 2^15), as far as a factor of 2^+-126 brings it
+                    const int ex = min(126, max(-126, 14 - (static_cast<int>((__float_as_uint(x) >> 23) & 255u) - 127)));
+                    const float sc = __uint_as_float(static_cast<uint32_t>(ex + 127) << 23);
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
-                    const uint32_t ax = qf[ks][0], ay = qf[ks][2], bx = qf[ks][1], by = qf[ks][3];
-                    qf[ks][0] = f16x2(bf16_lo(ax) * s0, bf16_lo(ay) * s0);
-                    qf[ks][2] = f16x2(bf16_hi(ax) * s0, bf16_hi(ay) * s0);
-                    qf[ks][1] = f16x2(bf16_lo(bx) * s1, bf16_lo(by) * s1);
-                    qf[ks][3] = f16x2(bf16_hi(bx) * s1, bf16_hi(by) * s1);
+                    for (int ks = 0; ks < KS; ++ks) {
+                        const uint32_t ax = qf[ks][n][0], ay = qf[ks][n][1];
+                        qf[ks][n][0] = f16x2(bf16_lo(ax) * sc, bf16_lo(ay) * sc);
+                        qf[ks][n][1] = f16x2(bf16_hi(ax) * sc, bf16_hi(ay) * sc);
+                    }
+                    const float back = (p.cache.k_scale != nullptr ? __ldg(p.cache.k_scale + cur.h) : 1.0f) * 256.0f * p.scale_log2 *
+                                       __uint_as_float(static_cast<uint32_t>(127 - ex) << 23);
+                    fac[n][0] = __shfl_sync(0xffffffffu, back, 8 * q);         // row 2 q of the tile is lane g = 2 q
+                    fac[n][1] = __shfl_sync(0xffffffffu, back, 8 * q + 4);
                 }
-                const float ksc = (p.cache.k_scale != nullptr ? __ldg(p.cache.k_scale + cur.h) : 1.0f) * 256.0f * p.scale_log2;
-                f0 = ksc * __uint_as_float(static_cast<uint32_t>(127 - e0) << 23);
-                f1 = ksc * __uint_as_float(static_cast<uint32_t>(127 - e1) << 23);
             }
         }
         cp_async_wait<NST - 2>();
         if (RW == 1) __syncwarp();
         else asm volatile("bar.sync %0, %1;" ::"r"(1 + kg), "n"(GT) : "memory");
         // page ids of the tile that goes into the stage just freed: requested now, used after this tile's products
-        const bool more = i + NST - 1 < n_units;
+        const bool more = ld.left > 0;
         const int page = more ? page_of_lane(ld) : -2;
 
         const int key0 = cur.j * UK + kg * KT;
         if (key0 < cur.rq.len) {
             const uint32_t kt = ring + stage * C::STAGE, vt = kt + KT * RB;
-            float s[NT][4];
+            float s[MT][NB][4];                            // scores, transposed: keys on the 16-row side
 #pragma unroll
-            for (int n = 0; n < NT; ++n) s[n][0] = s[n][1] = s[n][2] = s[n][3] = 0.0f;
-            // ---- S = Q K^T
+            for (int t = 0; t < MT; ++t)
+#pragma unroll
+                for (int n = 0; n < NB; ++n) s[t][n][0] = s[t][n][1] = s[t][n][2] = s[t][n][3] = 0.0f;
+            // ---- S^T = K Q^T
             if (!E4M3) {
 #pragma unroll
                 for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-                    for (int n = 0; n < NT; n += 2) {
-                        uint32_t b[4];                     // (keys 0..7, 8..15) x (two chunks of the step)
-                        ldsm_x4(b, kt + swz<RB>(8 * n + ((lane >> 4) << 3) + (lane & 7), 2 * ks + ((lane >> 3) & 1)));
-                        mma16<false>(s[n], qf[ks], b[0], b[1]);
-                        mma16<false>(s[n + 1], qf[ks], b[2], b[3]);
+                    for (int t = 0; t < MT; ++t) {
+                        uint32_t a[4];                     // keys (0..7, 8..15) x the step's two chunks
+                        ldsm_x4(a, kt + swz<RB>(16 * t + (lane & 15), 2 * ks + (lane >> 4)));
+#pragma unroll
+                        for (int n = 0; n < NB; ++n) mma16<false>(s[t][n], a, qf[ks][n][0], qf[ks][n][1]);
                     }
             } else {
 #pragma unroll
                 for (int ks = 0; ks < KS; ks += 2)
 #pragma unroll
-                    for (int n = 0; n < NT; n += 2) {
-                        uint32_t b[4], ev, od;             // (keys 0..7, 8..15) x (two steps, one chunk each)
-                        ldsm_x4(b, kt + swz<RB>(8 * n + ((lane >> 4) << 3) + (lane & 7), ks + ((lane >> 3) & 1)));
-                        e4m3_to_f16(b[0], ev, od); mma16<true>(s[n], qf[ks], ev, od);
-                        e4m3_to_f16(b[1], ev, od); mma16<true>(s[n], qf[ks + 1], ev, od);
-                        e4m3_to_f16(b[2], ev, od); mma16<true>(s[n + 1], qf[ks], ev, od);
-                        e4m3_to_f16(b[3], ev, od); mma16<true>(s[n + 1], qf[ks + 1], ev, od);
+                    for (int t = 0; t < MT; ++t) {
+                        uint32_t r[4], a[4];               // keys (0..7, 8..15) x two chunks, a step each
+                        ldsm_x4(r, kt + swz<RB>(16 * t + (lane & 15), ks + (lane >> 4)));
+                        e4m3_to_f16(r[0], a[0], a[2]);
+                        e4m3_to_f16(r[1], a[1], a[3]);
+#pragma unroll
+                        for (int n = 0; n < NB; ++n) mma16<true>(s[t][n], a, qf[ks][n][0], qf[ks][n][1]);
+                        e4m3_to_f16(r[2], a[0], a[2]);
+                        e4m3_to_f16(r[3], a[1], a[3]);
+#pragma unroll
+                        for (int n = 0; n < NB; ++n) mma16<true>(s[t][n], a, qf[ks + 1][n][0], qf[ks + 1][n][1]);
                     }
             }
             // ---- running maximum and sum (base 2)
-            float x0 = -INFINITY, x1 = -INFINITY;
-            const bool edge = key0 + KT > min(lim0, lim1);
+            const bool edge = key0 + KT > lim_min;
+            uint32_t ph[MT][NB][2], pl[LO == 2 ? MT : 1][NB][2];
+            bool moved = false;
+            float cor[NB][2];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                s[n][0] *= f0; s[n][1] *= f0; s[n][2] *= f1; s[n][3] *= f1;
-                if (edge) {
-                    const int k = key0 + 8 * n + 2 * q;
-                    if (k >= lim0) s[n][0] = -INFINITY;
-                    if (k + 1 >= lim0) s[n][1] = -INFINITY;
-                    if (k >= lim1) s[n][2] = -INFINITY;
-                    if (k + 1 >= lim1) s[n][3] = -INFINITY;
-                }
-                x0 = fmaxf(x0, fmaxf(s[n][0], s[n][1]));
-                x1 = fmaxf(x1, fmaxf(s[n][2], s[n][3]));
-            }
+            for (int n = 0; n < NB; ++n) {
+                float x0 = -INFINITY, x1 = -INFINITY;
 #pragma unroll
-            for (int o = 1; o < 4; o <<= 1) {
-                x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, o));
-                x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, o));
-            }
-            const float n0 = fmaxf(m0, x0), n1 = fmaxf(m1, x1);
-            const float u0 = n0 == -INFINITY ? 0.0f : n0, u1 = n1 == -INFINITY ? 0.0f : n1;      // an empty row so far: exp2(-inf - 0) = 0
-            const float c0 = exp2_approx(m0 - u0), c1 = PL == 1 ? c0 : exp2_approx(m1 - u1);
-            m0 = n0; m1 = n1;
-            l0 *= c0; l1 *= c1;
-            if (__any_sync(0xffffffffu, c0 != 1.0f || c1 != 1.0f)) {
-#pragma unroll
-                for (int t = 0; t < DT; ++t) { acc[t][0] *= c0; acc[t][1] *= c0; acc[t][2] *= c1; acc[t][3] *= c1; }
-            }
-            uint32_t ph[NT / 2][4], pl[PL == 2 ? NT / 2 : 1][4];
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const int kk = n >> 1, e = (n & 1) << 1;   // a0, a1 from the even key tile, a2, a3 from the odd one
-                const float e0 = exp2_approx(s[n][0] - u0), e1 = exp2_approx(s[n][1] - u0);
-                l0 += e0 + e1;
-                if (E4M3) {
-                    const float e2 = exp2_approx(s[n][2] - u1), e3 = exp2_approx(s[n][3] - u1);
-                    l1 += e2 + e3;
-                    ph[kk][e] = f16x2(e0, e1);
-                    ph[kk][e + 1] = f16x2(e2, e3);
-                } else if (PL == 1) {
-                    const uint32_t hi = bf16x2(e0, e1);
-                    ph[kk][e] = hi;
-                    ph[kk][e + 1] = bf16x2(e0 - bf16_lo(hi), e1 - bf16_hi(hi));
-                } else {
-                    const float e2 = exp2_approx(s[n][2] - u1), e3 = exp2_approx(s[n][3] - u1);
-                    l1 += e2 + e3;
-                    const uint32_t h0 = bf16x2(e0, e1), h1 = bf16x2(e2, e3);
-                    ph[kk][e] = h0;
-                    ph[kk][e + 1] = h1;
-                    if (PL == 2) {
-                        pl[kk][e] = bf16x2(e0 - bf16_lo(h0), e1 - bf16_hi(h0));
-                        pl[kk][e + 1] = bf16x2(e2 - bf16_lo(h1), e3 - bf16_hi(h1));
+                for (int t = 0; t < MT; ++t) {
+                    s[t][n][0] *= fac[n][0]; s[t][n][1] *= fac[n][1]; s[t][n][2] *= fac[n][0]; s[t][n][3] *= fac[n][1];
+                    if (edge) {
+                        const int k = key0 + 16 * t + g;
+                        if (k >= lim[n][0]) s[t][n][0] = -INFINITY;
+                        if (k >= lim[n][1]) s[t][n][1] = -INFINITY;
+                        if (k + 8 >= lim[n][0]) s[t][n][2] = -INFINITY;
+                        if (k + 8 >= lim[n][1]) s[t][n][3] = -INFINITY;
                     }
+                    x0 = fmaxf(x0, fmaxf(s[t][n][0], s[t][n][2]));
+                    x1 = fmaxf(x1, fmaxf(s[t][n][1], s[t][n][3]));
                 }
-            }
-            // ---- O += P V
 #pragma unroll
-            for (int kk = 0; kk < KT / 16; ++kk) {
+                for (int o = 4; o < 32; o <<= 1) {
+                    x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, o));
+                    x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, o));
+                }
+                const float n0 = fmaxf(mx[n][0], x0), n1 = fmaxf(mx[n][1], x1);
+                const float u0 = n0 == -INFINITY ? 0.0f : n0, u1 = n1 == -INFINITY ? 0.0f : n1;  // an empty row so far: exp2(-inf - 0) = 0
+                cor[n][0] = exp2_approx(mx[n][0] - u0);
+                cor[n][1] = exp2_approx(mx[n][1] - u1);
+                moved |= cor[n][0] != 1.0f || cor[n][1] != 1.0f;
+                mx[n][0] = n0; mx[n][1] = n1;
+                float l0 = 0.0f, l1 = 0.0f;
+#pragma unroll
+                for (int t = 0; t < MT; ++t) {
+                    const float e0 = exp2_approx(s[t][n][0] - u0), e1 = exp2_approx(s[t][n][1] - u1);
+                    const float e2 = exp2_approx(s[t][n][2] - u0), e3 = exp2_approx(s[t][n][3] - u1);
+                    l0 += e0 + e2;
+                    l1 += e1 + e3;
+                    if (E4M3) {
+                        ph[t][n][0] = f16x2(e0, e1);
+                        ph[t][n][1] = f16x2(e2, e3);
+                    } else {
+                        const uint32_t h0 = bf16x2(e0, e1), h1 = bf16x2(e2, e3);
+                        ph[t][n][0] = h0;
+                        ph[t][n][1] = h1;
+                        if (LO != 0) {
+                            const uint32_t w0 = bf16x2(e0 - bf16_lo(h0), e1 - bf16_hi(h0)), w1 = bf16x2(e2 - bf16_lo(h1), e3 - bf16_hi(h1));
+                            if (LO == 1) {
+                                if (q >= 2) { ph[t][n][0] = w0; ph[t][n][1] = w1; }
+                            } else {
+                                pl[LO == 2 ? t : 0][n][0] = transpose8x8(w0);
+                                pl[LO == 2 ? t : 0][n][1] = transpose8x8(w1);
+                            }
+                        }
+                    }
+                    ph[t][n][0] = transpose8x8(ph[t][n][0]);
+                    ph[t][n][1] = transpose8x8(ph[t][n][1]);
+                }
+                sum[n][0] = sum[n][0] * cor[n][0] + l0;
+                sum[n][1] = sum[n][1] * cor[n][1] + l1;
+            }
+            if (__any_sync(0xffffffffu, moved)) {
+#pragma unroll
+                for (int t = 0; t < DT; ++t)
+#pragma unroll
+                    for (int n = 0; n < NB; ++n) {
+                        acc[t][n][0] *= cor[n][0]; acc[t][n][1] *= cor[n][1]; acc[t][n][2] *= cor[n][0]; acc[t][n][3] *= cor[n][1];
+                    }
+            }
+            // ---- O^T += V^T P^T
+#pragma unroll
+            for (int kk = 0; kk < MT; ++kk) {
                 if (!E4M3) {
 #pragma unroll
-                    for (int t = 0; t < DT; t += 2) {
-                        uint32_t b[4];                     // (keys 0..7, 8..15) of two channel tiles
-                        ldsm_x4_t(b, vt + swz<RB>(16 * kk + (((lane >> 3) & 1) << 3) + (lane & 7), t + (lane >> 4)));
-                        mma16<false>(acc[t], ph[kk], b[0], b[1]);
-                        mma16<false>(acc[t + 1], ph[kk], b[2], b[3]);
-                        if (PL == 2) {
-                            mma16<false>(acc[t], pl[PL == 2 ? kk : 0], b[0], b[1]);
-                            mma16<false>(acc[t + 1], pl[PL == 2 ? kk : 0], b[2], b[3]);
+                    for (int t = 0; t < DT; ++t) {
+                        uint32_t a[4];                     // channels (0..7, 8..15) x keys (0..7, 8..15)
+                        ldsm_x4_t(a, vt + swz<RB>(16 * kk + ((lane >> 4) << 3) + (lane & 7), 2 * t + ((lane >> 3) & 1)));
+#pragma unroll
+                        for (int n = 0; n < NB; ++n) {
+                            mma16<false>(acc[t][n], a, ph[kk][n][0], ph[kk][n][1]);
+                            if (LO == 2) mma16<false>(acc[t][n], a, pl[LO == 2 ? kk : 0][n][0], pl[LO == 2 ? kk : 0][n][1]);
                         }
                     }
                 } else {
 #pragma unroll
-                    for (int t = 0; t < DT; t += 4) {
-                        uint32_t b[4], e0, o0, e1, o1;     // two chunks of 16 channels; a register = 2 keys x channels (2 g, 2 g + 1)
-                        ldsm_x4_t(b, vt + swz<RB>(16 * kk + (((lane >> 3) & 1) << 3) + (lane & 7), (t >> 1) + (lane >> 4)));
-                        e4m3_to_f16(b[0], e0, o0);
-                        e4m3_to_f16(b[1], e1, o1);
-                        mma16<true>(acc[t], ph[kk], e0, e1);
-                        mma16<true>(acc[t + 1], ph[kk], o0, o1);
-                        e4m3_to_f16(b[2], e0, o0);
-                        e4m3_to_f16(b[3], e1, o1);
-                        mma16<true>(acc[t + 2], ph[kk], e0, e1);
-                        mma16<true>(acc[t + 3], ph[kk], o0, o1);
+                    for (int t = 0; t < DT; t += 2) {
+                        uint32_t r[4], a[4];               // keys (0..7, 8..15) of two chunks; a register = 2 keys x channels (2 g, 2 g + 1)
+                        ldsm_x4_t(r, vt + swz<RB>(16 * kk + (lane & 15), t + (lane >> 4)));
+                        e4m3_to_f16(r[0], a[0], a[1]);     // row g of the product is channel 2 g, row g + 8 channel 2 g + 1
+                        e4m3_to_f16(r[1], a[2], a[3]);
+#pragma unroll
+                        for (int n = 0; n < NB; ++n) mma16<true>(acc[t][n], a, ph[kk][n][0], ph[kk][n][1]);
+                        e4m3_to_f16(r[2], a[0], a[1]);
+                        e4m3_to_f16(r[3], a[2], a[3]);
+#pragma unroll
+                        for (int n = 0; n < NB; ++n) mma16<true>(acc[t + 1][n], a, ph[kk][n][0], ph[kk][n][1]);
                     }
                 }
             }
         }
         if (more) {
-            issue(ld, page, (i + NST - 1) % NST);
+            issue(ld, page, stage == 0 ? NST - 1 : stage - 1);
             ld.advance(p);
         }
         cp_async_commit();
+        stage = stage + 1 == NST ? 0 : stage + 1;
 
         const bool item_end = cur.j + 1 == cur.nt;
-        if (item_end || i + 1 == n_units) {
-            // ---- end of an item or of this run: join the warp groups, write the rows or the part
-            if (!E4M3 && PL == 1) {
+        if (item_end || cur.left == 1) {
+            // ---- end of an item or of this run: add the warp groups, write the rows or the part
+            float* box = reinterpret_cast<float*>(smem + C::RING);
+            float2* ml = reinterpret_cast<float2*>(smem + C::RING + C::BOX);
+            const bool entire = item_end && part_j == 0;
+            const int slot = 2 * blockIdx.x + (first_part ? 0 : 1);              // part at the start of the run, or at its end
+            const int R = cur.rq.qlen * p.group;
+            const float vs = E4M3 ? (p.cache.v_scale != nullptr ? __ldg(p.cache.v_scale + cur.h) : 1.0f) * 256.0f : 1.0f;
 #pragma unroll
-                for (int t = 0; t < DT; ++t) { acc[t][0] += acc[t][2]; acc[t][1] += acc[t][3]; }
-            }
+            for (int n = 0; n < NB; ++n)
 #pragma unroll
-            for (int o = 1; o < 4; o <<= 1) {
-                l0 += __shfl_xor_sync(0xffffffffu, l0, o);
-                l1 += __shfl_xor_sync(0xffffffffu, l1, o);
-            }
-            float4* box = reinterpret_cast<float4*>(smem + C::RING);
-            float4* box_ml = box + (KW / 2) * RW * 32 * DT;
+                for (int e = 0; e < 2; ++e) {
+                    float l = sum[n][e];
 #pragma unroll
-            for (int step = KW / 2; step >= 1; step >>= 1) {
-                __syncthreads();                           // readers of the box before
-                if (kg >= step && kg < 2 * step) {
-                    const int at = (kg - step) * RW + rw;
-#pragma unroll
-                    for (int t = 0; t < DT; ++t) box[(at * DT + t) * 32 + lane] = make_float4(acc[t][0], acc[t][1], acc[t][2], acc[t][3]);
-                    box_ml[at * 32 + lane] = make_float4(m0, m1, l0, l1);
+                    for (int o = 4; o < 32; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+                    if (g == 0) ml[kg * ROWS + rw * 8 * NB + 8 * n + 2 * q + e] = make_float2(mx[n][e], l);
                 }
-                __syncthreads();
-                if (kg < step) {
-                    const int at = kg * RW + rw;
-                    const float4 o = box_ml[at * 32 + lane];
-                    const float n0 = fmaxf(m0, o.x), n1 = fmaxf(m1, o.y);
-                    const float u0 = n0 == -INFINITY ? 0.0f : n0, u1 = n1 == -INFINITY ? 0.0f : n1;
-                    const float a0 = exp2_approx(m0 - u0), a1 = exp2_approx(m1 - u1), b0 = exp2_approx(o.x - u0), b1 = exp2_approx(o.y - u1);
-                    m0 = n0; m1 = n1;
-                    l0 = l0 * a0 + o.z * b0;
-                    l1 = l1 * a1 + o.w * b1;
+            __syncthreads();
+            float wgt[NB][2];
 #pragma unroll
-                    for (int t = 0; t < DT; ++t) {
-                        const float4 v = box[(at * DT + t) * 32 + lane];
-                        acc[t][0] = acc[t][0] * a0 + v.x * b0;
-                        acc[t][1] = acc[t][1] * a0 + v.y * b0;
-                        acc[t][2] = acc[t][2] * a1 + v.z * b1;
-                        acc[t][3] = acc[t][3] * a1 + v.w * b1;
+            for (int n = 0; n < NB; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const int rl = rw * 8 * NB + 8 * n + 2 * q + e;
+                    float m = mx[n][e], l = 0.0f;
+#pragma unroll
+                    for (int w = 0; w < KW; ++w) m = fmaxf(m, ml[w * ROWS + rl].x);
+                    const float u = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+                    for (int w = 0; w < KW; ++w) {
+                        const float2 o = ml[w * ROWS + rl];
+                        l += o.y * exp2_approx(o.x - u);
                     }
-                }
-            }
-            if (kg == 0) {
-                const int R = cur.rq.qlen * p.group;
-                const int seg_units = i + 1 < cur.j + 1 ? i + 1 : cur.j + 1;     // units of this item in this run so far
-                const bool entire = item_end && seg_units == cur.nt;
-                const int slot = 2 * blockIdx.x + (seg_units == i + 1 ? 0 : 1);  // part at the start of the run, or at its end
-                const float vs = E4M3 ? (p.cache.v_scale != nullptr ? __ldg(p.cache.v_scale + cur.h) : 1.0f) * 256.0f : 1.0f;
-#pragma unroll
-                for (int half = 0; half < (PL == 1 && !E4M3 ? 1 : 2); ++half) {
-                    const int rl = rw * 16 + g + 8 * half, r = cur.rt * ROWS + rl;
-                    if (r >= R) continue;
-                    const float m = half ? m1 : m0, l = half ? l1 : l0;
-                    const float f = entire ? (l > 0.0f ? vs / l : 0.0f) : vs;
-                    const int t_row = r / p.group, hh = cur.h * p.group + r % p.group;
-                    uint16_t* orow = p.O + static_cast<size_t>(cur.rq.row0 + t_row) * p.ldo + static_cast<size_t>(hh) * D;
-                    float* prow = p.part_o + (static_cast<size_t>(slot) * ROWS + rl) * D;
-                    if (!E4M3) {
-#pragma unroll
-                        for (int t = 0; t < DT; ++t) {
-                            const float a = acc[t][2 * half] * f, b = acc[t][2 * half + 1] * f;
-                            if (entire) *reinterpret_cast<uint32_t*>(orow + 8 * t + 2 * q) = bf16x2(a, b);
-                            else *reinterpret_cast<float2*>(prow + 8 * t + 2 * q) = make_float2(a, b);
-                        }
-                    } else {
-#pragma unroll
-                        for (int t = 0; t < DT; t += 2) {  // even and odd channels of a chunk of 16: a lane holds 4 q .. 4 q + 3
-                            const float a = acc[t][2 * half] * f, b = acc[t + 1][2 * half] * f, c = acc[t][2 * half + 1] * f, d = acc[t + 1][2 * half + 1] * f;
-                            if (entire) *reinterpret_cast<uint2*>(orow + 8 * t + 4 * q) = make_uint2(bf16x2(a, b), bf16x2(c, d));
-                            else *reinterpret_cast<float4*>(prow + 8 * t + 4 * q) = make_float4(a, b, c, d);
+                    wgt[n][e] = exp2_approx(mx[n][e] - u) * vs * (entire ? (l > 0.0f ? 1.0f / l : 0.0f) : 1.0f);
+                    if (kg == 0 && g == 0) {
+                        const int r = cur.rt * ROWS + rl;
+                        if (r < R) {
+                            if (!entire) p.part_ml[static_cast<size_t>(slot) * ROWS + rl] = make_float2(m, l);
+                            else if (p.lse != nullptr)
+                                p.lse[static_cast<size_t>(cur.rq.row0 + r / p.group) * p.heads + cur.h * p.group + r % p.group] =
+                                    l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
                         }
                     }
-                    if (q == 0) {
-                        if (entire) {
-                            if (p.lse != nullptr)
-                                p.lse[static_cast<size_t>(cur.rq.row0 + t_row) * p.heads + hh] = l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
+                }
+            const int rows_here = min(ROWS, R - cur.rt * ROWS);
+#pragma unroll
+            for (int round = 0; round < C::ROUNDS; ++round) {
+                if (round > 0) __syncthreads();
+                float* mine = box + (kg * ROWS + rw * 8 * NB) * (DC + 4);
+#pragma unroll
+                for (int t = 0; t < DC / 16; ++t)
+#pragma unroll
+                    for (int n = 0; n < NB; ++n) {
+                        const float* c = acc[round * (DC / 16) + t][n];
+                        float* b0 = mine + (8 * n + 2 * q) * (DC + 4) + 16 * t;
+                        float* b1 = b0 + DC + 4;
+                        if (E4M3) {
+                            *reinterpret_cast<float2*>(b0 + 2 * g) = make_float2(c[0] * wgt[n][0], c[2] * wgt[n][0]);
+                            *reinterpret_cast<float2*>(b1 + 2 * g) = make_float2(c[1] * wgt[n][1], c[3] * wgt[n][1]);
                         } else {
-                            p.part_ml[static_cast<size_t>(slot) * ROWS + rl] = make_float2(m, l);
+                            b0[g] = c[0] * wgt[n][0]; b0[g + 8] = c[2] * wgt[n][0];
+                            b1[g] = c[1] * wgt[n][1]; b1[g + 8] = c[3] * wgt[n][1];
                         }
                     }
+                __syncthreads();
+                for (int i = tid; i < rows_here * (DC / 4); i += C::THREADS) {
+                    const int rl = i / (DC / 4), d = 4 * (i % (DC / 4));
+                    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+                    for (int w = 0; w < KW; ++w) {
+                        const float4 v = *reinterpret_cast<const float4*>(box + (w * ROWS + rl) * (DC + 4) + d);
+                        o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w;
+                        if (LO == 1) {                     // the low parts of row rl are row rl + 4
+                            const float4 x = *reinterpret_cast<const float4*>(box + (w * ROWS + rl + 4) * (DC + 4) + d);
+                            o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
+                        }
+                    }
+                    const int r = cur.rt * ROWS + rl;
+                    if (entire)
+                        *reinterpret_cast<uint2*>(p.O + static_cast<size_t>(cur.rq.row0 + r / p.group) * p.ldo + static_cast<size_t>(cur.h * p.group + r % p.group) * D +
+                                                  round * DC + d) = make_uint2(bf16x2(o.x, o.y), bf16x2(o.z, o.w));
+                    else
+                        *reinterpret_cast<float4*>(p.part_o + (static_cast<size_t>(slot) * ROWS + rl) * D + round * DC + d) = o;
                 }
             }
             fresh = true;
+            first_part = false;
+            // (the next item's end writes `ml` only after every thread has read it: each reads before the barrier above)
         }
         cur.advance(p);
     }
@@ -686,19 +743,58 @@ __global__ void __launch_bounds__(JOIN_THREADS) attention_join_kernel(const Attn
 
 // ---- variants: warps over rows (RW) and keys (KW), keys per tile, stages.  The ring is about 130 to 200 KB: it is what keeps
 // enough of the cache in flight with one CTA per SM.
-template <int D, bool E4M3, int RWS, int PL>
+#ifndef VE_KW
+#define VE_KW 8
+#define VE_KT 32
+#define VE_NST 3
+#endif
+#ifndef VB_KW
+#define VB_KW 8
+#define VB_KT 16
+#define VB_NST 3
+#endif
+#ifndef V64_KW
+#define V64_KW 8
+#define V64_KT 32
+#define V64_NST 3
+#endif
+#ifndef V64E_KW
+#define V64E_KW 16
+#define V64E_KT 32
+#define V64E_NST 3
+#endif
+#ifndef VC_NB
+#define VC_NB 2
+#define VC_RW 4
+#define VC_KW 2
+#define VC_KT 32
+#define VC_NST 5
+#endif
+// CLS: rows of an item up to 4, 8, 16, 32, more
+template <int D, bool E4M3, int CLS>
 struct Pick;
-template <bool E4M3, int PL> struct Pick<64, E4M3, 1, PL> { using C = AttnCfg<64, E4M3, 1, 4, 32, 5, PL>; };
-template <bool E4M3, int PL> struct Pick<64, E4M3, 2, PL> { using C = AttnCfg<64, E4M3, 2, 4, 32, 5, PL>; };
-template <bool E4M3, int PL> struct Pick<64, E4M3, 4, PL> { using C = AttnCfg<64, E4M3, 4, 2, 32, 5, PL>; };
-template <bool E4M3, int PL> struct Pick<128, E4M3, 1, PL> { using C = AttnCfg<128, E4M3, 1, 4, 32, E4M3 ? 5 : 3, PL>; };
-template <bool E4M3, int PL> struct Pick<128, E4M3, 2, PL> { using C = AttnCfg<128, E4M3, 2, 2, 32, 5, PL>; };
-template <bool E4M3, int PL> struct Pick<128, E4M3, 4, PL> { using C = AttnCfg<128, E4M3, 4, 2, 32, 5, PL>; };
-template <bool E4M3, int PL> struct Pick<256, E4M3, 1, PL> { using C = AttnCfg<256, E4M3, 1, 4, 16, 3, PL>; };
-template <bool E4M3, int PL> struct Pick<256, E4M3, 2, PL> { using C = AttnCfg<256, E4M3, 2, 2, 16, 4, PL>; };
-template <bool E4M3, int PL> struct Pick<256, E4M3, 4, PL> { using C = AttnCfg<256, E4M3, 4, 2, 16, 4, PL>; };
+template <int CLS> constexpr int kLo = CLS == 0 ? 1 : 2;
+template <int CLS> struct Pick<64, false, CLS> { using C = AttnCfg<64, false, CLS <= 1 ? 1 : 2, 1, V64_KW, V64_KT, V64_NST, kLo<CLS>>; };
+template <int CLS> struct Pick<64, true, CLS> { using C = AttnCfg<64, true, CLS <= 1 ? 1 : 2, 1, CLS <= 1 ? V64E_KW : 8, V64E_KT, CLS <= 1 ? V64E_NST : 5, 0>; };
+template <int CLS> struct Pick<128, false, CLS> { using C = AttnCfg<128, false, CLS <= 1 ? 1 : 2, 1, VB_KW, VB_KT, VB_NST, kLo<CLS>>; };
+template <int CLS> struct Pick<128, true, CLS> { using C = AttnCfg<128, true, CLS <= 1 ? 1 : 2, 1, VE_KW, VE_KT, VE_NST, 0>; };
+template <int CLS> struct Pick<256, false, CLS> { using C = AttnCfg<256, false, CLS <= 1 ? 1 : 2, 1, 4, 16, 3, kLo<CLS>>; };
+template <int CLS> struct Pick<256, true, CLS> { using C = AttnCfg<256, true, CLS <= 1 ? 1 : 2, 1, 8, 16, 3, 0>; };
+template <> struct Pick<64, false, 3> { using C = AttnCfg<64, false, 2, 2, 4, 32, 5, 2>; };
+template <> struct Pick<64, true, 3> { using C = AttnCfg<64, true, 2, 2, 4, 32, 5, 0>; };
+template <> struct Pick<128, false, 3> { using C = AttnCfg<128, false, 2, 2, 4, 16, 5, 2>; };
+template <> struct Pick<128, true, 3> { using C = AttnCfg<128, true, 2, 2, 4, 32, 5, 0>; };
+template <> struct Pick<256, false, 3> { using C = AttnCfg<256, false, 2, 2, 4, 16, 3, 2>; };
+template <> struct Pick<256, true, 3> { using C = AttnCfg<256, true, 2, 2, 4, 16, 5, 0>; };
+template <> struct Pick<64, false, 4> { using C = AttnCfg<64, false, VC_NB, VC_RW, VC_KW, 32, 5, 2>; };
+template <> struct Pick<64, true, 4> { using C = AttnCfg<64, true, VC_NB, VC_RW, VC_KW, 32, 5, 0>; };
+template <> struct Pick<128, false, 4> { using C = AttnCfg<128, false, VC_NB, VC_RW, VC_KW, VC_KT, VC_NST, 2>; };
+template <> struct Pick<128, true, 4> { using C = AttnCfg<128, true, VC_NB, VC_RW, VC_KW, VC_KT, VC_NST, 0>; };
+template <> struct Pick<256, false, 4> { using C = AttnCfg<256, false, 2, 4, 2, 16, 5, 2>; };
+template <> struct Pick<256, true, 4> { using C = AttnCfg<256, true, 2, 4, 2, 16, 5, 0>; };
 
-int row_warps(int max_rows) { return max_rows <= 16 ? 1 : (max_rows <= 32 ? 2 : 4); }
+int rows_class(int max_rows) { return max_rows <= 4 ? 0 : (max_rows <= 8 ? 1 : (max_rows <= 16 ? 2 : (max_rows <= 32 ? 3 : 4))); }
+int tile_rows(int max_rows) { return max_rows <= 8 ? 8 : (max_rows <= 16 ? 16 : (max_rows <= 32 ? 32 : 64)); }      // ROWS of the variant
 
 template <class C>
 cudaError_t launch_main(const AttnParams& p, cudaStream_t st)
@@ -741,33 +837,40 @@ cudaError_t run_one(AttnParams p, int max_rows, long long max_kv, cudaStream_t s
     if (items <= p.G && (max_kv + C::UK - 1) / C::UK <= p.whole_units) return cudaSuccess;
     return launch_join<C::D>(p, C::ROWS, max_rows, st);
 }
+template <int D, bool E4M3>
+cudaError_t run_df(const AttnParams& p, int max_rows, long long max_kv, cudaStream_t st)
+{
+    static_assert(Pick<D, E4M3, 0>::C::ROWS == 8 && Pick<D, E4M3, 2>::C::ROWS == 16 && Pick<D, E4M3, 3>::C::ROWS == 32 && Pick<D, E4M3, 4>::C::ROWS == 64, "tile_rows()");
+    switch (rows_class(max_rows)) {
+        case 0: return run_one<typename Pick<D, E4M3, E4M3 ? 1 : 0>::C>(p, max_rows, max_kv, st);
+        case 1: return run_one<typename Pick<D, E4M3, 1>::C>(p, max_rows, max_kv, st);
+        case 2: return run_one<typename Pick<D, E4M3, 2>::C>(p, max_rows, max_kv, st);
+        case 3: return run_one<typename Pick<D, E4M3, 3>::C>(p, max_rows, max_kv, st);
+        default: return run_one<typename Pick<D, E4M3, 4>::C>(p, max_rows, max_kv, st);
+    }
+}
 template <int D>
 cudaError_t run_d(const AttnParams& p, bool e4m3, int max_rows, long long max_kv, cudaStream_t st)
 {
-    const int rw = row_warps(max_rows);
-    if (e4m3) {
-        if (rw == 1) return run_one<typename Pick<D, true, 1, 0>::C>(p, max_rows, max_kv, st);
-        if (rw == 2) return run_one<typename Pick<D, true, 2, 0>::C>(p, max_rows, max_kv, st);
-        return run_one<typename Pick<D, true, 4, 0>::C>(p, max_rows, max_kv, st);
-    }
-    if (max_rows <= 8) return run_one<typename Pick<D, false, 1, 1>::C>(p, max_rows, max_kv, st);
-    if (rw == 1) return run_one<typename Pick<D, false, 1, 2>::C>(p, max_rows, max_kv, st);
-    if (rw == 2) return run_one<typename Pick<D, false, 2, 2>::C>(p, max_rows, max_kv, st);
-    return run_one<typename Pick<D, false, 4, 2>::C>(p, max_rows, max_kv, st);
+    return e4m3 ? run_df<D, true>(p, max_rows, max_kv, st) : run_df<D, false>(p, max_rows, max_kv, st);
 }
 template <class C>
 cudaError_t init_one_attn() { return cudaFuncSetAttribute(attention_paged_kernel<C>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM); }
+template <int D, bool E4M3>
+cudaError_t init_df()
+{
+    cudaError_t e = init_one_attn<typename Pick<D, E4M3, E4M3 ? 1 : 0>::C>();
+    if (e == cudaSuccess) e = init_one_attn<typename Pick<D, E4M3, 1>::C>();
+    if (e == cudaSuccess) e = init_one_attn<typename Pick<D, E4M3, 2>::C>();
+    if (e == cudaSuccess) e = init_one_attn<typename Pick<D, E4M3, 3>::C>();
+    if (e == cudaSuccess) e = init_one_attn<typename Pick<D, E4M3, 4>::C>();
+    return e;
+}
 template <int D>
 cudaError_t init_d()
 {
-    cudaError_t e = init_one_attn<typename Pick<D, true, 1, 0>::C>();
-    if (e == cudaSuccess) e = init_one_attn<typename Pick<D, true, 2, 0>::C>();
-    if (e == cudaSuccess) e = init_one_attn<typename Pick<D, true, 4, 0>::C>();
-    if (e == cudaSuccess) e = init_one_attn<typename Pick<D, false, 1, 1>::C>();
-    if (e == cudaSuccess) e = init_one_attn<typename Pick<D, false, 1, 2>::C>();
-    if (e == cudaSuccess) e = init_one_attn<typename Pick<D, false, 2, 2>::C>();
-    if (e == cudaSuccess) e = init_one_attn<typename Pick<D, false, 4, 2>::C>();
-    return e;
+    cudaError_t e = init_df<D, false>();
+    return e == cudaSuccess ? init_df<D, true>() : e;
 }
 
 }  // namespace
@@ -783,7 +886,7 @@ cudaError_t attention_paged_init()
 // Workspace: descriptors, (maximum, sum) and fp32 outputs of at most two parts per CTA.
 size_t attention_workspace_bytes(int max_rows, int head_dim, int sm_count)
 {
-    const size_t rows = 2 * static_cast<size_t>(sm_count) * 16 * row_warps(max_rows);
+    const size_t rows = 2 * static_cast<size_t>(sm_count) * tile_rows(max_rows);
     const size_t desc = (static_cast<size_t>(sm_count) * 32 + 255) / 256 * 256;
     return desc + (rows * sizeof(float2) + 255) / 256 * 256 + rows * head_dim * sizeof(float);
 }
@@ -801,7 +904,7 @@ cudaError_t launch_attention_paged(const AttnArgs& a, void* workspace, int sm_co
     p.group = a.heads / a.kv_heads; p.causal = a.causal;
     p.G = sm_count;
     const int max_rows = a.max_q * p.group;
-    const size_t rows = 2 * static_cast<size_t>(sm_count) * 16 * row_warps(max_rows);
+    const size_t rows = 2 * static_cast<size_t>(sm_count) * tile_rows(max_rows);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     p.desc = reinterpret_cast<int*>(ws);
     ws += (static_cast<size_t>(sm_count) * 32 + 255) / 256 * 256;
