@@ -470,7 +470,7 @@ def _on_one_device(*tensors) -> int:
 
 def _launch_stream(device: int, stream):
     """Raw stream to launch on.  Like every call of the library, the buffers' device must be the current one."""
-    if torch.cuda.current_device() != device:
+    if torch._C._cuda_getDevice() != device:
         raise RudderError(ERR_ARG, f"buffers are on device {device}, device {torch.cuda.current_device()} is current")
     if stream is not None:
         return stream.cuda_stream
@@ -604,14 +604,23 @@ def rudder_attention_paged(args: AttentionArgs, workspace: torch.Tensor | None =
 
 def rudder_linear_a16(w: Weight, X: torch.Tensor, bias=None, Y=None, stream=None) -> torch.Tensor:
     """One to sixteen rows through a packed weight with 16-bit activations (no activation quantisation)."""
-    assert X.is_cuda and X.dtype == torch.bfloat16 and X.dim() == 2 and X.stride(1) == 1 and X.shape[1] == w.K
+    M, K = X.shape
+    ldx, one = X.stride()
+    device = X.get_device()
     if Y is None:
-        Y = torch.empty((X.shape[0], w.N), dtype=torch.bfloat16, device=X.device)
-    assert Y.dtype == torch.bfloat16 and Y.stride(1) == 1 and Y.shape == (X.shape[0], w.N)
-    assert bias is None or (bias.dtype == torch.float32 and bias.is_contiguous() and bias.numel() == w.N and bias.device == X.device)
-    assert Y.device == X.device
-    _check(lib().rudder_linear_a16(w.handle, X.data_ptr(), _rows(X), X.shape[0], bias.data_ptr() if bias is not None else None, Y.data_ptr(), _rows(Y),
-                                   _launch_stream(X.device.index, stream)), "rudder_linear_a16")
+        Y = torch.empty((M, w.N), dtype=torch.bfloat16, device=X.device)
+    ldy, one_y = Y.stride()
+    assert device >= 0 and X.dtype is torch.bfloat16 and K == w.K and one == 1
+    assert Y.dtype is torch.bfloat16 and one_y == 1 and Y.shape == (M, w.N) and Y.get_device() == device
+    b = None
+    if bias is not None:
+        assert bias.dtype is torch.float32 and bias.numel() == w.N and bias.is_contiguous() and bias.get_device() == device
+        b = bias.data_ptr()
+    if M == 1:                                       # one row has no leading dimension of its own
+        ldx, ldy = max(ldx, K), max(ldy, w.N)
+    s = lib().rudder_linear_a16(w.handle, X.data_ptr(), ldx, M, b, Y.data_ptr(), ldy, _launch_stream(device, stream))
+    if s:
+        _check(s, "rudder_linear_a16")
     return Y
 
 

@@ -70,8 +70,8 @@ __device__ __forceinline__ uint32_t weight_pair(uint32_t w, int t, uint32_t mul)
         const uint32_t hi = (w << (24 - 8 * t)) & 0x80000000u;
         return mag | lo | hi;
     }
-    const uint32_t n = w >> (4 * t);
-    return hmul2_bf16(((n & 0x00070007u) << 6) | ((n & 0x00080008u) << 12), mul);
+    const uint32_t mag = (t < 2 ? w << (6 - 4 * t) : w >> (4 * t - 6)) & 0x01C001C0u;
+    return hmul2_bf16(((w << (12 - 4 * t)) & 0x80008000u) | mag, mul);
 }
 // Offsets (inside the lane's channels of a 64-channel block) of the two channels of pair t of word j.
 //   INT: lane q holds channels base .. base + 7 and base + 16 .. base + 23, base = 32 (q >> 1) + 8 (q & 1): byte b of the
@@ -97,104 +97,134 @@ __device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t&
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(lo) : "f"(rb), "f"(ra));
 }
 
-constexpr int kPrefetch = 4;        // 64-channel blocks of weights a warp holds in registers at once
+__device__ __forceinline__ void cluster_sync_all() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float ld_dsmem(const void* local, uint32_t rank) {
+    uint32_t a;
+    float v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(local)), "r"(rank));
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+    return v;
+}
 
-// NT: tiles of 8 columns (4 rows each).  Shared memory: v fragments, one block of 64 channels =
-// [4 steps][NT tiles][8 columns][4 lanes q][8 bytes], padded by 32 bytes so that the blocks start on different banks.
-template <int LAYOUT, int NT, int WARPS>
-__global__ void __launch_bounds__(32 * WARPS) linear_a16_kernel(const LinearA16Params p)
+// NT: tiles of 8 columns (4 rows each).  KS: CTAs of a cluster that share 16 KS output channels, each with 1 / KS of the input
+// channels.  PF: 64-channel blocks of weights a warp holds in registers at once.  Shared memory: v fragments, one block of 64
+// channels = [4 steps][NT tiles][8 columns][4 lanes q][8 bytes], padded by 32 bytes so that the blocks start on different banks.
+template <int LAYOUT, int NT, int KS>
+struct A16Cfg {
+    static constexpr int WARPS = KS == 1 ? 8 : 16, THREADS = 32 * WARPS;
+    static constexpr int WK = WARPS / KS;                  // warps that share a tile of 16 channels: every WK-th block each
+    static constexpr int PF = KS == 1 ? 4 : (NT == 4 ? 4 : 8);
+    static constexpr int kBlockBytes = 4 * NT * 256 + 32;
+};
+
+template <int LAYOUT, int NT, int KS>
+__global__ void __launch_bounds__(A16Cfg<LAYOUT, NT, KS>::THREADS) linear_a16_kernel(const LinearA16Params p)
 {
-    constexpr int THREADS = 32 * WARPS;
-    constexpr int kBlockBytes = 4 * NT * 256 + 32;
+    using C = A16Cfg<LAYOUT, NT, KS>;
+    constexpr int WARPS = C::WARPS, THREADS = C::THREADS, WK = C::WK, PF = C::PF, kBlockBytes = C::kBlockBytes;
     extern __shared__ __align__(16) uint8_t vfrag[];
     __shared__ float red[WARPS][4 * NT][17];
+    __shared__ float part[KS > 1 ? KS : 1][4 * NT][17];    // this CTA's sums for its cluster
     pdl_launch_dependents();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int g = lane >> 2, q = lane & 3;
-    const int n_blocks = p.K >> 6;
-    const int n_tiles = p.N >> 4;
+    const int mt = warp % KS, wk = warp / KS;
+    const int rank = KS > 1 ? static_cast<int>(blockIdx.x % KS) : 0;
+    const int all_blocks = p.K >> 6, per_cta = (all_blocks + KS - 1) / KS;
+    const int b_begin = min(all_blocks, rank * per_cta), b_end = min(all_blocks, b_begin + per_cta);
+    const int n_tiles = p.N / (16 * KS);
     const size_t row_bytes = static_cast<size_t>(p.K >> 1);
     const uint32_t lane_off = (LAYOUT == A16_NVFP4) ? 8u * q : 16u * (q >> 1) + 8u * (q & 1);
     // UE4M3 scale x 2^117: together with the 2^-126 of the raw codes the weights come out times 2^-9 (448 x 2^117 is in range)
     const float out_scale = (LAYOUT == A16_NVFP4) ? 512.0f * __ldg(p.tensor_scale) : 16.0f;
     bool waited = false;
 
-    for (int tile = blockIdx.x; tile < n_tiles; tile += gridDim.x) {
-        const int n0 = tile * 16;
+    for (int tile = blockIdx.x / KS; tile < n_tiles; tile += gridDim.x / KS) {
+        const int n0 = (tile * KS + mt) * 16;              // this warp's channels
         const uint8_t* w0 = p.codes + static_cast<size_t>(n0 + g) * row_bytes + lane_off;
         const uint8_t* w1 = w0 + 8 * row_bytes;
         float acc[NT][4];
 #pragma unroll
         for (int t = 0; t < NT; ++t) acc[t][0] = acc[t][1] = acc[t][2] = acc[t][3] = 0.0f;
 
-        for (int c0 = 0; c0 < n_blocks; c0 += p.chunk) {
-            const int c1 = min(n_blocks, c0 + p.chunk);
+        for (int c0 = b_begin; c0 < b_end; c0 += p.chunk) {
+            const int c1 = min(b_end, c0 + p.chunk);
             // first weights of this chunk: requested before v is staged (and before waiting for the kernel before this one)
-            uint2 wa[kPrefetch], wb[kPrefetch];
-            float sa[kPrefetch], sb[kPrefetch];
+            uint2 wa[PF], wb[PF];
+            uint32_t sa[PF], sb[PF];
             auto fetch = [&](int first) {
 #pragma unroll
-                for (int i = 0; i < kPrefetch; ++i) {
-                    const int blk = min(first + i * WARPS, n_blocks - 1);       // past the end: a valid address, never used
+                for (int i = 0; i < PF; ++i) {
+                    const int blk = min(first + i * WK, all_blocks - 1);        // past the end: a valid address, never used
                     wa[i] = ldg_weights(w0 + 32 * blk);
                     wb[i] = ldg_weights(w1 + 32 * blk);
                     if (LAYOUT == A16_NVFP4) {
                         const uint8_t* sp = p.scales_c + static_cast<size_t>(n0 + g) * (p.K >> 4) + 4 * blk + q;
-                        sa[i] = __uint_as_float(__ldg(sp));
-                        sb[i] = __uint_as_float(__ldg(sp + 8 * static_cast<size_t>(p.K >> 4)));
+                        sa[i] = __ldg(sp);
+                        sb[i] = __ldg(sp + 8 * static_cast<size_t>(p.K >> 4));
                     } else {
                         const float* sp = p.scales_t + static_cast<size_t>((blk << 6) / p.G) * p.N + n0 + g;
-                        sa[i] = __ldg(sp);
-                        sb[i] = __ldg(sp + 8);
+                        sa[i] = __float_as_uint(__ldg(sp));
+                        sb[i] = __float_as_uint(__ldg(sp + 8));
                     }
                 }
             };
-            fetch(c0 + warp);
+            fetch(c0 + wk);
             if (!waited) { pdl_wait(); waited = true; }
-            if (p.chunk < n_blocks || tile == static_cast<int>(blockIdx.x)) {
-                // v of this chunk: item = (row, block, lane q): 16 channels -> 4 steps x (hi, lo) x 8 bytes
+            if (p.chunk < per_cta || tile == static_cast<int>(blockIdx.x) / KS) {
+                // v of this chunk: item = (block, lane q), rows m, m + groups, ...: 16 channels -> 4 steps x (hi, lo) x 8 bytes
                 __syncthreads();                                                // readers of the chunk before
-                const int per_row = 4 * (c1 - c0);
-                for (int it = tid; it < p.M * per_row; it += THREADS) {
-                    const int m = it / per_row, r = it - m * per_row;
+                const int items = 4 * (c1 - c0);
+                const int groups = items < THREADS ? THREADS / items : 1;       // threads that share an item, every groups-th row each
+                const int stride = items < THREADS ? items : THREADS;
+                for (int r = tid % stride, m0 = tid / stride; r < items && m0 < groups; r += stride) {
                     const int blk = r >> 2, qq = r & 3;
                     const int ch = 64 * (c0 + blk) + (LAYOUT == A16_NVFP4 ? 16 * qq : 32 * (qq >> 1) + 8 * (qq & 1));
-                    const int second = (LAYOUT == A16_NVFP4) ? 8 : 16;
-                    float v[16];
+                    constexpr int second = (LAYOUT == A16_NVFP4) ? 8 : 16;
+                    float dd[16];
 #pragma unroll
                     for (int hh = 0; hh < 2; ++hh) {
-                        const uint4 x4 = *reinterpret_cast<const uint4*>(p.X + static_cast<size_t>(m) * p.ldx + ch + hh * second);
                         const float4 d0 = __ldg(reinterpret_cast<const float4*>(p.dinv + ch + hh * second));
                         const float4 d1 = __ldg(reinterpret_cast<const float4*>(p.dinv + ch + hh * second) + 1);
-                        const uint32_t xw[4] = {x4.x, x4.y, x4.z, x4.w};
-                        const float dd[8] = {d0.x, d0.y, d0.z, d0.w, d1.x, d1.y, d1.z, d1.w};
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            v[8 * hh + 2 * i] = __fmul_rn(__uint_as_float(xw[i] << 16), dd[2 * i]);
-                            v[8 * hh + 2 * i + 1] = __fmul_rn(__uint_as_float(xw[i] & 0xFFFF0000u), dd[2 * i + 1]);
-                        }
+                        dd[8 * hh] = d0.x; dd[8 * hh + 1] = d0.y; dd[8 * hh + 2] = d0.z; dd[8 * hh + 3] = d0.w;
+                        dd[8 * hh + 4] = d1.x; dd[8 * hh + 5] = d1.y; dd[8 * hh + 6] = d1.z; dd[8 * hh + 7] = d1.w;
                     }
-                    uint8_t* dst = vfrag + static_cast<size_t>(blk) * kBlockBytes + (m >> 2) * 256 + 2 * (m & 3) * 32 + qq * 8;
+                    for (int m = m0; m < p.M; m += groups) {
+                        float v[16];
 #pragma unroll
-                    for (int st = 0; st < 4; ++st) {                            // step st = pairs 2 (st & 1), + 1 of word st >> 1
-                        uint2 hi, lo;
-                        split2(v[pair_index<LAYOUT>(st >> 1, 2 * (st & 1), 0)], v[pair_index<LAYOUT>(st >> 1, 2 * (st & 1), 1)], hi.x, lo.x);
-                        split2(v[pair_index<LAYOUT>(st >> 1, 2 * (st & 1) + 1, 0)], v[pair_index<LAYOUT>(st >> 1, 2 * (st & 1) + 1, 1)], hi.y, lo.y);
-                        *reinterpret_cast<uint2*>(dst + st * NT * 256) = hi;
-                        *reinterpret_cast<uint2*>(dst + st * NT * 256 + 32) = lo;
+                        for (int hh = 0; hh < 2; ++hh) {
+                            const uint4 x4 = *reinterpret_cast<const uint4*>(p.X + static_cast<size_t>(m) * p.ldx + ch + hh * second);
+                            const uint32_t xw[4] = {x4.x, x4.y, x4.z, x4.w};
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                v[8 * hh + 2 * i] = __fmul_rn(__uint_as_float(xw[i] << 16), dd[8 * hh + 2 * i]);
+                                v[8 * hh + 2 * i + 1] = __fmul_rn(__uint_as_float(xw[i] & 0xFFFF0000u), dd[8 * hh + 2 * i + 1]);
+                            }
+                        }
+                        uint8_t* dst = vfrag + static_cast<size_t>(blk) * kBlockBytes + (m >> 2) * 256 + 2 * (m & 3) * 32 + qq * 8;
+#pragma unroll
+                        for (int st = 0; st < 4; ++st) {                        // step st = pairs 2 (st & 1), + 1 of word st >> 1
+                            uint2 hi, lo;
+                            split2(v[pair_index<LAYOUT>(st >> 1, 2 * (st & 1), 0)], v[pair_index<LAYOUT>(st >> 1, 2 * (st & 1), 1)], hi.x, lo.x);
+                            split2(v[pair_index<LAYOUT>(st >> 1, 2 * (st & 1) + 1, 0)], v[pair_index<LAYOUT>(st >> 1, 2 * (st & 1) + 1, 1)], hi.y, lo.y);
+                            *reinterpret_cast<uint2*>(dst + st * NT * 256) = hi;
+                            *reinterpret_cast<uint2*>(dst + st * NT * 256 + 32) = lo;
+                        }
                     }
                 }
                 __syncthreads();
             }
-            for (int first = c0 + warp; first < c1; first += kPrefetch * WARPS) {
-                if (first != c0 + warp) fetch(first);
+            for (int first = c0 + wk; first < c1; first += PF * WK) {
+                if (first != c0 + wk) fetch(first);
 #pragma unroll
-                for (int i = 0; i < kPrefetch; ++i) {
-                    const int blk = first + i * WARPS;
+                for (int i = 0; i < PF; ++i) {
+                    const int blk = first + i * WK;
                     if (blk < c1) {
                         uint32_t ma = 0, mb = 0;
                         if (LAYOUT == A16_NVFP4) {
-                            const float fa = ue4m3_to_f32(__float_as_uint(sa[i])) * 0x1p117f, fb = ue4m3_to_f32(__float_as_uint(sb[i])) * 0x1p117f;
+                            const float fa = ue4m3_to_f32(sa[i]) * 0x1p117f, fb = ue4m3_to_f32(sb[i]) * 0x1p117f;
                             ma = __float_as_uint(fa) >> 16; ma |= ma << 16;      // 4 significant bits: exact in bf16
                             mb = __float_as_uint(fb) >> 16; mb |= mb << 16;
                         }
@@ -214,7 +244,7 @@ __global__ void __launch_bounds__(32 * WARPS) linear_a16_kernel(const LinearA16P
                                 mma_bf16(c[t], a0, a1, a2, a3, b.x, b.y);
                             }
                         }
-                        const float ga = (LAYOUT == A16_NVFP4) ? 1.0f : sa[i], gb = (LAYOUT == A16_NVFP4) ? 1.0f : sb[i];
+                        const float ga = (LAYOUT == A16_NVFP4) ? 1.0f : __uint_as_float(sa[i]), gb = (LAYOUT == A16_NVFP4) ? 1.0f : __uint_as_float(sb[i]);
 #pragma unroll
                         for (int t = 0; t < NT; ++t) {
                             acc[t][0] = fmaf(c[t][0], ga, acc[t][0]);
@@ -226,7 +256,8 @@ __global__ void __launch_bounds__(32 * WARPS) linear_a16_kernel(const LinearA16P
                 }
             }
         }
-        // hi and lo of row 4 t + q are the two columns this lane holds; the warps' sums in warp order
+        if (!waited) { pdl_wait(); waited = true; }        // (a CTA without input channels of its own)
+        // hi and lo of row 4 t + q are the two columns this lane holds; the warps' sums in warp order, the CTAs' in rank order
         __syncthreads();                                                        // readers of `red` of the tile before
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
@@ -234,66 +265,87 @@ __global__ void __launch_bounds__(32 * WARPS) linear_a16_kernel(const LinearA16P
             red[warp][4 * t + q][g + 8] = acc[t][2] + acc[t][3];
         }
         __syncthreads();
-        for (int o = tid; o < 16 * p.M; o += THREADS) {
-            const int m = o >> 4, n = o & 15;
+        for (int o = tid; o < 16 * KS * p.M; o += THREADS) {
+            const int n = o & 15, t = (o >> 4) % KS, m = (o >> 4) / KS;
             float sum = 0.0f;
 #pragma unroll
-            for (int w = 0; w < WARPS; ++w) sum += red[w][m][n];
-            const float b = p.bias != nullptr ? __ldg(p.bias + n0 + n) : 0.0f;
-            p.Y[static_cast<size_t>(m) * p.ldy + n0 + n] = __bfloat16_as_ushort(__float2bfloat16_rn(fmaf(sum, out_scale, b)));
+            for (int w = 0; w < WK; ++w) sum += red[w * KS + t][m][n];
+            if (KS > 1) {
+                part[t][m][n] = sum;
+            } else {
+                const float b = p.bias != nullptr ? __ldg(p.bias + tile * 16 + n) : 0.0f;
+                p.Y[static_cast<size_t>(m) * p.ldy + tile * 16 + n] = __bfloat16_as_ushort(__float2bfloat16_rn(fmaf(sum, out_scale, b)));
+            }
+        }
+        if (KS > 1) {
+            cluster_sync_all();
+            for (int o = tid; o < 16 * p.M; o += THREADS) {                     // rank r finishes the r-th 16 channels
+                const int n = o & 15, m = o >> 4, col = (tile * KS + rank) * 16 + n;
+                float sum = 0.0f;
+#pragma unroll
+                for (int r = 0; r < KS; ++r) sum += ld_dsmem(&part[rank][m][n], r);
+                const float b = p.bias != nullptr ? __ldg(p.bias + col) : 0.0f;
+                p.Y[static_cast<size_t>(m) * p.ldy + col] = __bfloat16_as_ushort(__float2bfloat16_rn(fmaf(sum, out_scale, b)));
+            }
+            cluster_sync_all();                                                 // the peers have read `part`
         }
     }
 }
 
 constexpr int kMaxSmem = 200 * 1024;
 
-template <int LAYOUT, int NT, int WARPS>
+template <int LAYOUT, int NT, int KS>
 cudaError_t launch_one(LinearA16Params p, int sm_count, cudaStream_t st)
 {
-    constexpr int kBlockBytes = 4 * NT * 256 + 32;
-    const int n_blocks = p.K >> 6;
+    using C = A16Cfg<LAYOUT, NT, KS>;
+    const int n_blocks = ((p.K >> 6) + KS - 1) / KS;
     // all of v when it fits, else equal chunks
-    int chunk = kMaxSmem / kBlockBytes;
+    int chunk = kMaxSmem / C::kBlockBytes;
     if (n_blocks <= chunk) chunk = n_blocks;
     else chunk = (n_blocks + (n_blocks + chunk - 1) / chunk - 1) / ((n_blocks + chunk - 1) / chunk);
     p.chunk = chunk;
-    const int smem = chunk * kBlockBytes;
-    int per_sm = 220 * 1024 / (smem + WARPS * 4 * NT * 17 * 4 + 1024);
-    const int by_threads = 2048 / (32 * WARPS) / 2;                               // half of the register file's threads at 64 registers each
+    const int smem = chunk * C::kBlockBytes;
+    int per_sm = 220 * 1024 / (smem + (C::WARPS + KS) * 4 * NT * 17 * 4 + 1024);
+    const int by_threads = 1024 / C::THREADS;                                     // 64 registers a thread at the least
     if (per_sm > by_threads) per_sm = by_threads;
     if (per_sm < 1) per_sm = 1;
-    const int tiles = p.N >> 4;
-    int blocks = tiles < sm_count * per_sm ? tiles : sm_count * per_sm;
+    const int tiles = p.N / (16 * KS);
+    const int most = sm_count * per_sm / KS;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(blocks), 1, 1);
-    cfg.blockDim = dim3(32 * WARPS, 1, 1);
+    cfg.gridDim = dim3(static_cast<unsigned>((tiles < most ? tiles : most) * KS), 1, 1);
+    cfg.blockDim = dim3(C::THREADS, 1, 1);
     cfg.dynamicSmemBytes = static_cast<size_t>(smem);
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = KS; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, linear_a16_kernel<LAYOUT, NT, WARPS>, p);
+    cfg.numAttrs = KS > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, linear_a16_kernel<LAYOUT, NT, KS>, p);
 }
+#ifndef A16_SPLIT
+#define A16_SPLIT 8192
+#endif
 template <int LAYOUT, int NT>
-cudaError_t launch_warps(const LinearA16Params& p, int sm_count, cudaStream_t st)
+cudaError_t launch_split(const LinearA16Params& p, int sm_count, cudaStream_t st)
 {
-    return p.K >= 4096 ? launch_one<LAYOUT, NT, 16>(p, sm_count, st) : launch_one<LAYOUT, NT, 8>(p, sm_count, st);
+    return p.M * p.K >= A16_SPLIT ? launch_one<LAYOUT, NT, 4>(p, sm_count, st) : launch_one<LAYOUT, NT, 1>(p, sm_count, st);
 }
 template <int LAYOUT>
 cudaError_t launch_layout(const LinearA16Params& p, int sm_count, cudaStream_t st)
 {
-    if (p.M <= 4) return launch_warps<LAYOUT, 1>(p, sm_count, st);
-    if (p.M <= 8) return launch_warps<LAYOUT, 2>(p, sm_count, st);
-    return launch_warps<LAYOUT, 4>(p, sm_count, st);
+    if (p.M <= 4) return launch_split<LAYOUT, 1>(p, sm_count, st);
+    if (p.M <= 8) return launch_split<LAYOUT, 2>(p, sm_count, st);
+    return launch_split<LAYOUT, 4>(p, sm_count, st);
 }
 template <int LAYOUT, int NT>
 cudaError_t init_one()
 {
-    cudaError_t e = cudaFuncSetAttribute(linear_a16_kernel<LAYOUT, NT, 8>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
+    cudaError_t e = cudaFuncSetAttribute(linear_a16_kernel<LAYOUT, NT, 1>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
     if (e != cudaSuccess) return e;
-    return cudaFuncSetAttribute(linear_a16_kernel<LAYOUT, NT, 16>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
+    return cudaFuncSetAttribute(linear_a16_kernel<LAYOUT, NT, 4>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxSmem);
 }
 template <int LAYOUT>
 cudaError_t init_layout()
