@@ -165,7 +165,7 @@ rudder_status rudder_linear_a16(const rudder_weight* w, const uint16_t* X, int64
 {
     if (!w || !X || !Y) return RUDDER_ERR_ARG;
     if (!on_weights_device(w)) return RUDDER_ERR_ARG;
-    if (M < 1 || M > 16) return RUDDER_ERR_SHAPE;
+    if (M < 1 || M > 16 || !linear_a16_fits(w->K)) return RUDDER_ERR_SHAPE;
     if (!aligned(X, 16) || !aligned(Y, 16) || ldx % 8 != 0 || ldy % 8 != 0 || ldx < w->K || ldy < w->N || (bias && !aligned(bias, 16))) return RUDDER_ERR_ALIGN;
     rudder_status s = ensure_paged_init();
     if (s != RUDDER_OK) return s;

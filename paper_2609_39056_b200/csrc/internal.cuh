@@ -186,6 +186,7 @@ cudaError_t attention_paged_init();
 size_t attention_workspace_bytes(int max_rows, int head_dim, int sm_count);
 cudaError_t launch_attention_paged(const AttnArgs& a, void* workspace, int sm_count, cudaStream_t st);
 cudaError_t linear_a16_init();
+bool linear_a16_fits(int K);              // the widest layer whose rows fit in shared memory
 cudaError_t launch_linear_a16(const rudder_weight* w, const uint16_t* X, int64_t ldx, int M, const float* bias, uint16_t* Y, int64_t ldy, int sm_count,
                               cudaStream_t st);
 

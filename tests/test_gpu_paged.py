@@ -414,7 +414,7 @@ def test_attention_output_over_queries(rd):
 A16 = [("w4a8", 64), ("w4a8", 128), ("w4a8", 0), ("w4a4", 64), ("w4a4", 128), ("w4a4", 0), ("nvfp4", 16)]
 
 
-@pytest.mark.parametrize("K,N", [(256, 64), (768, 320), (2048, 2048), (4608, 192), (8192, 128), (14336, 64)])
+@pytest.mark.parametrize("K,N", [(256, 64), (768, 320), (2048, 2048), (4608, 192), (8192, 128), (14336, 64), (18432, 64)])
 @pytest.mark.parametrize("scheme,group", A16)
 def test_linear_a16(rd, scheme, group, K, N):
     rng = np.random.default_rng(K + N)
@@ -454,6 +454,10 @@ def test_linear_a16_refusals(rd):
     for bad in ((p + 2, 128, None, o, 64), (p, 120, None, o, 64), (p, 132, None, o, 64), (p, 128, None, o + 8, 64), (p, 128, None, o, 56), (p, 128, p + 4, o, 64)):
         assert L.rudder_linear_a16(h, bad[0], bad[1], 1, bad[2], bad[3], bad[4], None) == rd.ERR_ALIGN
     assert (y == 0).all().item()
+    wide = rd.rudder_pack_weights(torch.randn(64, 36864 + 128, device="cuda"), None, rd.W4A8_INT, 64)
+    with pytest.raises(rd.RudderError) as e:
+        rd.rudder_linear_a16(wide, torch.zeros((1, wide.K), dtype=torch.bfloat16, device="cuda"))
+    assert e.value.status == rd.ERR_SHAPE
 
 
 def test_arguments_on_another_device_are_refused(rd):
