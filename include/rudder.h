@@ -328,7 +328,9 @@ rudder_status rudder_page_tables(const rudder_page_table_args* args, void* strea
  * its first `rot` channels the pairs (i, i + rot/2) (RUDDER_ROPE_HALF) or (2i, 2i + 1) (RUDDER_ROPE_PAIRS) become
  * (y_i c - y_j s, y_j c + y_i s), c and s the entry i of row positions[m] of the tables.  Q = bf16 of the result; K likewise, or in
  * the cache at slots[m] (bf16, or E4M3 of value x (1 / scale), saturating); V = the values unchanged, cache only.
- * Bit-defined: fp32, every operation rounded once, sums of squares by lanes of 8 channels combined by the exchange l ^ D/16 .. 1.
+ * Bit-defined: fp32, every operation rounded once.  Sum of squares: D / 8 lanes of 8 channels -- lane l < rot / 8 the channels 4l .. 4l + 3
+ * and the same + rot/2 with RUDDER_ROPE_HALF, else 8 neighbours -- each its even places in order, its odd places in order, then
+ * the two; the lanes combined by the exchange l ^ D/16, .., 1.
  * A row with positions[m] < 0 is padding and left as it was; one with slots[m] < 0 is not appended.  Slots of one call are
  * distinct (which of two equal ones stays is not defined).  Q may be X itself (same leading dimension) and K the keys' place in X. */
 typedef enum { RUDDER_ROPE_HALF = 0, RUDDER_ROPE_PAIRS = 1 } rudder_rope_style;

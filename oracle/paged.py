@@ -35,18 +35,24 @@ def page_tables(old, new, free, table, page, capacity):
     return table, slots, positions, starts.astype(np.int32), taken
 
 
-def head_norm(x, w, eps):
-    """RMS norm of [..., D] fp32 in the order of the kernel: lanes of 8 channels, sums combined by the exchange l ^ D/16, ..., 1."""
+def head_norm(x, w, eps, rot=0, pairs=True):
+    """RMS norm of [..., D] fp32 in the order of the kernel: lanes of 8 channels (both members of its half-split pairs in one lane), a lane's
+    even and odd places on their own, the lanes combined by the exchange l ^ D/16, ..., 1."""
     D = x.shape[-1]
-    sq = (x * x).astype(F).reshape(*x.shape[:-1], D // 8, 8)
-    s = sq[..., 0]
-    for i in range(1, 8):
-        s = (s + sq[..., i]).astype(F)
-    o = D // 16
+    place = np.arange(D).reshape(D // 8, 8)
+    if rot and not pairs:
+        for l in range(rot // 8):
+            place[l] = np.concatenate([np.arange(4 * l, 4 * l + 4), rot // 2 + np.arange(4 * l, 4 * l + 4)])
+    sq = (x * x).astype(F)[..., place]
+    e, o = sq[..., 0], sq[..., 1]
+    for i in range(1, 4):
+        e, o = (e + sq[..., 2 * i]).astype(F), (o + sq[..., 2 * i + 1]).astype(F)
+    s = (e + o).astype(F)
+    d = D // 16
     lanes = np.arange(D // 8)
-    while o:
-        s = (s + s[..., lanes ^ o]).astype(F)
-        o >>= 1
+    while d:
+        s = (s + s[..., lanes ^ d]).astype(F)
+        d >>= 1
     mean = (s[..., :1] * F(1.0 / D)).astype(F)
     with np.errstate(divide="ignore", invalid="ignore"):
         r = (F(1) / np.sqrt((mean + F(eps)).astype(F)).astype(F)).astype(F)
@@ -72,7 +78,7 @@ def qk_norm_rope(x, heads, kv_heads, D, qw, kw, eps, cos, sin, rot, pairs, posit
     M = x.shape[0]
     x = x.reshape(M, heads + 2 * kv_heads, D).astype(F)
     q, k, v = x[:, :heads], x[:, heads:heads + kv_heads], x[:, heads + kv_heads:]
-    q, k = head_norm(q, qw, eps), head_norm(k, kw, eps)
+    q, k = head_norm(q, qw, eps, rot, pairs), head_norm(k, kw, eps, rot, pairs)
     if rot:
         at = np.maximum(positions, 0)
         q, k = rotate(q, cos[at], sin[at], rot, pairs), rotate(k, cos[at], sin[at], rot, pairs)

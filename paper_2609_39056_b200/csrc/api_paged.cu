@@ -60,7 +60,7 @@ rudder_status check_qk(const rudder_qk_args* a, QkArgs* out)
     if (to_cache ? (!a->slots || a->K) : (!a->K || a->slots)) return RUDDER_ERR_ARG;          // keys go to the cache or to K, not both
     if (!(a->eps >= 0.0f)) return RUDDER_ERR_ARG;
     if (a->style != RUDDER_ROPE_HALF && a->style != RUDDER_ROPE_PAIRS) return RUDDER_ERR_UNSUPPORTED;
-    if (a->M < 1 || a->heads < 1 || a->kv_heads < 1 || a->heads > 1024 || a->kv_heads > 1024 || !head_dim_ok(a->head_dim)) return RUDDER_ERR_SHAPE;
+    if (a->M < 1 || a->heads < 1 || a->kv_heads < 1 || a->heads > 1024 || a->kv_heads > kMaxKvHeads || !head_dim_ok(a->head_dim)) return RUDDER_ERR_SHAPE;
     if (a->rot < 0 || a->rot > a->head_dim || a->rot % 16 != 0) return RUDDER_ERR_SHAPE;
     if (a->rot > 0 && (!a->cos || !a->sin || !a->positions || a->n_pos < 1)) return RUDDER_ERR_ARG;
     const int64_t width = static_cast<int64_t>(a->heads + 2 * a->kv_heads) * a->head_dim;
@@ -76,7 +76,7 @@ rudder_status check_qk(const rudder_qk_args* a, QkArgs* out)
         if (s != RUDDER_OK) return s;
     }
     o.X = a->X; o.ldx = a->ldx; o.M = a->M; o.heads = a->heads; o.kv_heads = a->kv_heads;
-    o.q_weight = a->q_weight; o.k_weight = a->k_weight; o.eps = a->eps;
+    o.q_weight = a->q_weight; o.k_weight = a->k_weight; o.eps = a->eps; o.one = 1.0f;
     o.cos = a->cos; o.sin = a->sin; o.n_pos = a->n_pos; o.rot = a->rot; o.pairs = a->style == RUDDER_ROPE_PAIRS;
     o.positions = a->positions; o.Q = a->Q; o.ldq = a->ldq; o.K = a->K; o.ldk = a->ldk; o.slots = a->slots;
     *out = o;

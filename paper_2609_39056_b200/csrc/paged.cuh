@@ -32,10 +32,13 @@ struct CacheParams {
     int n_pages, page_shift;
 };
 
+constexpr int kMaxKvHeads = 1024;
+
 struct QkArgs {
     const uint16_t* X; int64_t ldx; int M;
     int heads, kv_heads;
     const float* q_weight; const float* k_weight; float eps;
+    float one;                            // 1, see add2 in qk_norm_rope.cu
     const float* cos; const float* sin; int n_pos, rot;
     bool pairs;
     const int32_t* positions;             // or nullptr: every row is real (rot = 0)

@@ -7,14 +7,15 @@
 //     Q <- bf16(u), K <- bf16(u) or e4m3(u (1 / k_scale)), V <- x or e4m3(x (1 / v_scale))
 //
 // Every operation is a single correctly rounded fp32 add, multiply, divide or square root in the order written here
-// (no fused multiply-add), rounded once to the output type: bit-defined like the other glue.  The head's sum of
-// squares: lane l of the D / 8 lanes that hold the head adds its 8 squares in channel order, the lanes' sums are
-// combined by the exchange with l ^ (D / 16), ..., 2, 1.
+// (no fused multiply-add), rounded once to the output type: bit-defined like the other glue.  A head is held by D / 8 lanes of 8
+// channels, two runs of four: lane l < rot / 8 has 4 l .. 4 l + 3 and the same + rot / 2 with half-split pairs (both members of its
+// pairs), every other lane 8 neighbours.  A lane adds the squares of its even and of its odd places in order, then the
+// two; the lanes' sums are combined by the exchange with l ^ (D / 16), ..., 2, 1.
 //
-// Bound by HBM for long inputs (each row is read once and written once) and by one chain of dependent loads
-// (position -> angles) for a few rows.  D / 8 lanes per head, 16 bytes per lane: every access of a head is one
-// contiguous run.  A CTA takes one row at a time; a thread keeps its place l inside the head for all the heads it
-// handles, so angles and norm weights are read once per row and thread, not once per head.
+// Bound by HBM for long inputs (each row is read once and written once), by issue slots close behind it, and by one chain of dependent
+// loads (position -> angles) for a few rows.  Hence two-lane arithmetic (f32x2: the same roundings, half the instructions), both members of
+// a pair in one lane (no exchange), angles read once per row and thread for all its heads, and four steps of loads in flight.
+// Every access of a head is one or two contiguous runs.
 #include "internal.cuh"
 #include "paged.cuh"
 
@@ -31,64 +32,54 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-__device__ __forceinline__ uint32_t pack_e4m3x4(float a, float b, float c, float d) {
+// Two fp32 numbers in one register pair; each operation rounds both on their own.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 make2(float a, float b) {
+    f32x2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 split(f32x2 v) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+// a + b as a 1 + b with a 1 that the compiler does not know (a kernel argument): a two-lane addition is merged with the
+// multiplication in front of it into one operation with one rounding, .rn or not (seen: results one bf16 step off the defined bits).
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b, f32x2 one) {
+    f32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(one), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 widen(uint32_t w) { return make2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)); }
+__device__ __forceinline__ f32x2 swap2(f32x2 v) { const float2 t = split(v); return make2(t.y, t.x); }
+__device__ __forceinline__ uint32_t to_bf16(f32x2 v) { const float2 t = split(v); return pack_bf16(t.x, t.y); }
+__device__ __forceinline__ uint32_t to_e4m3(f32x2 a, f32x2 b) {
+    const float2 s = split(a), t = split(b);
     uint16_t lo, hi;
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(b), "f"(a));
-    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(d), "f"(c));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(s.y), "f"(s.x));
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(t.y), "f"(t.x));
     return static_cast<uint32_t>(lo) | (static_cast<uint32_t>(hi) << 16);
 }
-__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
-    const float4 a = __ldg(reinterpret_cast<const float4*>(p)), b = __ldg(reinterpret_cast<const float4*>(p) + 1);
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-}
-
-// Heads of one kind that a CTA takes in one step, 8 channels per lane: see the kernel below.
-struct QkLane {
-    float c[8], s[8];                                      // angles of this lane's channels
-    int partner;                                           // half-split pairs: the lane with the other channels
-    float sign;
-    bool turns;
-};
-
-// x r w of one head, its sum of squares over the LPH lanes that hold it, and the rotation.
-template <int D, bool PAIRS>
-__device__ __forceinline__ void norm_and_turn(float (&y)[8], const float (&x)[8], const float (&w)[8], float eps, bool rot, const QkLane& t, int l)
-{
-    constexpr int LPH = D / 8;
-    float sum = __fmul_rn(x[0], x[0]);
-#pragma unroll
-    for (int i = 1; i < 8; ++i) sum = __fadd_rn(sum, __fmul_rn(x[i], x[i]));
-#pragma unroll
-    for (int o = LPH / 2; o > 0; o >>= 1) sum = __fadd_rn(sum, __shfl_xor_sync(0xffffffffu, sum, o));
-    const float r = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(__fmul_rn(sum, 1.0f / D), eps)));
-#pragma unroll
-    for (int i = 0; i < 8; ++i) y[i] = __fmul_rn(__fmul_rn(x[i], r), w[i]);
-    if (!rot) return;
-    if (PAIRS) {
-        if (t.turns) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float u = y[2 * i], v = y[2 * i + 1];
-                y[2 * i] = __fsub_rn(__fmul_rn(u, t.c[i]), __fmul_rn(v, t.s[i]));
-                y[2 * i + 1] = __fadd_rn(__fmul_rn(v, t.c[i]), __fmul_rn(u, t.s[i]));
-            }
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float o = __shfl_sync(0xffffffffu, y[i], t.partner, LPH);
-            if (t.turns) y[i] = __fadd_rn(__fmul_rn(y[i], t.c[i]), __fmul_rn(o, t.s[i]));     // (sign of the sine: negated where it is subtracted)
-        }
-    }
+__device__ __forceinline__ void load4(const float* p, f32x2& a, f32x2& b) {
+    const float4 v = __ldg(reinterpret_cast<const float4*>(p));
+    a = make2(v.x, v.y);
+    b = make2(v.z, v.w);
 }
 
 // D: channels of a head; PAIRS: neighbours (2i, 2i+1) are turned together, else (i, i + rot/2); E4M3: format of the cache.
 template <int D, bool PAIRS, bool E4M3>
-__global__ void __launch_bounds__(QK_THREADS, 3) qk_norm_rope_kernel(const QkArgs a)
+__global__ void __launch_bounds__(QK_THREADS, 4) qk_norm_rope_kernel(const QkArgs a)
 {
     constexpr int LPH = D / 8;                             // lanes of a head
     constexpr int HPC = QK_THREADS / LPH;                  // heads a CTA has in hand at once
-    constexpr int U = 4;                                   // steps whose loads are in flight together
+    constexpr int U = 3;                                   // steps whose loads are in flight together
+    __shared__ float s_inv[E4M3 ? 2 * kMaxKvHeads : 1];    // reciprocals of the cache's scales: keys, values
     pdl_launch_dependents();
     const int tid = threadIdx.x;
     const int l = tid & (LPH - 1), h0 = tid / LPH;
@@ -97,21 +88,31 @@ __global__ void __launch_bounds__(QK_THREADS, 3) qk_norm_rope_kernel(const QkArg
     const int n_qk = a.heads + a.kv_heads;
     const bool to_cache = a.slots != nullptr;
     const int n_heads = to_cache ? n_qk + a.kv_heads : n_qk;
-    QkLane t;
-    t.turns = 8 * l < a.rot;
-    t.partner = !t.turns ? l : (8 * l < half) ? l + (half >> 3) : l - (half >> 3);
-    const bool first = 8 * l < half;
+    const bool turns = 8 * l < a.rot;
+    // the two runs of four channels of this lane
+    const int ca = (PAIRS || !turns) ? 8 * l : 4 * l;
+    const int cb = (PAIRS || !turns) ? ca + 4 : ca + half;
     const long long n_slots = static_cast<long long>(a.cache.n_pages) << a.cache.page_shift;
-    const bool w_null_q = a.q_weight == nullptr, w_null_k = a.k_weight == nullptr;
+    if (E4M3) {
+        for (int i = tid; i < 2 * a.kv_heads; i += QK_THREADS) {
+            const float* sc = i < a.kv_heads ? a.cache.k_scale : a.cache.v_scale;
+            const int h = i < a.kv_heads ? i : i - a.kv_heads;
+            s_inv[i] = sc != nullptr ? __fdiv_rn(1.0f, __ldg(sc + h)) : 1.0f;
+        }
+        __syncthreads();
+    }
+    const uint2 zero2 = make_uint2(0, 0);
+    const f32x2 one = make2(a.one, a.one);
 
     for (int m = blockIdx.x; m < a.M; m += gridDim.x) {
-        const uint16_t* xr = a.X + static_cast<size_t>(m) * a.ldx + 8 * l;
+        const uint16_t* xr = a.X + static_cast<size_t>(m) * a.ldx;
         // the row's data does not depend on its position: both are requested together
-        uint4 x4[U];
+        uint2 xa[U], xb[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int h = h0 + u * HPC;
-            x4[u] = h < n_heads ? *reinterpret_cast<const uint4*>(xr + static_cast<size_t>(h) * D) : make_uint4(0, 0, 0, 0);
+            xa[u] = h < n_heads ? *reinterpret_cast<const uint2*>(xr + h * D + ca) : zero2;
+            xb[u] = h < n_heads ? *reinterpret_cast<const uint2*>(xr + h * D + cb) : zero2;
         }
         const int pos = a.positions != nullptr ? a.positions[m] : 0;
         long long slot = to_cache ? a.slots[m] : -1;
@@ -127,21 +128,18 @@ __global__ void __launch_bounds__(QK_THREADS, 3) qk_norm_rope_kernel(const QkArg
         const int heads = (to_cache && slot < 0) ? a.heads : n_heads;               // nothing to append: queries only
         const long long token_off = slot < 0 ? 0 : (slot >> a.cache.page_shift) * a.cache.page_stride +
                                                    (slot & ((1 << a.cache.page_shift) - 1)) * a.cache.token_stride;
-        if (t.turns) {
-            const float* cp = a.cos + static_cast<size_t>(pos) * half;
-            const float* sp = a.sin + static_cast<size_t>(pos) * half;
+        // half-split: c and s of the four pairs; neighbours: (c, c) and (-s, s) of the four pairs
+        f32x2 c[PAIRS ? 4 : 2], s[PAIRS ? 4 : 2];
+        if (turns) {
+            const float* cp = a.cos + static_cast<size_t>(pos) * half + 4 * l;
+            const float* sp = a.sin + static_cast<size_t>(pos) * half + 4 * l;
             if (PAIRS) {
-                const float4 c4 = __ldg(reinterpret_cast<const float4*>(cp) + l), s4 = __ldg(reinterpret_cast<const float4*>(sp) + l);
-                t.c[0] = c4.x; t.c[1] = c4.y; t.c[2] = c4.z; t.c[3] = c4.w;
-                t.s[0] = s4.x; t.s[1] = s4.y; t.s[2] = s4.z; t.s[3] = s4.w;
+                const float4 c4 = __ldg(reinterpret_cast<const float4*>(cp)), s4 = __ldg(reinterpret_cast<const float4*>(sp));
+                c[0] = make2(c4.x, c4.x); c[1] = make2(c4.y, c4.y); c[PAIRS ? 2 : 0] = make2(c4.z, c4.z); c[PAIRS ? 3 : 0] = make2(c4.w, c4.w);
+                s[0] = make2(-s4.x, s4.x); s[1] = make2(-s4.y, s4.y); s[PAIRS ? 2 : 0] = make2(-s4.z, s4.z); s[PAIRS ? 3 : 0] = make2(-s4.w, s4.w);
             } else {
-                const int at = first ? 8 * l : 8 * l - half;
-                load8(cp + at, t.c);
-                load8(sp + at, t.s);
-                if (first) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) t.s[i] = -t.s[i];
-                }
+                load4(cp, c[0], c[1]);
+                load4(sp, s[0], s[1]);
             }
         }
         // all lanes of a warp stay together (the exchanges): the loops run to the same bounds in every thread
@@ -150,57 +148,73 @@ __global__ void __launch_bounds__(QK_THREADS, 3) qk_norm_rope_kernel(const QkArg
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
                     const int h = hb + h0 + u * HPC;
-                    x4[u] = h < heads ? *reinterpret_cast<const uint4*>(xr + static_cast<size_t>(h) * D) : make_uint4(0, 0, 0, 0);
+                    xa[u] = h < heads ? *reinterpret_cast<const uint2*>(xr + h * D + ca) : zero2;
+                    xb[u] = h < heads ? *reinterpret_cast<const uint2*>(xr + h * D + cb) : zero2;
                 }
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int hw = hb + u * HPC;
-                if (hw >= heads) break;
-                const int h = hw + h0;
-                const uint32_t w4[4] = {x4[u].x, x4[u].y, x4[u].z, x4[u].w};
-                float x[8], y[8];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    x[2 * i] = __uint_as_float(w4[i] << 16);
-                    x[2 * i + 1] = __uint_as_float(w4[i] & 0xFFFF0000u);
-                }
+                if (hb + u * HPC >= heads) break;
+                const int h = hb + u * HPC + h0;
+                f32x2 y[4] = {widen(xa[u].x), widen(xa[u].y), widen(xb[u].x), widen(xb[u].y)};
                 // a warp whose heads are all values has nothing to compute
                 if (__any_sync(0xffffffffu, h < n_qk)) {
-                    float w[8];
-                    const bool is_q = h < a.heads;
-                    if (is_q ? w_null_q : w_null_k) {
+                    f32x2 sq = mul2(y[0], y[0]);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) w[i] = 1.0f;
-                    } else {
-                        load8((is_q ? a.q_weight : a.k_weight) + 8 * l, w);
+                    for (int i = 1; i < 4; ++i) sq = add2(mul2(y[i], y[i]), sq, one);
+                    const float2 both = split(sq);
+                    float sum = __fadd_rn(both.x, both.y);
+#pragma unroll
+                    for (int o = LPH / 2; o > 0; o >>= 1) sum = __fadd_rn(sum, __shfl_xor_sync(0xffffffffu, sum, o));
+                    const float r = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(__fmul_rn(sum, 1.0f / D), a.eps)));
+                    if (h < n_qk) {
+                        const f32x2 rr = make2(r, r);
+                        const float* wp = h < a.heads ? a.q_weight : a.k_weight;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) y[i] = mul2(y[i], rr);
+                        if (wp != nullptr) {
+                            f32x2 w[4];
+                            load4(wp + ca, w[0], w[1]);
+                            load4(wp + cb, w[2], w[3]);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) y[i] = mul2(y[i], w[i]);
+                        }
+                        if (turns) {
+                            if (PAIRS) {
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) y[i] = add2(mul2(swap2(y[i]), s[PAIRS ? i : 0]), mul2(y[i], c[PAIRS ? i : 0]), one);
+                            } else {
+#pragma unroll
+                                for (int i = 0; i < 2; ++i) {
+                                    const f32x2 p = y[i], n = y[2 + i], ns = mul2(n, s[i]);
+                                    const float2 t = split(ns);
+                                    y[i] = add2(make2(-t.x, -t.y), mul2(p, c[i]), one);
+                                    y[2 + i] = add2(mul2(p, s[i]), mul2(n, c[i]), one);
+                                }
+                            }
+                        }
                     }
-                    norm_and_turn<D, PAIRS>(y, x, w, a.eps, a.rot > 0, t, l);
                 }
                 if (h >= heads) continue;
-                if (h < a.heads) {
-                    *reinterpret_cast<uint4*>(a.Q + static_cast<size_t>(m) * a.ldq + static_cast<size_t>(h) * D + 8 * l) =
-                        make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
+                if (h < a.heads || !to_cache) {
+                    uint16_t* out = h < a.heads ? a.Q + static_cast<size_t>(m) * a.ldq + h * D : a.K + static_cast<size_t>(m) * a.ldk + (h - a.heads) * D;
+                    *reinterpret_cast<uint2*>(out + ca) = make_uint2(to_bf16(y[0]), to_bf16(y[1]));
+                    *reinterpret_cast<uint2*>(out + cb) = make_uint2(to_bf16(y[2]), to_bf16(y[3]));
                     continue;
                 }
                 const bool is_v = h >= n_qk;
                 const int kvh = is_v ? h - n_qk : h - a.heads;
-                if (!to_cache) {
-                    *reinterpret_cast<uint4*>(a.K + static_cast<size_t>(m) * a.ldk + static_cast<size_t>(kvh) * D + 8 * l) =
-                        make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
-                    continue;
-                }
-                const long long off = token_off + static_cast<long long>(kvh) * a.cache.head_stride + 8 * l;
+                const long long off = token_off + static_cast<long long>(kvh) * a.cache.head_stride;
                 uint8_t* base = is_v ? a.cache.v : a.cache.k;
                 if (E4M3) {
-                    const float* sc = is_v ? a.cache.v_scale : a.cache.k_scale;
-                    const float inv = sc != nullptr ? __fdiv_rn(1.0f, __ldg(sc + kvh)) : 1.0f;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) y[i] = __fmul_rn(is_v ? x[i] : y[i], inv);
-                    *reinterpret_cast<uint2*>(base + off) = make_uint2(pack_e4m3x4(y[0], y[1], y[2], y[3]), pack_e4m3x4(y[4], y[5], y[6], y[7]));
+                    const float iv = s_inv[is_v ? a.kv_heads + kvh : kvh];
+                    const f32x2 inv = make2(iv, iv);
+                    *reinterpret_cast<uint32_t*>(base + off + ca) = to_e4m3(mul2(y[0], inv), mul2(y[1], inv));
+                    *reinterpret_cast<uint32_t*>(base + off + cb) = to_e4m3(mul2(y[2], inv), mul2(y[3], inv));
                 } else {
-                    *reinterpret_cast<uint4*>(base + 2 * off) =
-                        is_v ? x4[u] : make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
+                    uint16_t* out = reinterpret_cast<uint16_t*>(base) + off;
+                    *reinterpret_cast<uint2*>(out + ca) = is_v ? xa[u] : make_uint2(to_bf16(y[0]), to_bf16(y[1]));
+                    *reinterpret_cast<uint2*>(out + cb) = is_v ? xb[u] : make_uint2(to_bf16(y[2]), to_bf16(y[3]));
                 }
             }
         }
@@ -218,7 +232,7 @@ cudaError_t launch_d(const QkArgs& a, bool e4m3, const cudaLaunchConfig_t& cfg)
 
 cudaError_t launch_qk_norm_rope(const QkArgs& a, int head_dim, bool e4m3, int sm_count, cudaStream_t st)
 {
-    const int cap = sm_count * 3;                          // CTAs resident at once
+    const int cap = sm_count * 4;                          // CTAs resident at once
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(a.M < cap ? a.M : cap), 1, 1);
     cfg.blockDim = dim3(QK_THREADS, 1, 1);
