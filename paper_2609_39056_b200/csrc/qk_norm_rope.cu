@@ -73,16 +73,17 @@ __device__ __forceinline__ void load4(const float* p, f32x2& a, f32x2& b) {
 }
 
 // D: channels of a head; PAIRS: neighbours (2i, 2i+1) are turned together, else (i, i + rot/2); E4M3: format of the cache.
+// `share` warps work on a row: warp p of them takes the steps p, p + share, ... of 32 / (D / 8) heads each.
 template <int D, bool PAIRS, bool E4M3>
-__global__ void __launch_bounds__(QK_THREADS, 4) qk_norm_rope_kernel(const QkArgs a)
+__global__ void __launch_bounds__(QK_THREADS, 4) qk_norm_rope_kernel(const QkArgs a, int share)
 {
     constexpr int LPH = D / 8;                             // lanes of a head
-    constexpr int HPC = QK_THREADS / LPH;                  // heads a CTA has in hand at once
-    constexpr int U = 3;                                   // steps whose loads are in flight together
+    constexpr int HPW = 32 / LPH;                          // heads of a step
+    constexpr int U = 4;                                   // steps in hand at once: their loads are in flight together
     __shared__ float s_inv[E4M3 ? 2 * kMaxKvHeads : 1];    // reciprocals of the cache's scales: keys, values
     pdl_launch_dependents();
-    const int tid = threadIdx.x;
-    const int l = tid & (LPH - 1), h0 = tid / LPH;
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int l = tid & (LPH - 1), h0 = lane / LPH;
     pdl_wait();
     const int half = a.rot >> 1;
     const int n_qk = a.heads + a.kv_heads;
@@ -103,31 +104,39 @@ __global__ void __launch_bounds__(QK_THREADS, 4) qk_norm_rope_kernel(const QkArg
     }
     const uint2 zero2 = make_uint2(0, 0);
     const f32x2 one = make2(a.one, a.one);
+    const int warp = blockIdx.x * (QK_THREADS / 32) + (tid >> 5), part = warp % share;
 
-    for (int m = blockIdx.x; m < a.M; m += gridDim.x) {
+    for (int m = warp / share; m < a.M; m += gridDim.x * (QK_THREADS / 32) / share) {
         const uint16_t* xr = a.X + static_cast<size_t>(m) * a.ldx;
         // the row's data does not depend on its position: both are requested together
         uint2 xa[U], xb[U];
+        auto fetch = [&](int step, int n) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int h = h0 + u * HPC;
-            xa[u] = h < n_heads ? *reinterpret_cast<const uint2*>(xr + h * D + ca) : zero2;
-            xb[u] = h < n_heads ? *reinterpret_cast<const uint2*>(xr + h * D + cb) : zero2;
-        }
+            for (int u = 0; u < U; ++u) {
+                const int h = (step + u * share) * HPW + h0;
+                xa[u] = h < n ? *reinterpret_cast<const uint2*>(xr + h * D + ca) : zero2;
+                xb[u] = h < n ? *reinterpret_cast<const uint2*>(xr + h * D + cb) : zero2;
+            }
+        };
+        fetch(part, n_heads);
         const int pos = a.positions != nullptr ? a.positions[m] : 0;
         long long slot = to_cache ? a.slots[m] : -1;
         if (pos < 0) continue;                             // a row of padding: left as it was
         if (a.rot > 0 && pos >= a.n_pos) {
-            if (tid == 0) record_bad_data(kBadPosition);
+            if (lane == 0) record_bad_data(kBadPosition);
             continue;
         }
         if (slot >= n_slots) {
-            if (tid == 0) record_bad_data(kBadSlot);
+            if (lane == 0) record_bad_data(kBadSlot);
             slot = -1;
         }
         const int heads = (to_cache && slot < 0) ? a.heads : n_heads;               // nothing to append: queries only
         const long long token_off = slot < 0 ? 0 : (slot >> a.cache.page_shift) * a.cache.page_stride +
                                                    (slot & ((1 << a.cache.page_shift) - 1)) * a.cache.token_stride;
+        uint16_t* const q_row = a.Q + static_cast<size_t>(m) * a.ldq;
+        uint16_t* const k_row = to_cache ? nullptr : a.K + static_cast<size_t>(m) * a.ldk;
+        uint8_t* const k_tok = a.cache.k + (E4M3 ? 1 : 2) * token_off;
+        uint8_t* const v_tok = a.cache.v + (E4M3 ? 1 : 2) * token_off;
         // half-split: c and s of the four pairs; neighbours: (c, c) and (-s, s) of the four pairs
         f32x2 c[PAIRS ? 4 : 2], s[PAIRS ? 4 : 2];
         if (turns) {
@@ -142,70 +151,73 @@ __global__ void __launch_bounds__(QK_THREADS, 4) qk_norm_rope_kernel(const QkArg
                 load4(sp, s[0], s[1]);
             }
         }
-        // all lanes of a warp stay together (the exchanges): the loops run to the same bounds in every thread
-        for (int hb = 0; hb < heads; hb += U * HPC) {
-            if (hb > 0) {
+        // all lanes of a warp stay together (the exchanges): the loops run to the same bounds in every lane
+        for (int step = part; step * HPW < heads; step += U * share) {
+            if (step != part) fetch(step, heads);
+            float rr[U];
+            if (step * HPW < n_qk) {                       // (else only values: nothing to compute)
+                float sum[U];
 #pragma unroll
                 for (int u = 0; u < U; ++u) {
-                    const int h = hb + h0 + u * HPC;
-                    xa[u] = h < heads ? *reinterpret_cast<const uint2*>(xr + h * D + ca) : zero2;
-                    xb[u] = h < heads ? *reinterpret_cast<const uint2*>(xr + h * D + cb) : zero2;
-                }
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (hb + u * HPC >= heads) break;
-                const int h = hb + u * HPC + h0;
-                f32x2 y[4] = {widen(xa[u].x), widen(xa[u].y), widen(xb[u].x), widen(xb[u].y)};
-                // a warp whose heads are all values has nothing to compute
-                if (__any_sync(0xffffffffu, h < n_qk)) {
+                    const f32x2 y[4] = {widen(xa[u].x), widen(xa[u].y), widen(xb[u].x), widen(xb[u].y)};
                     f32x2 sq = mul2(y[0], y[0]);
 #pragma unroll
                     for (int i = 1; i < 4; ++i) sq = add2(mul2(y[i], y[i]), sq, one);
                     const float2 both = split(sq);
-                    float sum = __fadd_rn(both.x, both.y);
+                    sum[u] = __fadd_rn(both.x, both.y);
+                }
 #pragma unroll
-                    for (int o = LPH / 2; o > 0; o >>= 1) sum = __fadd_rn(sum, __shfl_xor_sync(0xffffffffu, sum, o));
-                    const float r = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(__fmul_rn(sum, 1.0f / D), a.eps)));
-                    if (h < n_qk) {
-                        const f32x2 rr = make2(r, r);
-                        const float* wp = h < a.heads ? a.q_weight : a.k_weight;
+                for (int o = LPH / 2; o > 0; o >>= 1)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) y[i] = mul2(y[i], rr);
-                        if (wp != nullptr) {
-                            f32x2 w[4];
-                            load4(wp + ca, w[0], w[1]);
-                            load4(wp + cb, w[2], w[3]);
+                    for (int u = 0; u < U; ++u) sum[u] = __fadd_rn(sum[u], __shfl_xor_sync(0xffffffffu, sum[u], o));
+                // the division and the square root once for the four steps: lane 4 i + u of a head does the head's step u
+                const float mine = (lane & 2) ? ((lane & 1) ? sum[3] : sum[2]) : ((lane & 1) ? sum[1] : sum[0]);
+                const float r = __fdiv_rn(1.0f, __fsqrt_rn(__fadd_rn(__fmul_rn(mine, 1.0f / D), a.eps)));
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) y[i] = mul2(y[i], w[i]);
-                        }
-                        if (turns) {
-                            if (PAIRS) {
+                for (int u = 0; u < U; ++u) rr[u] = __shfl_sync(0xffffffffu, r, (lane & ~3) | u);
+            }
 #pragma unroll
-                                for (int i = 0; i < 4; ++i) y[i] = add2(mul2(swap2(y[i]), s[PAIRS ? i : 0]), mul2(y[i], c[PAIRS ? i : 0]), one);
-                            } else {
+            for (int u = 0; u < U; ++u) {
+                const int h = (step + u * share) * HPW + h0;
+                if (h >= heads) break;
+                f32x2 y[4] = {widen(xa[u].x), widen(xa[u].y), widen(xb[u].x), widen(xb[u].y)};
+                if (h < n_qk) {
+                    const f32x2 r2 = make2(rr[u], rr[u]);
+                    const float* wp = h < a.heads ? a.q_weight : a.k_weight;
 #pragma unroll
-                                for (int i = 0; i < 2; ++i) {
-                                    const f32x2 p = y[i], n = y[2 + i], ns = mul2(n, s[i]);
-                                    const float2 t = split(ns);
-                                    y[i] = add2(make2(-t.x, -t.y), mul2(p, c[i]), one);
-                                    y[2 + i] = add2(mul2(p, s[i]), mul2(n, c[i]), one);
-                                }
+                    for (int i = 0; i < 4; ++i) y[i] = mul2(y[i], r2);
+                    if (wp != nullptr) {
+                        f32x2 w[4];
+                        load4(wp + ca, w[0], w[1]);
+                        load4(wp + cb, w[2], w[3]);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) y[i] = mul2(y[i], w[i]);
+                    }
+                    if (turns) {
+                        if (PAIRS) {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) y[i] = add2(mul2(swap2(y[i]), s[PAIRS ? i : 0]), mul2(y[i], c[PAIRS ? i : 0]), one);
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) {
+                                const f32x2 p = y[i], n = y[2 + i], ns = mul2(n, s[i]);
+                                const float2 t = split(ns);
+                                y[i] = add2(make2(-t.x, -t.y), mul2(p, c[i]), one);
+                                y[2 + i] = add2(mul2(p, s[i]), mul2(n, c[i]), one);
                             }
                         }
                     }
-                }
-                if (h >= heads) continue;
-                if (h < a.heads || !to_cache) {
-                    uint16_t* out = h < a.heads ? a.Q + static_cast<size_t>(m) * a.ldq + h * D : a.K + static_cast<size_t>(m) * a.ldk + (h - a.heads) * D;
-                    *reinterpret_cast<uint2*>(out + ca) = make_uint2(to_bf16(y[0]), to_bf16(y[1]));
-                    *reinterpret_cast<uint2*>(out + cb) = make_uint2(to_bf16(y[2]), to_bf16(y[3]));
-                    continue;
+                    if (h < a.heads || !to_cache) {
+                        uint16_t* out = h < a.heads ? q_row + h * D : k_row + (h - a.heads) * D;
+                        *reinterpret_cast<uint2*>(out + ca) = make_uint2(to_bf16(y[0]), to_bf16(y[1]));
+                        *reinterpret_cast<uint2*>(out + cb) = make_uint2(to_bf16(y[2]), to_bf16(y[3]));
+                        continue;
+                    }
                 }
                 const bool is_v = h >= n_qk;
                 const int kvh = is_v ? h - n_qk : h - a.heads;
-                const long long off = token_off + static_cast<long long>(kvh) * a.cache.head_stride;
-                uint8_t* base = is_v ? a.cache.v : a.cache.k;
+                const long long off = static_cast<long long>(kvh) * a.cache.head_stride;
+                uint8_t* const base = is_v ? v_tok : k_tok;
                 if (E4M3) {
                     const float iv = s_inv[is_v ? a.kv_heads + kvh : kvh];
                     const f32x2 inv = make2(iv, iv);
@@ -217,24 +229,36 @@ __global__ void __launch_bounds__(QK_THREADS, 4) qk_norm_rope_kernel(const QkArg
                     *reinterpret_cast<uint2*>(out + cb) = is_v ? xb[u] : make_uint2(to_bf16(y[2]), to_bf16(y[3]));
                 }
             }
+            __syncwarp();
         }
     }
 }
 
 template <int D>
-cudaError_t launch_d(const QkArgs& a, bool e4m3, const cudaLaunchConfig_t& cfg)
+cudaError_t launch_d(const QkArgs& a, bool e4m3, const cudaLaunchConfig_t& cfg, int share)
 {
-    if (a.pairs) return e4m3 ? cudaLaunchKernelEx(&cfg, qk_norm_rope_kernel<D, true, true>, a) : cudaLaunchKernelEx(&cfg, qk_norm_rope_kernel<D, true, false>, a);
-    return e4m3 ? cudaLaunchKernelEx(&cfg, qk_norm_rope_kernel<D, false, true>, a) : cudaLaunchKernelEx(&cfg, qk_norm_rope_kernel<D, false, false>, a);
+    if (a.pairs) return e4m3 ? cudaLaunchKernelEx(&cfg, qk_norm_rope_kernel<D, true, true>, a, share) : cudaLaunchKernelEx(&cfg, qk_norm_rope_kernel<D, true, false>, a, share);
+    return e4m3 ? cudaLaunchKernelEx(&cfg, qk_norm_rope_kernel<D, false, true>, a, share) : cudaLaunchKernelEx(&cfg, qk_norm_rope_kernel<D, false, false>, a, share);
 }
 
 }  // namespace
 
 cudaError_t launch_qk_norm_rope(const QkArgs& a, int head_dim, bool e4m3, int sm_count, cudaStream_t st)
 {
-    const int cap = sm_count * 4;                          // CTAs resident at once
+    constexpr int kWarps = QK_THREADS / 32;
+    // Warps that share a row.  A row costs a warp about 4 steps before its first head; up to one warp per slot (32 per SM) everything runs
+    // at once, beyond that in proportion: the share with the least (4 + steps / share) x max(1, rows x share / slots).  Measured, 48 heads of
+    // 128: 1024 rows 18.7, 11.7, 7.7, 8.2 us with 1, 2, 4, 8 warps, 3000 rows 24.3, 20.5, 20.7, 24.2 us, 17000 rows 78, 79, 92, 122 us.
+    const int steps = (a.heads + 2 * a.kv_heads) * head_dim / 256;
+    int share = 1;
+    double best = 0.0;
+    for (int s = 1; s <= 32 && (s == 1 || s <= steps); s *= 2) {
+        const double load = static_cast<double>(a.M) * s / (sm_count * 32.0), cost = (4.0 + static_cast<double>(steps) / s) * (load > 1.0 ? load : 1.0);
+        if (s == 1 || cost < best) { best = cost; share = s; }
+    }
+    const long long need = (static_cast<long long>(a.M) * share + kWarps - 1) / kWarps;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(a.M < cap ? a.M : cap), 1, 1);
+    cfg.gridDim = dim3(static_cast<unsigned>(need < (1 << 20) ? need : (1 << 20)), 1, 1);
     cfg.blockDim = dim3(QK_THREADS, 1, 1);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
@@ -242,9 +266,9 @@ cudaError_t launch_qk_norm_rope(const QkArgs& a, int head_dim, bool e4m3, int sm
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (head_dim == 64) return launch_d<64>(a, e4m3, cfg);
-    if (head_dim == 128) return launch_d<128>(a, e4m3, cfg);
-    return launch_d<256>(a, e4m3, cfg);
+    if (head_dim == 64) return launch_d<64>(a, e4m3, cfg, share);
+    if (head_dim == 128) return launch_d<128>(a, e4m3, cfg, share);
+    return launch_d<256>(a, e4m3, cfg, share);
 }
 
 }  // namespace rudder
