@@ -1,0 +1,221 @@
+// What the two attention kernels share: parameters, the sequence of work units and its split into runs, small helpers.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "internal.cuh"
+#include "paged.cuh"
+
+namespace rudder {
+
+namespace {
+
+constexpr float kLn2 = 0.6931471805599453f;
+
+struct AttnParams {
+    const uint16_t* Q; int64_t ldq;
+    uint16_t* O; int64_t ldo;
+    float* lse;
+    CacheParams cache;                  // strides in BYTES here
+    const int32_t* table; int64_t ld_table;
+    const int32_t* kv_lens;
+    const int32_t* q_starts;
+    float* part_o;                      // [2 G][rows of a tile][D]
+    float2* part_ml;                    // [2 G][rows of a tile]
+    int* desc;                          // [G][8]
+    float scale_log2;
+    int max_pages, B, max_q, M, heads, kv_heads, group, causal;
+    int whole_units;                    // items of at most this many units are not cut when there is a CTA for each
+    int G;                              // CTAs
+};
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid) {
+    const int n = valid ? 16 : 0;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ float exp2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
+// Four E4M3 bytes as f16 numbers (exact): bytes 0 and 1, bytes 2 and 3.  (The conversion instruction: moving the bits by shifts and masks is
+// 7 operations instead of 2 and cost 101 instead of 86 us on 4 x 126k keys.)
+__device__ __forceinline__ void e4m3_to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
+    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(w));
+}
+// The same for bytes 0 and 2, bytes 1 and 3.
+__device__ __forceinline__ void e4m3_to_f16_split(uint32_t w, uint32_t& even, uint32_t& odd) { e4m3_to_f16(__byte_perm(w, 0, 0x3120), even, odd); }
+
+// What the kernels know of a request.
+struct Req { int len, row0, qlen; };
+__device__ __forceinline__ Req load_request(const AttnParams& p, int b) {
+    Req r;
+    const long long cap = static_cast<long long>(p.max_pages) << p.cache.page_shift;      // below 2^31 (checked on the host)
+    const int len = p.kv_lens[b];
+    r.len = static_cast<int>(len < 0 ? 0 : (len > cap ? cap : len));
+    if (p.q_starts != nullptr) {
+        const int s0 = p.q_starts[b], s1 = p.q_starts[b + 1];
+        r.row0 = min(max(s0, 0), p.M);
+        const int end = min(max(s1, r.row0), p.M);
+        r.qlen = min(end - r.row0, p.max_q);
+        if (r.len != len || r.row0 != s0 || r.row0 + r.qlen != s1) record_bad_data(kBadLength);
+    } else {
+        r.row0 = b * p.max_q;
+        r.qlen = p.max_q;
+        if (r.len != len) record_bad_data(kBadLength);
+    }
+    return r;
+}
+
+// A place in the sequence of units: request, kv head, row tile, unit inside the item, and what is left of the run from there on.
+// What starting and ending an item costs, in units (queries, merge of the warp groups, output): an item counts as its units + kItemCost,
+// the cost in front.  A cut inside the cost leaves the item whole to the run behind.
+#ifndef ITEM_COST
+#define ITEM_COST 2
+#endif
+constexpr int kItemCost = ITEM_COST;
+
+template <int ROWS, int UK>
+struct Cursor {
+    int b, h, rt, j, nt, n_rt;
+    long long left;
+    Req rq;
+    __device__ __forceinline__ void set_request(const AttnParams& p, int bb) {
+        b = bb;
+        rq = load_request(p, bb);
+        nt = max(1, (rq.len + UK - 1) / UK);
+        n_rt = (rq.qlen * p.group + ROWS - 1) / ROWS;
+    }
+    __device__ __forceinline__ void next_item(const AttnParams& p) {
+        j = 0;
+        if (++rt < n_rt) return;
+        rt = 0;
+        if (++h < p.kv_heads) return;
+        h = 0;
+        int bb = b + 1;
+        while (bb < p.B) {
+            set_request(p, bb);
+            if (n_rt > 0) break;
+            ++bb;
+        }
+    }
+    __device__ __forceinline__ void advance(const AttnParams& p) {
+        ++j;
+        if (--left <= 0 || j < nt) return;
+        left -= kItemCost;
+        if (left > 0) next_item(p);
+    }
+};
+
+// This CTA's run of units: sums over the requests (threads over consecutive requests), the place of its first unit, and the descriptor that
+// the join reads.  All threads call it; false = nothing to do.
+template <int ROWS, int UK, int THREADS>
+__device__ __forceinline__ bool start_of_run(const AttnParams& p, Cursor<ROWS, UK>& cur)
+{
+    __shared__ long long s_units[THREADS / 32];
+    __shared__ int s_items[THREADS / 32];
+    __shared__ int s_max[THREADS / 32];
+    __shared__ int s_place[4];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int per = (p.B + THREADS - 1) / THREADS;
+    const int rb0 = min(p.B, tid * per), rb1 = min(p.B, rb0 + per);
+    long long t_units = 0;
+    int t_items = 0, t_max = 0;
+    for (int b = rb0; b < rb1; ++b) {
+        const Req r = load_request(p, b);
+        const int n_rt = (r.qlen * p.group + ROWS - 1) / ROWS, nt = max(1, (r.len + UK - 1) / UK);
+        t_units += static_cast<long long>(n_rt) * p.kv_heads * (nt + kItemCost);
+        t_items += n_rt * p.kv_heads;
+        if (n_rt > 0) t_max = max(t_max, nt);
+    }
+    long long i_units = t_units;
+    int i_items = t_items;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const long long u = __shfl_up_sync(0xffffffffu, i_units, d);
+        const int v = __shfl_up_sync(0xffffffffu, i_items, d);
+        if (lane >= d) { i_units += u; i_items += v; }
+        t_max = max(t_max, __shfl_xor_sync(0xffffffffu, t_max, d));
+    }
+    if (lane == 31) { s_units[warp] = i_units; s_items[warp] = i_items; s_max[warp] = t_max; }
+    __syncthreads();
+    long long total = 0, e_units = i_units - t_units;
+    int items = 0, e_items = i_items - t_items, most = 0;
+    for (int w = 0; w < THREADS / 32; ++w) {
+        if (w < warp) { e_units += s_units[w]; e_items += s_items[w]; }
+        total += s_units[w];
+        items += s_items[w];
+        most = max(most, s_max[w]);
+    }
+    const bool whole = items <= p.G && most <= p.whole_units;
+    const long long share = whole ? 1 : (total + p.G - 1) / p.G;
+    const long long all = whole ? items : total;
+    const long long u_begin = min(all, share * blockIdx.x), u_end = min(all, u_begin + share);
+    if (u_begin >= u_end) {
+        if (tid == 0) p.desc[8 * blockIdx.x] = 0;
+        return false;
+    }
+    {
+        const long long mine0 = whole ? e_items : e_units, mine1 = mine0 + (whole ? t_items : t_units);
+        if (u_begin >= mine0 && u_begin < mine1) {         // exactly one thread
+            long long at = mine0;
+            for (int b = rb0; b < rb1; ++b) {
+                const Req r = load_request(p, b);
+                const int n_rt = (r.qlen * p.group + ROWS - 1) / ROWS, nt = whole ? 1 : max(1, (r.len + UK - 1) / UK) + kItemCost;
+                const long long here = static_cast<long long>(n_rt) * p.kv_heads * nt;
+                if (u_begin < at + here) {
+                    const long long off = u_begin - at;
+                    const int item = static_cast<int>(off / nt);
+                    s_place[0] = b;
+                    s_place[1] = item / n_rt;
+                    s_place[2] = item % n_rt;
+                    s_place[3] = static_cast<int>(off % nt);      // place inside the item, its cost included
+                    break;
+                }
+                at += here;
+            }
+        }
+    }
+    __syncthreads();
+    cur.set_request(p, s_place[0]);
+    cur.h = s_place[1]; cur.rt = s_place[2];
+    const int place = whole ? kItemCost : s_place[3];
+    cur.j = max(0, place - kItemCost);
+    cur.left = whole ? cur.nt : (u_end - u_begin) - max(0, kItemCost - place);      // of this run, from unit cur.j on
+    if (cur.left <= 0) {                                       // nothing but a part of an item's cost
+        if (tid == 0) p.desc[8 * blockIdx.x] = 0;
+        return false;
+    }
+    if (tid == 0) {
+        // the join of the item that this run starts inside belongs to its first cut, i.e. to the run behind its first owner
+        int* d = p.desc + 8 * blockIdx.x;
+        const long long unit0 = u_begin - cur.j;           // place of the item's first unit
+        const long long before = share * (static_cast<long long>(blockIdx.x) - 1);
+        const bool first_cut = !whole && cur.j > 0 && unit0 >= before;
+        d[1] = cur.h; d[2] = cur.rt; d[3] = cur.rq.row0; d[4] = cur.rq.qlen;
+        d[5] = static_cast<int>((unit0 + cur.nt - 1) / share);                   // last owner
+        d[6] = unit0 <= before + kItemCost ? 0 : 1;        // slot of the first owner's part: its run starts with this item (or inside its cost)
+        d[0] = first_cut ? 1 : 0;
+    }
+    return true;
+}
+
+}  // namespace
+
+}  // namespace rudder

@@ -26,42 +26,12 @@
 // Rounding: Q, K and V enter exactly.  E4M3 numbers are f16 numbers, Q is brought to f16
 // by a power of two per row.  Scores and sums are fp32.  The probabilities (<= 1) enter the second product as f16
 // with E4M3 values (2^-12), and as TWO bf16 numbers hi + lo (2^-17) with bf16 values where that is free or cheap (PL).
-#include "internal.cuh"
-#include "paged.cuh"
-
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
+#include "attention_rows.cu"
 
 namespace rudder {
 
 namespace {
 
-constexpr float kLn2 = 0.6931471805599453f;
-
-struct AttnParams {
-    const uint16_t* Q; int64_t ldq;
-    uint16_t* O; int64_t ldo;
-    float* lse;
-    CacheParams cache;                  // strides in BYTES here
-    const int32_t* table; int64_t ld_table;
-    const int32_t* kv_lens;
-    const int32_t* q_starts;
-    float* part_o;                      // [2 G][rows of a tile][D]
-    float2* part_ml;                    // [2 G][rows of a tile]
-    int* desc;                          // [G][8]
-    float scale_log2;
-    int max_pages, B, max_q, M, heads, kv_heads, group, causal;
-    int whole_units;                    // items of at most this many units are not cut when there is a CTA for each
-    int G;                              // CTAs
-};
-
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid) {
-    const int n = valid ? 16 : 0;
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void ldsm_x4(uint32_t (&r)[4], uint32_t addr) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
@@ -83,92 +53,6 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
-__device__ __forceinline__ float exp2_approx(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-__device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
-    uint32_t r;
-    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
-__device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
-    uint32_t r;
-    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
-__device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
-__device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
-// Four E4M3 bytes as f16 numbers (exact): bytes 0 and 1, bytes 2 and 3.  (The conversion instruction: moving the bits by shifts and masks is
-// 7 operations instead of 2 and cost 101 instead of 86 us on 4 x 126k keys.)
-__device__ __forceinline__ void e4m3_to_f16(uint32_t w, uint32_t& lo, uint32_t& hi) {
-    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(w));
-}
-// The same for bytes 0 and 2, bytes 1 and 3.
-__device__ __forceinline__ void e4m3_to_f16_split(uint32_t w, uint32_t& even, uint32_t& odd) { e4m3_to_f16(__byte_perm(w, 0, 0x3120), even, odd); }
-
-// What the kernels know of a request.
-struct Req { int len, row0, qlen; };
-__device__ __forceinline__ Req load_request(const AttnParams& p, int b) {
-    Req r;
-    const long long cap = static_cast<long long>(p.max_pages) << p.cache.page_shift;      // below 2^31 (checked on the host)
-    const int len = p.kv_lens[b];
-    r.len = static_cast<int>(len < 0 ? 0 : (len > cap ? cap : len));
-    if (p.q_starts != nullptr) {
-        const int s0 = p.q_starts[b], s1 = p.q_starts[b + 1];
-        r.row0 = min(max(s0, 0), p.M);
-        const int end = min(max(s1, r.row0), p.M);
-        r.qlen = min(end - r.row0, p.max_q);
-        if (r.len != len || r.row0 != s0 || r.row0 + r.qlen != s1) record_bad_data(kBadLength);
-    } else {
-        r.row0 = b * p.max_q;
-        r.qlen = p.max_q;
-        if (r.len != len) record_bad_data(kBadLength);
-    }
-    return r;
-}
-
-// A place in the sequence of units: request, kv head, row tile, unit inside the item, and what is left of the run from there on.
-// What starting and ending an item costs, in units (queries, merge of the warp groups, output): an item counts as its units + kItemCost,
-// the cost in front.  A cut inside the cost leaves the item whole to the run behind.
-#ifndef ITEM_COST
-#define ITEM_COST 2
-#endif
-constexpr int kItemCost = ITEM_COST;
-
-template <int ROWS, int UK>
-struct Cursor {
-    int b, h, rt, j, nt, n_rt;
-    long long left;
-    Req rq;
-    __device__ __forceinline__ void set_request(const AttnParams& p, int bb) {
-        b = bb;
-        rq = load_request(p, bb);
-        nt = max(1, (rq.len + UK - 1) / UK);
-        n_rt = (rq.qlen * p.group + ROWS - 1) / ROWS;
-    }
-    __device__ __forceinline__ void next_item(const AttnParams& p) {
-        j = 0;
-        if (++rt < n_rt) return;
-        rt = 0;
-        if (++h < p.kv_heads) return;
-        h = 0;
-        int bb = b + 1;
-        while (bb < p.B) {
-            set_request(p, bb);
-            if (n_rt > 0) break;
-            ++bb;
-        }
-    }
-    __device__ __forceinline__ void advance(const AttnParams& p) {
-        ++j;
-        if (--left <= 0 || j < nt) return;
-        left -= kItemCost;
-        if (left > 0) next_item(p);
-    }
-};
-
 // RB bytes per row of a tile: the 16-byte chunk c of row r sits at chunk swz(r, c).
 template <int RB>
 __device__ __forceinline__ uint32_t swz(int r, int c) {
@@ -216,11 +100,6 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
     static_assert(KT == 16 || KT == 32, "a lane holds the place of one key of the tile");
     static_assert(GT % CH == 0 || CH % GT == 0, "rows are copied by whole groups of lanes");
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ long long s_units[C::THREADS / 32];
-    __shared__ int s_items[C::THREADS / 32];
-    __shared__ int s_max[C::THREADS / 32];
-    __shared__ int s_place[4];
-
     pdl_launch_dependents();
     pdl_wait();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -228,88 +107,8 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
     const int kg = warp / RW, rw = warp % RW;
     const int gt = tid - kg * GT;                          // thread inside the warp group
 
-    // ---- this CTA's run of units: sums over the requests, threads over consecutive requests
-    const int per = (p.B + C::THREADS - 1) / C::THREADS;
-    const int rb0 = min(p.B, tid * per), rb1 = min(p.B, rb0 + per);
-    long long t_units = 0;
-    int t_items = 0, t_max = 0;
-    for (int b = rb0; b < rb1; ++b) {
-        const Req r = load_request(p, b);
-        const int n_rt = (r.qlen * p.group + ROWS - 1) / ROWS, nt = max(1, (r.len + UK - 1) / UK);
-        t_units += static_cast<long long>(n_rt) * p.kv_heads * (nt + kItemCost);
-        t_items += n_rt * p.kv_heads;
-        if (n_rt > 0) t_max = max(t_max, nt);
-    }
-    long long i_units = t_units;
-    int i_items = t_items;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const long long u = __shfl_up_sync(0xffffffffu, i_units, d);
-        const int v = __shfl_up_sync(0xffffffffu, i_items, d);
-        if (lane >= d) { i_units += u; i_items += v; }
-        t_max = max(t_max, __shfl_xor_sync(0xffffffffu, t_max, d));
-    }
-    if (lane == 31) { s_units[warp] = i_units; s_items[warp] = i_items; s_max[warp] = t_max; }
-    __syncthreads();
-    long long total = 0, e_units = i_units - t_units;
-    int items = 0, e_items = i_items - t_items, most = 0;
-    for (int w = 0; w < C::THREADS / 32; ++w) {
-        if (w < warp) { e_units += s_units[w]; e_items += s_items[w]; }
-        total += s_units[w];
-        items += s_items[w];
-        most = max(most, s_max[w]);
-    }
-    const bool whole = items <= p.G && most <= p.whole_units;
-    const long long share = whole ? 1 : (total + p.G - 1) / p.G;
-    const long long all = whole ? items : total;
-    const long long u_begin = min(all, share * blockIdx.x), u_end = min(all, u_begin + share);
-    if (u_begin >= u_end) {
-        if (tid == 0) p.desc[8 * blockIdx.x] = 0;
-        return;
-    }
-    {
-        const long long mine0 = whole ? e_items : e_units, mine1 = mine0 + (whole ? t_items : t_units);
-        if (u_begin >= mine0 && u_begin < mine1) {         // exactly one thread
-            long long at = mine0;
-            for (int b = rb0; b < rb1; ++b) {
-                const Req r = load_request(p, b);
-                const int n_rt = (r.qlen * p.group + ROWS - 1) / ROWS, nt = whole ? 1 : max(1, (r.len + UK - 1) / UK) + kItemCost;
-                const long long here = static_cast<long long>(n_rt) * p.kv_heads * nt;
-                if (u_begin < at + here) {
-                    const long long off = u_begin - at;
-                    const int item = static_cast<int>(off / nt);
-                    s_place[0] = b;
-                    s_place[1] = item / n_rt;
-                    s_place[2] = item % n_rt;
-                    s_place[3] = static_cast<int>(off % nt);      // place inside the item, its cost included
-                    break;
-                }
-                at += here;
-            }
-        }
-    }
-    __syncthreads();
     Cursor<ROWS, UK> cur;
-    cur.set_request(p, s_place[0]);
-    cur.h = s_place[1]; cur.rt = s_place[2];
-    const int place = whole ? kItemCost : s_place[3];
-    cur.j = max(0, place - kItemCost);
-    cur.left = whole ? cur.nt : (u_end - u_begin) - max(0, kItemCost - place);      // of this run, from unit cur.j on
-    if (cur.left <= 0) {                                       // nothing but a part of an item's cost
-        if (tid == 0) p.desc[8 * blockIdx.x] = 0;
-        return;
-    }
-    if (tid == 0) {
-        // the join of the item that this run starts inside belongs to its first cut, i.e. to the run behind its first owner
-        int* d = p.desc + 8 * blockIdx.x;
-        const long long unit0 = u_begin - cur.j;           // place of the item's first unit
-        const long long before = share * (static_cast<long long>(blockIdx.x) - 1);
-        const bool first_cut = !whole && cur.j > 0 && unit0 >= before;
-        d[1] = cur.h; d[2] = cur.rt; d[3] = cur.rq.row0; d[4] = cur.rq.qlen;
-        d[5] = static_cast<int>((unit0 + cur.nt - 1) / share);                   // last owner
-        d[6] = unit0 <= before + kItemCost ? 0 : 1;        // slot of the first owner's part: its run starts with this item (or inside its cost)
-        d[0] = first_cut ? 1 : 0;
-    }
+    if (!start_of_run<ROWS, UK, C::THREADS>(p, cur)) return;
 
     // ---- the ring of this warp group
     const uint32_t ring = smem_u32(smem) + kg * (NST * C::STAGE);
@@ -764,14 +563,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) attention_join_kernel(const Attn
 #define V64E_KT 32
 #define V64E_NST 3
 #endif
-#ifndef VC_NB
-#define VC_NB 2
-#define VC_RW 4
-#define VC_KW 2
-#define VC_KT 32
-#define VC_NST 5
-#endif
-// CLS: rows of an item up to 4, 8, 16, 32, more
+// CLS: rows of an item up to 4, 8, 16 (more: attention_rows.cu)
 template <int D, bool E4M3, int CLS>
 struct Pick;
 template <int CLS> constexpr int kLo = CLS == 0 ? 1 : 2;
@@ -781,24 +573,13 @@ template <int CLS> struct Pick<128, false, CLS> { using C = AttnCfg<128, false, 
 template <int CLS> struct Pick<128, true, CLS> { using C = AttnCfg<128, true, CLS <= 1 ? 1 : 2, 1, VE_KW, VE_KT, VE_NST, 0>; };
 template <int CLS> struct Pick<256, false, CLS> { using C = AttnCfg<256, false, CLS <= 1 ? 1 : 2, 1, 4, 16, 3, kLo<CLS>>; };
 template <int CLS> struct Pick<256, true, CLS> { using C = AttnCfg<256, true, CLS <= 1 ? 1 : 2, 1, 8, 16, 3, 0>; };
-template <> struct Pick<64, false, 3> { using C = AttnCfg<64, false, 2, 2, 4, 32, 5, 2>; };
-template <> struct Pick<64, true, 3> { using C = AttnCfg<64, true, 2, 2, 4, 32, 5, 0>; };
-template <> struct Pick<128, false, 3> { using C = AttnCfg<128, false, 2, 2, 4, 16, 5, 2>; };
-template <> struct Pick<128, true, 3> { using C = AttnCfg<128, true, 2, 2, 4, 32, 5, 0>; };
-template <> struct Pick<256, false, 3> { using C = AttnCfg<256, false, 2, 2, 4, 16, 3, 2>; };
-template <> struct Pick<256, true, 3> { using C = AttnCfg<256, true, 2, 2, 4, 16, 5, 0>; };
-template <> struct Pick<64, false, 4> { using C = AttnCfg<64, false, VC_NB, VC_RW, VC_KW, 32, 5, 2>; };
-template <> struct Pick<64, true, 4> { using C = AttnCfg<64, true, VC_NB, VC_RW, VC_KW, 32, 5, 0>; };
-template <> struct Pick<128, false, 4> { using C = AttnCfg<128, false, VC_NB, VC_RW, VC_KW, VC_KT, VC_NST, 2>; };
-template <> struct Pick<128, true, 4> { using C = AttnCfg<128, true, VC_NB, VC_RW, VC_KW, VC_KT, VC_NST, 0>; };
-template <> struct Pick<256, false, 4> { using C = AttnCfg<256, false, 2, 4, 2, 16, 5, 2>; };
-template <> struct Pick<256, true, 4> { using C = AttnCfg<256, true, 2, 4, 2, 16, 5, 0>; };
+int rows_class(int max_rows) { return max_rows <= 4 ? 0 : (max_rows <= 8 ? 1 : (max_rows <= 16 ? 2 : 3)); }
+int tile_rows(int max_rows) { return max_rows <= 8 ? 8 : (max_rows <= 16 ? 16 : 128); }      // ROWS of the variant
 
-int rows_class(int max_rows) { return max_rows <= 4 ? 0 : (max_rows <= 8 ? 1 : (max_rows <= 16 ? 2 : (max_rows <= 32 ? 3 : 4))); }
-int tile_rows(int max_rows) { return max_rows <= 8 ? 8 : (max_rows <= 16 ? 16 : (max_rows <= 32 ? 32 : 64)); }      // ROWS of the variant
-
+template <int D, bool E4M3>
+cudaError_t launch_main(const AttnParams& p, cudaStream_t st, RowsCfg<D, E4M3>) { return launch_rows<RowsCfg<D, E4M3>>(p, st); }
 template <class C>
-cudaError_t launch_main(const AttnParams& p, cudaStream_t st)
+cudaError_t launch_main(const AttnParams& p, cudaStream_t st, C)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(p.G), 1, 1);
@@ -831,7 +612,7 @@ template <class C>
 cudaError_t run_one(AttnParams p, int max_rows, long long max_kv, cudaStream_t st)
 {
     p.whole_units = kAttnWholeKeys / C::UK;
-    cudaError_t e = launch_main<C>(p, st);
+    cudaError_t e = launch_main(p, st, C());
     if (e != cudaSuccess) return e;
     // no item can be cut: there is a CTA for each and the table has no room for a longer one
     const long long items = static_cast<long long>(p.B) * p.kv_heads * ((max_rows + C::ROWS - 1) / C::ROWS);
@@ -841,13 +622,12 @@ cudaError_t run_one(AttnParams p, int max_rows, long long max_kv, cudaStream_t s
 template <int D, bool E4M3>
 cudaError_t run_df(const AttnParams& p, int max_rows, long long max_kv, cudaStream_t st)
 {
-    static_assert(Pick<D, E4M3, 0>::C::ROWS == 8 && Pick<D, E4M3, 2>::C::ROWS == 16 && Pick<D, E4M3, 3>::C::ROWS == 32 && Pick<D, E4M3, 4>::C::ROWS == 64, "tile_rows()");
+    static_assert(Pick<D, E4M3, 0>::C::ROWS == 8 && Pick<D, E4M3, 2>::C::ROWS == 16 && RowsCfg<D, E4M3>::ROWS == 128, "tile_rows()");
     switch (rows_class(max_rows)) {
         case 0: return run_one<typename Pick<D, E4M3, E4M3 ? 1 : 0>::C>(p, max_rows, max_kv, st);
         case 1: return run_one<typename Pick<D, E4M3, 1>::C>(p, max_rows, max_kv, st);
         case 2: return run_one<typename Pick<D, E4M3, 2>::C>(p, max_rows, max_kv, st);
-        case 3: return run_one<typename Pick<D, E4M3, 3>::C>(p, max_rows, max_kv, st);
-        default: return run_one<typename Pick<D, E4M3, 4>::C>(p, max_rows, max_kv, st);
+        default: return run_one<RowsCfg<D, E4M3>>(p, max_rows, max_kv, st);
     }
 }
 template <int D>
@@ -863,8 +643,7 @@ cudaError_t init_df()
     cudaError_t e = init_one_attn<typename Pick<D, E4M3, E4M3 ? 1 : 0>::C>();
     if (e == cudaSuccess) e = init_one_attn<typename Pick<D, E4M3, 1>::C>();
     if (e == cudaSuccess) e = init_one_attn<typename Pick<D, E4M3, 2>::C>();
-    if (e == cudaSuccess) e = init_one_attn<typename Pick<D, E4M3, 3>::C>();
-    if (e == cudaSuccess) e = init_one_attn<typename Pick<D, E4M3, 4>::C>();
+    if (e == cudaSuccess) e = init_rows<RowsCfg<D, E4M3>>();
     return e;
 }
 template <int D>
