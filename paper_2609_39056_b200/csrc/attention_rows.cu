@@ -8,13 +8,15 @@
 //                  operand is "MN-major", no transposition anywhere),  O in tensor memory
 // and the read of the cache is the bound again.
 //
-// Warps: 0..3 softmax, a thread per row (no exchange between lanes); 4 issues the MMAs; the others load, half of them K, half V.
+// Warps: two sets of four softmax warps that take the tiles in turn, a thread per row (no exchange between lanes; one set for D = 256), each with
+// its own reference, sum and O; then one warp that issues the MMAs; the others load, half of them K, half V.
 //   Loading: 16-byte cp.async per row piece, page by page, straight into the 128-byte-swizzled layout the tensor core reads; keys at or
 //     behind the request's length become zeros.  E4M3 goes through registers and becomes f16 (exact; Q as in attention_paged.cu).
 //   Softmax: pass 1 takes the maximum of the row's KT scores, pass 2 turns them into probabilities and writes them over the scores they
 //     came from: f16, or bf16 hi in the first and lo in the second half of every 32 columns (two products; see attention_paged.cu on the
 //     rounding).  The reference the exponent is taken from is raised only when the maximum exceeds it by 2^8: O is rescaled
-//     (read, multiplied, written) a few times per item instead of once per tile; sums stay fp32 and exact either way.
+//     (read, multiplied, written) a few times per item instead of once per tile; sums stay fp32 either way.
+//   At the end of an item the first set adds the two O (in that order) and writes the rows or the part.
 //
 // Every wait is bounded; a role that gives up records the wait and makes the others leave (see ptx.cuh).
 #include "attention_common.cuh"
@@ -23,26 +25,29 @@ namespace rudder {
 
 namespace {
 
-enum RowsWhere { W_R_Q_EMPTY = 1001, W_R_KV_EMPTY = 1002, W_R_Q_FULL = 1101, W_R_K_FULL = 1102, W_R_V_FULL = 1103, W_R_P_FULL = 1104, W_R_O_FREE = 1105,
-                 W_R_S_FULL = 1201, W_R_PV_DONE = 1202, W_R_DRAIN = 1301 };
+enum RowsWhere { W_R_Q_EMPTY = 1001, W_R_KV_EMPTY = 1002, W_R_Q_FULL = 1101, W_R_KV_FULL = 1102, W_R_P_FULL = 1104, W_R_O_FREE = 1105,
+                 W_R_S_FULL = 1201, W_R_PV_DONE = 1202, W_R_ML_FULL = 1203 };
 
 template <int D_, bool E4M3_>
 struct RowsCfg {
     static constexpr int D = D_;
     static constexpr bool E4M3 = E4M3_;
     static constexpr int ROWS = 128;
-    static constexpr int UK = D <= 128 ? 128 : 64;
+    static constexpr int UK = 64;
     static constexpr int KT = UK;                          // keys of a tile: a unit of the work split
-    static constexpr int ST = D == 64 ? 4 : (D == 128 ? 3 : 2);
-    static constexpr int LW = E4M3 ? 4 : 2;                // loading warps per operand
-    static constexpr int THREADS = 32 * (5 + 2 * LW);
+    static constexpr int ST = D == 64 ? 8 : (D == 128 ? 6 : 2);
+    static constexpr int SETS = D <= 128 ? 2 : 1;          // sets of four softmax warps that take the tiles in turn, each with an O of its own
+    static constexpr int LW = 3;                           // loading warps (12 warps in all: 168 registers a thread)
+    static constexpr int LANDED = E4M3 ? LW : 32 * LW;     // arrivals that make a stage full: warps that stored it, or threads whose copies have landed
+    static constexpr int MMA_WARP = 4 * SETS;
+    static constexpr int THREADS = 32 * (MMA_WARP + 1 + LW);
     static constexpr int BLK = KT * 128;                   // a tile is D / 64 blocks of [KT keys][64 channels]
     static constexpr int TILE = D / 64 * BLK;
     static constexpr int QBLK = ROWS * 128;
     static constexpr int QBYTES = D / 64 * QBLK;
     static constexpr int SMEM = 1024 + QBYTES + 2 * ST * TILE;
     static constexpr int O_COL = 2 * KT;                   // tensor memory columns: two S / P buffers, O
-    static_assert(O_COL + D <= 512 && SMEM <= 226 * 1024, "tensor memory and shared memory");
+    static_assert(O_COL + SETS * D <= 512 && SMEM <= 226 * 1024, "tensor memory and shared memory");
 };
 
 // kind::f16, A and B both f16 or both bf16, fp32 accumulators; b_mn: B with its N axis contiguous.
@@ -70,6 +75,15 @@ __device__ __forceinline__ void umma_f16_ts(uint32_t tmem_d, uint32_t tmem_a, ui
         "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
         "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}\n" ::"r"(tmem_d), "r"(tmem_a), "l"(db), "r"(idesc), "r"(accumulate) : "memory");
 }
+__device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+        ::"r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]),
+          "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]),
+          "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]), "r"(taddr)
+        : "memory");
+}
 __device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t (&r)[16]) {
     asm volatile(
         "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
@@ -79,14 +93,24 @@ __device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t (&r)[
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// Sixteen E4M3 numbers as two pieces of eight f16 numbers in shared memory.
+__device__ __forceinline__ void store_f16(uint32_t at0, uint32_t at1, uint4 v) {
+    uint32_t h[8];
+    e4m3_to_f16(v.x, h[0], h[1]); e4m3_to_f16(v.y, h[2], h[3]);
+    e4m3_to_f16(v.z, h[4], h[5]); e4m3_to_f16(v.w, h[6], h[7]);
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at0), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at1), "r"(h[4]), "r"(h[5]), "r"(h[6]), "r"(h[7]) : "memory");
+}
+
 template <class C>
 __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const AttnParams p)
 {
-    constexpr int D = C::D, KT = C::KT, ST = C::ST, LW = C::LW, ROWS = C::ROWS;
+    constexpr int D = C::D, KT = C::KT, ST = C::ST, LW = C::LW, ROWS = C::ROWS, SETS = C::SETS, MMA_WARP = C::MMA_WARP;
     constexpr bool E4M3 = C::E4M3;
     extern __shared__ uint8_t smem_raw_rows[];
-    __shared__ __align__(8) uint64_t bars[4 * ST + 8];
-    __shared__ float s_fac[ROWS];                          // E4M3: what the row's power of two has to be undone by
+    __shared__ __align__(8) uint64_t bars[2 * ST + 10];
+    __shared__ float2 s_ml[ROWS];                          // (reference, sum) of the second set's rows
+    __shared__ int8_t s_exp[E4M3 ? ROWS : 1];              // E4M3: the power of two that a row of Q was multiplied by
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_word;
 
@@ -99,25 +123,21 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
     const uint32_t base = (smem_u32(smem_raw_rows) + 1023u) & ~1023u;
     const uint32_t q_s = base, k_s = base + C::QBYTES, v_s = k_s + ST * C::TILE;
     const uint32_t bar0 = smem_u32(bars);
-    auto k_full = [&](int i) { return bar0 + 8u * i; };
-    auto k_empty = [&](int i) { return bar0 + 8u * (ST + i); };
-    auto v_full = [&](int i) { return bar0 + 8u * (2 * ST + i); };
-    auto v_empty = [&](int i) { return bar0 + 8u * (3 * ST + i); };
-    auto s_full = [&](int i) { return bar0 + 8u * (4 * ST + i); };
-    auto p_full = [&](int i) { return bar0 + 8u * (4 * ST + 2 + i); };
-    const uint32_t pv_done = bar0 + 8u * (4 * ST + 4), o_free = pv_done + 8u, q_full = pv_done + 16u, q_empty = pv_done + 24u;
+    auto kv_full = [&](int i) { return bar0 + 8u * i; };
+    auto kv_empty = [&](int i) { return bar0 + 8u * (ST + i); };
+    auto s_full = [&](int i) { return bar0 + 8u * (2 * ST + i); };
+    auto p_full = [&](int i) { return bar0 + 8u * (2 * ST + 2 + i); };
+    auto pv_done = [&](int set) { return bar0 + 8u * (2 * ST + 4 + set); };
+    const uint32_t ml_full = bar0 + 8u * (2 * ST + 6), o_free = ml_full + 8u, q_full = ml_full + 16u, q_empty = ml_full + 24u;
     if (tid == 0) {
         abort_word = 0;
-        for (int i = 0; i < ST; ++i) {
-            mbar_init(k_full(i), LW); mbar_init(k_empty(i), 1);
-            mbar_init(v_full(i), LW); mbar_init(v_empty(i), 1);
-        }
-        for (int i = 0; i < 2; ++i) { mbar_init(s_full(i), 1); mbar_init(p_full(i), 4); }
-        mbar_init(pv_done, 1); mbar_init(o_free, 4);
-        mbar_init(q_full, LW); mbar_init(q_empty, 5);      // the last S of the item, and the four softmax warps
+        for (int i = 0; i < ST; ++i) { mbar_init(kv_full(i), C::LANDED); mbar_init(kv_empty(i), 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(s_full(i), 1); mbar_init(p_full(i), 4); mbar_init(pv_done(i), 1); }
+        mbar_init(ml_full, 4); mbar_init(o_free, 4);
+        mbar_init(q_full, C::LANDED); mbar_init(q_empty, 1 + 4 * SETS);                 // the last S of the item, and the softmax warps
         fence_mbar_init();
     }
-    if (warp == 4) {
+    if (warp == MMA_WARP) {
         tmem_alloc(smem_u32(&tmem_slot), 512);
         tmem_relinquish();
     }
@@ -128,23 +148,26 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
     volatile int* abortp = &abort_word;
     auto wait_all = [&](uint32_t bar, uint32_t parity, int where) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abortp, where)) != 0; };
 
-    if (warp < 4) {
+    if (warp < MMA_WARP) {
         // ---------------------------------------------------------------------------------------- softmax and output
-        const int row = 32 * warp + lane;
-        const uint32_t lanes = static_cast<uint32_t>(32 * warp) << 16;
-        const float vs_base = 1.0f;
-        int t = 0, item = 0, part_j = 0;
-        bool ok = true, fresh = true, first_part = true, live_warp = false, first_tile = false;
+        const int set = warp >> 2, quad = warp & 3;
+        const int row = 32 * quad + lane;
+        const uint32_t lanes = static_cast<uint32_t>(32 * quad) << 16;
+        const uint32_t o_t = tmem + lanes + C::O_COL;
+        int t = 0, item = 0, part_j = 0, last_other = -1;  // last_other: the other set's last tile of the item
+        int mine = 0;                                      // tiles of this item that were this set's
+        bool ok = true, fresh = true, first_part = true, live_warp = false;
         int lim = 0, lim_warp = 0, R = 0, r = 0;
         float f = 0.0f, m = -INFINITY, l = 0.0f;
         while (cur.left > 0) {
             if (fresh) {
                 fresh = false;
-                first_tile = true;
+                mine = 0;
+                last_other = -1;
                 part_j = cur.j;
                 R = cur.rq.qlen * p.group;
                 r = cur.rt * ROWS + row;
-                live_warp = cur.rt * ROWS + 32 * warp < R;
+                live_warp = cur.rt * ROWS + 32 * quad < R;
                 lim = (p.causal && r < R) ? cur.rq.len - cur.rq.qlen + r / p.group + 1 : cur.rq.len;
                 lim_warp = __reduce_min_sync(0xffffffffu, lim);
                 m = -INFINITY;
@@ -152,179 +175,234 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                 f = p.scale_log2;
                 ok = wait_all(q_full, item & 1, W_R_Q_FULL);
                 if (!ok) break;
-                if (E4M3) f *= s_fac[row] * (p.cache.k_scale != nullptr ? __ldg(p.cache.k_scale + cur.h) : 1.0f);
+                if (E4M3) f *= __uint_as_float(static_cast<uint32_t>(127 - s_exp[row]) << 23) * (p.cache.k_scale != nullptr ? __ldg(p.cache.k_scale + cur.h) : 1.0f);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(q_empty);
                 ++item;
             }
             const int buf = t & 1;
-            ok = wait_all(s_full(buf), (t >> 1) & 1, W_R_S_FULL);
-            if (!ok) break;
             const bool item_end = cur.j + 1 == cur.nt, ends = item_end || cur.left == 1;
-            if (live_warp) {
-                tcgen05_fence_after_sync();
-                const uint32_t s_t = tmem + lanes + buf * KT;
-                const int key0 = cur.j * KT;
-                const bool edge = key0 + KT > lim_warp;    // some row of this warp does not see all keys
-                // pass 1: the maximum
-                float mx = -INFINITY;
+            if (SETS == 2 && buf != set) {
+                last_other = t;
+            } else {
+                ok = wait_all(s_full(buf), (t >> 1) & 1, W_R_S_FULL);
+                if (!ok) break;
+                if (live_warp) {
+                    tcgen05_fence_after_sync();
+                    const uint32_t s_t = tmem + lanes + buf * KT;
+                    const int key0 = cur.j * KT;
+                    const bool edge = key0 + KT > lim_warp;                      // some row of this warp does not see all keys
+                    // pass 1: the maximum of s f
+                    uint32_t x[KT / 32][32];
 #pragma unroll
-                for (int c = 0; c < KT / 32; ++c) {
-                    uint32_t x[32];
-                    tmem_ld_32x32b_x32(s_t + 32 * c, x);
+                    for (int c = 0; c < KT / 32; ++c) tmem_ld_32x32b_x32(s_t + 32 * c, x[c]);
                     tmem_wait_ld();
                     if (edge) {
+                        const uint32_t gone = __float_as_uint(f < 0.0f ? INFINITY : -INFINITY);
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) {
-                            const float v = __uint_as_float(x[i]) * f;
-                            mx = fmaxf(mx, key0 + 32 * c + i < lim ? v : -INFINITY);
-                        }
-                    } else {
+                        for (int c = 0; c < KT / 32; ++c)
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) mx = fmaxf(mx, __uint_as_float(x[i]) * f);
+                            for (int i = 0; i < 32; ++i) x[c][i] = key0 + 32 * c + i < lim ? x[c][i] : gone;
                     }
-                }
-                if (first_tile) {
-                    m = mx;
-                } else if (__any_sync(0xffffffffu, mx > m + 8.0f)) {
-                    // raise the reference: O so far must be complete, then it is rescaled
-                    ok = wait_all(pv_done, (t - 1) & 1, W_R_PV_DONE);
-                    if (!ok) break;
-                    tcgen05_fence_after_sync();
-                    const float n = fmaxf(m, mx), cor = n == -INFINITY ? 1.0f : exp2_approx(m - n);
-                    m = n;
-                    l *= cor;
+                    float mx;
+                    {
+                        float q[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                        if (f >= 0.0f) {
 #pragma unroll
-                    for (int c = 0; c < D / 16; ++c) {
-                        uint32_t o[16];
-                        tmem_ld_32x32b_x16(tmem + lanes + C::O_COL + 16 * c, o);
-                        tmem_wait_ld();
+                            for (int c = 0; c < KT / 32; ++c)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * cor);
-                        tmem_st_x16(tmem + lanes + C::O_COL + 16 * c, o);
-                    }
-                    tmem_wait_st();
-                }
-                const float u = m == -INFINITY ? 0.0f : m;
-                // pass 2: probabilities over the scores
-#pragma unroll
-                for (int c = 0; c < KT / 32; ++c) {
-                    uint32_t x[32], hi[16], lo[16];
-                    tmem_ld_32x32b_x32(s_t + 32 * c, x);
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        float a = exp2_approx(fmaf(__uint_as_float(x[2 * i]), f, -u)), b = exp2_approx(fmaf(__uint_as_float(x[2 * i + 1]), f, -u));
-                        if (edge) {
-                            if (key0 + 32 * c + 2 * i >= lim) a = 0.0f;
-                            if (key0 + 32 * c + 2 * i + 1 >= lim) b = 0.0f;
-                        }
-                        l += a + b;
-                        if (E4M3) {
-                            hi[i] = f16x2(a, b);
+                                for (int i = 0; i < 32; i += 2) q[(i >> 1) & 3] = fmaxf(q[(i >> 1) & 3], fmaxf(__uint_as_float(x[c][i]), __uint_as_float(x[c][i + 1])));
                         } else {
-                            hi[i] = bf16x2(a, b);
-                            lo[i] = bf16x2(a - bf16_lo(hi[i]), b - bf16_hi(hi[i]));
+#pragma unroll
+                            for (int c = 0; c < KT / 32; ++c)
+#pragma unroll
+                                for (int i = 0; i < 32; ++i) q[i & 3] = fmaxf(q[i & 3], -__uint_as_float(x[c][i]));
                         }
+                        mx = fmaxf(fmaxf(q[0], q[1]), fmaxf(q[2], q[3]));
+                        mx = mx == -INFINITY ? mx : mx * fabsf(f);               // (no key seen stays -inf whatever f is)
                     }
-                    tmem_st_x16(s_t + 32 * c, hi);
-                    if (!E4M3) tmem_st_x16(s_t + 32 * c + 16, lo);
-                }
-                tmem_wait_st();
-                tcgen05_fence_before_sync();
-            }
-            first_tile = false;
-            __syncwarp();
-            if (lane == 0) mbar_arrive(p_full(buf));
-            if (ends) {
-                if (live_warp) {
-                    ok = wait_all(pv_done, t & 1, W_R_PV_DONE);
-                    if (!ok) break;
-                    tcgen05_fence_after_sync();
-                    const bool entire = item_end && part_j == 0;
-                    const float vs = E4M3 && p.cache.v_scale != nullptr ? __ldg(p.cache.v_scale + cur.h) : vs_base;
-                    const float w = entire ? (l > 0.0f ? vs / l : 0.0f) : vs;
-                    const int slot = 2 * blockIdx.x + (first_part ? 0 : 1);
-                    const int tok = r / p.group, hh = cur.h * p.group + r % p.group;
-                    uint16_t* orow = p.O + static_cast<size_t>(cur.rq.row0 + tok) * p.ldo + static_cast<size_t>(hh) * D;
-                    float* prow = p.part_o + (static_cast<size_t>(slot) * ROWS + row) * D;
+                    if (mine == 0) {
+                        m = mx;
+                    } else if (__any_sync(0xffffffffu, mx > m + 8.0f)) {
+                        // raise the reference: O so far must be complete, then it is rescaled
+                        const int before = SETS == 2 ? (t >> 1) - 1 : t - 1;
+                        ok = wait_all(pv_done(set), before & 1, W_R_PV_DONE);
+                        if (!ok) break;
+                        tcgen05_fence_after_sync();
+                        const float n = fmaxf(m, mx), cor = n == -INFINITY ? 1.0f : exp2_approx(m - n);
+                        m = n;
+                        l *= cor;
+#pragma unroll 1
+                        for (int c = 0; c < D / 16; ++c) {                       // (rare: small code before speed)
+                            uint32_t o[16];
+                            tmem_ld_32x32b_x16(o_t + set * D + 16 * c, o);
+                            tmem_wait_ld();
 #pragma unroll
-                    for (int c = 0; c < D / 16; ++c) {
-                        uint32_t o[16];
-                        tmem_ld_32x32b_x16(tmem + lanes + C::O_COL + 16 * c, o);
-                        tmem_wait_ld();
-                        if (r < R) {
-                            float v[16];
+                            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * cor);
+                            tmem_st_x16(o_t + set * D + 16 * c, o);
+                        }
+                        tmem_wait_st();
+                    }
+                    // pass 2: probabilities over the scores they come from
+                    const float u = m == -INFINITY ? 0.0f : m;
+                    float l0 = 0.0f, l1 = 0.0f;
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(o[i]) * w;
-                            if (entire) {
-                                *reinterpret_cast<uint4*>(orow + 16 * c) = make_uint4(bf16x2(v[0], v[1]), bf16x2(v[2], v[3]), bf16x2(v[4], v[5]), bf16x2(v[6], v[7]));
-                                *reinterpret_cast<uint4*>(orow + 16 * c + 8) =
-                                    make_uint4(bf16x2(v[8], v[9]), bf16x2(v[10], v[11]), bf16x2(v[12], v[13]), bf16x2(v[14], v[15]));
+                    for (int c = 0; c < KT / 32; ++c) {
+                        uint32_t w[32];                    // hi (or f16) in the first half, lo in the second
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            float a = exp2_approx(fmaf(__uint_as_float(x[c][2 * i]), f, -u)), b = exp2_approx(fmaf(__uint_as_float(x[c][2 * i + 1]), f, -u));
+                            if (edge && f == 0.0f) {       // (0 x infinity)
+                                if (key0 + 32 * c + 2 * i >= lim) a = 0.0f;
+                                if (key0 + 32 * c + 2 * i + 1 >= lim) b = 0.0f;
+                            }
+                            l0 += a;
+                            l1 += b;
+                            if (E4M3) {
+                                w[i] = f16x2(a, b);
                             } else {
-#pragma unroll
-                                for (int i = 0; i < 16; i += 4) *reinterpret_cast<float4*>(prow + 16 * c + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                                w[i] = bf16x2(a, b);
+                                w[16 + i] = bf16x2(a - bf16_lo(w[i]), b - bf16_hi(w[i]));
                             }
                         }
+                        if (E4M3) tmem_st_x16(s_t + 32 * c, reinterpret_cast<const uint32_t (&)[16]>(w));
+                        else tmem_st_x32(s_t + 32 * c, w);
                     }
-                    if (r < R) {
-                        if (!entire) p.part_ml[static_cast<size_t>(slot) * ROWS + row] = make_float2(m, l);
-                        else if (p.lse != nullptr)
-                            p.lse[static_cast<size_t>(cur.rq.row0 + tok) * p.heads + hh] = l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
-                    }
+                    l += l0 + l1;
+                    tmem_wait_st();
                     tcgen05_fence_before_sync();
                 }
+                ++mine;
                 __syncwarp();
-                if (lane == 0) mbar_arrive(o_free);
+                if (lane == 0) mbar_arrive(p_full(buf));
+            }
+            if (ends) {
+                if (SETS == 2 && set == 1) {
+                    // the second set leaves its references and sums to the first, once that has read those of the item before
+                    if (item > 1) {
+                        ok = wait_all(o_free, (item - 2) & 1, W_R_O_FREE);
+                        if (!ok) break;
+                    }
+                    s_ml[row] = make_float2(m, l);
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(ml_full);
+                } else {
+                    if (live_warp) {
+                        const int last_mine = (SETS == 2 && buf != set) ? t - 1 : t;       // this set's last tile of the item, if it had one
+                        if (mine > 0) {
+                            ok = wait_all(pv_done(set), (SETS == 2 ? last_mine >> 1 : last_mine) & 1, W_R_PV_DONE);
+                            if (!ok) break;
+                        }
+                        float w0 = 1.0f, w1 = 0.0f, mm = m, ll = l;
+                        if (SETS == 2) {
+                            ok = wait_all(ml_full, (item - 1) & 1, W_R_ML_FULL);
+                            if (!ok) break;
+                            if (last_other >= 0) {
+                                ok = wait_all(pv_done(1), (last_other >> 1) & 1, W_R_PV_DONE);
+                                if (!ok) break;
+                                const float2 o = s_ml[row];
+                                mm = fmaxf(m, o.x);
+                                const float u = mm == -INFINITY ? 0.0f : mm;
+                                w0 = exp2_approx(m - u);
+                                w1 = exp2_approx(o.x - u);
+                                ll = l * w0 + o.y * w1;
+                            }
+                        }
+                        tcgen05_fence_after_sync();
+                        const bool entire = item_end && part_j == 0;
+                        const float vs = E4M3 && p.cache.v_scale != nullptr ? __ldg(p.cache.v_scale + cur.h) : 1.0f;
+                        const float w = entire ? (ll > 0.0f ? vs / ll : 0.0f) : vs;
+                        w0 *= w;
+                        w1 *= w;
+                        const int slot = 2 * blockIdx.x + (first_part ? 0 : 1);
+                        const int tok = r / p.group, hh = cur.h * p.group + r % p.group;
+                        uint16_t* orow = p.O + static_cast<size_t>(cur.rq.row0 + tok) * p.ldo + static_cast<size_t>(hh) * D;
+                        float* prow = p.part_o + (static_cast<size_t>(slot) * ROWS + row) * D;
+#pragma unroll 1
+                        for (int c = 0; c < D / 16; ++c) {
+                            uint32_t o[16], o2[16];
+                            // (an O that no product of this item has written is not read)
+                            if (mine > 0) tmem_ld_32x32b_x16(o_t + 16 * c, o);
+                            if (SETS == 2 && last_other >= 0) tmem_ld_32x32b_x16(o_t + D + 16 * c, o2);
+                            tmem_wait_ld();
+                            float v[16];
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                v[i] = mine > 0 ? __uint_as_float(o[i]) * w0 : 0.0f;
+                                if (SETS == 2 && last_other >= 0) v[i] = fmaf(__uint_as_float(o2[i]), w1, v[i]);
+                            }
+                            if (r < R) {
+                                if (entire) {
+                                    *reinterpret_cast<uint4*>(orow + 16 * c) =
+                                        make_uint4(bf16x2(v[0], v[1]), bf16x2(v[2], v[3]), bf16x2(v[4], v[5]), bf16x2(v[6], v[7]));
+                                    *reinterpret_cast<uint4*>(orow + 16 * c + 8) =
+                                        make_uint4(bf16x2(v[8], v[9]), bf16x2(v[10], v[11]), bf16x2(v[12], v[13]), bf16x2(v[14], v[15]));
+                                } else {
+#pragma unroll
+                                    for (int i = 0; i < 16; i += 4) *reinterpret_cast<float4*>(prow + 16 * c + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                                }
+                            }
+                        }
+                        if (r < R) {
+                            if (!entire) p.part_ml[static_cast<size_t>(slot) * ROWS + row] = make_float2(mm, ll);
+                            else if (p.lse != nullptr)
+                                p.lse[static_cast<size_t>(cur.rq.row0 + tok) * p.heads + hh] = ll > 0.0f ? (mm + log2f(ll)) * kLn2 : -INFINITY;
+                        }
+                        tcgen05_fence_before_sync();
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(o_free);
+                }
                 fresh = true;
                 first_part = false;
             }
             ++t;
             cur.advance(p);
         }
-    } else if (warp == 4) {
+    } else {
+    if (warp == MMA_WARP) {
         // ---------------------------------------------------------------------------------------- MMA issue
         const bool leader = elect_one();
         const uint32_t idesc_s = umma_idesc_f16(ROWS, KT, !E4M3, false), idesc_o = umma_idesc_f16(ROWS, D, !E4M3, true);
-        int t = 0, item = 0, outs = 0;
-        bool ok = true, fresh = true, prev_first = false;
-        // O += P V of tile `pt`
-        auto pv = [&](int pt, bool first) -> bool {
-            const int buf = pt & 1, slot = pt % ST;
+        int t = 0, item = 0, in_item = 0;
+        bool ok = true, fresh = true;
+        int prev_in_item = 0, prev_item = 0;
+        // O += P V of tile `pt`, the `nth` of item `it`: the first SETS tiles of an item start their O
+        auto pv = [&](int pt, int nth, int it) -> bool {
+            const int buf = pt & 1, slot = pt % ST, set = SETS == 2 ? buf : 0;
             if (!wait_all(p_full(buf), (pt >> 1) & 1, W_R_P_FULL)) return false;
-            if (!wait_all(v_full(slot), (pt / ST) & 1, W_R_V_FULL)) return false;
-            if (first && outs > 0 && !wait_all(o_free, (outs - 1) & 1, W_R_O_FREE)) return false;     // the item before has been read out
-            if (first) ++outs;
+            if (nth == 0 && it > 0 && !wait_all(o_free, (it - 1) & 1, W_R_O_FREE)) return false;      // the item before has been read out
             tcgen05_fence_after_sync();
             if (leader) {
-                const uint32_t v0 = v_s + slot * C::TILE;
+                const uint32_t v0 = v_s + slot * C::TILE, o = tmem + C::O_COL + set * D;
 #pragma unroll
                 for (int kk = 0; kk < KT / 16; ++kk) {
                     const uint64_t db = umma_desc_sw128_mn(v0 + kk * 2048, C::BLK);
                     const uint32_t pa = tmem + buf * KT + 32 * (kk >> 1) + 8 * (kk & 1);
-                    umma_f16_ts(tmem + C::O_COL, pa, db, idesc_o, (first && kk == 0) ? 0u : 1u);
-                    if (!E4M3) umma_f16_ts(tmem + C::O_COL, pa + 16, db, idesc_o, 1u);
+                    umma_f16_ts(o, pa, db, idesc_o, (nth < SETS && kk == 0) ? 0u : 1u);
+                    if (!E4M3) umma_f16_ts(o, pa + 16, db, idesc_o, 1u);
                 }
-                umma_commit(v_empty(slot));
-                umma_commit(pv_done);
+                umma_commit(kv_empty(slot));                   // (and the S of this stage, issued before)
+                umma_commit(pv_done(set));
             }
             __syncwarp();
             return true;
         };
         while (cur.left > 0) {
-            const bool first = fresh;
             if (fresh) {
                 fresh = false;
+                in_item = 0;
                 ok = wait_all(q_full, item & 1, W_R_Q_FULL);
                 if (!ok) break;
                 ++item;
             }
             const bool ends = cur.j + 1 == cur.nt || cur.left == 1;
             const int slot = t % ST;
-            ok = wait_all(k_full(slot), (t / ST) & 1, W_R_K_FULL);
+            ok = wait_all(kv_full(slot), (t / ST) & 1, W_R_KV_FULL);
             // S goes over the probabilities of two tiles ago: their product must be complete (products into different accumulators are not ordered)
-            if (ok && t >= 2) ok = wait_all(pv_done, t & 1, W_R_PV_DONE);
+            if (ok && t >= 2) ok = SETS == 2 ? wait_all(pv_done(t & 1), ((t >> 1) - 1) & 1, W_R_PV_DONE) : wait_all(pv_done(0), t & 1, W_R_PV_DONE);
             if (!ok) break;
+            fence_proxy_async_smem();                      // the loaders' writes -> the tensor core's reads, K and V of the stage
             tcgen05_fence_after_sync();
             if (leader) {
                 const uint32_t k0 = k_s + slot * C::TILE;
@@ -333,130 +411,140 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                     umma_f16_ss(tmem + (t & 1) * KT, umma_desc_sw128(q_s + (ks >> 2) * C::QBLK) + 2u * (ks & 3),
                                 umma_desc_sw128(k0 + (ks >> 2) * C::BLK) + 2u * (ks & 3), idesc_s, ks > 0 ? 1u : 0u);
                 umma_commit(s_full(t & 1));
-                umma_commit(k_empty(slot));
                 if (ends) umma_commit(q_empty);
             }
             __syncwarp();
             if (t > 0) {
-                ok = pv(t - 1, prev_first);
+                ok = pv(t - 1, prev_in_item, prev_item);
                 if (!ok) break;
             }
-            prev_first = first;
+            prev_in_item = in_item++;
+            prev_item = item - 1;
             fresh = ends;
             ++t;
             cur.advance(p);
         }
-        if (ok && t > 0) pv(t - 1, prev_first);
+        if (ok && t > 0) pv(t - 1, prev_in_item, prev_item);
     } else {
         // ---------------------------------------------------------------------------------------- loading
-        const int lw = warp - 5;
-        const bool is_v = lw >= LW;
-        const int w = is_v ? lw - LW : lw;
-        constexpr int RPW = KT / LW;                       // keys of a warp
-        static_assert(RPW % 32 == 0 || RPW == 16, "a lane holds the place of whole keys");
-        constexpr int OFFS = (RPW + 31) / 32;
-        const uint32_t ring = is_v ? v_s : k_s;
-        const uint8_t* cache = is_v ? p.cache.v : p.cache.k;
-        int t = 0, item = 0, pending = -1;
+        const int w = warp - MMA_WARP - 1;
+        // The keys of a tile in runs of 8, every LW-th run a warp's, K and V alike: in pages of 8 tokens or more a run lies in one page, and its
+        // rows are one stride apart.  Lane i keeps the page of the warp's i-th run, requested a tile ahead.
+        constexpr int RUN = 8, NRUN = KT / RUN, MINE = (NRUN + LW - 1) / LW;
+        constexpr int CH = E4M3 ? D / 16 : D / 8;          // 16-byte pieces of a key
+        constexpr int STEP = 32 / CH, N = RUN / STEP;      // keys per instruction of the warp, instructions per run and operand
+        static_assert(STEP <= RUN, "a run is whole instructions");
+        const int c = lane % CH, sub = lane / CH;
+        const int64_t key_step = static_cast<int64_t>(STEP) * p.cache.token_stride;
+        const bool run_in_page = p.cache.page_shift >= 3;
+        int t = 0, item = 0;
         bool ok = true, fresh = true;
-        auto full = [&](int i) { return is_v ? v_full(i) : k_full(i); };
-        // the tile before this one has landed (bf16: its copies are the group before the last)
-        auto signal = [&](int slot) {
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(full(slot));
+        // a stage counts as full when this thread's copies have landed; the issuing warp makes them visible to the tensor core (a proxy fence
+        // here would wait for the copies in flight: measured, the loading warps then held one tile at a time and bounded the kernel)
+        auto signal = [&](uint32_t bar) {
+            if (!E4M3) {
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+            } else {
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar);
+            }
         };
+        auto page_of = [&](int key) -> int {
+            return key < cur.rq.len ? __ldg(p.table + static_cast<size_t>(cur.b) * p.ld_table + (key >> p.cache.page_shift)) : -1;
+        };
+        auto place = [&](int page, int key) -> long long {
+            return page * p.cache.page_stride + static_cast<long long>(cur.h) * p.cache.head_stride +
+                   static_cast<long long>(key & ((1 << p.cache.page_shift) - 1)) * p.cache.token_stride;
+        };
+        auto run_pages = [&]() -> int {
+            const int run = w + lane * LW;
+            return run_in_page && lane < MINE && run < NRUN ? page_of(cur.j * KT + RUN * run) : -1;
+        };
+        int pages = run_pages();
         while (cur.left > 0) {
             const bool ends = cur.j + 1 == cur.nt || cur.left == 1;
             const int slot = t % ST;
             const bool new_item = fresh;
             fresh = ends;
-            // places of this warp's keys: lane i of run k holds key w RPW + 32 k + i
-            long long off[OFFS];
-#pragma unroll
-            for (int k = 0; k < OFFS; ++k) {
-                const int key = cur.j * KT + w * RPW + 32 * k + lane;
-                off[k] = -1;
-                if ((RPW >= 32 || lane < RPW) && key < cur.rq.len) {
-                    const int page = __ldg(p.table + static_cast<size_t>(cur.b) * p.ld_table + (key >> p.cache.page_shift));
-                    if (page < 0 || page >= p.cache.n_pages) record_bad_data(kBadPage);
-                    else
-                        off[k] = page * p.cache.page_stride + static_cast<long long>(cur.h) * p.cache.head_stride +
-                                 static_cast<long long>(key & ((1 << p.cache.page_shift) - 1)) * p.cache.token_stride;
-                }
-            }
-            if (!E4M3 && pending >= 0 && !__all_sync(0xffffffffu, mbar_try_wait(is_v ? v_empty(slot) : k_empty(slot), ((t / ST) & 1) ^ 1))) {
-                // about to wait for a free stage: hand over what has landed meanwhile
-                cp_async_wait<0>();
-                signal(pending);
-                pending = -1;
-            }
-            ok = wait_all(is_v ? v_empty(slot) : k_empty(slot), ((t / ST) & 1) ^ 1, W_R_KV_EMPTY);
+            ok = wait_all(kv_empty(slot), ((t / ST) & 1) ^ 1, W_R_KV_EMPTY);
             if (!ok) break;
-            const uint32_t dst = ring + slot * C::TILE;
-            if (!E4M3) {
-                constexpr int CH = D / 8;                  // 16-byte pieces of a key
-                constexpr int STEP = 32 / CH > 0 ? 32 / CH : 1;                  // keys per instruction of the warp (CH = 32: one)
+            const uint32_t k_dst = k_s + slot * C::TILE, v_dst = v_s + slot * C::TILE;
+            uint4 xk[E4M3 ? MINE * N : 1], xv[E4M3 ? MINE * N : 1];              // E4M3: this warp's share of the tile, all in flight together
 #pragma unroll
-                for (int k = 0; k < OFFS; ++k)
-#pragma unroll 8
-                    for (int i = 0; i < (RPW < 32 ? RPW : 32); i += STEP) {
-                        const int rr = i + lane / CH, c = lane % CH;
-                        const long long o = __shfl_sync(0xffffffffu, off[k], rr);
-                        const int key = w * RPW + 32 * k + rr;
-                        cp_async16(dst + (c >> 3) * C::BLK + key * 128 + (((c & 7) ^ (key & 7)) << 4), cache + (o >= 0 ? o : 0) + 16 * c, o >= 0);
+            for (int k = 0; k < MINE; ++k) {
+                const int run = w + k * LW;
+                if (run >= NRUN) break;
+                const int key0 = cur.j * KT + RUN * run;
+                const int page = __shfl_sync(0xffffffffu, pages, k);
+                // place of this lane's first key in the run, and whether the others follow at a stride
+                const bool whole = run_in_page && key0 + RUN <= cur.rq.len && page >= 0 && page < p.cache.n_pages;
+                long long off = 0;
+                if (whole) {
+                    off = place(page, key0 + sub) + 16 * c;
+                } else {
+                    // the end of the request, pages of less than 8 tokens, or a bad page: lane i looks up key i
+                    const int key = key0 + lane, pg = lane < RUN ? page_of(key) : -1;
+                    off = -1;
+                    if (lane < RUN && key < cur.rq.len) {
+                        if (pg < 0 || pg >= p.cache.n_pages) record_bad_data(kBadPage);
+                        else off = place(pg, key);
                     }
-                cp_async_commit();
-            } else {
-                constexpr int CH = D / 16;                 // 16-byte pieces of a key, 16 numbers each
-                constexpr int STEP = 32 / CH;
-                constexpr int N = (RPW < 32 ? RPW : 32) / STEP, B = N < 8 ? N : 8;
-#pragma unroll
-                for (int k = 0; k < OFFS; ++k)
-#pragma unroll
-                    for (int i0 = 0; i0 < N; i0 += B) {
-                        uint4 x[B];
-#pragma unroll
-                        for (int i = 0; i < B; ++i) {
-                            const long long o = __shfl_sync(0xffffffffu, off[k], (i0 + i) * STEP + lane / CH);
-                            x[i] = make_uint4(0, 0, 0, 0);
-                            if (o >= 0) x[i] = __ldcg(reinterpret_cast<const uint4*>(cache + o + 16 * (lane % CH)));
-                        }
-#pragma unroll
-                        for (int i = 0; i < B; ++i) {
-                            const int key = w * RPW + 32 * k + (i0 + i) * STEP + lane / CH, c = 2 * (lane % CH);
-                            uint32_t h[8];
-                            e4m3_to_f16(x[i].x, h[0], h[1]); e4m3_to_f16(x[i].y, h[2], h[3]);
-                            e4m3_to_f16(x[i].z, h[4], h[5]); e4m3_to_f16(x[i].w, h[6], h[7]);
-                            const uint32_t at = dst + (c >> 3) * C::BLK + key * 128;
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + (((c & 7) ^ (key & 7)) << 4)), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at + ((((c & 7) + 1) ^ (key & 7)) << 4)), "r"(h[4]), "r"(h[5]), "r"(h[6]), "r"(h[7]) : "memory");
-                        }
-                    }
-            }
-            if (new_item && !is_v) {
-                // the item's queries, rows w 128 / LW .. of the tile; rows that do not exist become zeros.  The item before must be through its
-                // last S: hand its last tile over first.
-                if (pending >= 0) {
-                    cp_async_wait<1>();
-                    signal(pending);
-                    pending = -1;
                 }
+                const uint32_t row = (E4M3 ? 0 : (c >> 3) * C::BLK) + (RUN * run + sub) * 128;
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    long long o = off + i * key_step;
+                    bool valid = true;
+                    if (!whole) {
+                        o = __shfl_sync(0xffffffffu, off, i * STEP + sub);
+                        valid = o >= 0;
+                        o = valid ? o + 16 * c : 0;
+                    }
+                    if (!E4M3) {
+                        const uint32_t at = row + i * STEP * 128 + ((((c & 7) ^ sub) ^ ((i * STEP) & 7)) << 4);
+                        cp_async16(k_dst + at, p.cache.k + o, valid);
+                        cp_async16(v_dst + at, p.cache.v + o, valid);
+                    } else {
+                        xk[E4M3 ? k * N + i : 0] = xv[E4M3 ? k * N + i : 0] = make_uint4(0, 0, 0, 0);
+                        if (valid) {
+                            xk[E4M3 ? k * N + i : 0] = __ldcg(reinterpret_cast<const uint4*>(p.cache.k + o));
+                            xv[E4M3 ? k * N + i : 0] = __ldcg(reinterpret_cast<const uint4*>(p.cache.v + o));
+                        }
+                    }
+                }
+            }
+            if (E4M3) {
+#pragma unroll
+                for (int k = 0; k < MINE; ++k) {
+                    const int run = w + k * LW;
+                    if (run >= NRUN) break;
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        const int kr = i * STEP + sub, c2 = 2 * c;               // key of the run, first of its two 16-byte pieces of f16
+                        const uint32_t row = (c2 >> 3) * C::BLK + (RUN * run + kr) * 128;
+                        const uint32_t at0 = row + (((c2 & 7) ^ (kr & 7)) << 4), at1 = row + ((((c2 & 7) + 1) ^ (kr & 7)) << 4);
+                        store_f16(k_dst + at0, k_dst + at1, xk[E4M3 ? k * N + i : 0]);
+                        store_f16(v_dst + at0, v_dst + at1, xv[E4M3 ? k * N + i : 0]);
+                    }
+                }
+            }
+            signal(kv_full(slot));
+            if (new_item) {
+                // the item's queries, each warp its share of the 128 rows; rows that do not exist become zeros
                 if (item > 0) {
                     ok = wait_all(q_empty, (item - 1) & 1, W_R_Q_EMPTY);
                     if (!ok) break;
                 }
                 ++item;
-                constexpr int QR = ROWS / LW;
                 const int R = cur.rq.qlen * p.group;
-                constexpr int CH = D / 8, STEP = 32 / CH;
+                constexpr int QCH = D / 8, QSTEP = 32 / QCH;
 #pragma unroll 4
-                for (int i = 0; i < QR; i += STEP) {
-                    const int rl = w * QR + i + lane / CH, c = lane % CH, r = cur.rt * ROWS + rl;
+                for (int i = w * QSTEP; i < ROWS; i += LW * QSTEP) {
+                    const int rl = i + lane / QCH, qc = lane % QCH, r = cur.rt * ROWS + rl;
                     const bool live = r < R;
-                    const uint16_t* src = p.Q + 8 * c;
+                    const uint16_t* src = p.Q + 8 * qc;
                     if (live) src += static_cast<size_t>(cur.rq.row0 + r / p.group) * p.ldq + static_cast<size_t>(cur.h * p.group + r % p.group) * D;
-                    const uint32_t at = q_s + (c >> 3) * C::QBLK + rl * 128 + (((c & 7) ^ (rl & 7)) << 4);
+                    const uint32_t at = q_s + (qc >> 3) * C::QBLK + rl * 128 + (((qc & 7) ^ (rl & 7)) << 4);
                     if (!E4M3) {
                         cp_async16(at, src, live);
                     } else {
@@ -467,50 +555,33 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
 #pragma unroll
                         for (int e = 0; e < 4; ++e) mx = fmaxf(mx, fmaxf(fabsf(bf16_lo(xw[e])), fabsf(bf16_hi(xw[e]))));
 #pragma unroll
-                        for (int o = CH / 2; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+                        for (int o = QCH / 2; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
                         const int ex = min(126, max(-126, 14 - (static_cast<int>((__float_as_uint(mx) >> 23) & 255u) - 127)));
                         const float sc = __uint_as_float(static_cast<uint32_t>(ex + 127) << 23);
                         uint32_t h[4];
 #pragma unroll
                         for (int e = 0; e < 4; ++e) h[e] = f16x2(bf16_lo(xw[e]) * sc, bf16_hi(xw[e]) * sc);
                         asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");
-                        if (c == 0) s_fac[rl] = __uint_as_float(static_cast<uint32_t>(127 - ex) << 23);
+                        if (qc == 0) s_exp[rl] = static_cast<int8_t>(ex);
                     }
                 }
-                if (!E4M3) {
-                    cp_async_commit();
-                    cp_async_wait<0>();                    // queries and this tile together
-                }
-                fence_proxy_async_smem();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(q_full);
-                if (!E4M3) signal(slot);
-            } else if (!E4M3) {
-                if (pending >= 0) {
-                    cp_async_wait<1>();
-                    signal(pending);
-                }
-                pending = slot;
+                signal(q_full);
             }
-            if (E4M3) signal(slot);
             ++t;
             cur.advance(p);
+            if (cur.left > 0) pages = run_pages();
         }
-        if (!E4M3) {
-            cp_async_wait<0>();
-            if (ok && pending >= 0) signal(pending);
-        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+    }
     }
 
-    // ---- teardown: no MMA of this CTA is in flight when its tensor memory goes (the softmax warps have waited for the last product; after an
-    // aborted wait the issuing thread waits for its own, bounded)
-    if (warp == 4 && abort_word != 0) {
-        if (elect_one()) umma_commit(pv_done);
-        for (uint32_t it = 0; it < (1u << 14); ++it) { __nanosleep(100); if (abort_word == 0) break; }
-    }
+    // ---- teardown: no MMA of this CTA is in flight when its tensor memory goes (the first softmax set has waited for the last products; after
+    // an aborted wait the issued ones get a millisecond, a thousand times what they take)
+    if (warp == MMA_WARP && *abortp != 0)
+        for (int it = 0; it < 1000; ++it) __nanosleep(1000);
     tcgen05_fence_before_sync();
     __syncthreads();
-    if (warp == 4) {
+    if (warp == MMA_WARP) {
         __syncwarp();
         tcgen05_fence_after_sync();
         tmem_dealloc(tmem, 512);
