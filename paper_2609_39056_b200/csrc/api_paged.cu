@@ -83,6 +83,22 @@ rudder_status check_qk(const rudder_qk_args* a, QkArgs* out)
     return RUDDER_OK;
 }
 
+// Tensor map over one tensor of the cache; false if the strides do not fit one.
+bool make_tmap_cache(CUtensorMap* tm, const void* base, const rudder_paged_cache* c)
+{
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return false;
+    const cuuint64_t row = static_cast<cuuint64_t>(c->head_dim) * 2;
+    cuuint64_t gdim[4] = {static_cast<cuuint64_t>(c->head_dim), static_cast<cuuint64_t>(c->page_size), static_cast<cuuint64_t>(c->heads), static_cast<cuuint64_t>(c->n_pages)};
+    // (an axis of one element may have any stride)
+    cuuint64_t gstride[3] = {c->page_size > 1 ? static_cast<cuuint64_t>(c->token_stride) * 2 : row, c->heads > 1 ? static_cast<cuuint64_t>(c->head_stride) * 2 : row,
+                             c->n_pages > 1 ? static_cast<cuuint64_t>(c->page_stride) * 2 : row};
+    cuuint32_t box[4] = {64, static_cast<cuuint32_t>(c->page_size < 64 ? c->page_size : 64), 1, 1};
+    cuuint32_t estr[4] = {1, 1, 1, 1};
+    return fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), gdim, gstride, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 rudder_status check_attention_shape(const rudder_attention_args* a)
 {
     if (!a || !a->cache) return RUDDER_ERR_ARG;
@@ -113,6 +129,12 @@ rudder_status check_attention(const rudder_attention_args* a, AttnArgs* out)
     o.B = a->B; o.max_q = a->max_q; o.causal = a->causal != 0; o.scale = a->scale;
     *out = o;
     return RUDDER_OK;
+}
+
+// Where the kernel that the call runs takes the cache by TMA: the tensor maps (without them it copies row by row).
+void add_maps(const rudder_paged_cache* c, AttnArgs* a)
+{
+    if (attention_uses_maps(a->max_q * (a->heads / a->kv_heads), a->e4m3, c->page_size)) a->tma = make_tmap_cache(&a->tm_k, c->k, c) && make_tmap_cache(&a->tm_v, c->v, c);
 }
 
 }  // namespace
@@ -158,6 +180,7 @@ rudder_status rudder_attention_paged(const rudder_attention_args* args, void* wo
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < rudder_attention_workspace_bytes(args)) return RUDDER_ERR_WORKSPACE;
     s = ensure_paged_init();
     if (s != RUDDER_OK) return s;
+    add_maps(args->cache, &a);
     return launch_attention_paged(a, workspace, sm_count(), static_cast<cudaStream_t>(stream)) == cudaSuccess ? RUDDER_OK : RUDDER_ERR_CUDA;
 }
 
@@ -229,6 +252,7 @@ rudder_status rudder_block_cached(const rudder_block_args* args, const rudder_bl
     AttnArgs tp;
     if ((s = check_qk(&qa, &qp)) != RUDDER_OK || (s = check_attention(&ta, &tp)) != RUDDER_OK) return s;
     if ((s = ensure_init()) != RUDDER_OK || (s = ensure_paged_init()) != RUDDER_OK) return s;
+    add_maps(ta.cache, &tp);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const int sms = sm_count();
     auto lin = [&](int l, const uint16_t* x, int64_t ldx, bool gelu_first) {

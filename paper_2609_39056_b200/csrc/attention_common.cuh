@@ -28,6 +28,7 @@ struct AttnParams {
     int max_pages, B, max_q, M, heads, kv_heads, group, causal;
     int whole_units;                    // items of at most this many units are not cut when there is a CTA for each
     int G;                              // CTAs
+    int tma;                            // many rows: tensor maps over the cache are there
 };
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid) {

@@ -577,9 +577,9 @@ int rows_class(int max_rows) { return max_rows <= 4 ? 0 : (max_rows <= 8 ? 1 : (
 int tile_rows(int max_rows) { return max_rows <= 8 ? 8 : (max_rows <= 16 ? 16 : 128); }      // ROWS of the variant
 
 template <int D, bool E4M3>
-cudaError_t launch_main(const AttnParams& p, cudaStream_t st, RowsCfg<D, E4M3>) { return launch_rows<RowsCfg<D, E4M3>>(p, st); }
+cudaError_t launch_main(const AttnParams& p, const AttnArgs& a, cudaStream_t st, RowsCfg<D, E4M3>) { return launch_rows<RowsCfg<D, E4M3>>(p, &a.tm_k, &a.tm_v, st); }
 template <class C>
-cudaError_t launch_main(const AttnParams& p, cudaStream_t st, C)
+cudaError_t launch_main(const AttnParams& p, const AttnArgs&, cudaStream_t st, C)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(p.G), 1, 1);
@@ -609,10 +609,10 @@ cudaError_t launch_join(const AttnParams& p, int rows_of_tile, int max_rows, cud
     return cudaLaunchKernelEx(&cfg, attention_join_kernel<D>, p, rows_of_tile);
 }
 template <class C>
-cudaError_t run_one(AttnParams p, int max_rows, long long max_kv, cudaStream_t st)
+cudaError_t run_one(AttnParams p, const AttnArgs& a, int max_rows, long long max_kv, cudaStream_t st)
 {
     p.whole_units = kAttnWholeKeys / C::UK;
-    cudaError_t e = launch_main(p, st, C());
+    cudaError_t e = launch_main(p, a, st, C());
     if (e != cudaSuccess) return e;
     // no item can be cut: there is a CTA for each and the table has no room for a longer one
     const long long items = static_cast<long long>(p.B) * p.kv_heads * ((max_rows + C::ROWS - 1) / C::ROWS);
@@ -620,20 +620,20 @@ cudaError_t run_one(AttnParams p, int max_rows, long long max_kv, cudaStream_t s
     return launch_join<C::D>(p, C::ROWS, max_rows, st);
 }
 template <int D, bool E4M3>
-cudaError_t run_df(const AttnParams& p, int max_rows, long long max_kv, cudaStream_t st)
+cudaError_t run_df(const AttnParams& p, const AttnArgs& a, int max_rows, long long max_kv, cudaStream_t st)
 {
     static_assert(Pick<D, E4M3, 0>::C::ROWS == 8 && Pick<D, E4M3, 2>::C::ROWS == 16 && RowsCfg<D, E4M3>::ROWS == 128, "tile_rows()");
     switch (rows_class(max_rows)) {
-        case 0: return run_one<typename Pick<D, E4M3, E4M3 ? 1 : 0>::C>(p, max_rows, max_kv, st);
-        case 1: return run_one<typename Pick<D, E4M3, 1>::C>(p, max_rows, max_kv, st);
-        case 2: return run_one<typename Pick<D, E4M3, 2>::C>(p, max_rows, max_kv, st);
-        default: return run_one<RowsCfg<D, E4M3>>(p, max_rows, max_kv, st);
+        case 0: return run_one<typename Pick<D, E4M3, E4M3 ? 1 : 0>::C>(p, a, max_rows, max_kv, st);
+        case 1: return run_one<typename Pick<D, E4M3, 1>::C>(p, a, max_rows, max_kv, st);
+        case 2: return run_one<typename Pick<D, E4M3, 2>::C>(p, a, max_rows, max_kv, st);
+        default: return run_one<RowsCfg<D, E4M3>>(p, a, max_rows, max_kv, st);
     }
 }
 template <int D>
-cudaError_t run_d(const AttnParams& p, bool e4m3, int max_rows, long long max_kv, cudaStream_t st)
+cudaError_t run_d(const AttnParams& p, const AttnArgs& a, bool e4m3, int max_rows, long long max_kv, cudaStream_t st)
 {
-    return e4m3 ? run_df<D, true>(p, max_rows, max_kv, st) : run_df<D, false>(p, max_rows, max_kv, st);
+    return e4m3 ? run_df<D, true>(p, a, max_rows, max_kv, st) : run_df<D, false>(p, a, max_rows, max_kv, st);
 }
 template <class C>
 cudaError_t init_one_attn() { return cudaFuncSetAttribute(attention_paged_kernel<C>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM); }
@@ -664,6 +664,8 @@ cudaError_t attention_paged_init()
 }
 
 // Workspace: descriptors, (maximum, sum) and fp32 outputs of at most two parts per CTA.
+bool attention_uses_maps(int max_rows, bool e4m3, int page_size) { return rows_class(max_rows) == 3 && !e4m3 && page_size >= 8; }
+
 size_t attention_workspace_bytes(int max_rows, int head_dim, int sm_count)
 {
     const size_t rows = 2 * static_cast<size_t>(sm_count) * tile_rows(max_rows);
@@ -683,6 +685,7 @@ cudaError_t launch_attention_paged(const AttnArgs& a, void* workspace, int sm_co
     p.max_pages = a.max_pages; p.B = a.B; p.max_q = a.max_q; p.M = a.M; p.heads = a.heads; p.kv_heads = a.kv_heads;
     p.group = a.heads / a.kv_heads; p.causal = a.causal;
     p.G = sm_count;
+    p.tma = a.tma;
     const int max_rows = a.max_q * p.group;
     const size_t rows = 2 * static_cast<size_t>(sm_count) * tile_rows(max_rows);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
@@ -692,9 +695,9 @@ cudaError_t launch_attention_paged(const AttnArgs& a, void* workspace, int sm_co
     ws += (rows * sizeof(float2) + 255) / 256 * 256;
     p.part_o = reinterpret_cast<float*>(ws);
     const long long max_kv = static_cast<long long>(a.max_pages) << a.cache.page_shift;
-    if (a.head_dim == 64) return run_d<64>(p, a.e4m3, max_rows, max_kv, st);
-    if (a.head_dim == 128) return run_d<128>(p, a.e4m3, max_rows, max_kv, st);
-    return run_d<256>(p, a.e4m3, max_rows, max_kv, st);
+    if (a.head_dim == 64) return run_d<64>(p, a, a.e4m3, max_rows, max_kv, st);
+    if (a.head_dim == 128) return run_d<128>(p, a, a.e4m3, max_rows, max_kv, st);
+    return run_d<256>(p, a, a.e4m3, max_rows, max_kv, st);
 }
 
 }  // namespace rudder

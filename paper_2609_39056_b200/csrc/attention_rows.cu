@@ -93,6 +93,12 @@ __device__ __forceinline__ void tmem_st_x16(uint32_t taddr, const uint32_t (&r)[
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// Tiled load of [rows of a page][64 channels] of one head, 128-byte swizzle: coordinates channel, token of the page, head, page.
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* tm, int x, int y, int z, int w, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];" ::"r"(dst),
+                 "l"(reinterpret_cast<uint64_t>(tm)), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w)
+                 : "memory");
+}
 // Sixteen E4M3 numbers as two pieces of eight f16 numbers in shared memory.
 __device__ __forceinline__ void store_f16(uint32_t at0, uint32_t at1, uint4 v) {
     uint32_t h[8];
@@ -103,7 +109,7 @@ __device__ __forceinline__ void store_f16(uint32_t at0, uint32_t at1, uint4 v) {
 }
 
 template <class C>
-__global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const AttnParams p)
+__global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const AttnParams p, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v)
 {
     constexpr int D = C::D, KT = C::KT, ST = C::ST, LW = C::LW, ROWS = C::ROWS, SETS = C::SETS, MMA_WARP = C::MMA_WARP;
     constexpr bool E4M3 = C::E4M3;
@@ -469,6 +475,29 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
             ok = wait_all(kv_empty(slot), ((t / ST) & 1) ^ 1, W_R_KV_EMPTY);
             if (!ok) break;
             const uint32_t k_dst = k_s + slot * C::TILE, v_dst = v_s + slot * C::TILE;
+            const int tile0 = cur.j * KT;
+            // a whole tile in pages of 8 tokens or more: TMA, one box per page and 64 channels.  Its rows land where the copies below put them.
+            const bool by_tma = !E4M3 && p.tma && tile0 + KT <= cur.rq.len;
+            if (by_tma) {
+                const int rows = min(KT, 1 << p.cache.page_shift), boxes = KT / rows;
+                if (w == 0) {
+                    if (lane == 0) mbar_expect_tx(kv_full(slot), 2 * C::TILE);
+                    else mbar_arrive(kv_full(slot));
+                    __syncwarp();
+                    if (lane < boxes) {
+                        int page = __ldg(p.table + static_cast<size_t>(cur.b) * p.ld_table + ((tile0 + rows * lane) >> p.cache.page_shift));
+                        if (page < 0 || page >= p.cache.n_pages) { record_bad_data(kBadPage); page = p.cache.n_pages; }      // out of range: zeros
+                        const int tok = tile0 & ((1 << p.cache.page_shift) - 1);              // 0 in pages of up to KT tokens
+#pragma unroll
+                        for (int blk = 0; blk < D / 64; ++blk) {
+                            tma_load_4d(k_dst + blk * C::BLK + rows * lane * 128, &tm_k, 64 * blk, tok, cur.h, page, kv_full(slot));
+                            tma_load_4d(v_dst + blk * C::BLK + rows * lane * 128, &tm_v, 64 * blk, tok, cur.h, page, kv_full(slot));
+                        }
+                    }
+                } else {
+                    mbar_arrive(kv_full(slot));
+                }
+            } else {
             uint4 xk[E4M3 ? MINE * N : 1], xv[E4M3 ? MINE * N : 1];              // E4M3: this warp's share of the tile, all in flight together
 #pragma unroll
             for (int k = 0; k < MINE; ++k) {
@@ -529,6 +558,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                 }
             }
             signal(kv_full(slot));
+            }
             if (new_item) {
                 // the item's queries, each warp its share of the 128 rows; rows that do not exist become zeros
                 if (item > 0) {
@@ -589,7 +619,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
 }
 
 template <class C>
-cudaError_t launch_rows(const AttnParams& p, cudaStream_t st)
+cudaError_t launch_rows(const AttnParams& p, const CUtensorMap* tm_k, const CUtensorMap* tm_v, cudaStream_t st)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(p.G), 1, 1);
@@ -601,7 +631,7 @@ cudaError_t launch_rows(const AttnParams& p, cudaStream_t st)
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, attention_rows_kernel<C>, p);
+    return cudaLaunchKernelEx(&cfg, attention_rows_kernel<C>, p, *tm_k, *tm_v);
 }
 template <class C>
 cudaError_t init_rows() { return cudaFuncSetAttribute(attention_rows_kernel<C>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM); }

@@ -57,6 +57,8 @@ struct AttnArgs {
     const int32_t* kv_lens; const int32_t* q_starts;
     int B, max_q, causal;
     float scale;
+    bool tma;                             // tensor maps over K and V: see attention_rows.cu
+    CUtensorMap tm_k, tm_v;               // [pages][heads][tokens][channels], box {64, min(64, page size), 1, 1}, 128-byte swizzle
 };
 
 __device__ __forceinline__ void pdl_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
