@@ -8,8 +8,8 @@
 //                  operand is "MN-major", no transposition anywhere),  O in tensor memory
 // and the read of the cache is the bound again.
 //
-// Warps: two sets of four softmax warps that take the tiles in turn, a thread per row (no exchange between lanes; one set for D = 256), each with
-// its own reference, sum and O; then one warp that issues the MMAs; the others load, half of them K, half V.
+// Warps: two sets of four softmax warps that take half of a tile's keys each, a thread per row (no exchange between lanes; one set for D = 256), each
+// set with its own reference, sum and O; then one warp that issues the MMAs; three load.
 //   Loading: 16-byte cp.async per row piece, page by page, straight into the 128-byte-swizzled layout the tensor core reads; keys at or
 //     behind the request's length become zeros.  E4M3 goes through registers and becomes f16 (exact; Q as in attention_paged.cu).
 //   Softmax: pass 1 takes the maximum of the row's KT scores, pass 2 turns them into probabilities and writes them over the scores they
@@ -33,10 +33,11 @@ struct RowsCfg {
     static constexpr int D = D_;
     static constexpr bool E4M3 = E4M3_;
     static constexpr int ROWS = 128;
-    static constexpr int UK = 64;
+    static constexpr int UK = D <= 128 ? 128 : 64;
     static constexpr int KT = UK;                          // keys of a tile: a unit of the work split
-    static constexpr int ST = D == 64 ? 8 : (D == 128 ? 6 : 2);
-    static constexpr int SETS = D <= 128 ? 2 : 1;          // sets of four softmax warps that take the tiles in turn, each with an O of its own
+    static constexpr int ST = D == 64 ? 4 : (D == 128 ? 3 : 2);
+    static constexpr int SETS = D <= 128 ? 2 : 1;          // sets of four softmax warps: each takes its share of a tile's keys, with an O of its own
+    static constexpr int HALF = KT / SETS;
     static constexpr int LW = 3;                           // loading warps (12 warps in all: 168 registers a thread)
     static constexpr int LANDED = E4M3 ? LW : 32 * LW;     // arrivals that make a stage full: warps that stored it, or threads whose copies have landed
     static constexpr int MMA_WARP = 4 * SETS;
@@ -111,10 +112,10 @@ __device__ __forceinline__ void store_f16(uint32_t at0, uint32_t at1, uint4 v) {
 template <class C>
 __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const AttnParams p, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v)
 {
-    constexpr int D = C::D, KT = C::KT, ST = C::ST, LW = C::LW, ROWS = C::ROWS, SETS = C::SETS, MMA_WARP = C::MMA_WARP;
+    constexpr int D = C::D, KT = C::KT, ST = C::ST, LW = C::LW, ROWS = C::ROWS, SETS = C::SETS, HALF = C::HALF, MMA_WARP = C::MMA_WARP;
     constexpr bool E4M3 = C::E4M3;
     extern __shared__ uint8_t smem_raw_rows[];
-    __shared__ __align__(8) uint64_t bars[2 * ST + 10];
+    __shared__ __align__(8) uint64_t bars[2 * ST + 12];
     __shared__ float2 s_ml[ROWS];                          // (reference, sum) of the second set's rows
     __shared__ int8_t s_exp[E4M3 ? ROWS : 1];              // E4M3: the power of two that a row of Q was multiplied by
     __shared__ uint32_t tmem_slot;
@@ -132,13 +133,13 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
     auto kv_full = [&](int i) { return bar0 + 8u * i; };
     auto kv_empty = [&](int i) { return bar0 + 8u * (ST + i); };
     auto s_full = [&](int i) { return bar0 + 8u * (2 * ST + i); };
-    auto p_full = [&](int i) { return bar0 + 8u * (2 * ST + 2 + i); };
-    auto pv_done = [&](int set) { return bar0 + 8u * (2 * ST + 4 + set); };
-    const uint32_t ml_full = bar0 + 8u * (2 * ST + 6), o_free = ml_full + 8u, q_full = ml_full + 16u, q_empty = ml_full + 24u;
+    auto p_full = [&](int buf, int set) { return bar0 + 8u * (2 * ST + 2 + buf + 2 * set); };
+    auto pv_done = [&](int set) { return bar0 + 8u * (2 * ST + 6 + set); };
+    const uint32_t ml_full = bar0 + 8u * (2 * ST + 8), o_free = ml_full + 8u, q_full = ml_full + 16u, q_empty = ml_full + 24u;
     if (tid == 0) {
         abort_word = 0;
         for (int i = 0; i < ST; ++i) { mbar_init(kv_full(i), C::LANDED); mbar_init(kv_empty(i), 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(s_full(i), 1); mbar_init(p_full(i), 4); mbar_init(pv_done(i), 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(s_full(i), 1); mbar_init(p_full(i, 0), 4); mbar_init(p_full(i, 1), 4); mbar_init(pv_done(i), 1); }
         mbar_init(ml_full, 4); mbar_init(o_free, 4);
         mbar_init(q_full, C::LANDED); mbar_init(q_empty, 1 + 4 * SETS);                 // the last S of the item, and the softmax warps
         fence_mbar_init();
@@ -160,16 +161,14 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
         const int row = 32 * quad + lane;
         const uint32_t lanes = static_cast<uint32_t>(32 * quad) << 16;
         const uint32_t o_t = tmem + lanes + C::O_COL;
-        int t = 0, item = 0, part_j = 0, last_other = -1;  // last_other: the other set's last tile of the item
-        int mine = 0;                                      // tiles of this item that were this set's
-        bool ok = true, fresh = true, first_part = true, live_warp = false;
+        int t = 0, item = 0, part_j = 0;
+        bool ok = true, fresh = true, first_part = true, live_warp = false, first_tile = false;
         int lim = 0, lim_warp = 0, R = 0, r = 0;
         float f = 0.0f, m = -INFINITY, l = 0.0f;
         while (cur.left > 0) {
             if (fresh) {
                 fresh = false;
-                mine = 0;
-                last_other = -1;
+                first_tile = true;
                 part_j = cur.j;
                 R = cur.rq.qlen * p.group;
                 r = cur.rt * ROWS + row;
@@ -188,25 +187,23 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
             }
             const int buf = t & 1;
             const bool item_end = cur.j + 1 == cur.nt, ends = item_end || cur.left == 1;
-            if (SETS == 2 && buf != set) {
-                last_other = t;
-            } else {
-                ok = wait_all(s_full(buf), (t >> 1) & 1, W_R_S_FULL);
-                if (!ok) break;
+            ok = wait_all(s_full(buf), (t >> 1) & 1, W_R_S_FULL);
+            if (!ok) break;
+            {
                 if (live_warp) {
                     tcgen05_fence_after_sync();
-                    const uint32_t s_t = tmem + lanes + buf * KT;
-                    const int key0 = cur.j * KT;
-                    const bool edge = key0 + KT > lim_warp;                      // some row of this warp does not see all keys
+                    const uint32_t s_t = tmem + lanes + buf * KT + set * HALF;
+                    const int key0 = cur.j * KT + set * HALF;
+                    const bool edge = key0 + HALF > lim_warp;                      // some row of this warp does not see all keys
                     // pass 1: the maximum of s f
-                    uint32_t x[KT / 32][32];
+                    uint32_t x[HALF / 32][32];
 #pragma unroll
-                    for (int c = 0; c < KT / 32; ++c) tmem_ld_32x32b_x32(s_t + 32 * c, x[c]);
+                    for (int c = 0; c < HALF / 32; ++c) tmem_ld_32x32b_x32(s_t + 32 * c, x[c]);
                     tmem_wait_ld();
                     if (edge) {
                         const uint32_t gone = __float_as_uint(f < 0.0f ? INFINITY : -INFINITY);
 #pragma unroll
-                        for (int c = 0; c < KT / 32; ++c)
+                        for (int c = 0; c < HALF / 32; ++c)
 #pragma unroll
                             for (int i = 0; i < 32; ++i) x[c][i] = key0 + 32 * c + i < lim ? x[c][i] : gone;
                     }
@@ -215,24 +212,23 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                         float q[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
                         if (f >= 0.0f) {
 #pragma unroll
-                            for (int c = 0; c < KT / 32; ++c)
+                            for (int c = 0; c < HALF / 32; ++c)
 #pragma unroll
                                 for (int i = 0; i < 32; i += 2) q[(i >> 1) & 3] = fmaxf(q[(i >> 1) & 3], fmaxf(__uint_as_float(x[c][i]), __uint_as_float(x[c][i + 1])));
                         } else {
 #pragma unroll
-                            for (int c = 0; c < KT / 32; ++c)
+                            for (int c = 0; c < HALF / 32; ++c)
 #pragma unroll
                                 for (int i = 0; i < 32; ++i) q[i & 3] = fmaxf(q[i & 3], -__uint_as_float(x[c][i]));
                         }
                         mx = fmaxf(fmaxf(q[0], q[1]), fmaxf(q[2], q[3]));
                         mx = mx == -INFINITY ? mx : mx * fabsf(f);               // (no key seen stays -inf whatever f is)
                     }
-                    if (mine == 0) {
+                    if (first_tile) {
                         m = mx;
                     } else if (__any_sync(0xffffffffu, mx > m + 8.0f)) {
                         // raise the reference: O so far must be complete, then it is rescaled
-                        const int before = SETS == 2 ? (t >> 1) - 1 : t - 1;
-                        ok = wait_all(pv_done(set), before & 1, W_R_PV_DONE);
+                        ok = wait_all(pv_done(set), (t - 1) & 1, W_R_PV_DONE);
                         if (!ok) break;
                         tcgen05_fence_after_sync();
                         const float n = fmaxf(m, mx), cor = n == -INFINITY ? 1.0f : exp2_approx(m - n);
@@ -253,7 +249,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                     const float u = m == -INFINITY ? 0.0f : m;
                     float l0 = 0.0f, l1 = 0.0f;
 #pragma unroll
-                    for (int c = 0; c < KT / 32; ++c) {
+                    for (int c = 0; c < HALF / 32; ++c) {
                         uint32_t w[32];                    // hi (or f16) in the first half, lo in the second
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
@@ -278,9 +274,9 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                     tmem_wait_st();
                     tcgen05_fence_before_sync();
                 }
-                ++mine;
+                first_tile = false;
                 __syncwarp();
-                if (lane == 0) mbar_arrive(p_full(buf));
+                if (lane == 0) mbar_arrive(p_full(buf, set));
             }
             if (ends) {
                 if (SETS == 2 && set == 1) {
@@ -294,26 +290,18 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                     if (lane == 0) mbar_arrive(ml_full);
                 } else {
                     if (live_warp) {
-                        const int last_mine = (SETS == 2 && buf != set) ? t - 1 : t;       // this set's last tile of the item, if it had one
-                        if (mine > 0) {
-                            ok = wait_all(pv_done(set), (SETS == 2 ? last_mine >> 1 : last_mine) & 1, W_R_PV_DONE);
-                            if (!ok) break;
-                        }
+                        ok = wait_all(pv_done(0), t & 1, W_R_PV_DONE);
                         float w0 = 1.0f, w1 = 0.0f, mm = m, ll = l;
                         if (SETS == 2) {
-                            ok = wait_all(ml_full, (item - 1) & 1, W_R_ML_FULL);
-                            if (!ok) break;
-                            if (last_other >= 0) {
-                                ok = wait_all(pv_done(1), (last_other >> 1) & 1, W_R_PV_DONE);
-                                if (!ok) break;
-                                const float2 o = s_ml[row];
-                                mm = fmaxf(m, o.x);
-                                const float u = mm == -INFINITY ? 0.0f : mm;
-                                w0 = exp2_approx(m - u);
-                                w1 = exp2_approx(o.x - u);
-                                ll = l * w0 + o.y * w1;
-                            }
+                            ok = ok && wait_all(ml_full, (item - 1) & 1, W_R_ML_FULL) && wait_all(pv_done(1), t & 1, W_R_PV_DONE);
+                            const float2 o = s_ml[row];
+                            mm = fmaxf(m, o.x);
+                            const float u = mm == -INFINITY ? 0.0f : mm;
+                            w0 = exp2_approx(m - u);
+                            w1 = exp2_approx(o.x - u);
+                            ll = l * w0 + o.y * w1;
                         }
+                        if (!ok) break;
                         tcgen05_fence_after_sync();
                         const bool entire = item_end && part_j == 0;
                         const float vs = E4M3 && p.cache.v_scale != nullptr ? __ldg(p.cache.v_scale + cur.h) : 1.0f;
@@ -327,15 +315,14 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
 #pragma unroll 1
                         for (int c = 0; c < D / 16; ++c) {
                             uint32_t o[16], o2[16];
-                            // (an O that no product of this item has written is not read)
-                            if (mine > 0) tmem_ld_32x32b_x16(o_t + 16 * c, o);
-                            if (SETS == 2 && last_other >= 0) tmem_ld_32x32b_x16(o_t + D + 16 * c, o2);
+                            tmem_ld_32x32b_x16(o_t + 16 * c, o);
+                            if (SETS == 2) tmem_ld_32x32b_x16(o_t + D + 16 * c, o2);
                             tmem_wait_ld();
                             float v[16];
 #pragma unroll
                             for (int i = 0; i < 16; ++i) {
-                                v[i] = mine > 0 ? __uint_as_float(o[i]) * w0 : 0.0f;
-                                if (SETS == 2 && last_other >= 0) v[i] = fmaf(__uint_as_float(o2[i]), w1, v[i]);
+                                v[i] = __uint_as_float(o[i]) * w0;
+                                if (SETS == 2) v[i] = fmaf(__uint_as_float(o2[i]), w1, v[i]);
                             }
                             if (r < R) {
                                 if (entire) {
@@ -370,34 +357,36 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
         // ---------------------------------------------------------------------------------------- MMA issue
         const bool leader = elect_one();
         const uint32_t idesc_s = umma_idesc_f16(ROWS, KT, !E4M3, false), idesc_o = umma_idesc_f16(ROWS, D, !E4M3, true);
-        int t = 0, item = 0, in_item = 0;
-        bool ok = true, fresh = true;
-        int prev_in_item = 0, prev_item = 0;
-        // O += P V of tile `pt`, the `nth` of item `it`: the first SETS tiles of an item start their O
-        auto pv = [&](int pt, int nth, int it) -> bool {
-            const int buf = pt & 1, slot = pt % ST, set = SETS == 2 ? buf : 0;
-            if (!wait_all(p_full(buf), (pt >> 1) & 1, W_R_P_FULL)) return false;
-            if (nth == 0 && it > 0 && !wait_all(o_free, (it - 1) & 1, W_R_O_FREE)) return false;      // the item before has been read out
-            tcgen05_fence_after_sync();
-            if (leader) {
-                const uint32_t v0 = v_s + slot * C::TILE, o = tmem + C::O_COL + set * D;
+        int t = 0, item = 0, prev_item = 0;
+        bool ok = true, fresh = true, prev_first = false;
+        // O += P V of tile `pt` of item `it`, a set's keys each; the first tile of an item starts its O
+        auto pv = [&](int pt, bool first, int it) -> bool {
+            const int buf = pt & 1, slot = pt % ST;
+            if (first && it > 0 && !wait_all(o_free, (it - 1) & 1, W_R_O_FREE)) return false;         // the item before has been read out
 #pragma unroll
-                for (int kk = 0; kk < KT / 16; ++kk) {
-                    const uint64_t db = umma_desc_sw128_mn(v0 + kk * 2048, C::BLK);
-                    const uint32_t pa = tmem + buf * KT + 32 * (kk >> 1) + 8 * (kk & 1);
-                    umma_f16_ts(o, pa, db, idesc_o, (nth < SETS && kk == 0) ? 0u : 1u);
-                    if (!E4M3) umma_f16_ts(o, pa + 16, db, idesc_o, 1u);
+            for (int set = 0; set < SETS; ++set) {
+                if (!wait_all(p_full(buf, set), (pt >> 1) & 1, W_R_P_FULL)) return false;
+                tcgen05_fence_after_sync();
+                if (leader) {
+                    const uint32_t v0 = v_s + slot * C::TILE + set * HALF * 128, o = tmem + C::O_COL + set * D;
+#pragma unroll
+                    for (int kk = 0; kk < HALF / 16; ++kk) {
+                        const uint64_t db = umma_desc_sw128_mn(v0 + kk * 2048, C::BLK);
+                        const uint32_t pa = tmem + buf * KT + set * HALF + 32 * (kk >> 1) + 8 * (kk & 1);
+                        umma_f16_ts(o, pa, db, idesc_o, (first && kk == 0) ? 0u : 1u);
+                        if (!E4M3) umma_f16_ts(o, pa + 16, db, idesc_o, 1u);
+                    }
+                    if (set == SETS - 1) umma_commit(kv_empty(slot));            // (and the S of this stage, issued before)
+                    umma_commit(pv_done(set));
                 }
-                umma_commit(kv_empty(slot));                   // (and the S of this stage, issued before)
-                umma_commit(pv_done(set));
+                __syncwarp();
             }
-            __syncwarp();
             return true;
         };
         while (cur.left > 0) {
+            const bool first = fresh;
             if (fresh) {
                 fresh = false;
-                in_item = 0;
                 ok = wait_all(q_full, item & 1, W_R_Q_FULL);
                 if (!ok) break;
                 ++item;
@@ -406,7 +395,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
             const int slot = t % ST;
             ok = wait_all(kv_full(slot), (t / ST) & 1, W_R_KV_FULL);
             // S goes over the probabilities of two tiles ago: their product must be complete (products into different accumulators are not ordered)
-            if (ok && t >= 2) ok = SETS == 2 ? wait_all(pv_done(t & 1), ((t >> 1) - 1) & 1, W_R_PV_DONE) : wait_all(pv_done(0), t & 1, W_R_PV_DONE);
+            if (ok && t >= 2) ok = wait_all(pv_done(0), t & 1, W_R_PV_DONE) && (SETS == 1 || wait_all(pv_done(1), t & 1, W_R_PV_DONE));
             if (!ok) break;
             fence_proxy_async_smem();                      // the loaders' writes -> the tensor core's reads, K and V of the stage
             tcgen05_fence_after_sync();
@@ -421,16 +410,16 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
             }
             __syncwarp();
             if (t > 0) {
-                ok = pv(t - 1, prev_in_item, prev_item);
+                ok = pv(t - 1, prev_first, prev_item);
                 if (!ok) break;
             }
-            prev_in_item = in_item++;
+            prev_first = first;
             prev_item = item - 1;
             fresh = ends;
             ++t;
             cur.advance(p);
         }
-        if (ok && t > 0) pv(t - 1, prev_in_item, prev_item);
+        if (ok && t > 0) pv(t - 1, prev_first, prev_item);
     } else {
         // ---------------------------------------------------------------------------------------- loading
         const int w = warp - MMA_WARP - 1;
@@ -467,6 +456,10 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
             return run_in_page && lane < MINE && run < NRUN ? page_of(cur.j * KT + RUN * run) : -1;
         };
         int pages = run_pages();
+        // TMA boxes of a tile, and the page of lane i's, requested a tile ahead as well
+        const int box_rows = min(64, 1 << p.cache.page_shift), boxes = KT / box_rows;
+        auto box_pages = [&]() -> int { return w == 0 && lane < boxes ? page_of(cur.j * KT + box_rows * lane) : -1; };
+        int box_page = box_pages();
         while (cur.left > 0) {
             const bool ends = cur.j + 1 == cur.nt || cur.left == 1;
             const int slot = t % ST;
@@ -479,19 +472,18 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
             // a whole tile in pages of 8 tokens or more: TMA, one box per page and 64 channels.  Its rows land where the copies below put them.
             const bool by_tma = !E4M3 && p.tma && tile0 + KT <= cur.rq.len;
             if (by_tma) {
-                const int rows = min(KT, 1 << p.cache.page_shift), boxes = KT / rows;
                 if (w == 0) {
                     if (lane == 0) mbar_expect_tx(kv_full(slot), 2 * C::TILE);
                     else mbar_arrive(kv_full(slot));
                     __syncwarp();
                     if (lane < boxes) {
-                        int page = __ldg(p.table + static_cast<size_t>(cur.b) * p.ld_table + ((tile0 + rows * lane) >> p.cache.page_shift));
+                        int page = box_page;
                         if (page < 0 || page >= p.cache.n_pages) { record_bad_data(kBadPage); page = p.cache.n_pages; }      // out of range: zeros
-                        const int tok = tile0 & ((1 << p.cache.page_shift) - 1);              // 0 in pages of up to KT tokens
+                        const int tok = (tile0 + box_rows * lane) & ((1 << p.cache.page_shift) - 1);
 #pragma unroll
                         for (int blk = 0; blk < D / 64; ++blk) {
-                            tma_load_4d(k_dst + blk * C::BLK + rows * lane * 128, &tm_k, 64 * blk, tok, cur.h, page, kv_full(slot));
-                            tma_load_4d(v_dst + blk * C::BLK + rows * lane * 128, &tm_v, 64 * blk, tok, cur.h, page, kv_full(slot));
+                            tma_load_4d(k_dst + blk * C::BLK + box_rows * lane * 128, &tm_k, 64 * blk, tok, cur.h, page, kv_full(slot));
+                            tma_load_4d(v_dst + blk * C::BLK + box_rows * lane * 128, &tm_v, 64 * blk, tok, cur.h, page, kv_full(slot));
                         }
                     }
                 } else {
@@ -599,7 +591,10 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
             }
             ++t;
             cur.advance(p);
-            if (cur.left > 0) pages = run_pages();
+            if (cur.left > 0) {
+                pages = run_pages();
+                box_page = box_pages();
+            }
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
     }
