@@ -21,11 +21,12 @@ struct AttnParams {
     const int32_t* table; int64_t ld_table;
     const int32_t* kv_lens;
     const int32_t* q_starts;
-    float* part_o;                      // [2 G][rows of a tile][D]
+    float* part_o;                      // [2 G][rows of a tile][D]; many rows: [2 G][D / 4][rows of a tile][4]
     float2* part_ml;                    // [2 G][rows of a tile]
     int* desc;                          // [G][8]
     float scale_log2;
     int max_pages, B, max_q, M, heads, kv_heads, group, causal;
+    uint32_t group_inv;                 // ceil(2^32 / group), 0 for a group of one: see row_of
     int whole_units;                    // items of at most this many units are not cut when there is a CTA for each
     int G;                              // CTAs
     int tma;                            // many rows: tensor maps over the cache are there
@@ -62,6 +63,16 @@ __device__ __forceinline__ void e4m3_to_f16(uint32_t w, uint32_t& lo, uint32_t& 
 }
 // The same for bytes 0 and 2, bytes 1 and 3.
 __device__ __forceinline__ void e4m3_to_f16_split(uint32_t w, uint32_t& even, uint32_t& odd) { e4m3_to_f16(__byte_perm(w, 0, 0x3120), even, odd); }
+
+// Row r of an item: which of the request's new tokens, which head of its group.  r < 2^20 and a group of at most 1024 heads make the
+// product exact: r (ceil(2^32 / g) g - 2^32) < 2^32.
+struct RowOf { int token, head; };
+__device__ __forceinline__ RowOf row_of(const AttnParams& p, int r) {
+    RowOf o;
+    o.token = p.group_inv ? static_cast<int>(__umulhi(static_cast<uint32_t>(r), p.group_inv)) : r;
+    o.head = r - o.token * p.group;
+    return o;
+}
 
 // What the kernels know of a request.
 struct Req { int len, row0, qlen; };

@@ -175,14 +175,15 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const int r = first_row + 8 * n + (LO == 1 ? (2 * q + e) & 3 : 2 * q + e);
-                    lim[n][e] = (p.causal && r < R) ? cur.rq.len - cur.rq.qlen + r / p.group + 1 : cur.rq.len;
+                    lim[n][e] = (p.causal && r < R) ? cur.rq.len - cur.rq.qlen + row_of(p, r).token + 1 : cur.rq.len;
                     lim_min = min(lim_min, lim[n][e]);
                     fac[n][e] = p.scale_log2;
                 }
                 const int r = first_row + 8 * n + (LO == 1 ? g & 3 : g);
                 const bool live = r < R;
                 const uint16_t* qr = p.Q;
-                if (live) qr += static_cast<size_t>(cur.rq.row0 + r / p.group) * p.ldq + static_cast<size_t>(cur.h * p.group + r % p.group) * D;
+                const RowOf at = row_of(p, r);
+                if (live) qr += static_cast<size_t>(cur.rq.row0 + at.token) * p.ldq + static_cast<size_t>(cur.h * p.group + at.head) * D;
                 if (!E4M3) {
 #pragma unroll
                     for (int ks = 0; ks < KS; ++ks) {
@@ -406,9 +407,10 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
                         const int r = cur.rt * ROWS + rl;
                         if (r < R) {
                             if (!entire) p.part_ml[static_cast<size_t>(slot) * ROWS + rl] = make_float2(m, l);
-                            else if (p.lse != nullptr)
-                                p.lse[static_cast<size_t>(cur.rq.row0 + r / p.group) * p.heads + cur.h * p.group + r % p.group] =
-                                    l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
+                            else if (p.lse != nullptr) {
+                                const RowOf at = row_of(p, r);
+                                p.lse[static_cast<size_t>(cur.rq.row0 + at.token) * p.heads + cur.h * p.group + at.head] = l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
+                            }
                         }
                     }
                 }
@@ -445,9 +447,9 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
                             o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w;
                         }
                     }
-                    const int r = cur.rt * ROWS + rl;
+                    const RowOf at = row_of(p, cur.rt * ROWS + rl);
                     if (entire)
-                        *reinterpret_cast<uint2*>(p.O + static_cast<size_t>(cur.rq.row0 + r / p.group) * p.ldo + static_cast<size_t>(cur.h * p.group + r % p.group) * D +
+                        *reinterpret_cast<uint2*>(p.O + static_cast<size_t>(cur.rq.row0 + at.token) * p.ldo + static_cast<size_t>(cur.h * p.group + at.head) * D +
                                                   round * DC + d) = make_uint2(bf16x2(o.x, o.y), bf16x2(o.z, o.w));
                     else
                         *reinterpret_cast<float4*>(p.part_o + (static_cast<size_t>(slot) * ROWS + rl) * D + round * DC + d) = o;
@@ -466,6 +468,14 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
 // JOIN_ROWS y .. + JOIN_ROWS - 1 of its tile.  JOIN_SPLIT warps per row take the parts in turn.
 constexpr int JOIN_THREADS = 256, JOIN_ROWS = 2, JOIN_SPLIT = JOIN_THREADS / 32 / JOIN_ROWS;
 
+// The item that run c starts inside; false if its join is another CTA's or there is none.
+struct Cut { int h, rt, row0, qlen, first, n, slot_first; };
+__device__ __forceinline__ bool load_cut(const AttnParams& p, int c, Cut& x) {
+    const int4 a = __ldcg(reinterpret_cast<const int4*>(p.desc + 8 * c)), b = __ldcg(reinterpret_cast<const int4*>(p.desc + 8 * c + 4));
+    x.h = a.y; x.rt = a.z; x.row0 = a.w; x.qlen = b.x; x.first = c - 1; x.n = b.y - (c - 1) + 1; x.slot_first = b.z;
+    return a.x != 0;
+}
+
 template <int D>
 __global__ void __launch_bounds__(JOIN_THREADS) attention_join_kernel(const AttnParams p, int rows_of_tile)
 {
@@ -473,33 +483,29 @@ __global__ void __launch_bounds__(JOIN_THREADS) attention_join_kernel(const Attn
     __shared__ float2 s_ml[JOIN_ROWS][JOIN_SPLIT];
     pdl_launch_dependents();
     pdl_wait();
-    const int c = blockIdx.x;
-    const int* d = p.desc + 8 * c;
-    if (d[0] == 0) return;
-    const int h = d[1], rt = d[2], row0 = d[3], qlen = d[4], last = d[5], slot_first = d[6];
+    Cut x;
+    if (!load_cut(p, blockIdx.x, x)) return;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int ry = warp / JOIN_SPLIT, part = warp % JOIN_SPLIT;
-    const int rl = blockIdx.y * JOIN_ROWS + ry, r = rt * rows_of_tile + rl;
-    const bool live = r < qlen * p.group;
+    const int rl = blockIdx.y * JOIN_ROWS + ry, r = x.rt * rows_of_tile + rl;
+    const bool live = r < x.qlen * p.group;
     constexpr int V = D / 32;                              // channels of a lane
     float o[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) o[i] = 0.0f;
     float m = -INFINITY, l = 0.0f;
     if (live) {
-        const int n = last - (c - 1) + 1;
-        for (int s = part; s < n; s += JOIN_SPLIT) {
-            const int slot = 2 * (c - 1 + s) + (s == 0 ? slot_first : 0);
-            const size_t at = static_cast<size_t>(slot) * rows_of_tile + rl;
+        for (int s = part; s < x.n; s += JOIN_SPLIT) {
+            const size_t at = (2 * static_cast<size_t>(x.first + s) + (s == 0 ? x.slot_first : 0)) * rows_of_tile + rl;
             const float2 ml = __ldcg(p.part_ml + at);
             const float* src = p.part_o + at * D + lane * V;
             float v[V];
-            if (V == 2) { const float2 x = __ldcg(reinterpret_cast<const float2*>(src)); v[0] = x.x; v[1] = x.y; }
+            if (V == 2) { const float2 t = __ldcg(reinterpret_cast<const float2*>(src)); v[0] = t.x; v[1] = t.y; }
             else {
 #pragma unroll
                 for (int i = 0; i < V; i += 4) {
-                    const float4 x = __ldcg(reinterpret_cast<const float4*>(src + i));
-                    v[i] = x.x; v[i + 1] = x.y; v[i + 2] = x.z; v[i + 3] = x.w;
+                    const float4 t = __ldcg(reinterpret_cast<const float4*>(src + i));
+                    v[i] = t.x; v[i + 1] = t.y; v[i + 2] = t.z; v[i + 3] = t.w;
                 }
             }
             const float nm = fmaxf(m, ml.x), u = nm == -INFINITY ? 0.0f : nm;
@@ -525,8 +531,9 @@ __global__ void __launch_bounds__(JOIN_THREADS) attention_join_kernel(const Attn
         ll += s_ml[ry][s].y * w[s];
     }
     const float inv = ll > 0.0f ? 1.0f / ll : 0.0f;
-    const int t_row = r / p.group, hh = h * p.group + r % p.group;
-    uint16_t* orow = p.O + static_cast<size_t>(row0 + t_row) * p.ldo + static_cast<size_t>(hh) * D + lane * V;
+    const RowOf at = row_of(p, r);
+    const int hh = x.h * p.group + at.head;
+    uint16_t* orow = p.O + static_cast<size_t>(x.row0 + at.token) * p.ldo + static_cast<size_t>(hh) * D + lane * V;
 #pragma unroll
     for (int i = 0; i < V; i += 2) {
         float a = 0.0f, b = 0.0f;
@@ -537,8 +544,44 @@ __global__ void __launch_bounds__(JOIN_THREADS) attention_join_kernel(const Attn
         }
         *reinterpret_cast<uint32_t*>(orow + i) = bf16x2(a * inv, b * inv);
     }
-    if (lane == 0 && p.lse != nullptr)
-        p.lse[static_cast<size_t>(row0 + t_row) * p.heads + hh] = ll > 0.0f ? (mm + log2f(ll)) * kLn2 : -INFINITY;
+    if (lane == 0 && p.lse != nullptr) p.lse[static_cast<size_t>(x.row0 + at.token) * p.heads + hh] = ll > 0.0f ? (mm + log2f(ll)) * kLn2 : -INFINITY;
+}
+
+// The same for many rows: a lane per row, as the parts lie; a warp has 32 rows x 8 channels, a CTA 64 channels, y = row block x channel block.
+template <int D>
+__global__ void __launch_bounds__(JOIN_THREADS) attention_join_rows_kernel(const AttnParams p, int rows_of_tile)
+{
+    pdl_launch_dependents();
+    pdl_wait();
+    Cut x;
+    if (!load_cut(p, blockIdx.x, x)) return;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int rl = blockIdx.y / (D / 64) * 32 + lane, ch = blockIdx.y % (D / 64) * 64 + warp * 8;
+    const int r = x.rt * rows_of_tile + rl;
+    if (r >= x.qlen * p.group) return;
+    float o[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = 0.0f;
+    float m = -INFINITY, l = 0.0f;
+#pragma unroll 4
+    for (int s = 0; s < x.n; ++s) {
+        const size_t slot = 2 * static_cast<size_t>(x.first + s) + (s == 0 ? x.slot_first : 0);
+        const float2 ml = __ldcg(p.part_ml + slot * rows_of_tile + rl);
+        const float* src = p.part_o + slot * rows_of_tile * D + (static_cast<size_t>(ch / 4) * rows_of_tile + rl) * 4;
+        const float4 v0 = __ldcg(reinterpret_cast<const float4*>(src)), v1 = __ldcg(reinterpret_cast<const float4*>(src + 4 * rows_of_tile));
+        const float nm = fmaxf(m, ml.x), u = nm == -INFINITY ? 0.0f : nm;
+        const float a = exp2_approx(m - u), b = exp2_approx(ml.x - u);
+        m = nm;
+        l = l * a + ml.y * b;
+        o[0] = o[0] * a + v0.x * b; o[1] = o[1] * a + v0.y * b; o[2] = o[2] * a + v0.z * b; o[3] = o[3] * a + v0.w * b;
+        o[4] = o[4] * a + v1.x * b; o[5] = o[5] * a + v1.y * b; o[6] = o[6] * a + v1.z * b; o[7] = o[7] * a + v1.w * b;
+    }
+    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+    const RowOf at = row_of(p, r);
+    const int hh = x.h * p.group + at.head;
+    *reinterpret_cast<uint4*>(p.O + static_cast<size_t>(x.row0 + at.token) * p.ldo + static_cast<size_t>(hh) * D + ch) =
+        make_uint4(bf16x2(o[0] * inv, o[1] * inv), bf16x2(o[2] * inv, o[3] * inv), bf16x2(o[4] * inv, o[5] * inv), bf16x2(o[6] * inv, o[7] * inv));
+    if (ch == 0 && p.lse != nullptr) p.lse[static_cast<size_t>(x.row0 + at.token) * p.heads + hh] = l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
 }
 
 // ---- variants: warps over rows (RW) and keys (KW), keys per tile, stages.  The ring is about 130 to 200 KB: it is what keeps
@@ -597,8 +640,9 @@ template <int D>
 cudaError_t launch_join(const AttnParams& p, int rows_of_tile, int max_rows, cudaStream_t st)
 {
     const int rows = max_rows < rows_of_tile ? max_rows : rows_of_tile;
+    const bool many = rows_class(max_rows) == 3;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(p.G), static_cast<unsigned>((rows + JOIN_ROWS - 1) / JOIN_ROWS), 1);
+    cfg.gridDim = dim3(static_cast<unsigned>(p.G), static_cast<unsigned>(many ? (rows + 31) / 32 * (D / 64) : (rows + JOIN_ROWS - 1) / JOIN_ROWS), 1);
     cfg.blockDim = dim3(JOIN_THREADS, 1, 1);
     cfg.stream = st;
     cudaLaunchAttribute attr[1];
@@ -606,7 +650,7 @@ cudaError_t launch_join(const AttnParams& p, int rows_of_tile, int max_rows, cud
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, attention_join_kernel<D>, p, rows_of_tile);
+    return many ? cudaLaunchKernelEx(&cfg, attention_join_rows_kernel<D>, p, rows_of_tile) : cudaLaunchKernelEx(&cfg, attention_join_kernel<D>, p, rows_of_tile);
 }
 template <class C>
 cudaError_t run_one(AttnParams p, const AttnArgs& a, int max_rows, long long max_kv, cudaStream_t st)
@@ -684,6 +728,7 @@ cudaError_t launch_attention_paged(const AttnArgs& a, void* workspace, int sm_co
     p.scale_log2 = a.scale * 1.4426950408889634f;
     p.max_pages = a.max_pages; p.B = a.B; p.max_q = a.max_q; p.M = a.M; p.heads = a.heads; p.kv_heads = a.kv_heads;
     p.group = a.heads / a.kv_heads; p.causal = a.causal;
+    p.group_inv = p.group == 1 ? 0u : static_cast<uint32_t>(((1ull << 32) + p.group - 1) / p.group);
     p.G = sm_count;
     p.tma = a.tma;
     const int max_rows = a.max_q * p.group;

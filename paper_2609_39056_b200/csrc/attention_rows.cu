@@ -39,7 +39,7 @@ struct RowsCfg {
     static constexpr int SETS = D <= 128 ? 2 : 1;          // sets of four softmax warps: each takes its share of a tile's keys, with an O of its own
     static constexpr int HALF = KT / SETS;
     static constexpr int LW = 3;                           // loading warps (12 warps in all: 168 registers a thread)
-    static constexpr int LANDED = E4M3 ? LW : 32 * LW;     // arrivals that make a stage full: warps that stored it, or threads whose copies have landed
+    static constexpr int QW = 2;                           // of them, those that load the queries (the first issues the TMA loads and waits for nothing else)
     static constexpr int MMA_WARP = 4 * SETS;
     static constexpr int THREADS = 32 * (MMA_WARP + 1 + LW);
     static constexpr int BLK = KT * 128;                   // a tile is D / 64 blocks of [KT keys][64 channels]
@@ -138,10 +138,10 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
     const uint32_t ml_full = bar0 + 8u * (2 * ST + 8), o_free = ml_full + 8u, q_full = ml_full + 16u, q_empty = ml_full + 24u;
     if (tid == 0) {
         abort_word = 0;
-        for (int i = 0; i < ST; ++i) { mbar_init(kv_full(i), C::LANDED); mbar_init(kv_empty(i), 1); }
+        for (int i = 0; i < ST; ++i) { mbar_init(kv_full(i), LW); mbar_init(kv_empty(i), 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(s_full(i), 1); mbar_init(p_full(i, 0), 4); mbar_init(p_full(i, 1), 4); mbar_init(pv_done(i), 1); }
         mbar_init(ml_full, 4); mbar_init(o_free, 4);
-        mbar_init(q_full, C::LANDED); mbar_init(q_empty, 1 + 4 * SETS);                 // the last S of the item, and the softmax warps
+        mbar_init(q_full, C::QW); mbar_init(q_empty, 1 + 4 * SETS);                 // the last S of the item, and the softmax warps
         fence_mbar_init();
     }
     if (warp == MMA_WARP) {
@@ -173,14 +173,14 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                 R = cur.rq.qlen * p.group;
                 r = cur.rt * ROWS + row;
                 live_warp = cur.rt * ROWS + 32 * quad < R;
-                lim = (p.causal && r < R) ? cur.rq.len - cur.rq.qlen + r / p.group + 1 : cur.rq.len;
+                lim = (p.causal && r < R) ? cur.rq.len - cur.rq.qlen + row_of(p, r).token + 1 : cur.rq.len;
                 lim_warp = __reduce_min_sync(0xffffffffu, lim);
                 m = -INFINITY;
                 l = 0.0f;
-                f = p.scale_log2;
+                f = r < R ? p.scale_log2 : 0.0f;           // rows that do not exist hold whatever the buffer held: weight 0, nothing read from them
                 ok = wait_all(q_full, item & 1, W_R_Q_FULL);
                 if (!ok) break;
-                if (E4M3) f *= __uint_as_float(static_cast<uint32_t>(127 - s_exp[row]) << 23) * (p.cache.k_scale != nullptr ? __ldg(p.cache.k_scale + cur.h) : 1.0f);
+                if (E4M3 && r < R) f *= __uint_as_float(static_cast<uint32_t>(127 - s_exp[row]) << 23) * (p.cache.k_scale != nullptr ? __ldg(p.cache.k_scale + cur.h) : 1.0f);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(q_empty);
                 ++item;
@@ -224,9 +224,10 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                         mx = fmaxf(fmaxf(q[0], q[1]), fmaxf(q[2], q[3]));
                         mx = mx == -INFINITY ? mx : mx * fabsf(f);               // (no key seen stays -inf whatever f is)
                     }
+                    __syncwarp();                          // (the tensor memory instructions below want the whole warp together)
                     if (first_tile) {
                         m = mx;
-                    } else if (__any_sync(0xffffffffu, mx > m + 8.0f)) {
+                    } else if (__any_sync(0xffffffffu, r < R && mx > m + 8.0f)) {
                         // raise the reference: O so far must be complete, then it is rescaled
                         ok = wait_all(pv_done(set), (t - 1) & 1, W_R_PV_DONE);
                         if (!ok) break;
@@ -267,6 +268,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                                 w[16 + i] = bf16x2(a - bf16_lo(w[i]), b - bf16_hi(w[i]));
                             }
                         }
+                        __syncwarp();
                         if (E4M3) tmem_st_x16(s_t + 32 * c, reinterpret_cast<const uint32_t (&)[16]>(w));
                         else tmem_st_x32(s_t + 32 * c, w);
                     }
@@ -275,6 +277,12 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                     tcgen05_fence_before_sync();
                 }
                 first_tile = false;
+                // The product before must be complete before this one can begin: a barrier is waited for phase by phase (a wait for phase t while
+                // phase t - 1 is open would take phase t - 2 for it, and the rows would be read out too early).
+                if (t > 0) {
+                    ok = wait_all(pv_done(set), (t - 1) & 1, W_R_PV_DONE);
+                    if (!ok) break;
+                }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(p_full(buf, set));
             }
@@ -289,11 +297,13 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                     __syncwarp();
                     if (lane == 0) mbar_arrive(ml_full);
                 } else {
+                    // (every warp of the set waits, those without rows too: one that ran ahead would arrive twice at o_free in one phase)
+                    ok = wait_all(pv_done(0), t & 1, W_R_PV_DONE) &&
+                         (SETS == 1 || (wait_all(ml_full, (item - 1) & 1, W_R_ML_FULL) && wait_all(pv_done(1), t & 1, W_R_PV_DONE)));
+                    if (!ok) break;
                     if (live_warp) {
-                        ok = wait_all(pv_done(0), t & 1, W_R_PV_DONE);
                         float w0 = 1.0f, w1 = 0.0f, mm = m, ll = l;
                         if (SETS == 2) {
-                            ok = ok && wait_all(ml_full, (item - 1) & 1, W_R_ML_FULL) && wait_all(pv_done(1), t & 1, W_R_PV_DONE);
                             const float2 o = s_ml[row];
                             mm = fmaxf(m, o.x);
                             const float u = mm == -INFINITY ? 0.0f : mm;
@@ -301,7 +311,6 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                             w1 = exp2_approx(o.x - u);
                             ll = l * w0 + o.y * w1;
                         }
-                        if (!ok) break;
                         tcgen05_fence_after_sync();
                         const bool entire = item_end && part_j == 0;
                         const float vs = E4M3 && p.cache.v_scale != nullptr ? __ldg(p.cache.v_scale + cur.h) : 1.0f;
@@ -309,32 +318,34 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                         w0 *= w;
                         w1 *= w;
                         const int slot = 2 * blockIdx.x + (first_part ? 0 : 1);
-                        const int tok = r / p.group, hh = cur.h * p.group + r % p.group;
+                        const RowOf at = row_of(p, r);
+                        const int tok = at.token, hh = cur.h * p.group + at.head;
                         uint16_t* orow = p.O + static_cast<size_t>(cur.rq.row0 + tok) * p.ldo + static_cast<size_t>(hh) * D;
-                        float* prow = p.part_o + (static_cast<size_t>(slot) * ROWS + row) * D;
+                        float* prow = p.part_o + static_cast<size_t>(slot) * ROWS * D + 4 * row;             // [channels / 4][rows][4]: coalesced
 #pragma unroll 1
-                        for (int c = 0; c < D / 16; ++c) {
-                            uint32_t o[16], o2[16];
-                            tmem_ld_32x32b_x16(o_t + 16 * c, o);
-                            if (SETS == 2) tmem_ld_32x32b_x16(o_t + D + 16 * c, o2);
+                        for (int c = 0; c < D / 32; ++c) {
+                            uint32_t o[32], o2[32];
+                            tmem_ld_32x32b_x32(o_t + 32 * c, o);
+                            if (SETS == 2) tmem_ld_32x32b_x32(o_t + D + 32 * c, o2);
                             tmem_wait_ld();
-                            float v[16];
+                            float v[32];
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) {
+                            for (int i = 0; i < 32; ++i) {
                                 v[i] = __uint_as_float(o[i]) * w0;
                                 if (SETS == 2) v[i] = fmaf(__uint_as_float(o2[i]), w1, v[i]);
                             }
                             if (r < R) {
                                 if (entire) {
-                                    *reinterpret_cast<uint4*>(orow + 16 * c) =
-                                        make_uint4(bf16x2(v[0], v[1]), bf16x2(v[2], v[3]), bf16x2(v[4], v[5]), bf16x2(v[6], v[7]));
-                                    *reinterpret_cast<uint4*>(orow + 16 * c + 8) =
-                                        make_uint4(bf16x2(v[8], v[9]), bf16x2(v[10], v[11]), bf16x2(v[12], v[13]), bf16x2(v[14], v[15]));
+#pragma unroll
+                                    for (int i = 0; i < 32; i += 8)
+                                        *reinterpret_cast<uint4*>(orow + 32 * c + i) = make_uint4(bf16x2(v[i], v[i + 1]), bf16x2(v[i + 2], v[i + 3]),
+                                                                                                  bf16x2(v[i + 4], v[i + 5]), bf16x2(v[i + 6], v[i + 7]));
                                 } else {
 #pragma unroll
-                                    for (int i = 0; i < 16; i += 4) *reinterpret_cast<float4*>(prow + 16 * c + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                                    for (int i = 0; i < 32; i += 4) *reinterpret_cast<float4*>(prow + (8 * c + i / 4) * (4 * ROWS)) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
                                 }
                             }
+                            __syncwarp();                  // (lanes without a row come back together before the next load)
                         }
                         if (r < R) {
                             if (!entire) p.part_ml[static_cast<size_t>(slot) * ROWS + row] = make_float2(mm, ll);
@@ -397,7 +408,6 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
             // S goes over the probabilities of two tiles ago: their product must be complete (products into different accumulators are not ordered)
             if (ok && t >= 2) ok = wait_all(pv_done(0), t & 1, W_R_PV_DONE) && (SETS == 1 || wait_all(pv_done(1), t & 1, W_R_PV_DONE));
             if (!ok) break;
-            fence_proxy_async_smem();                      // the loaders' writes -> the tensor core's reads, K and V of the stage
             tcgen05_fence_after_sync();
             if (leader) {
                 const uint32_t k0 = k_s + slot * C::TILE;
@@ -434,15 +444,13 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
         const bool run_in_page = p.cache.page_shift >= 3;
         int t = 0, item = 0;
         bool ok = true, fresh = true;
-        // a stage counts as full when this thread's copies have landed; the issuing warp makes them visible to the tensor core (a proxy fence
-        // here would wait for the copies in flight: measured, the loading warps then held one tile at a time and bounded the kernel)
+        // this warp's share has landed and is visible to the tensor core.  (The proxy fence waits for every copy of the thread that is still in flight: with
+        // whole tiles copied this way the loading warps held one tile at a time and bounded the kernel, hence TMA for those.)
         auto signal = [&](uint32_t bar) {
-            if (!E4M3) {
-                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
-            } else {
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar);
-            }
+            if (!E4M3) asm volatile("cp.async.wait_all;" ::: "memory");
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar);
         };
         auto page_of = [&](int key) -> int {
             return key < cur.rq.len ? __ldg(p.table + static_cast<size_t>(cur.b) * p.ld_table + (key >> p.cache.page_shift)) : -1;
@@ -474,7 +482,6 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
             if (by_tma) {
                 if (w == 0) {
                     if (lane == 0) mbar_expect_tx(kv_full(slot), 2 * C::TILE);
-                    else mbar_arrive(kv_full(slot));
                     __syncwarp();
                     if (lane < boxes) {
                         int page = box_page;
@@ -486,7 +493,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                             tma_load_4d(v_dst + blk * C::BLK + box_rows * lane * 128, &tm_v, 64 * blk, tok, cur.h, page, kv_full(slot));
                         }
                     }
-                } else {
+                } else if (lane == 0) {
                     mbar_arrive(kv_full(slot));
                 }
             } else {
@@ -551,21 +558,22 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
             }
             signal(kv_full(slot));
             }
-            if (new_item) {
-                // the item's queries, each warp its share of the 128 rows; rows that do not exist become zeros
+            if (new_item && w >= LW - C::QW) {
+                // the item's queries, each warp its share of the rows that exist (the others never matter)
                 if (item > 0) {
                     ok = wait_all(q_empty, (item - 1) & 1, W_R_Q_EMPTY);
                     if (!ok) break;
                 }
                 ++item;
-                const int R = cur.rq.qlen * p.group;
+                const int rows_here = min(ROWS, cur.rq.qlen * p.group - cur.rt * ROWS);
                 constexpr int QCH = D / 8, QSTEP = 32 / QCH;
 #pragma unroll 4
-                for (int i = w * QSTEP; i < ROWS; i += LW * QSTEP) {
+                for (int i = (w - (LW - C::QW)) * QSTEP; i < rows_here; i += C::QW * QSTEP) {
                     const int rl = i + lane / QCH, qc = lane % QCH, r = cur.rt * ROWS + rl;
-                    const bool live = r < R;
+                    const bool live = rl < rows_here;
                     const uint16_t* src = p.Q + 8 * qc;
-                    if (live) src += static_cast<size_t>(cur.rq.row0 + r / p.group) * p.ldq + static_cast<size_t>(cur.h * p.group + r % p.group) * D;
+                    const RowOf qa = row_of(p, r);
+                    if (live) src += static_cast<size_t>(cur.rq.row0 + qa.token) * p.ldq + static_cast<size_t>(cur.h * p.group + qa.head) * D;
                     const uint32_t at = q_s + (qc >> 3) * C::QBLK + rl * 128 + (((qc & 7) ^ (rl & 7)) << 4);
                     if (!E4M3) {
                         cp_async16(at, src, live);
@@ -596,7 +604,6 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                 box_page = box_pages();
             }
         }
-        asm volatile("cp.async.wait_all;" ::: "memory");
     }
     }
 

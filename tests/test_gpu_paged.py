@@ -345,6 +345,24 @@ def test_attention_many_short_requests(rd):
 
 
 @pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("T,heads,kv,D", [(20, 2, 2, 64), (33, 1, 1, 128), (70, 2, 2, 128), (9, 4, 2, 256), (130, 1, 1, 64)])
+def test_attention_many_short_requests_of_many_rows(rd, T, heads, kv, D, fmt):
+    """Items of one tile each, most with warps that own no row: nothing may run ahead of the item that is being written out."""
+    rng = np.random.default_rng(T)
+    n = 500 if T < 70 else 160
+    lens = rng.integers(0, 140, n).tolist()
+    q_lens = rng.integers(1, T + 1, n).tolist()
+    a = Attention(rd, lens, q_lens, heads, kv, D, 16, fmt, seed=T)
+    first = None
+    for _ in range(5):
+        o, lse = a.run(False)
+        status_clean(rd)
+        assert first is None or (np.array_equal(o, first[0]) and np.array_equal(lse, first[1]))
+        first = (o, lse)
+    a.check(o, lse, False)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
 def test_attention_large_scores_and_small_queries(rd, fmt):
     a = Attention(rd, [260, 77], [2, 2], 4, 2, 128, 16, fmt, seed=2)
     for factor in (200.0, 2.0 ** -60, 2.0 ** -126):               # one key takes all; queries far below the range of f16
