@@ -134,7 +134,7 @@ rudder_status check_attention(const rudder_attention_args* a, AttnArgs* out)
 // Where the kernel that the call runs takes the cache by TMA: the tensor maps (without them it copies row by row).
 void add_maps(const rudder_paged_cache* c, AttnArgs* a)
 {
-    if (attention_uses_maps(a->max_q * (a->heads / a->kv_heads), a->e4m3, c->page_size)) a->tma = make_tmap_cache(&a->tm_k, c->k, c) && make_tmap_cache(&a->tm_v, c->v, c);
+    if (attention_uses_maps(a->max_q * (a->heads / a->kv_heads), a->head_dim, a->e4m3, c->page_size, static_cast<long long>(a->max_pages) * c->page_size)) a->tma = make_tmap_cache(&a->tm_k, c->k, c) && make_tmap_cache(&a->tm_v, c->v, c);
 }
 
 }  // namespace

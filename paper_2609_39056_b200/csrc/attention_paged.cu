@@ -606,7 +606,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) attention_join_rows_kernel(const
 #define V64E_KT 32
 #define V64E_NST 3
 #endif
-// CLS: rows of an item up to 4, 8, 16 (more: attention_rows.cu)
+// CLS: rows of an item up to 4, 8, 16, 32 (more: attention_rows.cu)
 template <int D, bool E4M3, int CLS>
 struct Pick;
 template <int CLS> constexpr int kLo = CLS == 0 ? 1 : 2;
@@ -616,8 +616,21 @@ template <int CLS> struct Pick<128, false, CLS> { using C = AttnCfg<128, false, 
 template <int CLS> struct Pick<128, true, CLS> { using C = AttnCfg<128, true, CLS <= 1 ? 1 : 2, 1, VE_KW, VE_KT, VE_NST, 0>; };
 template <int CLS> struct Pick<256, false, CLS> { using C = AttnCfg<256, false, CLS <= 1 ? 1 : 2, 1, 4, 16, 3, kLo<CLS>>; };
 template <int CLS> struct Pick<256, true, CLS> { using C = AttnCfg<256, true, CLS <= 1 ? 1 : 2, 1, 8, 16, 3, 0>; };
-int rows_class(int max_rows) { return max_rows <= 4 ? 0 : (max_rows <= 8 ? 1 : (max_rows <= 16 ? 2 : 3)); }
-int tile_rows(int max_rows) { return max_rows <= 8 ? 8 : (max_rows <= 16 ? 16 : 128); }      // ROWS of the variant
+template <> struct Pick<64, false, 3> { using C = AttnCfg<64, false, 2, 2, 4, 32, 5, 2>; };
+template <> struct Pick<64, true, 3> { using C = AttnCfg<64, true, 2, 2, 4, 32, 5, 0>; };
+template <> struct Pick<128, false, 3> { using C = AttnCfg<128, false, 2, 2, 4, 16, 5, 2>; };
+template <> struct Pick<128, true, 3> { using C = AttnCfg<128, true, 2, 2, 4, 32, 5, 0>; };
+template <> struct Pick<256, false, 3> { using C = AttnCfg<256, false, 2, 2, 4, 16, 3, 2>; };
+template <> struct Pick<256, true, 3> { using C = AttnCfg<256, true, 2, 2, 4, 16, 5, 0>; };
+
+int rows_class(int max_rows) { return max_rows <= 4 ? 0 : (max_rows <= 8 ? 1 : (max_rows <= 16 ? 2 : (max_rows <= 32 ? 3 : 4))); }
+// The tcgen05 kernel (attention_rows.cu): above 32 rows always; 17 to 32 rows in bf16 with D = 128 and a table of 4096 tokens or more.
+// Measured, this kernel / that one: 20 rows, 9 requests of up to 2500 keys, D = 64 10.5 / 13.6 us; D = 128, 32 rows x 1000 keys 13.2 / 14.7,
+// 32 x 4480 22.8 / 21.7, 20 x 8000 54 / 44, 32 x 126k 292 / 205; D = 64, 32 x 126k 157 / 178; E4M3 191 / 387; 64 rows x 4480 30.6 / 22.6,
+// 64 x 126k 429 / 205, D = 64 299 / 176, D = 256 279 / 159, E4M3 353 / 403 and 269 / 260 (D = 64).
+bool many_rows(int max_rows, int head_dim, bool e4m3, long long max_kv) { return max_rows > 32 || (max_rows > 16 && head_dim == 128 && !e4m3 && max_kv >= 4096); }
+// Rows of a part in the workspace (whichever kernel runs: the size depends on the shapes alone)
+int tile_rows(int max_rows) { return max_rows <= 8 ? 8 : (max_rows <= 16 ? 16 : 128); }
 
 template <int D, bool E4M3>
 cudaError_t launch_main(const AttnParams& p, const AttnArgs& a, cudaStream_t st, RowsCfg<D, E4M3>) { return launch_rows<RowsCfg<D, E4M3>>(p, &a.tm_k, &a.tm_v, st); }
@@ -640,7 +653,7 @@ template <int D>
 cudaError_t launch_join(const AttnParams& p, int rows_of_tile, int max_rows, cudaStream_t st)
 {
     const int rows = max_rows < rows_of_tile ? max_rows : rows_of_tile;
-    const bool many = rows_class(max_rows) == 3;
+    const bool many = rows_of_tile == 128;                 // the parts of attention_rows.cu
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(p.G), static_cast<unsigned>(many ? (rows + 31) / 32 * (D / 64) : (rows + JOIN_ROWS - 1) / JOIN_ROWS), 1);
     cfg.blockDim = dim3(JOIN_THREADS, 1, 1);
@@ -671,6 +684,7 @@ cudaError_t run_df(const AttnParams& p, const AttnArgs& a, int max_rows, long lo
         case 0: return run_one<typename Pick<D, E4M3, E4M3 ? 1 : 0>::C>(p, a, max_rows, max_kv, st);
         case 1: return run_one<typename Pick<D, E4M3, 1>::C>(p, a, max_rows, max_kv, st);
         case 2: return run_one<typename Pick<D, E4M3, 2>::C>(p, a, max_rows, max_kv, st);
+        case 3: if (!many_rows(max_rows, D, E4M3, max_kv)) return run_one<typename Pick<D, E4M3, 3>::C>(p, a, max_rows, max_kv, st); [[fallthrough]];
         default: return run_one<RowsCfg<D, E4M3>>(p, a, max_rows, max_kv, st);
     }
 }
@@ -687,6 +701,7 @@ cudaError_t init_df()
     cudaError_t e = init_one_attn<typename Pick<D, E4M3, E4M3 ? 1 : 0>::C>();
     if (e == cudaSuccess) e = init_one_attn<typename Pick<D, E4M3, 1>::C>();
     if (e == cudaSuccess) e = init_one_attn<typename Pick<D, E4M3, 2>::C>();
+    if (e == cudaSuccess) e = init_one_attn<typename Pick<D, E4M3, 3>::C>();
     if (e == cudaSuccess) e = init_rows<RowsCfg<D, E4M3>>();
     return e;
 }
@@ -708,7 +723,10 @@ cudaError_t attention_paged_init()
 }
 
 // Workspace: descriptors, (maximum, sum) and fp32 outputs of at most two parts per CTA.
-bool attention_uses_maps(int max_rows, bool e4m3, int page_size) { return rows_class(max_rows) == 3 && !e4m3 && page_size >= 8; }
+bool attention_uses_maps(int max_rows, int head_dim, bool e4m3, int page_size, long long max_kv)
+{
+    return many_rows(max_rows, head_dim, e4m3, max_kv) && !e4m3 && page_size >= 8;
+}
 
 size_t attention_workspace_bytes(int max_rows, int head_dim, int sm_count)
 {

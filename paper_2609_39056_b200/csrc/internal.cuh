@@ -183,7 +183,7 @@ struct QkArgs;
 cudaError_t launch_qk_norm_rope(const QkArgs& a, int head_dim, bool e4m3, int sm_count, cudaStream_t st);
 struct AttnArgs;
 cudaError_t attention_paged_init();
-bool attention_uses_maps(int max_rows, bool e4m3, int page_size);
+bool attention_uses_maps(int max_rows, int head_dim, bool e4m3, int page_size, long long max_kv);
 size_t attention_workspace_bytes(int max_rows, int head_dim, int sm_count);
 cudaError_t launch_attention_paged(const AttnArgs& a, void* workspace, int sm_count, cudaStream_t st);
 cudaError_t linear_a16_init();
