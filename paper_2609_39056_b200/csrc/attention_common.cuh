@@ -135,6 +135,12 @@ struct Cursor {
     }
 };
 
+// Quotient of non-negative numbers, in 32 bits where they fit (they nearly always do; a 64-bit division is a hundred instructions of latency).
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+    if (((a | b) >> 32) == 0) return static_cast<uint32_t>(a) / static_cast<uint32_t>(b);
+    return a / b;
+}
+
 // This CTA's run of units: sums over the requests (threads over consecutive requests), the place of its first unit, and the descriptor that
 // the join reads.  All threads call it; false = nothing to do.
 template <int ROWS, int UK, int THREADS>
@@ -176,7 +182,7 @@ __device__ __forceinline__ bool start_of_run(const AttnParams& p, Cursor<ROWS, U
         most = max(most, s_max[w]);
     }
     const bool whole = items <= p.G && most <= p.whole_units;
-    const long long share = whole ? 1 : (total + p.G - 1) / p.G;
+    const long long share = whole ? 1 : quotient(total + p.G - 1, p.G);
     const long long all = whole ? items : total;
     const long long u_begin = min(all, share * blockIdx.x), u_end = min(all, u_begin + share);
     if (u_begin >= u_end) {
@@ -193,11 +199,11 @@ __device__ __forceinline__ bool start_of_run(const AttnParams& p, Cursor<ROWS, U
                 const long long here = static_cast<long long>(n_rt) * p.kv_heads * nt;
                 if (u_begin < at + here) {
                     const long long off = u_begin - at;
-                    const int item = static_cast<int>(off / nt);
+                    const uint32_t item = static_cast<uint32_t>(quotient(off, nt));         // below kv_heads x n_rt
                     s_place[0] = b;
-                    s_place[1] = item / n_rt;
-                    s_place[2] = item % n_rt;
-                    s_place[3] = static_cast<int>(off % nt);      // place inside the item, its cost included
+                    s_place[1] = static_cast<int>(item / static_cast<uint32_t>(n_rt));
+                    s_place[2] = static_cast<int>(item % static_cast<uint32_t>(n_rt));
+                    s_place[3] = static_cast<int>(off - static_cast<long long>(item) * nt); // place inside the item, its cost included
                     break;
                 }
                 at += here;
@@ -221,7 +227,7 @@ __device__ __forceinline__ bool start_of_run(const AttnParams& p, Cursor<ROWS, U
         const long long before = share * (static_cast<long long>(blockIdx.x) - 1);
         const bool first_cut = !whole && cur.j > 0 && unit0 >= before;
         d[1] = cur.h; d[2] = cur.rt; d[3] = cur.rq.row0; d[4] = cur.rq.qlen;
-        d[5] = static_cast<int>((unit0 + cur.nt - 1) / share);                   // last owner
+        d[5] = static_cast<int>(quotient(unit0 + cur.nt - 1, share));            // last owner
         d[6] = unit0 <= before + kItemCost ? 0 : 1;        // slot of the first owner's part: its run starts with this item (or inside its cost)
         d[0] = first_cut ? 1 : 0;
     }

@@ -136,6 +136,40 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
     auto p_full = [&](int buf, int set) { return bar0 + 8u * (2 * ST + 2 + buf + 2 * set); };
     auto pv_done = [&](int set) { return bar0 + 8u * (2 * ST + 6 + set); };
     const uint32_t ml_full = bar0 + 8u * (2 * ST + 8), o_free = ml_full + 8u, q_full = ml_full + 16u, q_empty = ml_full + 24u;
+    // an item's queries, two warps their share each of the rows that exist (the others never matter)
+    auto load_queries = [&](int part) {
+                        const int rows_here = min(ROWS, cur.rq.qlen * p.group - cur.rt * ROWS);
+                        constexpr int QCH = D / 8, QSTEP = 32 / QCH;
+#pragma unroll 4
+                        for (int i = part * QSTEP; i < rows_here; i += C::QW * QSTEP) {
+                            const int rl = i + lane / QCH, qc = lane % QCH, r = cur.rt * ROWS + rl;
+                            const bool live = rl < rows_here;
+                            const uint16_t* src = p.Q + 8 * qc;
+                            const RowOf qa = row_of(p, r);
+                            if (live) src += static_cast<size_t>(cur.rq.row0 + qa.token) * p.ldq + static_cast<size_t>(cur.h * p.group + qa.head) * D;
+                            const uint32_t at = q_s + (qc >> 3) * C::QBLK + rl * 128 + (((qc & 7) ^ (rl & 7)) << 4);
+                            if (!E4M3) {
+                                cp_async16(at, src, live);
+                            } else {
+                                uint4 x = make_uint4(0, 0, 0, 0);
+                                if (live) x = *reinterpret_cast<const uint4*>(src);
+                                const uint32_t xw[4] = {x.x, x.y, x.z, x.w};
+                                float mx = 0.0f;
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) mx = fmaxf(mx, fmaxf(fabsf(bf16_lo(xw[e])), fabsf(bf16_hi(xw[e]))));
+#pragma unroll
+                                for (int o = QCH / 2; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+                                const int ex = min(126, max(-126, 14 - (static_cast<int>((__float_as_uint(mx) >> 23) & 255u) - 127)));
+                                const float sc = __uint_as_float(static_cast<uint32_t>(ex + 127) << 23);
+                                uint32_t h[4];
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) h[e] = f16x2(bf16_lo(xw[e]) * sc, bf16_hi(xw[e]) * sc);
+                                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");
+                                if (qc == 0) s_exp[rl] = static_cast<int8_t>(ex);
+                            }
+                        }
+    };
+    if (warp > MMA_WARP + LW - C::QW) load_queries(warp - 1 - MMA_WARP - (LW - C::QW));
     if (tid == 0) {
         abort_word = 0;
         for (int i = 0; i < ST; ++i) { mbar_init(kv_full(i), LW); mbar_init(kv_empty(i), 1); }
@@ -559,42 +593,13 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
             signal(kv_full(slot));
             }
             if (new_item && w >= LW - C::QW) {
-                // the item's queries, each warp its share of the rows that exist (the others never matter)
+                // (the first item's are already on their way)
                 if (item > 0) {
                     ok = wait_all(q_empty, (item - 1) & 1, W_R_Q_EMPTY);
                     if (!ok) break;
+                    load_queries(w - (LW - C::QW));
                 }
                 ++item;
-                const int rows_here = min(ROWS, cur.rq.qlen * p.group - cur.rt * ROWS);
-                constexpr int QCH = D / 8, QSTEP = 32 / QCH;
-#pragma unroll 4
-                for (int i = (w - (LW - C::QW)) * QSTEP; i < rows_here; i += C::QW * QSTEP) {
-                    const int rl = i + lane / QCH, qc = lane % QCH, r = cur.rt * ROWS + rl;
-                    const bool live = rl < rows_here;
-                    const uint16_t* src = p.Q + 8 * qc;
-                    const RowOf qa = row_of(p, r);
-                    if (live) src += static_cast<size_t>(cur.rq.row0 + qa.token) * p.ldq + static_cast<size_t>(cur.h * p.group + qa.head) * D;
-                    const uint32_t at = q_s + (qc >> 3) * C::QBLK + rl * 128 + (((qc & 7) ^ (rl & 7)) << 4);
-                    if (!E4M3) {
-                        cp_async16(at, src, live);
-                    } else {
-                        uint4 x = make_uint4(0, 0, 0, 0);
-                        if (live) x = *reinterpret_cast<const uint4*>(src);
-                        const uint32_t xw[4] = {x.x, x.y, x.z, x.w};
-                        float mx = 0.0f;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) mx = fmaxf(mx, fmaxf(fabsf(bf16_lo(xw[e])), fabsf(bf16_hi(xw[e]))));
-#pragma unroll
-                        for (int o = QCH / 2; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-                        const int ex = min(126, max(-126, 14 - (static_cast<int>((__float_as_uint(mx) >> 23) & 255u) - 127)));
-                        const float sc = __uint_as_float(static_cast<uint32_t>(ex + 127) << 23);
-                        uint32_t h[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) h[e] = f16x2(bf16_lo(xw[e]) * sc, bf16_hi(xw[e]) * sc);
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(h[0]), "r"(h[1]), "r"(h[2]), "r"(h[3]) : "memory");
-                        if (qc == 0) s_exp[rl] = static_cast<int8_t>(ex);
-                    }
-                }
                 signal(q_full);
             }
             ++t;
