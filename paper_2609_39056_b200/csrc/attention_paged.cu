@@ -668,11 +668,13 @@ cudaError_t launch_join(const AttnParams& p, int rows_of_tile, int max_rows, cud
 template <class C>
 cudaError_t run_one(AttnParams p, const AttnArgs& a, int max_rows, long long max_kv, cudaStream_t st)
 {
-    p.whole_units = kAttnWholeKeys / C::UK;
+    const long long items = static_cast<long long>(p.B) * p.kv_heads * ((max_rows + C::ROWS - 1) / C::ROWS);
+    // Short items are handed out whole: a join costs about 1.2 us, a unit of 128 keys in one CTA as much.  Measured, whole / cut: 16 items of 200 keys
+    // 6.2 / 7.4 us, 333 7.4 / 7.4, 500 8.7 / 7.5; 64 items of 333 7.6 / 9.7, 500 9.0 / 10.1, 1000 14.0 / 12.6.
+    p.whole_units = (4 * items > p.G ? 512 : 384) / C::UK;
     cudaError_t e = launch_main(p, a, st, C());
     if (e != cudaSuccess) return e;
     // no item can be cut: there is a CTA for each and the table has no room for a longer one
-    const long long items = static_cast<long long>(p.B) * p.kv_heads * ((max_rows + C::ROWS - 1) / C::ROWS);
     if (items <= p.G && (max_kv + C::UK - 1) / C::UK <= p.whole_units) return cudaSuccess;
     return launch_join<C::D>(p, C::ROWS, max_rows, st);
 }

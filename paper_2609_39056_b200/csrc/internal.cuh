@@ -166,7 +166,6 @@ inline bool gemm_i8_register_path(int M, int N, int K, int G, bool signmag) { re
 
 // ---- paged key-value cache: page tables, query / key norm with rotation, attention; products of a few rows with 4-bit weights ----
 constexpr int kMaxRequests = 8192;        // requests of one page-table call (their prefix sums sit in shared memory)
-constexpr int kAttnWholeKeys = 512;       // attention: items of at most this many keys are handed out whole, see attention_paged.cu
 
 struct CacheParams;                       // paged.cuh
 struct PageTablesArgs {
