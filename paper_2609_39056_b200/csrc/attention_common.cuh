@@ -151,6 +151,50 @@ __device__ __forceinline__ bool start_of_run(const AttnParams& p, Cursor<ROWS, U
     __shared__ int s_max[THREADS / 32];
     __shared__ int s_place[4];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    long long total, share, u_begin, u_end;
+    bool whole;
+    int place;
+    if (p.B <= 32) {
+        // a request per lane, every warp for itself: no barrier, nothing loaded twice (one request of 333 keys: 3200 -> 1300 clocks)
+        Req r = {0, 0, 0};
+        if (lane < p.B) r = load_request(p, lane);
+        const int n_rt = (r.qlen * p.group + ROWS - 1) / ROWS, nt = max(1, (r.len + UK - 1) / UK);
+        const long long t_units = static_cast<long long>(n_rt) * p.kv_heads * (nt + kItemCost);
+        const int t_items = n_rt * p.kv_heads;
+        long long i_units = t_units;
+        int i_items = t_items;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const long long u = __shfl_up_sync(0xffffffffu, i_units, d);
+            const int v = __shfl_up_sync(0xffffffffu, i_items, d);
+            if (lane >= d) { i_units += u; i_items += v; }
+        }
+        total = __shfl_sync(0xffffffffu, i_units, 31);
+        const int items = __shfl_sync(0xffffffffu, i_items, 31);
+        whole = items <= p.G && __reduce_max_sync(0xffffffffu, n_rt > 0 ? nt : 0) <= p.whole_units;
+        share = whole ? 1 : quotient(total + p.G - 1, p.G);
+        const long long all = whole ? items : total;
+        u_begin = min(all, share * blockIdx.x);
+        u_end = min(all, u_begin + share);
+        if (u_begin >= u_end) {
+            if (tid == 0) p.desc[8 * blockIdx.x] = 0;
+            return false;
+        }
+        const long long before = whole ? i_items - t_items : i_units - t_units, mine = whole ? t_items : t_units;
+        const int b = __ffs(__ballot_sync(0xffffffffu, u_begin >= before && u_begin < before + mine)) - 1;       // exactly one lane
+        cur.b = b;
+        cur.rq.len = __shfl_sync(0xffffffffu, r.len, b);
+        cur.rq.row0 = __shfl_sync(0xffffffffu, r.row0, b);
+        cur.rq.qlen = __shfl_sync(0xffffffffu, r.qlen, b);
+        cur.nt = __shfl_sync(0xffffffffu, nt, b);
+        cur.n_rt = __shfl_sync(0xffffffffu, n_rt, b);
+        const long long off = u_begin - __shfl_sync(0xffffffffu, before, b);
+        const int size = whole ? 1 : cur.nt + kItemCost;
+        const uint32_t item = static_cast<uint32_t>(quotient(off, size));
+        cur.h = static_cast<int>(item / static_cast<uint32_t>(cur.n_rt));
+        cur.rt = static_cast<int>(item % static_cast<uint32_t>(cur.n_rt));
+        place = whole ? kItemCost : static_cast<int>(off - static_cast<long long>(item) * size);
+    } else {
     const int per = (p.B + THREADS - 1) / THREADS;
     const int rb0 = min(p.B, tid * per), rb1 = min(p.B, rb0 + per);
     long long t_units = 0;
@@ -173,7 +217,8 @@ __device__ __forceinline__ bool start_of_run(const AttnParams& p, Cursor<ROWS, U
     }
     if (lane == 31) { s_units[warp] = i_units; s_items[warp] = i_items; s_max[warp] = t_max; }
     __syncthreads();
-    long long total = 0, e_units = i_units - t_units;
+    long long e_units = i_units - t_units;
+    total = 0;
     int items = 0, e_items = i_items - t_items, most = 0;
     for (int w = 0; w < THREADS / 32; ++w) {
         if (w < warp) { e_units += s_units[w]; e_items += s_items[w]; }
@@ -181,10 +226,11 @@ __device__ __forceinline__ bool start_of_run(const AttnParams& p, Cursor<ROWS, U
         items += s_items[w];
         most = max(most, s_max[w]);
     }
-    const bool whole = items <= p.G && most <= p.whole_units;
-    const long long share = whole ? 1 : quotient(total + p.G - 1, p.G);
+    whole = items <= p.G && most <= p.whole_units;
+    share = whole ? 1 : quotient(total + p.G - 1, p.G);
     const long long all = whole ? items : total;
-    const long long u_begin = min(all, share * blockIdx.x), u_end = min(all, u_begin + share);
+    u_begin = min(all, share * blockIdx.x);
+    u_end = min(all, u_begin + share);
     if (u_begin >= u_end) {
         if (tid == 0) p.desc[8 * blockIdx.x] = 0;
         return false;
@@ -213,7 +259,8 @@ __device__ __forceinline__ bool start_of_run(const AttnParams& p, Cursor<ROWS, U
     __syncthreads();
     cur.set_request(p, s_place[0]);
     cur.h = s_place[1]; cur.rt = s_place[2];
-    const int place = whole ? kItemCost : s_place[3];
+    place = whole ? kItemCost : s_place[3];
+    }
     cur.j = max(0, place - kItemCost);
     cur.left = whole ? cur.nt : (u_end - u_begin) - max(0, kItemCost - place);      // of this run, from unit cur.j on
     if (cur.left <= 0) {                                       // nothing but a part of an item's cost

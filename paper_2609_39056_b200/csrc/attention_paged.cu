@@ -138,10 +138,19 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
             }
         }
     };
+    int pages[NST - 1];                                    // of the first tiles: one wait for all of them
+    {
+        Cursor<ROWS, UK> ahead = cur;
+#pragma unroll
+        for (int s = 0; s < NST - 1; ++s) {
+            pages[s] = ahead.left > 0 ? page_of_lane(ahead) : -2;
+            if (ahead.left > 0) ahead.advance(p);
+        }
+    }
 #pragma unroll
     for (int s = 0; s < NST - 1; ++s) {
         if (ld.left > 0) {
-            issue(ld, page_of_lane(ld), s);
+            issue(ld, pages[s], s);
             ld.advance(p);
         }
         cp_async_commit();
