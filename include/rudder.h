@@ -360,7 +360,8 @@ rudder_status rudder_qk_norm_rope(const rudder_qk_args* args, void* stream);
  *     s_j = scale q . k_j,  O = sum_j exp(s_j - m) v_j / sum_j exp(s_j - m),  lse = m + ln sum_j exp(s_j - m)
  * over j < kv_lens[b] (the new tokens' own keys included when they have been appended); with `causal` token t of n sees
  * j <= kv_lens[b] - n + t.  Query head h uses key-value head h / (heads / cache heads).  A row that sees no key gets zeros and
- * lse = -infinity.  What the cache holds at and behind kv_lens[b] is never used.
+ * lse = -infinity.  What the cache holds at and behind kv_lens[b] is never used, and what a row does not see has no part in it (not a
+ * number or infinite as it may be); among the keys that only some rows of a request see, infinite values become infinities of the rows that see them.
  * Request b has the rows q_starts[b] .. q_starts[b+1] - 1 (at most max_q), or with q_starts NULL the rows b max_q ..
  * (b + 1) max_q - 1; all other rows of O and lse are left as they were.  O may be Q.
  * workspace: rudder_attention_workspace_bytes(args) bytes (from heads, max_q and the cache's shape alone), 256-byte

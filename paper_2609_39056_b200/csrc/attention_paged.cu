@@ -87,7 +87,8 @@ struct AttnCfg {
     static_assert(SMEM <= 226 * 1024, "shared memory of an SM");
 };
 
-template <class C>
+// CAUSAL: the rows of an item may see different numbers of keys.
+template <class C, bool CAUSAL>
 __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const AttnParams p)
 {
     constexpr int D = C::D, NB = C::NB, RW = C::RW, KW = C::KW, KT = C::KT, NST = C::NST, LO = C::LO, RB = C::RB, UK = C::UK, ROWS = C::ROWS, DC = C::DC;
@@ -100,6 +101,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
     static_assert(KT == 16 || KT == 32, "a lane holds the place of one key of the tile");
     static_assert(GT % CH == 0 || CH % GT == 0, "rows are copied by whole groups of lanes");
     extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ uint32_t s_dropped[RW * KW];                // per warp: see drop_nonfinite
     pdl_launch_dependents();
     pdl_wait();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -160,8 +162,8 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
     float acc[DT][NB][4];                                  // output, transposed: channels on the 16-row side, rows on the 8 columns
     float mx[NB][2], sum[NB][2], fac[NB][2];               // of rows 2 q and 2 q + 1 of every 8: running maximum and sum, score factor
     int lim[NB][2];                                        // keys the rows see
-    int lim_min = 0;
-    bool fresh = true, first_part = true;
+    int tail = 0;                                          // keys that all rows of the tile see: len where it is the same for all
+    bool fresh = true, first_part = true, dropped = false;
     int part_j = 0;                                        // the unit of the item this run starts it with
     int stage = 0;
 
@@ -170,12 +172,13 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
             // ---- a new item (or the rest of one): queries, limits, empty sums
             fresh = false;
             part_j = cur.j;
+            tail = CAUSAL ? tail_of(cur.rq.len, cur.rq.qlen, row_of(p, cur.rt * ROWS).token) : cur.rq.len;
+            dropped = false;
 #pragma unroll
             for (int t = 0; t < DT; ++t)
 #pragma unroll
                 for (int n = 0; n < NB; ++n) acc[t][n][0] = acc[t][n][1] = acc[t][n][2] = acc[t][n][3] = 0.0f;
             const int R = cur.rq.qlen * p.group, first_row = cur.rt * ROWS + rw * 8 * NB;
-            lim_min = cur.rq.len;
 #pragma unroll
             for (int n = 0; n < NB; ++n) {
                 mx[n][0] = mx[n][1] = -INFINITY;
@@ -184,8 +187,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
                     const int r = first_row + 8 * n + (LO == 1 ? (2 * q + e) & 3 : 2 * q + e);
-                    lim[n][e] = (p.causal && r < R) ? cur.rq.len - cur.rq.qlen + row_of(p, r).token + 1 : cur.rq.len;
-                    lim_min = min(lim_min, lim[n][e]);
+                    lim[n][e] = (CAUSAL && r < R) ? cur.rq.len - cur.rq.qlen + row_of(p, r).token + 1 : cur.rq.len;
                     fac[n][e] = p.scale_log2;
                 }
                 const int r = first_row + 8 * n + (LO == 1 ? g & 3 : g);
@@ -236,6 +238,13 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
         const int key0 = cur.j * UK + kg * KT;
         if (key0 < cur.rq.len) {
             const uint32_t kt = ring + stage * C::STAGE, vt = kt + KT * RB;
+            const bool edge = key0 + KT > tail;
+            if (CAUSAL && edge && tail < cur.rq.len) {
+                const int r0 = max(0, tail - key0), r1 = min(KT, cur.rq.len - key0);
+                for (int i = r0 * CH + gt; i < r1 * CH; i += GT) dropped |= drop_nonfinite<E4M3 ? kExpE4m3 : kExpBf16>(vt + 16 * i);
+                if (RW == 1) __syncwarp();
+                else asm volatile("bar.sync %0, %1;" ::"r"(1 + kg), "n"(GT) : "memory");
+            }
             float s[MT][NB][4];                            // scores, transposed: keys on the 16-row side
 #pragma unroll
             for (int t = 0; t < MT; ++t)
@@ -270,7 +279,6 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
                     }
             }
             // ---- running maximum and sum (base 2)
-            const bool edge = key0 + KT > lim_min;
             uint32_t ph[MT][NB][2], pl[LO == 2 ? MT : 1][NB][2];
             bool moved = false;
             float cor[NB][2];
@@ -395,7 +403,13 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
                     for (int o = 4; o < 32; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
                     if (g == 0) ml[kg * ROWS + rw * 8 * NB + 8 * n + 2 * q + e] = make_float2(mx[n][e], l);
                 }
+            if (CAUSAL && tail < cur.rq.len) {
+                dropped = __any_sync(0xffffffffu, dropped);
+                if (lane == 0) s_dropped[warp] = dropped;
+            }
             __syncthreads();
+            if (CAUSAL && tail < cur.rq.len)
+                for (int w = 0; w < RW * KW; ++w) dropped |= s_dropped[w] != 0;
             float wgt[NB][2];
 #pragma unroll
             for (int n = 0; n < NB; ++n)
@@ -411,14 +425,14 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
                         const float2 o = ml[w * ROWS + rl];
                         l += o.y * exp2_approx(o.x - u);
                     }
-                    wgt[n][e] = exp2_approx(mx[n][e] - u) * vs * (entire ? (l > 0.0f ? 1.0f / l : 0.0f) : 1.0f);
+                    wgt[n][e] = exp2_approx(mx[n][e] - u) * vs * (entire ? (l == 0.0f ? 0.0f : 1.0f / l) : 1.0f);
                     if (kg == 0 && g == 0) {
                         const int r = cur.rt * ROWS + rl;
                         if (r < R) {
                             if (!entire) p.part_ml[static_cast<size_t>(slot) * ROWS + rl] = make_float2(m, l);
                             else if (p.lse != nullptr) {
                                 const RowOf at = row_of(p, r);
-                                p.lse[static_cast<size_t>(cur.rq.row0 + at.token) * p.heads + cur.h * p.group + at.head] = l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
+                                p.lse[static_cast<size_t>(cur.rq.row0 + at.token) * p.heads + cur.h * p.group + at.head] = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
                             }
                         }
                     }
@@ -463,6 +477,24 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
                     else
                         *reinterpret_cast<float4*>(p.part_o + (static_cast<size_t>(slot) * ROWS + rl) * D + round * DC + d) = o;
                 }
+            }
+            if (CAUSAL && dropped) {
+                // each thread goes over what it has written
+                for (int round = 0; round < C::ROUNDS; ++round)
+                    for (int i = tid; i < rows_here * (DC / 4); i += C::THREADS) {
+                        const int rl = i / (DC / 4), d = round * DC + 4 * (i % (DC / 4));
+                        const RowOf at = row_of(p, cur.rt * ROWS + rl);
+                        const float4 z = nonfinite_values<E4M3>(p, cur.b, cur.h, max(tail, part_j * UK), min(cur.rq.len - cur.rq.qlen + at.token + 1, (cur.j + 1) * UK), d);
+                        if (entire) {
+                            uint2* o = reinterpret_cast<uint2*>(p.O + static_cast<size_t>(cur.rq.row0 + at.token) * p.ldo + static_cast<size_t>(cur.h * p.group + at.head) * D + d);
+                            const uint2 v = *o;
+                            *o = make_uint2(bf16x2(bf16_lo(v.x) + z.x, bf16_hi(v.x) + z.y), bf16x2(bf16_lo(v.y) + z.z, bf16_hi(v.y) + z.w));
+                        } else {
+                            float4* o = reinterpret_cast<float4*>(p.part_o + (static_cast<size_t>(slot) * ROWS + rl) * D + d);
+                            const float4 v = *o;
+                            *o = make_float4(v.x + z.x, v.y + z.y, v.z + z.z, v.w + z.w);
+                        }
+                    }
             }
             fresh = true;
             first_part = false;
@@ -539,7 +571,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) attention_join_kernel(const Attn
         w[s] = exp2_approx(s_ml[ry][s].x - u);
         ll += s_ml[ry][s].y * w[s];
     }
-    const float inv = ll > 0.0f ? 1.0f / ll : 0.0f;
+    const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
     const RowOf at = row_of(p, r);
     const int hh = x.h * p.group + at.head;
     uint16_t* orow = p.O + static_cast<size_t>(x.row0 + at.token) * p.ldo + static_cast<size_t>(hh) * D + lane * V;
@@ -553,7 +585,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) attention_join_kernel(const Attn
         }
         *reinterpret_cast<uint32_t*>(orow + i) = bf16x2(a * inv, b * inv);
     }
-    if (lane == 0 && p.lse != nullptr) p.lse[static_cast<size_t>(x.row0 + at.token) * p.heads + hh] = ll > 0.0f ? (mm + log2f(ll)) * kLn2 : -INFINITY;
+    if (lane == 0 && p.lse != nullptr) p.lse[static_cast<size_t>(x.row0 + at.token) * p.heads + hh] = ll == 0.0f ? -INFINITY : (mm + log2f(ll)) * kLn2;
 }
 
 // The same for many rows: a lane per row, as the parts lie; a warp has 32 rows x 8 channels, a CTA 64 channels, y = row block x channel block.
@@ -585,44 +617,24 @@ __global__ void __launch_bounds__(JOIN_THREADS) attention_join_rows_kernel(const
         o[0] = o[0] * a + v0.x * b; o[1] = o[1] * a + v0.y * b; o[2] = o[2] * a + v0.z * b; o[3] = o[3] * a + v0.w * b;
         o[4] = o[4] * a + v1.x * b; o[5] = o[5] * a + v1.y * b; o[6] = o[6] * a + v1.z * b; o[7] = o[7] * a + v1.w * b;
     }
-    const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     const RowOf at = row_of(p, r);
     const int hh = x.h * p.group + at.head;
     *reinterpret_cast<uint4*>(p.O + static_cast<size_t>(x.row0 + at.token) * p.ldo + static_cast<size_t>(hh) * D + ch) =
         make_uint4(bf16x2(o[0] * inv, o[1] * inv), bf16x2(o[2] * inv, o[3] * inv), bf16x2(o[4] * inv, o[5] * inv), bf16x2(o[6] * inv, o[7] * inv));
-    if (ch == 0 && p.lse != nullptr) p.lse[static_cast<size_t>(x.row0 + at.token) * p.heads + hh] = l > 0.0f ? (m + log2f(l)) * kLn2 : -INFINITY;
+    if (ch == 0 && p.lse != nullptr) p.lse[static_cast<size_t>(x.row0 + at.token) * p.heads + hh] = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
 // ---- variants: warps over rows (RW) and keys (KW), keys per tile, stages.  The ring is about 130 to 200 KB: it is what keeps
 // enough of the cache in flight with one CTA per SM.
-#ifndef VE_KW
-#define VE_KW 8
-#define VE_KT 32
-#define VE_NST 3
-#endif
-#ifndef VB_KW
-#define VB_KW 8
-#define VB_KT 16
-#define VB_NST 3
-#endif
-#ifndef V64_KW
-#define V64_KW 8
-#define V64_KT 32
-#define V64_NST 3
-#endif
-#ifndef V64E_KW
-#define V64E_KW 16
-#define V64E_KT 32
-#define V64E_NST 3
-#endif
 // CLS: rows of an item up to 4, 8, 16, 32 (more: attention_rows.cu)
 template <int D, bool E4M3, int CLS>
 struct Pick;
 template <int CLS> constexpr int kLo = CLS == 0 ? 1 : 2;
-template <int CLS> struct Pick<64, false, CLS> { using C = AttnCfg<64, false, CLS <= 1 ? 1 : 2, 1, V64_KW, V64_KT, V64_NST, kLo<CLS>>; };
-template <int CLS> struct Pick<64, true, CLS> { using C = AttnCfg<64, true, CLS <= 1 ? 1 : 2, 1, CLS <= 1 ? V64E_KW : 8, V64E_KT, CLS <= 1 ? V64E_NST : 5, 0>; };
-template <int CLS> struct Pick<128, false, CLS> { using C = AttnCfg<128, false, CLS <= 1 ? 1 : 2, 1, VB_KW, VB_KT, VB_NST, kLo<CLS>>; };
-template <int CLS> struct Pick<128, true, CLS> { using C = AttnCfg<128, true, CLS <= 1 ? 1 : 2, 1, VE_KW, VE_KT, VE_NST, 0>; };
+template <int CLS> struct Pick<64, false, CLS> { using C = AttnCfg<64, false, CLS <= 1 ? 1 : 2, 1, 8, 32, 3, kLo<CLS>>; };
+template <int CLS> struct Pick<64, true, CLS> { using C = AttnCfg<64, true, CLS <= 1 ? 1 : 2, 1, CLS <= 1 ? 16 : 8, 32, CLS <= 1 ? 3 : 5, 0>; };
+template <int CLS> struct Pick<128, false, CLS> { using C = AttnCfg<128, false, CLS <= 1 ? 1 : 2, 1, 8, 16, 3, kLo<CLS>>; };
+template <int CLS> struct Pick<128, true, CLS> { using C = AttnCfg<128, true, CLS <= 1 ? 1 : 2, 1, 8, 32, 3, 0>; };
 template <int CLS> struct Pick<256, false, CLS> { using C = AttnCfg<256, false, CLS <= 1 ? 1 : 2, 1, 4, 16, 3, kLo<CLS>>; };
 template <int CLS> struct Pick<256, true, CLS> { using C = AttnCfg<256, true, CLS <= 1 ? 1 : 2, 1, 8, 16, 3, 0>; };
 template <> struct Pick<64, false, 3> { using C = AttnCfg<64, false, 2, 2, 4, 32, 5, 2>; };
@@ -656,7 +668,7 @@ cudaError_t launch_main(const AttnParams& p, const AttnArgs&, cudaStream_t st, C
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, attention_paged_kernel<C>, p);
+    return cudaLaunchKernelEx(&cfg, p.causal ? attention_paged_kernel<C, true> : attention_paged_kernel<C, false>, p);
 }
 template <int D>
 cudaError_t launch_join(const AttnParams& p, int rows_of_tile, int max_rows, cudaStream_t st)
@@ -705,7 +717,11 @@ cudaError_t run_d(const AttnParams& p, const AttnArgs& a, bool e4m3, int max_row
     return e4m3 ? run_df<D, true>(p, a, max_rows, max_kv, st) : run_df<D, false>(p, a, max_rows, max_kv, st);
 }
 template <class C>
-cudaError_t init_one_attn() { return cudaFuncSetAttribute(attention_paged_kernel<C>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM); }
+cudaError_t init_one_attn()
+{
+    const cudaError_t e = cudaFuncSetAttribute(attention_paged_kernel<C, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+    return e == cudaSuccess ? cudaFuncSetAttribute(attention_paged_kernel<C, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) : e;
+}
 template <int D, bool E4M3>
 cudaError_t init_df()
 {
@@ -756,7 +772,7 @@ cudaError_t launch_attention_paged(const AttnArgs& a, void* workspace, int sm_co
     p.table = a.table; p.ld_table = a.ld_table; p.kv_lens = a.kv_lens; p.q_starts = a.q_starts;
     p.scale_log2 = a.scale * 1.4426950408889634f;
     p.max_pages = a.max_pages; p.B = a.B; p.max_q = a.max_q; p.M = a.M; p.heads = a.heads; p.kv_heads = a.kv_heads;
-    p.group = a.heads / a.kv_heads; p.causal = a.causal;
+    p.group = a.heads / a.kv_heads; p.causal = a.causal && a.max_q > 1;
     p.group_inv = p.group == 1 ? 0u : static_cast<uint32_t>(((1ull << 32) + p.group - 1) / p.group);
     p.G = sm_count;
     p.tma = a.tma;

@@ -120,6 +120,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
     __shared__ int8_t s_exp[E4M3 ? ROWS : 1];              // E4M3: the power of two that a row of Q was multiplied by
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_word;
+    __shared__ int s_dropped[2];                           // [item & 1]: the item, if values were dropped (see drop_nonfinite)
 
     pdl_launch_dependents();
     pdl_wait();
@@ -172,6 +173,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
     if (warp > MMA_WARP + LW - C::QW) load_queries(warp - 1 - MMA_WARP - (LW - C::QW));
     if (tid == 0) {
         abort_word = 0;
+        s_dropped[0] = s_dropped[1] = -1;
         for (int i = 0; i < ST; ++i) { mbar_init(kv_full(i), LW); mbar_init(kv_empty(i), 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(s_full(i), 1); mbar_init(p_full(i, 0), 4); mbar_init(p_full(i, 1), 4); mbar_init(pv_done(i), 1); }
         mbar_init(ml_full, 4); mbar_init(o_free, 4);
@@ -197,7 +199,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
         const uint32_t o_t = tmem + lanes + C::O_COL;
         int t = 0, item = 0, part_j = 0;
         bool ok = true, fresh = true, first_part = true, live_warp = false, first_tile = false;
-        int lim = 0, lim_warp = 0, R = 0, r = 0;
+        int lim = 0, lim_warp = 0, R = 0, r = 0, tail = 0;
         float f = 0.0f, m = -INFINITY, l = 0.0f;
         while (cur.left > 0) {
             if (fresh) {
@@ -209,6 +211,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                 live_warp = cur.rt * ROWS + 32 * quad < R;
                 lim = (p.causal && r < R) ? cur.rq.len - cur.rq.qlen + row_of(p, r).token + 1 : cur.rq.len;
                 lim_warp = __reduce_min_sync(0xffffffffu, lim);
+                tail = p.causal ? tail_of(cur.rq.len, cur.rq.qlen, row_of(p, cur.rt * ROWS).token) : cur.rq.len;
                 m = -INFINITY;
                 l = 0.0f;
                 f = r < R ? p.scale_log2 : 0.0f;           // rows that do not exist hold whatever the buffer held: weight 0, nothing read from them
@@ -266,7 +269,8 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                         ok = wait_all(pv_done(set), (t - 1) & 1, W_R_PV_DONE);
                         if (!ok) break;
                         tcgen05_fence_after_sync();
-                        const float n = fmaxf(m, mx), cor = n == -INFINITY ? 1.0f : exp2_approx(m - n);
+                        const float n = mx > m + 8.0f ? mx : m;                  // (row by row: what a row becomes does not depend on its neighbours)
+                        const float cor = n == -INFINITY ? 1.0f : exp2_approx(m - n);
                         m = n;
                         l *= cor;
 #pragma unroll 1
@@ -311,6 +315,22 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                     tcgen05_fence_before_sync();
                 }
                 first_tile = false;
+                if (tail < cur.rq.len) {
+                    const int key0 = cur.j * KT + set * HALF, r0 = max(0, tail - key0), r1 = min(HALF, cur.rq.len - key0);
+                    if (r0 < r1) {
+                        ok = wait_all(kv_full(t % ST), (t / ST) & 1, W_R_KV_FULL);           // (complete: the scores are; this thread has to have seen it)
+                        if (!ok) break;
+                        const uint32_t v0 = v_s + (t % ST) * C::TILE + set * HALF * 128;
+                        bool dropped = false;
+#pragma unroll 1
+                        for (int blk = 0; blk < D / 64; ++blk)
+                            for (int i = r0 * 8 + row; i < r1 * 8; i += 128) dropped |= drop_nonfinite<E4M3 ? kExpF16 : kExpBf16>(v0 + blk * C::BLK + 16 * i);
+                        if (dropped) {
+                            fence_proxy_async_smem();
+                            s_dropped[item & 1] = item;    // (no warp is more than an item behind another: they all release every item's queries)
+                        }
+                    }
+                }
                 // The product before must be complete before this one can begin: a barrier is waited for phase by phase (a wait for phase t while
                 // phase t - 1 is open would take phase t - 2 for it, and the rows would be read out too early).
                 if (t > 0) {
@@ -348,7 +368,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                         tcgen05_fence_after_sync();
                         const bool entire = item_end && part_j == 0;
                         const float vs = E4M3 && p.cache.v_scale != nullptr ? __ldg(p.cache.v_scale + cur.h) : 1.0f;
-                        const float w = entire ? (ll > 0.0f ? vs / ll : 0.0f) : vs;
+                        const float w = entire ? (ll == 0.0f ? 0.0f : vs / ll) : vs;
                         w0 *= w;
                         w1 *= w;
                         const int slot = 2 * blockIdx.x + (first_part ? 0 : 1);
@@ -381,10 +401,21 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                             }
                             __syncwarp();                  // (lanes without a row come back together before the next load)
                         }
+                        if (*const_cast<volatile int*>(&s_dropped[item & 1]) == item && r < R) {
+#pragma unroll 1
+                            for (int d = 0; d < D; d += 4) {
+                                const float4 z = nonfinite_values<E4M3>(p, cur.b, cur.h, max(tail, part_j * KT), min(lim, (cur.j + 1) * KT), d);
+                                const float zz[4] = {z.x, z.y, z.z, z.w};
+                                for (int e = 0; e < 4; ++e) {
+                                    if (entire) orow[d + e] = static_cast<uint16_t>(bf16x2(__uint_as_float(static_cast<uint32_t>(orow[d + e]) << 16) + zz[e], 0.0f) & 0xFFFFu);
+                                    else prow[(d / 4) * (4 * ROWS) + e] += zz[e];
+                                }
+                            }
+                        }
                         if (r < R) {
                             if (!entire) p.part_ml[static_cast<size_t>(slot) * ROWS + row] = make_float2(mm, ll);
                             else if (p.lse != nullptr)
-                                p.lse[static_cast<size_t>(cur.rq.row0 + tok) * p.heads + hh] = ll > 0.0f ? (mm + log2f(ll)) * kLn2 : -INFINITY;
+                                p.lse[static_cast<size_t>(cur.rq.row0 + tok) * p.heads + hh] = ll == 0.0f ? -INFINITY : (mm + log2f(ll)) * kLn2;
                         }
                         tcgen05_fence_before_sync();
                     }

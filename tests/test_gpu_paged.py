@@ -482,3 +482,150 @@ def test_arguments_on_another_device_are_refused(rd):
     a = Attention(rd, [5], [1], 1, 1, 64, 16, "bf16")
     with pytest.raises(rd.RudderError):
         rd.AttentionArgs(to_dev_bf16(a.qb), 1, a.cache, torch.zeros((1, 2), dtype=torch.int32), torch.zeros(1, dtype=torch.int32), 1.0, to_dev_bf16(a.qb))
+
+
+# ---- attention: more of what the calls allow ---------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("lens,n,heads,kv,D", [([40, 3, 333], 5, 2, 2, 128), ([3000], 9, 4, 2, 64), ([130, 2500], 7, 6, 2, 256), ([50, 257, 4, 64], 20, 1, 1, 64),
+                                               ([128, 90, 1700], 70, 2, 2, 128), ([9000], 40, 1, 1, 128), ([131, 3, 5000], 33, 2, 1, 256)])
+def test_attention_what_a_row_does_not_see_does_not_reach_it(rd, lens, n, heads, kv, D, fmt):
+    """Not a number or infinite among the new tokens' own keys and values: the rows in front of that token keep their bits."""
+    a = Attention(rd, lens, [n] * len(lens), heads, kv, D, 16, fmt, seed=n)
+    clean, lse = a.run(True)
+    a.check(clean, lse, True)
+
+    def at(b, key):                                                # page and place of a key
+        return int(a.table[b, key // 16]), key % 16
+    clean, lse = clean.reshape(len(lens), n, heads, D), lse.reshape(len(lens), n, heads)
+    if fmt == "bf16":
+        bits, poison = torch.int16, [(float("nan"), 0x7FC0, "v"), (float("inf"), 0x7F80, "v"), (-float("inf"), 0xFF80 - 0x10000, "v"), (float("nan"), 0x7FC0, "k")]
+    else:
+        bits, poison = torch.uint8, [(float("nan"), 0x7F, "v"), (float("nan"), 0xFF, "k")]
+    for back, (value, code, which) in zip((2, 1, n // 2, 3), poison):          # the key `back` before the end
+        cache = (a.vc if which == "v" else a.kc).view(bits)
+        saved = []
+        for b, length in enumerate(lens):
+            key = length - back
+            if key >= 0:
+                pg, pl = at(b, key)
+                saved.append((b, pg, pl, cache[pg, :, pl].clone()))
+                cache[pg, :, pl, 0::2] = code
+        o, l = a.run(True)
+        o, l = o.reshape(clean.shape), l.reshape(lse.shape)
+        for b, length in enumerate(lens):
+            for t in range(n):
+                if not 0 <= length - back <= length - n + t:       # not seen (or not there)
+                    assert np.array_equal(o[b, t], clean[b, t]) and np.array_equal(l[b, t], lse[b, t]), (b, t, back)
+                elif which == "k":
+                    assert np.isnan(o[b, t]).all() and np.isnan(l[b, t]).all(), (b, t)
+                else:
+                    assert np.array_equal(o[b, t][:, 1::2], clean[b, t][:, 1::2]) and np.array_equal(l[b, t], lse[b, t]), (b, t)
+                    even = o[b, t][:, 0::2]
+                    assert (np.isnan(even) if np.isnan(value) else even == value).all(), (b, t, back)
+        for b, pg, pl, x in saved:
+            cache[pg, :, pl] = x
+    again, _ = a.run(True)
+    assert np.array_equal(again.reshape(clean.shape), clean)
+    status_clean(rd)
+
+
+@pytest.mark.parametrize("order", ["heads", "tokens"])
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("page", [1, 2, 4, 8, 32, 64, 128, 1024])
+@pytest.mark.parametrize("n,heads,kv,D", [(40, 2, 2, 128), (9, 4, 1, 64), (33, 2, 2, 256), (3, 4, 2, 128)])
+def test_attention_page_sizes_and_orders(rd, n, heads, kv, D, page, fmt, order):
+    lens = [700, 129, 5, 2049]
+    a = Attention(rd, lens, [n] * 4, heads, kv, D, page, fmt, seed=page, order=order)
+    o, lse = a.run(True, pad=1, q_pad=8)
+    a.check(o, lse, True)
+    status_clean(rd)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("n,heads,kv,D", [(1, 2, 2, 128), (5, 4, 2, 64), (50, 2, 2, 128), (40, 1, 1, 256)])
+@pytest.mark.parametrize("scale", [-0.31, 0.0])
+def test_attention_scales_of_any_sign(rd, n, heads, kv, D, scale, fmt):
+    a = Attention(rd, [300, 17, 2000, n // 2], [n] * 4, heads, kv, D, 16, fmt, seed=n)
+    a.scale = scale
+    for causal in (False, True):
+        o, lse = a.run(causal)
+        a.check(o, lse, causal)
+    status_clean(rd)
+
+
+@pytest.mark.parametrize("n", [1, 6, 40])
+@pytest.mark.parametrize("B", [31, 32, 33, 100])
+def test_attention_request_counts(rd, B, n):
+    """Up to 32 requests are placed by each warp alone, more of them by the whole CTA; long ones are cut either way."""
+    rng = np.random.default_rng(B + n)
+    lens = rng.integers(0, 2500, B).tolist()
+    q_lens = rng.integers(0, n + 1, B).tolist()
+    q_lens[0] = n
+    a = Attention(rd, lens, q_lens, 2, 1, 64, 32, "bf16", seed=B)
+    o, lse = a.run(True, pad=2)
+    a.check(o, lse, True)
+    # nothing to do at all: no keys, then no queries
+    a.lens = [0] * B
+    o, lse = a.run(False)
+    assert (o == 0).all() and np.isneginf(lse).all()
+    _, _, kv_lens, O, q_starts, _ = a.args.keep
+    kv_lens.copy_(torch.tensor(lens, dtype=torch.int32))
+    q_starts.fill_(0)
+    O.fill_(3.0)
+    rd.rudder_attention_paged(a.args)
+    assert (O == 3.0).all().item()
+    status_clean(rd)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("n,D", [(40, 128), (20, 256), (64, 64)])
+def test_attention_bad_pages_under_many_rows(rd, n, D, fmt):
+    a = Attention(rd, [400, 400, 400], [n] * 3, 2, 1, D, 16, fmt, seed=6, dead=0.0)
+    good, _ = a.run(False)
+    keep = a.table.copy()
+    for where in (3, 24):                                          # in a whole tile, in the request's last one
+        for bad in (-1, 2 ** 30, a.kc.shape[0]):
+            a.table = keep.copy()
+            a.table[1, where] = bad
+            o, _ = a.run(False)
+            assert rd.rudder_device_status() == (rd.ERR_ARG, rd.BAD_PAGE)
+            assert np.array_equal(o[:n], good[:n]) and np.array_equal(o[2 * n:], good[2 * n:]) and np.isfinite(o).all()
+    a.table = keep
+    o, _ = a.run(False)
+    assert np.array_equal(o, good)
+    status_clean(rd)
+
+
+def test_attention_far_pages_under_many_rows(rd):
+    page, kv, D = 64, 8, 128
+    n_pages = (int(2.8e9) // (page * kv * D)) + 1
+    a = Attention(rd, [333, 64, 1], [40, 33, 1], 8, kv, D, page, "bf16", seed=4, far=n_pages)
+    o, lse = a.run(True)
+    a.check(o, lse, True)
+    status_clean(rd)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("n,heads,kv,D", [(1, 8, 2, 128), (40, 2, 2, 128)])
+def test_attention_captured_follows_the_lengths(rd, n, heads, kv, D, fmt):
+    """A captured call replayed with other lengths and tables, over its own queries: the device's data decide."""
+    a = Attention(rd, [3000, 70, 500], [n] * 3, heads, kv, D, 16, fmt, seed=5)
+    want, _ = a.run(True)
+    a.lens = [1200, 64, 1]
+    want2, _ = a.run(True)
+    a.lens = [3000, 70, 500]
+    lens = cuda(np.array(a.lens, np.int32))
+    Q = to_dev_bf16(a.qb)
+    X = Q.clone()
+    args = rd.AttentionArgs(X, heads, a.cache, cuda(a.table), lens, a.scale, X, max_q=n, causal=True)
+    rd.rudder_attention_paged(args)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        rd.rudder_attention_paged(args)
+    for L, w in (([3000, 70, 500], want), ([1200, 64, 1], want2), ([3000, 70, 500], want)):
+        lens.copy_(torch.tensor(L, dtype=torch.int32))
+        X.copy_(Q)
+        graph.replay()
+        assert np.array_equal(glue.bf16_to_f32(bf16_to_np(X)).reshape(w.shape), w)
+    status_clean(rd)
