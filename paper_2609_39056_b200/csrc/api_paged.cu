@@ -88,15 +88,17 @@ bool make_tmap_cache(CUtensorMap* tm, const void* base, const rudder_paged_cache
 {
     EncodeTiledFn fn = encode_tiled_fn();
     if (!fn) return false;
-    const cuuint64_t row = static_cast<cuuint64_t>(c->head_dim) * 2;
+    const bool e4m3 = c->format == RUDDER_CACHE_E4M3;
+    const cuuint64_t elt = e4m3 ? 1 : 2, row = static_cast<cuuint64_t>(c->head_dim) * elt;
     cuuint64_t gdim[4] = {static_cast<cuuint64_t>(c->head_dim), static_cast<cuuint64_t>(c->page_size), static_cast<cuuint64_t>(c->heads), static_cast<cuuint64_t>(c->n_pages)};
     // (an axis of one element may have any stride)
-    cuuint64_t gstride[3] = {c->page_size > 1 ? static_cast<cuuint64_t>(c->token_stride) * 2 : row, c->heads > 1 ? static_cast<cuuint64_t>(c->head_stride) * 2 : row,
-                             c->n_pages > 1 ? static_cast<cuuint64_t>(c->page_stride) * 2 : row};
-    cuuint32_t box[4] = {64, static_cast<cuuint32_t>(c->page_size < 64 ? c->page_size : 64), 1, 1};
+    cuuint64_t gstride[3] = {c->page_size > 1 ? static_cast<cuuint64_t>(c->token_stride) * elt : row, c->heads > 1 ? static_cast<cuuint64_t>(c->head_stride) * elt : row,
+                             c->n_pages > 1 ? static_cast<cuuint64_t>(c->page_stride) * elt : row};
+    // bf16: 64 channels, swizzled as the tensor core reads them; E4M3: whole rows as they are, converted on the way
+    cuuint32_t box[4] = {e4m3 ? static_cast<cuuint32_t>(c->head_dim) : 64, static_cast<cuuint32_t>(c->page_size < 64 ? c->page_size : 64), 1, 1};
     cuuint32_t estr[4] = {1, 1, 1, 1};
-    return fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), gdim, gstride, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return fn(tm, e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), gdim, gstride, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              e4m3 ? CU_TENSOR_MAP_SWIZZLE_NONE : CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 rudder_status check_attention_shape(const rudder_attention_args* a)

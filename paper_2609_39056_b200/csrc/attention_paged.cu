@@ -758,7 +758,7 @@ cudaError_t attention_paged_init()
 // Workspace: descriptors, (maximum, sum) and fp32 outputs of at most two parts per CTA.
 bool attention_uses_maps(int max_rows, int head_dim, bool e4m3, int page_size, long long max_kv)
 {
-    return many_rows(max_rows, head_dim, e4m3, max_kv) && !e4m3 && page_size >= 8;
+    return many_rows(max_rows, head_dim, e4m3, max_kv) && page_size >= 8;
 }
 
 size_t attention_workspace_bytes(int max_rows, int head_dim, int sm_count)

@@ -25,7 +25,7 @@ namespace rudder {
 
 namespace {
 
-enum RowsWhere { W_R_Q_EMPTY = 1001, W_R_KV_EMPTY = 1002, W_R_Q_FULL = 1101, W_R_KV_FULL = 1102, W_R_P_FULL = 1104, W_R_O_FREE = 1105,
+enum RowsWhere { W_R_Q_EMPTY = 1001, W_R_KV_EMPTY = 1002, W_R_RAW_FULL = 1003, W_R_RAW_EMPTY = 1004, W_R_Q_FULL = 1101, W_R_KV_FULL = 1102, W_R_P_FULL = 1104, W_R_O_FREE = 1105,
                  W_R_S_FULL = 1201, W_R_PV_DONE = 1202, W_R_ML_FULL = 1203 };
 
 template <int D_, bool E4M3_>
@@ -35,18 +35,21 @@ struct RowsCfg {
     static constexpr int ROWS = 128;
     static constexpr int UK = D <= 128 ? 128 : 64;
     static constexpr int KT = UK;                          // keys of a tile: a unit of the work split
-    static constexpr int ST = D == 64 ? 4 : (D == 128 ? 3 : 2);
+    static constexpr int ST = D == 64 ? 4 : (D == 128 && !E4M3 ? 3 : 2);
     static constexpr int SETS = D <= 128 ? 2 : 1;          // sets of four softmax warps: each takes its share of a tile's keys, with an O of its own
     static constexpr int HALF = KT / SETS;
-    static constexpr int LW = 3;                           // loading warps (12 warps in all: 168 registers a thread)
+    static constexpr int LW = E4M3 ? 4 : 3;                // loading warps (12 warps in all: 168 registers a thread),
+    static constexpr int TW = E4M3 ? 1 : 0;                // with E4M3 they convert, and one more issues the TMA loads (14 warps: 144)
     static constexpr int QW = 2;                           // of them, those that load the queries (the first issues the TMA loads and waits for nothing else)
     static constexpr int MMA_WARP = 4 * SETS;
-    static constexpr int THREADS = 32 * (MMA_WARP + 1 + LW);
+    static constexpr int THREADS = 32 * (MMA_WARP + 1 + LW + TW);
     static constexpr int BLK = KT * 128;                   // a tile is D / 64 blocks of [KT keys][64 channels]
     static constexpr int TILE = D / 64 * BLK;
     static constexpr int QBLK = ROWS * 128;
     static constexpr int QBYTES = D / 64 * QBLK;
-    static constexpr int SMEM = 1024 + QBYTES + 2 * ST * TILE;
+    static constexpr int RAW = KT * D;                     // E4M3: a K or a V tile as it lies in the cache,
+    static constexpr int RU = E4M3 ? (D == 64 ? 8 : (D == 128 ? 4 : 2)) : 0;     // and how many of them are on their way
+    static constexpr int SMEM = 1024 + QBYTES + 2 * ST * TILE + RU * RAW;
     static constexpr int O_COL = 2 * KT;                   // tensor memory columns: two S / P buffers, O
     static_assert(O_COL + SETS * D <= 512 && SMEM <= 226 * 1024, "tensor memory and shared memory");
 };
@@ -112,10 +115,10 @@ __device__ __forceinline__ void store_f16(uint32_t at0, uint32_t at1, uint4 v) {
 template <class C>
 __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const AttnParams p, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v)
 {
-    constexpr int D = C::D, KT = C::KT, ST = C::ST, LW = C::LW, ROWS = C::ROWS, SETS = C::SETS, HALF = C::HALF, MMA_WARP = C::MMA_WARP;
+    constexpr int D = C::D, KT = C::KT, ST = C::ST, RU = C::RU, LW = C::LW, ROWS = C::ROWS, SETS = C::SETS, HALF = C::HALF, MMA_WARP = C::MMA_WARP;
     constexpr bool E4M3 = C::E4M3;
     extern __shared__ uint8_t smem_raw_rows[];
-    __shared__ __align__(8) uint64_t bars[2 * ST + 12];
+    __shared__ __align__(8) uint64_t bars[2 * ST + 12 + 2 * C::RU];
     __shared__ float2 s_ml[ROWS];                          // (reference, sum) of the second set's rows
     __shared__ int8_t s_exp[E4M3 ? ROWS : 1];              // E4M3: the power of two that a row of Q was multiplied by
     __shared__ uint32_t tmem_slot;
@@ -137,6 +140,9 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
     auto p_full = [&](int buf, int set) { return bar0 + 8u * (2 * ST + 2 + buf + 2 * set); };
     auto pv_done = [&](int set) { return bar0 + 8u * (2 * ST + 6 + set); };
     const uint32_t ml_full = bar0 + 8u * (2 * ST + 8), o_free = ml_full + 8u, q_full = ml_full + 16u, q_empty = ml_full + 24u;
+    const uint32_t raw_s = v_s + ST * C::TILE;
+    auto raw_full = [&](int i) { return bar0 + 8u * (2 * ST + 12 + i); };
+    auto raw_empty = [&](int i) { return bar0 + 8u * (2 * ST + 12 + RU + i); };
     // an item's queries, two warps their share each of the rows that exist (the others never matter)
     auto load_queries = [&](int part) {
                         const int rows_here = min(ROWS, cur.rq.qlen * p.group - cur.rt * ROWS);
@@ -170,13 +176,14 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                             }
                         }
     };
-    if (warp > MMA_WARP + LW - C::QW) load_queries(warp - 1 - MMA_WARP - (LW - C::QW));
+    if (warp > MMA_WARP + LW - C::QW && warp <= MMA_WARP + LW) load_queries(warp - 1 - MMA_WARP - (LW - C::QW));
     if (tid == 0) {
         abort_word = 0;
         s_dropped[0] = s_dropped[1] = -1;
         for (int i = 0; i < ST; ++i) { mbar_init(kv_full(i), LW); mbar_init(kv_empty(i), 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(s_full(i), 1); mbar_init(p_full(i, 0), 4); mbar_init(p_full(i, 1), 4); mbar_init(pv_done(i), 1); }
         mbar_init(ml_full, 4); mbar_init(o_free, 4);
+        for (int i = 0; i < RU; ++i) { mbar_init(raw_full(i), 1); mbar_init(raw_empty(i), LW); }
         mbar_init(q_full, C::QW); mbar_init(q_empty, 1 + 4 * SETS);                 // the last S of the item, and the softmax warps
         fence_mbar_init();
     }
@@ -429,7 +436,33 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
             cur.advance(p);
         }
     } else {
-    if (warp == MMA_WARP) {
+    auto page_at = [&](const Cursor<ROWS, KT>& at, int key) -> int {
+        return key < at.rq.len ? __ldg(p.table + static_cast<size_t>(at.b) * p.ld_table + (key >> p.cache.page_shift)) : -1;
+    };
+    const int box_rows = min(64, 1 << p.cache.page_shift), boxes = KT / box_rows;
+    if (E4M3 && warp > MMA_WARP + LW) {
+        // ---------------------------------------------------------------------------------------- E4M3: whole K and V tiles as they lie in the cache
+        int issued = 0;
+        bool ok = p.tma != 0;
+        while (ok && cur.left > 0) {
+            if (cur.j * KT + KT <= cur.rq.len) {
+                int page = lane < boxes ? page_at(cur, cur.j * KT + box_rows * lane) : 0;
+                if (page < 0 || page >= p.cache.n_pages) { record_bad_data(kBadPage); page = p.cache.n_pages; }                // out of range: zeros
+                const int tok = (cur.j * KT + box_rows * lane) & ((1 << p.cache.page_shift) - 1);
+#pragma unroll
+                for (int half = 0; half < 2; ++half, ++issued) {
+                    const int at = issued % max(RU, 1);
+                    ok = wait_all(raw_empty(at), ((issued / max(RU, 1)) & 1) ^ 1, W_R_RAW_EMPTY);
+                    if (!ok) break;
+                    if (lane == 0) mbar_expect_tx(raw_full(at), C::RAW);
+                    __syncwarp();
+                    if (lane < boxes) tma_load_4d(raw_s + at * C::RAW + box_rows * lane * D, half ? &tm_v : &tm_k, 0, tok, cur.h, page, raw_full(at));
+                    __syncwarp();
+                }
+            }
+            cur.advance(p);
+        }
+    } else if (warp == MMA_WARP) {
         // ---------------------------------------------------------------------------------------- MMA issue
         const bool leader = elect_one();
         const uint32_t idesc_s = umma_idesc_f16(ROWS, KT, !E4M3, false), idesc_o = umma_idesc_f16(ROWS, D, !E4M3, true);
@@ -517,9 +550,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
             __syncwarp();
             if (lane == 0) mbar_arrive(bar);
         };
-        auto page_of = [&](int key) -> int {
-            return key < cur.rq.len ? __ldg(p.table + static_cast<size_t>(cur.b) * p.ld_table + (key >> p.cache.page_shift)) : -1;
-        };
+        auto page_of = [&](int key) -> int { return page_at(cur, key); };
         auto place = [&](int page, int key) -> long long {
             return page * p.cache.page_stride + static_cast<long long>(cur.h) * p.cache.head_stride +
                    static_cast<long long>(key & ((1 << p.cache.page_shift) - 1)) * p.cache.token_stride;
@@ -530,9 +561,9 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
         };
         int pages = run_pages();
         // TMA boxes of a tile, and the page of lane i's, requested a tile ahead as well
-        const int box_rows = min(64, 1 << p.cache.page_shift), boxes = KT / box_rows;
-        auto box_pages = [&]() -> int { return w == 0 && lane < boxes ? page_of(cur.j * KT + box_rows * lane) : -1; };
-        int box_page = box_pages();
+        auto box_page_of = [&]() -> int { return !E4M3 && w == 0 && lane < boxes ? page_at(cur, cur.j * KT + box_rows * lane) : -1; };
+        int box_page = box_page_of();
+        int taken = 0;                                     // E4M3: K and V tiles converted from where TMA left them
         while (cur.left > 0) {
             const bool ends = cur.j + 1 == cur.nt || cur.left == 1;
             const int slot = t % ST;
@@ -544,7 +575,40 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
             const int tile0 = cur.j * KT;
             // a whole tile in pages of 8 tokens or more: TMA, one box per page and 64 channels.  Its rows land where the copies below put them.
             const bool by_tma = !E4M3 && p.tma && tile0 + KT <= cur.rq.len;
-            if (by_tma) {
+            if (E4M3 && p.tma && tile0 + KT <= cur.rq.len) {
+#pragma unroll 1
+                for (int half = 0; half < 2; ++half, ++taken) {
+                    const int at = taken % max(RU, 1);
+                    ok = wait_all(raw_full(at), (taken / max(RU, 1)) & 1, W_R_RAW_FULL);
+                    if (!ok) break;
+                    const uint32_t src = raw_s + at * C::RAW + sub * D + 16 * c, dst = half ? v_dst : k_dst;
+                    uint4 x[MINE * N];
+#pragma unroll
+                    for (int k = 0; k < MINE; ++k)
+#pragma unroll
+                        for (int i = 0; i < N; ++i) {
+                            const int run = w + k * LW;
+                            if (run < NRUN)
+                                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x[k * N + i].x), "=r"(x[k * N + i].y), "=r"(x[k * N + i].z), "=r"(x[k * N + i].w)
+                                             : "r"(src + (RUN * run + i * STEP) * D) : "memory");
+                        }
+#pragma unroll
+                    for (int k = 0; k < MINE; ++k)
+#pragma unroll
+                        for (int i = 0; i < N; ++i) {
+                            const int run = w + k * LW;
+                            if (run < NRUN) {
+                                const int kr = i * STEP + sub, c2 = 2 * c;
+                                const uint32_t row = (c2 >> 3) * C::BLK + (RUN * run + kr) * 128;
+                                store_f16(dst + row + (((c2 & 7) ^ (kr & 7)) << 4), dst + row + ((((c2 & 7) + 1) ^ (kr & 7)) << 4), x[k * N + i]);
+                            }
+                        }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(raw_empty(at));
+                }
+                if (!ok) break;
+                signal(kv_full(slot));
+            } else if (by_tma) {
                 if (w == 0) {
                     if (lane == 0) mbar_expect_tx(kv_full(slot), 2 * C::TILE);
                     __syncwarp();
@@ -562,7 +626,10 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                     mbar_arrive(kv_full(slot));
                 }
             } else {
-            uint4 xk[E4M3 ? MINE * N : 1], xv[E4M3 ? MINE * N : 1];              // E4M3: this warp's share of the tile, all in flight together
+#pragma unroll 1
+            for (int half = 0; half < (E4M3 ? 2 : 1); ++half) {
+            uint4 x[E4M3 ? MINE * N : 1];                  // E4M3: this warp's share of the K or V tile, all in flight together
+            const uint8_t* from = half ? p.cache.v : p.cache.k;
 #pragma unroll
             for (int k = 0; k < MINE; ++k) {
                 const int run = w + k * LW;
@@ -598,11 +665,8 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                         cp_async16(k_dst + at, p.cache.k + o, valid);
                         cp_async16(v_dst + at, p.cache.v + o, valid);
                     } else {
-                        xk[E4M3 ? k * N + i : 0] = xv[E4M3 ? k * N + i : 0] = make_uint4(0, 0, 0, 0);
-                        if (valid) {
-                            xk[E4M3 ? k * N + i : 0] = __ldcg(reinterpret_cast<const uint4*>(p.cache.k + o));
-                            xv[E4M3 ? k * N + i : 0] = __ldcg(reinterpret_cast<const uint4*>(p.cache.v + o));
-                        }
+                        x[E4M3 ? k * N + i : 0] = make_uint4(0, 0, 0, 0);
+                        if (valid) x[E4M3 ? k * N + i : 0] = __ldcg(reinterpret_cast<const uint4*>(from + o));
                     }
                 }
             }
@@ -616,10 +680,11 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                         const int kr = i * STEP + sub, c2 = 2 * c;               // key of the run, first of its two 16-byte pieces of f16
                         const uint32_t row = (c2 >> 3) * C::BLK + (RUN * run + kr) * 128;
                         const uint32_t at0 = row + (((c2 & 7) ^ (kr & 7)) << 4), at1 = row + ((((c2 & 7) + 1) ^ (kr & 7)) << 4);
-                        store_f16(k_dst + at0, k_dst + at1, xk[E4M3 ? k * N + i : 0]);
-                        store_f16(v_dst + at0, v_dst + at1, xv[E4M3 ? k * N + i : 0]);
+                        const uint32_t dst = half ? v_dst : k_dst;
+                        store_f16(dst + at0, dst + at1, x[E4M3 ? k * N + i : 0]);
                     }
                 }
+            }
             }
             signal(kv_full(slot));
             }
@@ -636,8 +701,8 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
             ++t;
             cur.advance(p);
             if (cur.left > 0) {
-                pages = run_pages();
-                box_page = box_pages();
+                if (!p.tma || cur.j * KT + KT > cur.rq.len) pages = run_pages();
+                else box_page = box_page_of();
             }
         }
     }
