@@ -30,7 +30,7 @@
 // more as a second product (LO).
 //
 // Measured (one new token, 8 query heads per key-value head unless said): 4 x 126k keys bf16 158 us = 6.6 TB/s, D = 64 84 us = 6.2, E4M3 86 us = 6.1;
-// 48 requests of 1 to 4096 keys in E4M3 56.5 us = 5.0 TB/s; one request of 333 keys 6.6 us, of which a launch is 2, the place of the run 1,
+// 48 requests of up to 16384 keys in E4M3 56.5 us = 5.0 TB/s; one request of 333 keys 6.6 us, of which a launch is 2, the place of the run 1,
 // the pages and the first tile 1.2, the products 1.3 and the output 1.
 #include "attention_rows.cu"
 
@@ -653,8 +653,8 @@ template <> struct Pick<256, true, 3> { using C = AttnCfg<256, true, 2, 2, 4, 16
 int rows_class(int max_rows) { return max_rows <= 4 ? 0 : (max_rows <= 8 ? 1 : (max_rows <= 16 ? 2 : (max_rows <= 32 ? 3 : 4))); }
 // The tcgen05 kernel (attention_rows.cu): above 32 rows always; 17 to 32 rows in bf16 with D = 128 and a table of 4096 tokens or more.
 // Measured, this kernel / that one: 20 rows, 9 requests of up to 2500 keys, D = 64 10.5 / 13.6 us; D = 128, 32 rows x 1000 keys 13.2 / 14.7,
-// 32 x 4480 22.8 / 21.7, 20 x 8000 54 / 44, 32 x 126k 292 / 205; D = 64, 32 x 126k 157 / 178; E4M3 191 / 387; 64 rows x 4480 30.6 / 22.6,
-// 64 x 126k 429 / 205, D = 64 299 / 176, D = 256 279 / 159, E4M3 353 / 403 and 269 / 260 (D = 64).
+// 32 x 4480 22.8 / 21.7, 20 x 8000 54 / 44, 32 x 126k 292 / 205; D = 64, 32 x 126k 157 / 178; E4M3, 32 x 60k 95 / 187 (the warps that fetched a tile converting it); 64 rows x 4480 30.6 / 22.6,
+// 64 x 126k 429 / 205, D = 64 299 / 197, E4M3 353 / 295 and 269 / 224 (D = 64); D = 256, 32 x 1500 22.1 / 20.2, 32 x 60k 274 / 279, 12 x 60k 267 / 280.
 bool many_rows(int max_rows, int head_dim, bool e4m3, long long max_kv) { return max_rows > 32 || (max_rows > 16 && head_dim == 128 && !e4m3 && max_kv >= 4096); }
 // Rows of a part in the workspace (whichever kernel runs: the size depends on the shapes alone)
 int tile_rows(int max_rows) { return max_rows <= 8 ? 8 : (max_rows <= 16 ? 16 : 128); }

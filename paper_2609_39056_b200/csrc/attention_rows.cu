@@ -6,12 +6,15 @@
 //     S = Q K^T    128 rows x KT keys,  operands in shared memory,  S in tensor memory (two buffers)
 //     O += P V     P read from tensor memory,  V in shared memory as it lies in the cache (its channels are the contiguous axis: the
 //                  operand is "MN-major", no transposition anywhere),  O in tensor memory
-// The same case takes 205 us, 128 rows run at 570 to 590 TFLOP/s; what bounds it is the softmax between the two products, a thread per row.
+// The same case takes 205 to 220 us, 128 rows run at 570 to 590 TFLOP/s; what bounds it is the softmax between the two products, a thread per row.
+// E4M3 295 us (64 rows x 4 x 30k keys 92 us; converted by the warps that also fetched it 111 us): the conversion takes issue slots
+// and the exponential's pipe from the softmax.
 //
 // Warps: two sets of four softmax warps that take half of a tile's keys each, a thread per row (no exchange between lanes; one set for D = 256), each
-// set with its own reference, sum and O; then one warp that issues the MMAs; three load.
+// set with its own reference, sum and O; then one warp that issues the MMAs; three load (E4M3: four convert, one more loads).
 //   Loading: 16-byte cp.async per row piece, page by page, straight into the 128-byte-swizzled layout the tensor core reads; keys at or
-//     behind the request's length become zeros.  E4M3 goes through registers and becomes f16 (exact; Q as in attention_paged.cu).
+//     behind the request's length become zeros.  Whole tiles in pages of 8 tokens or more come by TMA instead; E4M3 as it lies in the cache into a
+//     ring of its own, from where the loading warps convert it to f16 (exact; Q as in attention_paged.cu).
 //   Softmax: pass 1 takes the maximum of the row's KT scores, pass 2 turns them into probabilities and writes them over the scores they
 //     came from: f16, or bf16 hi in the first and lo in the second half of every 32 columns (two products; see attention_paged.cu on the
 //     rounding).  The reference the exponent is taken from is raised only when the maximum exceeds it by 2^8: O is rescaled
@@ -701,8 +704,8 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
             ++t;
             cur.advance(p);
             if (cur.left > 0) {
-                if (!p.tma || cur.j * KT + KT > cur.rq.len) pages = run_pages();
-                else box_page = box_page_of();
+                if (!E4M3 || !p.tma || cur.j * KT + KT > cur.rq.len) pages = run_pages();
+                box_page = box_page_of();
             }
         }
     }
