@@ -24,10 +24,13 @@
 // sum) in the workspace and a second kernel joins them in order (deterministic).  When every item is short the items are
 // handed out whole and nothing is joined.
 //
-// Rounding: Q, K and V enter exactly.  E4M3 numbers are f16 numbers, Q is brought to f16
-// by a power of two per row.  Scores and sums are fp32.  The probabilities (<= 1) enter the second product as f16
-// with E4M3 values (2^-12), and as TWO bf16 numbers hi + lo (2^-17) with bf16 values: for up to 4 rows in the columns that would be empty, for
-// more as a second product (LO).
+// Rounding: K and V enter exactly, and so does Q with a bf16 cache.  E4M3 numbers are f16 numbers, Q is brought to f16
+// by a power of two per row: exact down to 2^-28 of the row's largest element, below that off by at most 2^-40 of it.
+// Scores and sums are fp32.  With bf16 values the probabilities enter the second product as TWO bf16 numbers hi + lo (2^-17): for up to 4 rows in
+// the columns that would be empty, for more as a second product (LO).  With E4M3 values they enter as one f16 number, and f16 has few exponents: the
+// reference of a row is its maximum less kTop, so that the largest probability is 2^kTop instead of 1 and 2^-11 holds for every key down to 2^-29 of the
+// largest, 2^-40 of the largest below that.  (With the maximum as the reference a key 2^20 below the largest kept four bits: what
+// is left of a row when its largest key is a sink with a small value.)  Sums and parts are relative to the same reference: nothing else changes.
 //
 // Measured (one new token, 8 query heads per key-value head unless said): 4 x 126k keys bf16 158 us = 6.6 TB/s, D = 64 84 us = 6.2, E4M3 86 us = 6.1;
 // 48 requests of up to 16384 keys in E4M3 56.5 us = 5.0 TB/s; one request of 333 keys 6.6 us, of which a launch is 2, the place of the run 1,
@@ -104,6 +107,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
     constexpr int MT = KT / 16;                            // key tiles of the first product
     constexpr int DT = D / 16;                             // channel tiles of the second
     constexpr int GT = 32 * RW;                            // threads of a warp group
+    constexpr float kTop = E4M3 ? 15.0f : 0.0f;            // log2 of the largest probability: f16 ends at 2^16
     static_assert(KT == 16 || KT == 32, "a lane holds the place of one key of the tile");
     static_assert(GT % CH == 0 || CH % GT == 0, "rows are copied by whole groups of lanes");
     extern __shared__ __align__(128) uint8_t smem[];
@@ -166,7 +170,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
 
     uint32_t qf[KS][NB][2];
     float acc[DT][NB][4];                                  // output, transposed: channels on the 16-row side, rows on the 8 columns
-    float mx[NB][2], sum[NB][2], fac[NB][2];               // of rows 2 q and 2 q + 1 of every 8: running maximum and sum, score factor
+    float mx[NB][2], sum[NB][2], fac[NB][2];               // of rows 2 q and 2 q + 1 of every 8: reference (running maximum - kTop) and sum, score factor
     int lim[NB][2];                                        // keys the rows see
     int tail = 0;                                          // keys that all rows of the tile see: len where it is the same for all
     bool fresh = true, first_part = true, dropped = false;
@@ -309,6 +313,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
                     x0 = fmaxf(x0, __shfl_xor_sync(0xffffffffu, x0, o));
                     x1 = fmaxf(x1, __shfl_xor_sync(0xffffffffu, x1, o));
                 }
+                if (E4M3) { x0 -= kTop; x1 -= kTop; }
                 const float n0 = fmaxf(mx[n][0], x0), n1 = fmaxf(mx[n][1], x1);
                 const float u0 = n0 == -INFINITY ? 0.0f : n0, u1 = n1 == -INFINITY ? 0.0f : n1;  // an empty row so far: exp2(-inf - 0) = 0
                 cor[n][0] = exp2_approx(mx[n][0] - u0);

@@ -17,8 +17,9 @@
 //     ring of its own, from where the loading warps convert it to f16 (exact; Q as in attention_paged.cu).
 //   Softmax: pass 1 takes the maximum of the row's KT scores, pass 2 turns them into probabilities and writes them over the scores they
 //     came from: f16, or bf16 hi in the first and lo in the second half of every 32 columns (two products; see attention_paged.cu on the
-//     rounding).  The reference the exponent is taken from is raised only when the maximum exceeds it by 2^8: O is rescaled
-//     (read, multiplied, written) a few times per item instead of once per tile; sums stay fp32 either way.
+//     rounding).  The reference the exponent is taken from is raised only when the maximum has grown by a factor of 2^8 (E4M3: 2^4): O is
+//     rescaled (read, multiplied, written) a few times per item instead of once per tile; sums stay fp32 either way.  With E4M3 it lies 2^11 below the
+//     maximum, so that f16 holds probabilities down to 2^-25 of the largest with all its bits (2^8 and 2^-21 took 0.3 % less time).
 //   At the end of an item the first set adds the two O (in that order) and writes the rows or the part.
 //
 // Every wait is bounded; a role that gives up records the wait and makes the others leave (see ptx.cuh).
@@ -43,6 +44,9 @@ struct RowsCfg {
     static constexpr int HALF = KT / SETS;
     static constexpr int LW = E4M3 ? 4 : 3;                // loading warps (12 warps in all: 168 registers a thread),
     static constexpr int TW = E4M3 ? 1 : 0;                // with E4M3 they convert, and one more issues the TMA loads (14 warps: 144)
+    // The reference is the maximum less TOP when it is taken and is raised when the maximum less TOP exceeds it by RAISE: probabilities up to 2^(TOP + RAISE),
+    // for E4M3 as high in f16 as they can be (see attention_paged.cu on the rounding)
+    static constexpr float RAISE = E4M3 ? 4.0f : 8.0f, TOP = E4M3 ? 15.0f - RAISE : 0.0f;
     static constexpr int QW = 2;                           // of them, those that load the queries (the first issues the TMA loads and waits for nothing else)
     static constexpr int MMA_WARP = 4 * SETS;
     static constexpr int THREADS = 32 * (MMA_WARP + 1 + LW + TW);
@@ -269,17 +273,17 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                                 for (int i = 0; i < 32; ++i) q[i & 3] = fmaxf(q[i & 3], -__uint_as_float(x[c][i]));
                         }
                         mx = fmaxf(fmaxf(q[0], q[1]), fmaxf(q[2], q[3]));
-                        mx = mx == -INFINITY ? mx : mx * fabsf(f);               // (no key seen stays -inf whatever f is)
+                        mx = mx == -INFINITY ? mx : mx * fabsf(f) - C::TOP;      // (no key seen stays -inf whatever f is)
                     }
                     __syncwarp();                          // (the tensor memory instructions below want the whole warp together)
                     if (first_tile) {
                         m = mx;
-                    } else if (__any_sync(0xffffffffu, r < R && mx > m + 8.0f)) {
+                    } else if (__any_sync(0xffffffffu, r < R && mx > m + C::RAISE)) {
                         // raise the reference: O so far must be complete, then it is rescaled
                         ok = wait_all(pv_done(set), (t - 1) & 1, W_R_PV_DONE);
                         if (!ok) break;
                         tcgen05_fence_after_sync();
-                        const float n = mx > m + 8.0f ? mx : m;                  // (row by row: what a row becomes does not depend on its neighbours)
+                        const float n = mx > m + C::RAISE ? mx : m;                // (row by row: what a row becomes does not depend on its neighbours)
                         const float cor = n == -INFINITY ? 1.0f : exp2_approx(m - n);
                         m = n;
                         l *= cor;
