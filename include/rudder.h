@@ -400,8 +400,9 @@ rudder_status rudder_linear_a16(const rudder_weight* w, const uint16_t* X, int64
  *     out = h + down( gelu( up( rmsnorm(h; norm2_weight) ) ) )
  * The M rows are the new tokens of attn->B requests; their keys and values are appended to the cache before attention reads it.
  * Shapes: QKV H -> (heads + 2 kv heads) D, O heads D -> H, up H -> F, down F -> H.  Of `qk` the members X, ldx, M, Q, ldq, K, ldk and of `attn`
- * Q, ldq, M, O, ldo are supplied by the block; both name the same cache.  attn->lse [M, heads] or NULL.  A row of padding attends to
- * nothing (its attention output is zero).  Workspace: rudder_block_cached_workspace_bytes(args, attn, M), 256-byte aligned. */
+ * Q, ldq, M, O, ldo are supplied by the block; both name the same cache.  attn->lse [M, heads] or NULL.  A row of padding (position < 0)
+ * attends to nothing, inside a request's rows or outside: its attention output is zero, its lse -infinity (outside: left as it was).  With `causal` it counts
+ * as one of its request's rows, so the padding of a request stands in front of its tokens.  Workspace: rudder_block_cached_workspace_bytes(args, attn, M), 256-byte aligned. */
 size_t rudder_block_cached_workspace_bytes(const rudder_block_args* args, const rudder_attention_args* attn, int M);
 rudder_status rudder_block_cached(const rudder_block_args* args, const rudder_block_glue* glue, const rudder_qk_args* qk,
                                   const rudder_attention_args* attn, int M, const rudder_segments* seg, int step, void* workspace,

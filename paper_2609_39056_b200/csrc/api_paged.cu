@@ -261,13 +261,15 @@ rudder_status rudder_block_cached(const rudder_block_args* args, const rudder_bl
         return linear_impl(args->w[l], x, ldx, M, seg, step, args->tab[l], args->bias[l], args->y[l], args->ldy[l], ws + lin_off[l],
                            workspace_bytes_for(args->w[l], M), st, nullptr, 0, 0, 0, 0, nullptr, gelu_first);
     };
-    // rows of padding (position or slot < 0, behind the last request) are written by nobody between here and the O projection: zeros
+    // rows outside every request are written by nobody between here and the O projection, the queries of padding are not either: zeros
     if (cudaMemsetAsync(qn, 0, 2 * row_a, st) != cudaSuccess) return RUDDER_ERR_CUDA;
     // attention half: h = x + O(attention(QKV(norm1(x)), cache))
     if (launch_rmsnorm(args->x[0], args->ldx[0], glue->norm1_weight, glue->eps, n1, H, M, H, st) != cudaSuccess) return RUDDER_ERR_CUDA;
     if ((s = lin(0, n1, H, false)) != RUDDER_OK) return s;
     if (launch_qk_norm_rope(qp, qa.head_dim, qa.cache->format == RUDDER_CACHE_E4M3, sms, st) != cudaSuccess) return RUDDER_ERR_CUDA;
     if (launch_attention_paged(tp, att_ws, sms, st) != cudaSuccess) return RUDDER_ERR_CUDA;
+    // (among a request's rows a row of padding has been a query of zeros, i.e. it holds the mean of the values)
+    if (qp.positions && launch_padding_rows(tp, qp.positions, st) != cudaSuccess) return RUDDER_ERR_CUDA;
     if ((s = lin(1, ao, A, false)) != RUDDER_OK) return s;
     if (launch_add(args->x[0], args->ldx[0], args->y[1], args->ldy[1], h1, H, M, H, sms, st) != cudaSuccess) return RUDDER_ERR_CUDA;
     // MLP half: out = h + down(gelu(up(norm2(h))))

@@ -185,6 +185,7 @@ cudaError_t attention_paged_init();
 bool attention_uses_maps(int max_rows, int head_dim, bool e4m3, int page_size, long long max_kv);
 size_t attention_workspace_bytes(int max_rows, int head_dim, int sm_count);
 cudaError_t launch_attention_paged(const AttnArgs& a, void* workspace, int sm_count, cudaStream_t st);
+cudaError_t launch_padding_rows(const AttnArgs& a, const int32_t* positions, cudaStream_t st);
 cudaError_t linear_a16_init();
 bool linear_a16_fits(int K);              // the widest layer whose rows fit in shared memory
 cudaError_t launch_linear_a16(const rudder_weight* w, const uint16_t* X, int64_t ldx, int M, const float* bias, uint16_t* Y, int64_t ldy, int sm_count,
