@@ -390,7 +390,7 @@ rudder_status rudder_attention_paged(const rudder_attention_args* args, void* wo
 /* rudder_linear_a16 -- 1 to 16 rows through a packed weight with the activations kept in 16 bits (a step embedding, a
  * handful of action tokens): Y_mj = bf16( sum_k (x_mk dinv_k) q_jk Delta_W[j, g(k)] + b_j ), no workspace, any scheme.
  * The gains of Eq. 8 cancel without an activation quantiser, so there are no segments, steps or tables.  fp32 sums; x dinv
- * enters the product with 16 significant bits (its row becomes NaN where it is infinite).  K up to 36864 (one launch; wide layers one per pass of
+ * enters the product with 16 significant bits (from halfway between the largest bf16 number and 2^128 on: as infinity).  K up to 36864 (one launch; wide layers one per pass of
  * rows: above K = 9216 8 at a time, above 17920 4).  Other shape and alignment rules as in rudder_linear. */
 rudder_status rudder_linear_a16(const rudder_weight* w, const uint16_t* X, int64_t ldx, int M, const float* bias, uint16_t* Y, int64_t ldy,
                                 void* stream);

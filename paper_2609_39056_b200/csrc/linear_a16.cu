@@ -94,10 +94,12 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
 __device__ __forceinline__ void copy8(uint32_t dst, const void* src) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
 }
-// The split of two fp32 values: hi and lo as packed bf16 pairs.
+// The split of two fp32 values: hi and lo as packed bf16 pairs.  An infinite one is all hi: what is left over would be infinity - infinity.
+// (8 rows x 8192 x 2048 8.85 -> 9.0 us; one look at the largest of 16 values and a branch 8.95, but 16 rows x 2048 x 2048 5.55 against 5.45.)
 __device__ __forceinline__ void split2(float a, float b, uint32_t& hi, uint32_t& lo) {
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(hi) : "f"(b), "f"(a));
-    const float ra = __fsub_rn(a, __uint_as_float(hi << 16)), rb = __fsub_rn(b, __uint_as_float(hi & 0xFFFF0000u));
+    const float ha = __uint_as_float(hi << 16), hb = __uint_as_float(hi & 0xFFFF0000u);
+    const float ra = fabsf(ha) == INFINITY ? 0.0f : __fsub_rn(a, ha), rb = fabsf(hb) == INFINITY ? 0.0f : __fsub_rn(b, hb);
     asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(lo) : "f"(rb), "f"(ra));
 }
 
