@@ -100,7 +100,7 @@ __device__ __forceinline__ float4 nonfinite_values(const AttnParams& p, int b, i
     float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll 1
     for (int k = k0; k < k1; ++k) {
-        const int page = __ldg(p.table + static_cast<size_t>(b) * p.ld_table + (k >> p.cache.page_shift));
+        const int page = p.table[static_cast<size_t>(b) * p.ld_table + (k >> p.cache.page_shift)];
         if (page < 0 || page >= p.cache.n_pages) continue;
         const uint8_t* v = p.cache.v + page * p.cache.page_stride + static_cast<long long>(h) * p.cache.head_stride +
                            static_cast<long long>(k & ((1 << p.cache.page_shift) - 1)) * p.cache.token_stride + d * (E4M3 ? 1 : 2);

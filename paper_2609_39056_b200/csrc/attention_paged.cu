@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
     // page ids of the tile `at` is about to load: lane i holds the one of key i (KT <= 32)
     auto page_of_lane = [&](const Cursor<ROWS, UK>& at) -> int {
         const int key = at.j * UK + kg * KT + lane;
-        return (lane < KT && key < at.rq.len) ? __ldg(p.table + static_cast<size_t>(at.b) * p.ld_table + (key >> p.cache.page_shift)) : -2;
+        return (lane < KT && key < at.rq.len) ? p.table[static_cast<size_t>(at.b) * p.ld_table + (key >> p.cache.page_shift)] : -2;
     };
     auto issue = [&](const Cursor<ROWS, UK>& at, int page, int stage) {
         const int key0 = at.j * UK + kg * KT;
@@ -231,7 +231,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
                         qf[ks][n][0] = f16x2(bf16_lo(ax) * sc, bf16_hi(ax) * sc);
                         qf[ks][n][1] = f16x2(bf16_lo(ay) * sc, bf16_hi(ay) * sc);
                     }
-                    const float back = (p.cache.k_scale != nullptr ? __ldg(p.cache.k_scale + cur.h) : 1.0f) * p.scale_log2 *
+                    const float back = (p.cache.k_scale != nullptr ? p.cache.k_scale[cur.h] : 1.0f) * p.scale_log2 *
                                        __uint_as_float(static_cast<uint32_t>(127 - ex) << 23);
                     fac[n][0] = __shfl_sync(0xffffffffu, back, 8 * q);         // row 2 q of the tile is lane g = 2 q
                     fac[n][1] = __shfl_sync(0xffffffffu, back, 8 * q + 4);
@@ -404,7 +404,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
             const bool entire = item_end && part_j == 0;
             const int slot = 2 * blockIdx.x + (first_part ? 0 : 1);              // part at the start of the run, or at its end
             const int R = cur.rq.qlen * p.group;
-            const float vs = E4M3 ? (p.cache.v_scale != nullptr ? __ldg(p.cache.v_scale + cur.h) : 1.0f) : 1.0f;
+            const float vs = E4M3 ? (p.cache.v_scale != nullptr ? p.cache.v_scale[cur.h] : 1.0f) : 1.0f;
 #pragma unroll
             for (int n = 0; n < NB; ++n)
 #pragma unroll

@@ -231,7 +231,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                 f = r < R ? p.scale_log2 : 0.0f;           // rows that do not exist hold whatever the buffer held: weight 0, nothing read from them
                 ok = wait_all(q_full, item & 1, W_R_Q_FULL);
                 if (!ok) break;
-                if (E4M3 && r < R) f *= __uint_as_float(static_cast<uint32_t>(127 - s_exp[row]) << 23) * (p.cache.k_scale != nullptr ? __ldg(p.cache.k_scale + cur.h) : 1.0f);
+                if (E4M3 && r < R) f *= __uint_as_float(static_cast<uint32_t>(127 - s_exp[row]) << 23) * (p.cache.k_scale != nullptr ? p.cache.k_scale[cur.h] : 1.0f);
                 __syncwarp();
                 if (lane == 0) mbar_arrive(q_empty);
                 ++item;
@@ -381,7 +381,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                         }
                         tcgen05_fence_after_sync();
                         const bool entire = item_end && part_j == 0;
-                        const float vs = E4M3 && p.cache.v_scale != nullptr ? __ldg(p.cache.v_scale + cur.h) : 1.0f;
+                        const float vs = E4M3 && p.cache.v_scale != nullptr ? p.cache.v_scale[cur.h] : 1.0f;
                         const float w = entire ? (ll == 0.0f ? 0.0f : vs / ll) : vs;
                         w0 *= w;
                         w1 *= w;
@@ -444,7 +444,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
         }
     } else {
     auto page_at = [&](const Cursor<ROWS, KT>& at, int key) -> int {
-        return key < at.rq.len ? __ldg(p.table + static_cast<size_t>(at.b) * p.ld_table + (key >> p.cache.page_shift)) : -1;
+        return key < at.rq.len ? p.table[static_cast<size_t>(at.b) * p.ld_table + (key >> p.cache.page_shift)] : -1;
     };
     const int box_rows = min(64, 1 << p.cache.page_shift), boxes = KT / box_rows;
     if (E4M3 && warp > MMA_WARP + LW) {

@@ -289,7 +289,7 @@ __global__ void __launch_bounds__(A16Cfg<LAYOUT, NT, KS>::THREADS, 1) linear_a16
             if (KS > 1) {
                 part[t][m][n] = sum;
             } else {
-                const float b = p.bias != nullptr ? __ldg(p.bias + tile * 16 + n) : 0.0f;
+                const float b = p.bias != nullptr ? p.bias[tile * 16 + n] : 0.0f;
                 p.Y[static_cast<size_t>(m) * p.ldy + tile * 16 + n] = __bfloat16_as_ushort(__float2bfloat16_rn(fmaf(sum, out_scale, b)));
             }
         }
@@ -300,7 +300,7 @@ __global__ void __launch_bounds__(A16Cfg<LAYOUT, NT, KS>::THREADS, 1) linear_a16
                 float sum = 0.0f;
 #pragma unroll
                 for (int r = 0; r < KS; ++r) sum += ld_dsmem(&part[rank][m][n], r);
-                const float b = p.bias != nullptr ? __ldg(p.bias + col) : 0.0f;
+                const float b = p.bias != nullptr ? p.bias[col] : 0.0f;
                 p.Y[static_cast<size_t>(m) * p.ldy + col] = __bfloat16_as_ushort(__float2bfloat16_rn(fmaf(sum, out_scale, b)));
             }
             cluster_sync_all();                                                 // the peers have read `part`

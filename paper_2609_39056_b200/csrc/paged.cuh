@@ -61,6 +61,9 @@ struct AttnArgs {
     CUtensorMap tm_k, tm_v;               // [pages][heads][tokens][channels], box {64, min(64, page size), 1, 1}, 128-byte swizzle
 };
 
+// A kernel that is launched early lives while the kernels in front of it still write.  Behind pdl_wait it sees what they wrote, but only by ordinary
+// loads: what a caller may write on the stream (tables, lengths, scales, biases, angles) is not read through __ldg, which asks for memory that nobody
+// writes while the kernel lives.  (Packed weights are complete when rudder_pack_weights returns.)
 __device__ __forceinline__ void pdl_launch_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 

@@ -68,7 +68,7 @@ __device__ __forceinline__ uint32_t to_e4m3(f32x2 a, f32x2 b) {
     return static_cast<uint32_t>(lo) | (static_cast<uint32_t>(hi) << 16);
 }
 __device__ __forceinline__ void load4(const float* p, f32x2& a, f32x2& b) {
-    const float4 v = __ldg(reinterpret_cast<const float4*>(p));
+    const float4 v = *reinterpret_cast<const float4*>(p);
     a = make2(v.x, v.y);
     b = make2(v.z, v.w);
 }
@@ -99,7 +99,7 @@ __global__ void __launch_bounds__(QK_THREADS, 4) qk_norm_rope_kernel(const QkArg
         for (int i = tid; i < 2 * a.kv_heads; i += QK_THREADS) {
             const float* sc = i < a.kv_heads ? a.cache.k_scale : a.cache.v_scale;
             const int h = i < a.kv_heads ? i : i - a.kv_heads;
-            s_inv[i] = sc != nullptr ? __fdiv_rn(1.0f, __ldg(sc + h)) : 1.0f;
+            s_inv[i] = sc != nullptr ? __fdiv_rn(1.0f, sc[h]) : 1.0f;
         }
         __syncthreads();
     }
@@ -144,7 +144,7 @@ __global__ void __launch_bounds__(QK_THREADS, 4) qk_norm_rope_kernel(const QkArg
             const float* cp = a.cos + static_cast<size_t>(pos) * half + 4 * l;
             const float* sp = a.sin + static_cast<size_t>(pos) * half + 4 * l;
             if (PAIRS) {
-                const float4 c4 = __ldg(reinterpret_cast<const float4*>(cp)), s4 = __ldg(reinterpret_cast<const float4*>(sp));
+                const float4 c4 = *reinterpret_cast<const float4*>(cp), s4 = *reinterpret_cast<const float4*>(sp);
                 c[0] = make2(c4.x, c4.x); c[1] = make2(c4.y, c4.y); c[PAIRS ? 2 : 0] = make2(c4.z, c4.z); c[PAIRS ? 3 : 0] = make2(c4.w, c4.w);
                 s[0] = make2(-s4.x, s4.x); s[1] = make2(-s4.y, s4.y); s[PAIRS ? 2 : 0] = make2(-s4.z, s4.z); s[PAIRS ? 3 : 0] = make2(-s4.w, s4.w);
             } else {
