@@ -361,7 +361,8 @@ rudder_status rudder_qk_norm_rope(const rudder_qk_args* args, void* stream);
  * over j < kv_lens[b] (the new tokens' own keys included when they have been appended); with `causal` token t of n sees
  * j <= kv_lens[b] - n + t.  Query head h uses key-value head h / (heads / cache heads).  A row that sees no key gets zeros and
  * lse = -infinity.  What the cache holds at and behind kv_lens[b] is never used, and what a row does not see has no part in it (not a
- * number or infinite as it may be); among the keys that only some rows of a request see, infinite values become infinities of the rows that see them.
+ * number or infinite as it may be).  A value that a row sees and that is infinite or not a number makes that channel of the row infinite or not a number.
+ * Rounding: scores and sums fp32; probabilities to 2^-17 with a bf16 cache; with E4M3 to 2^-11, those below 2^-25 of a row's largest to 2^-36 of that.
  * Request b has the rows q_starts[b] .. q_starts[b+1] - 1 (at most max_q), or with q_starts NULL the rows b max_q ..
  * (b + 1) max_q - 1; all other rows of O and lse are left as they were.  O may be Q.
  * workspace: rudder_attention_workspace_bytes(args) bytes (from heads, max_q and the cache's shape alone), 256-byte
@@ -374,7 +375,7 @@ typedef struct {
     const rudder_paged_cache* cache;
     const int32_t* page_table;   /* [B, ld_table] */
     int64_t ld_table;
-    int max_pages;               /* columns that may be read; max_pages x page_size < 2^31 - 2^16 */
+    int max_pages;               /* columns that may be read; max_pages x page_size <= 2^31 - 2^16 */
     const int32_t* kv_lens;      /* [B] */
     const int32_t* q_starts;     /* [B + 1] or NULL */
     int B, max_q;

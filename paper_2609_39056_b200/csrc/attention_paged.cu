@@ -25,15 +25,15 @@
 // handed out whole and nothing is joined.
 //
 // Rounding: K and V enter exactly, and so does Q with a bf16 cache.  E4M3 numbers are f16 numbers, Q is brought to f16
-// by a power of two per row: exact down to 2^-28 of the row's largest element, below that off by at most 2^-40 of it.
+// by a power of two per row: exact down to 2^-28 of the row's largest element, below that off by at most 2^-39 of it.
 // Scores and sums are fp32.  With bf16 values the probabilities enter the second product as TWO bf16 numbers hi + lo (2^-17): for up to 4 rows in
 // the columns that would be empty, for more as a second product (LO).  With E4M3 values they enter as one f16 number, and f16 has few exponents: the
 // reference of a row is its maximum less kTop, so that the largest probability is 2^kTop instead of 1 and 2^-11 holds for every key down to 2^-29 of the
 // largest, 2^-40 of the largest below that.  (With the maximum as the reference a key 2^20 below the largest kept four bits: what
 // is left of a row when its largest key is a sink with a small value.)  Sums and parts are relative to the same reference: nothing else changes.
 //
-// Measured (one new token, 8 query heads per key-value head unless said): 4 x 126k keys bf16 158 us = 6.6 TB/s, D = 64 84 us = 6.2, E4M3 86 us = 6.1;
-// 48 requests of up to 16384 keys in E4M3 56.5 us = 5.0 TB/s; one request of 333 keys 6.6 us, of which a launch is 2, the place of the run 1,
+// Measured (one new token, 8 query heads per key-value head unless said): 4 x 126k keys bf16 158 us = 6.6 TB/s, D = 64 86 us = 6.1, E4M3 86 us = 6.1;
+// 48 requests of up to 16384 keys in E4M3 57.5 us = 4.9 TB/s; one request of 333 keys 6.6 us, of which a launch is 2, the place of the run 1,
 // the pages and the first tile 1.2, the products 1.3 and the output 1.
 #include "attention_rows.cu"
 
@@ -656,10 +656,12 @@ template <> struct Pick<256, false, 3> { using C = AttnCfg<256, false, 2, 2, 4, 
 template <> struct Pick<256, true, 3> { using C = AttnCfg<256, true, 2, 2, 4, 16, 5, 0>; };
 
 int rows_class(int max_rows) { return max_rows <= 4 ? 0 : (max_rows <= 8 ? 1 : (max_rows <= 16 ? 2 : (max_rows <= 32 ? 3 : 4))); }
-// The tcgen05 kernel (attention_rows.cu): above 32 rows always; 17 to 32 rows in bf16 with D = 128 and a table of 4096 tokens or more.
-// Measured, this kernel / that one: 20 rows, 9 requests of up to 2500 keys, D = 64 10.5 / 13.6 us; D = 128, 32 rows x 1000 keys 13.2 / 14.7,
-// 32 x 4480 22.8 / 21.7, 20 x 8000 54 / 44, 32 x 126k 292 / 205; D = 64, 32 x 126k 157 / 178; E4M3, 32 x 60k 95 / 187 (the warps that fetched a tile converting it); 64 rows x 4480 30.6 / 22.6,
-// 64 x 126k 429 / 205, D = 64 299 / 197, E4M3 353 / 295 and 269 / 224 (D = 64); D = 256, 32 x 1500 22.1 / 20.2, 32 x 60k 274 / 279, 12 x 60k 267 / 280.
+// The tcgen05 kernel (attention_rows.cu): above 32 rows always; 17 to 32 rows in bf16 with D = 128 and a table of 4096 tokens or more (the lengths
+// themselves are device data).  Measured, this kernel / that one, 4 requests x 4 key-value heads unless said:
+//   bf16, D = 128: 32 rows x 1000 keys 13.1 / 14.4 us, 1 request x 16 heads of 32 x 4480 22.6 / 21.5, 20 x 8000 30.4 / 30.9, 32 x 126k 293 / 210, 64 x 126k 429 / 218;
+//   D = 64: 20 rows, 9 requests of up to 2500 keys 10.5 / 13.6, 32 x 126k 155 to 193 / 220 to 250, 64 x 126k 299 / 197; D = 256: 32 x 1500 21.1 / 20.0, 32 x 60k 265 / 278;
+//   E4M3, D = 128: 20 x 1000 12.1 / 15.9, 32 x 8000 25 / 36, 32 x 60k 96 / 144, 32 x 126k 189 / 282, 64 x 126k 353 / 295; D = 64: 20 x 8000 18.3 / 25.5, 32 x 126k 143 / 227,
+//   64 x 126k 269 / 227; D = 256: 32 x 1500 19.1 / 21.4, 32 x 60k 219 / 244.
 bool many_rows(int max_rows, int head_dim, bool e4m3, long long max_kv) { return max_rows > 32 || (max_rows > 16 && head_dim == 128 && !e4m3 && max_kv >= 4096); }
 // Rows of a part in the workspace (whichever kernel runs: the size depends on the shapes alone)
 int tile_rows(int max_rows) { return max_rows <= 8 ? 8 : (max_rows <= 16 ? 16 : 128); }

@@ -6,9 +6,10 @@
 //     S = Q K^T    128 rows x KT keys,  operands in shared memory,  S in tensor memory (two buffers)
 //     O += P V     P read from tensor memory,  V in shared memory as it lies in the cache (its channels are the contiguous axis: the
 //                  operand is "MN-major", no transposition anywhere),  O in tensor memory
-// The same case takes 205 to 220 us, 128 rows run at 570 to 590 TFLOP/s; what bounds it is the softmax between the two products, a thread per row.
-// E4M3 295 us (64 rows x 4 x 30k keys 92 us; converted by the warps that also fetched it 111 us): the conversion takes issue slots
-// and the exponential's pipe from the softmax.
+// The same case takes 205 to 220 us, 128 rows run at 565 to 590 TFLOP/s.  No pipe is full (64 rows x 4 x 30k keys: tensor 39 %, DRAM 42 %, issue slots 27 %,
+// exponentials 13 %): what bounds it is the chain of a tile, scores -> tensor memory -> softmax, a thread per row -> P -> product, with two tiles in hand.
+// E4M3 295 us (64 rows x 4 x 30k keys 92 us; converted by the warps that also fetched it 111 us): tensor 18 %, issue slots 22 %, exponentials 9 %; the conversion adds a
+// step in front of that chain (shared memory -> registers -> shared memory, fence, barrier) with two stages to cover it.
 //
 // Warps: two sets of four softmax warps that take half of a tile's keys each, a thread per row (no exchange between lanes; one set for D = 256), each
 // set with its own reference, sum and O; then one warp that issues the MMAs; three load (E4M3: four convert, one more loads).

@@ -19,8 +19,8 @@
 // inside a 64-channel block is free as long as both operands use the same one: each is the order in which the packed
 // layout's nibbles come out of a word by one shift and one mask per pair.
 //
-// Measured: 1 row x 2048 x 2048 W4A8 2.9 us (an empty launch 2.0), 8 rows x 8192 x 2048 NVFP4 8.8 us = 1.1 TB/s: the latency of the first
-// weights, the staging of v and the sums over the warps.
+// Measured: 1 row x 2048 x 2048 W4A8 3.0 us (an empty launch 2.0), 8 rows x 8192 x 2048 NVFP4 9.0 us = 1.1 TB/s, 1 row x 8192 x 8192 W4A8 17.5 us = 2.0 TB/s: the latency
+// of the first weights, the staging of v, and for many tiles the sums over the warps between two barriers of each (issue slots 48 %, ALU 48 %, DRAM a fifth).
 #include "internal.cuh"
 #include "paged.cuh"
 
@@ -128,7 +128,7 @@ struct A16Cfg {
     static constexpr int kBlockBytes = 4 * NT * 256 + 32;
     static constexpr int kRing = WARPS * ST * kStage;
     static constexpr int kRed = (WARPS + KS) * 4 * NT * 17 * 4;
-    static int smem(int n_blocks) { return kRing + kRed + n_blocks * kBlockBytes; }
+    static constexpr int smem(int n_blocks) { return kRing + kRed + n_blocks * kBlockBytes; }
 };
 
 template <int LAYOUT, int NT, int KS>
@@ -335,10 +335,13 @@ cudaError_t launch_one(const LinearA16Params& p, int sm_count, cudaStream_t st)
 }
 template <int LAYOUT, int NT, int KS>
 bool fits(int K) { return A16Cfg<LAYOUT, NT, KS>::smem(2 * (((K >> 7) + KS - 1) / KS)) <= kMaxSmem; }
-// One CTA per 16 channels while v fits beside the ring (K up to about 8000, 4000, 2000 for 4, 8, 16 rows); a cluster of four
+// One CTA per 16 channels while v fits beside the ring (K up to 9216, 4480, 2432 for 4, 8, 16 rows); a cluster of four
 // with a quarter of K each beyond that.  Measured, one / four: 1 x 2048 x 2048 2.9 / 4.0 us, 8 x 4096 x 4096 7.8 / 11.2 us (the cluster's
 // two barriers per tile); where v does not fit, four against the CTA that stages it in pieces: 8 x 8192 x 2048 8.8 / 11.0 us,
 // 16 x 8192 x 2048 11.1 / 17.9 us.
+template <int NT, int KS>
+constexpr bool widest(int K) { return A16Cfg<A16_INT, NT, KS>::smem(2 * (K / 128 / KS)) <= kMaxSmem && A16Cfg<A16_INT, NT, KS>::smem(2 * (K / 128 / KS + 1)) > kMaxSmem; }
+static_assert(widest<1, 1>(9216) && widest<2, 1>(4480) && widest<4, 1>(2432) && widest<1, 4>(36864) && widest<2, 4>(17920) && widest<4, 4>(9216), "limits stated here and in rudder.h");
 template <int LAYOUT, int NT>
 cudaError_t launch_nt(const LinearA16Params& p, int sm_count, cudaStream_t st)
 {

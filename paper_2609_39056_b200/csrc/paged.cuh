@@ -58,7 +58,7 @@ struct AttnArgs {
     int B, max_q, causal;
     float scale;
     bool tma;                             // tensor maps over K and V: see attention_rows.cu
-    CUtensorMap tm_k, tm_v;               // [pages][heads][tokens][channels], box {64, min(64, page size), 1, 1}, 128-byte swizzle
+    CUtensorMap tm_k, tm_v;               // [pages][heads][tokens][channels], box of min(64, page size) tokens: bf16 64 channels, 128-byte swizzle; E4M3 whole rows as they lie
 };
 
 // A kernel that is launched early lives while the kernels in front of it still write.  Behind pdl_wait it sees what they wrote, but only by ordinary
