@@ -521,9 +521,9 @@ def rudder_page_tables(args: PageTableArgs, stream=None):
 
 
 def _rows(t: torch.Tensor) -> int:
-    """Leading dimension of a [M, N] view with contiguous channels (one row has none of its own)."""
+    """Leading dimension of a [M, N] view with contiguous channels (one row has none of its own, whatever pitch its buffer has)."""
     assert t.dim() == 2 and t.stride(1) == 1
-    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), -(-t.shape[1] // 8) * 8)
+    return t.stride(0) if t.shape[0] > 1 else -(-t.shape[1] // 8) * 8
 
 
 class QkArgs:
@@ -617,7 +617,7 @@ def rudder_linear_a16(w: Weight, X: torch.Tensor, bias=None, Y=None, stream=None
         assert bias.dtype is torch.float32 and bias.numel() == w.N and bias.is_contiguous() and bias.get_device() == device
         b = bias.data_ptr()
     if M == 1:                                       # one row has no leading dimension of its own
-        ldx, ldy = max(ldx, K), max(ldy, w.N)
+        ldx, ldy = K, w.N
     s = lib().rudder_linear_a16(w.handle, X.data_ptr(), ldx, M, b, Y.data_ptr(), ldy, _launch_stream(device, stream))
     if s:
         _check(s, "rudder_linear_a16")
