@@ -409,6 +409,132 @@ rudder_status rudder_block_cached(const rudder_block_args* args, const rudder_bl
                                   const rudder_attention_args* attn, int M, const rudder_segments* seg, int step, void* workspace,
                                   size_t workspace_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Many requests that continue one context (candidate action chunks of one robot, robots with adapters of their own).  The paper has no
+ * counterpart.  What the kernels find wrong in device data is left out and recorded as above; 917 = an adapter's index or rank.
+ *
+ * The operators on pages know a request by its row of page_table [B, ld_table] and its length lens[b]: it holds the first
+ * ceil(lens[b] / page_size) entries of its row.  `caches` (HOST) are the caches of n_caches layers, 0..128, that one page table serves: the same format, shape
+ * and strides, and 2 x layers x heads x entries of a list below 2^31.
+ *
+ * rudder_page_fork -- request dst[i] becomes a copy of request src[i] up to l = fork_lens[i] (NULL: its whole length), one launch: the full pages
+ * are shared (both rows name them), l % page_size tokens of the page behind them are copied in every layer to a page of the free list:
+ *     page_table[dst][j] = page_table[src][j], j < l / page_size,   page_table[dst][l / page_size] = free_pages[taken + children with such tokens before i]
+ * and lens[dst] = l.  Left out (row and length as they were): a child whose dst is a source of the call or the dst of a child before it, whose rows or
+ * lengths do not exist, or for which the free list has no page (an entry below 0 is none).  used = pages asked for.  Calling again with
+ * the same inputs writes the same. */
+typedef struct {
+    int32_t* page_table;         /* [B, ld_table], in and out */
+    int64_t ld_table;
+    int max_pages;               /* columns, <= ld_table */
+    int32_t* lens;               /* [B], in and out */
+    int B;                       /* 1..8192 */
+    int page_size;
+    const int32_t* src;          /* [n] */
+    const int32_t* dst;          /* [n] */
+    const int32_t* fork_lens;    /* [n] or NULL */
+    int n;                       /* 1..8192 */
+    const int32_t* free_pages;   /* [n_free]; may be NULL when n_free is 0 */
+    int n_free;
+    const int32_t* taken;        /* [1] entries of the free list that are gone already (`used` of the call before), or NULL = 0 */
+    int32_t* copies;             /* [n, 3] out: page copied from, to (-1, -1 for none), tokens; or NULL */
+    int32_t* used;               /* [1] out */
+} rudder_page_fork_args;
+rudder_status rudder_page_fork(const rudder_page_fork_args* args, const rudder_paged_cache* caches, int n_caches, void* stream);
+
+/* rudder_page_copy -- tokens 0 .. copies[i][2] - 1 of page copies[i][0] to page copies[i][1] in every layer; entries with a page below 0 are none.  The pages
+ * copied to are distinct and none is copied from (what two such copies leave is not defined). */
+typedef struct {
+    const int32_t* copies;       /* [n, 3] */
+    const int32_t* count;        /* [1] entries in use, or NULL = n */
+    int n;                       /* 1.. */
+} rudder_page_copy_args;
+rudder_status rudder_page_copy(const rudder_page_copy_args* args, const rudder_paged_cache* caches, int n_caches, void* stream);
+
+/* rudder_page_release -- lens[drop[i]] = 0, then refs[p] = entries of page p that requests hold, free_pages = the pages with none in ascending
+ * order, -1 behind the last, n_free = their number.  One launch; nothing is kept between calls, so it also makes the first free list. */
+typedef struct {
+    const int32_t* page_table;   /* [B, ld_table] */
+    int64_t ld_table;
+    int max_pages;
+    int32_t* lens;               /* [B], in and out */
+    int B;                       /* 1..2^20 */
+    int page_size;
+    const int32_t* drop;         /* [n_drop]; may be NULL when n_drop is 0 */
+    int n_drop;
+    int n_pages;                 /* 1..2^30 */
+    int32_t* refs;               /* [n_pages] out */
+    int32_t* free_pages;         /* [n_pages] out */
+    int32_t* n_free;             /* [1] out */
+} rudder_page_release_args;
+rudder_status rudder_page_release(const rudder_page_release_args* args, void* stream);
+
+/* rudder_page_compact -- the n_live pages that requests hold move to the ids 0 .. n_live - 1: the k-th of those at or above n_live, ascending, to the
+ * k-th unused one below.  copies = these moves (whole pages), in the form of rudder_page_copy, which the call runs on `caches` (n_caches 0: the plan alone).
+ * new_table = page_table with the entries that requests hold renamed, all others as they are; it may be page_table itself (then ld_new = ld_table).
+ * remap[p] = the new id of page p, -1 for a page that no request holds.  Rows of copies at and behind n_copies are left as they were. */
+typedef struct {
+    const int32_t* page_table;   /* [B, ld_table] */
+    int64_t ld_table;
+    int max_pages;
+    const int32_t* lens;         /* [B] */
+    int B;                       /* 1..2^20 */
+    int page_size;
+    int n_pages;                 /* 1..2^30; with caches: theirs */
+    int32_t* new_table;          /* [B, ld_new] out */
+    int64_t ld_new;
+    int32_t* remap;              /* [n_pages] out */
+    int32_t* copies;             /* [n_pages / 2, 3] out; may be NULL when n_pages is 1 */
+    int32_t* n_copies;           /* [1] out */
+    int32_t* n_live;             /* [1] out */
+} rudder_page_compact_args;
+rudder_status rudder_page_compact(const rudder_page_compact_args* args, const rudder_paged_cache* caches, int n_caches, void* stream);
+
+/* rudder_attention_shared -- rudder_attention_paged for requests in groups whose first tokens lie in the same pages: requests group_starts[g] ..
+ * group_starts[g + 1] - 1 share their first prefix_lens[g] tokens, which are read once for all of them, through row prefix_rows[g] of attn.page_table.  The
+ * result is that of rudder_attention_paged to the rounding of fp32 sums.  A request with a row that does not see the whole prefix (shorter, or more new tokens than it
+ * has of its own under `causal`) reads all of its tokens through its own row of the table, as does a request of no group.  prefix_lens need not be a
+ * multiple of the page size, and 0 is allowed; the requests' own rows of the table name the prefix's pages, too, or pages with the same tokens.
+ * Groups do not overlap.  group_q, the most new tokens that a group has, chooses the kernel; a group with more is computed all the same.
+ * M x heads / cache heads up to 2^20.  workspace: rudder_attention_shared_workspace_bytes(args) bytes, rules as in rudder_attention_paged. */
+typedef struct {
+    rudder_attention_args attn;
+    const int32_t* group_starts; /* [n_groups + 1], not descending */
+    const int32_t* prefix_lens;  /* [n_groups] */
+    const int32_t* prefix_rows;  /* [n_groups], each in [0, table_rows) */
+    int n_groups;                /* 1..2^20 */
+    int table_rows;              /* rows of attn.page_table, >= attn.B */
+    int group_q;                 /* 1.. */
+} rudder_attention_shared_args;
+size_t rudder_attention_shared_workspace_bytes(const rudder_attention_shared_args* args);
+rudder_status rudder_attention_shared(const rudder_attention_shared_args* args, void* workspace, size_t workspace_bytes, void* stream);
+
+/* rudder_lora -- low-rank adapters beside a shared projection (whose output is `base`), a = adapters[m] for every row m:
+ *     Y_m = bf16( base_m + scales[a] sum_{r < ranks[a]} (sum_k x_mk A_a[r][k]) B_a[.][r] ),    Y_m = base_m where a is -1
+ * Sums fp32, the inner sum enters the outer one with 16 significant bits, one rounding at the end.  What A and B hold at and behind ranks[a] is never used, and
+ * another row's numbers have no part in a row.  Y may be base (same leading dimension).  workspace: rudder_lora_workspace_bytes(args) bytes (from M, K, R and
+ * n_adapters alone), 256-byte aligned; calls that may overlap on the GPU need one each. */
+typedef struct {
+    const uint16_t* X;           /* bf16 [M, ldx] */
+    int64_t ldx;
+    int M, K;                    /* K % 8 == 0 */
+    const uint16_t* A;           /* bf16 [n_adapters][R][lda], adapters a_stride elements apart */
+    int64_t a_stride, lda;
+    const uint16_t* B;           /* bf16 [n_adapters][N][ldb] */
+    int64_t b_stride, ldb;
+    int N, R;                    /* N % 8 == 0; R the most an adapter may have: a multiple of 8, 8..256 */
+    int n_adapters;              /* 1..4096 */
+    const int32_t* ranks;        /* [n_adapters], each 0..R */
+    const float* scales;         /* [n_adapters] */
+    const int32_t* adapters;     /* [M], each -1..n_adapters - 1, in any order */
+    const uint16_t* base;        /* bf16 [M, ld_base], or NULL = zeros */
+    int64_t ld_base;
+    uint16_t* Y;                 /* bf16 [M, ldy] */
+    int64_t ldy;
+} rudder_lora_args;
+size_t rudder_lora_workspace_bytes(const rudder_lora_args* args);
+rudder_status rudder_lora(const rudder_lora_args* args, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Reads and clears the device status word (SYNCHRONISES the device).  *last (HOST) receives
  * RUDDER_OK, RUDDER_ERR_TIMEOUT or RUDDER_ERR_ARG (bad device data, see above); *where (HOST, may be NULL) a code
  * naming the wait that gave up or what was bad. */

@@ -22,7 +22,7 @@ RANGE_PER_TOKEN, RANGE_STATIC = 0, 1
 CACHE_BF16, CACHE_E4M3 = 0, 1
 ROPE_HALF, ROPE_PAIRS = 0, 1
 # second value of rudder_device_status after ERR_ARG: what a kernel found in the caller's device data
-BAD_PAGE, BAD_LENGTH, BAD_POSITION, BAD_SLOT, NO_PAGES, NO_ROOM = range(911, 917)
+BAD_PAGE, BAD_LENGTH, BAD_POSITION, BAD_SLOT, NO_PAGES, NO_ROOM, BAD_ADAPTER = range(911, 918)
 SCHEMES = {"w4a8": W4A8_INT, "w4a4": W4A4_INT, "nvfp4": W4A4_NVFP4}
 
 EXPORTED = [
@@ -35,6 +35,8 @@ EXPORTED = [
     "rudder_block_dit", "rudder_block_dit_workspace_bytes", "rudder_gelu_quantize_activations",
     "rudder_page_tables", "rudder_qk_norm_rope", "rudder_attention_workspace_bytes", "rudder_attention_paged", "rudder_linear_a16",
     "rudder_block_cached_workspace_bytes", "rudder_block_cached",
+    "rudder_page_fork", "rudder_page_copy", "rudder_page_release", "rudder_page_compact", "rudder_attention_shared_workspace_bytes", "rudder_attention_shared",
+    "rudder_lora_workspace_bytes", "rudder_lora",
 ]
 
 
@@ -91,6 +93,40 @@ class _AttentionArgs(ctypes.Structure):
                 ("page_table", ctypes.c_void_p), ("ld_table", ctypes.c_int64), ("max_pages", ctypes.c_int), ("kv_lens", ctypes.c_void_p),
                 ("q_starts", ctypes.c_void_p), ("B", ctypes.c_int), ("max_q", ctypes.c_int), ("causal", ctypes.c_int), ("scale", ctypes.c_float),
                 ("O", ctypes.c_void_p), ("ldo", ctypes.c_int64), ("lse", ctypes.c_void_p)]
+
+
+class _PageForkArgs(ctypes.Structure):
+    _fields_ = [("page_table", ctypes.c_void_p), ("ld_table", ctypes.c_int64), ("max_pages", ctypes.c_int), ("lens", ctypes.c_void_p), ("B", ctypes.c_int),
+                ("page_size", ctypes.c_int), ("src", ctypes.c_void_p), ("dst", ctypes.c_void_p), ("fork_lens", ctypes.c_void_p), ("n", ctypes.c_int),
+                ("free_pages", ctypes.c_void_p), ("n_free", ctypes.c_int), ("taken", ctypes.c_void_p), ("copies", ctypes.c_void_p), ("used", ctypes.c_void_p)]
+
+
+class _PageCopyArgs(ctypes.Structure):
+    _fields_ = [("copies", ctypes.c_void_p), ("count", ctypes.c_void_p), ("n", ctypes.c_int)]
+
+
+class _PageReleaseArgs(ctypes.Structure):
+    _fields_ = [("page_table", ctypes.c_void_p), ("ld_table", ctypes.c_int64), ("max_pages", ctypes.c_int), ("lens", ctypes.c_void_p), ("B", ctypes.c_int),
+                ("page_size", ctypes.c_int), ("drop", ctypes.c_void_p), ("n_drop", ctypes.c_int), ("n_pages", ctypes.c_int), ("refs", ctypes.c_void_p),
+                ("free_pages", ctypes.c_void_p), ("n_free", ctypes.c_void_p)]
+
+
+class _PageCompactArgs(ctypes.Structure):
+    _fields_ = [("page_table", ctypes.c_void_p), ("ld_table", ctypes.c_int64), ("max_pages", ctypes.c_int), ("lens", ctypes.c_void_p), ("B", ctypes.c_int),
+                ("page_size", ctypes.c_int), ("n_pages", ctypes.c_int), ("new_table", ctypes.c_void_p), ("ld_new", ctypes.c_int64), ("remap", ctypes.c_void_p),
+                ("copies", ctypes.c_void_p), ("n_copies", ctypes.c_void_p), ("n_live", ctypes.c_void_p)]
+
+
+class _SharedAttentionArgs(ctypes.Structure):
+    _fields_ = [("attn", _AttentionArgs), ("group_starts", ctypes.c_void_p), ("prefix_lens", ctypes.c_void_p), ("prefix_rows", ctypes.c_void_p),
+                ("n_groups", ctypes.c_int), ("table_rows", ctypes.c_int), ("group_q", ctypes.c_int)]
+
+
+class _LoraArgs(ctypes.Structure):
+    _fields_ = [("X", ctypes.c_void_p), ("ldx", ctypes.c_int64), ("M", ctypes.c_int), ("K", ctypes.c_int), ("A", ctypes.c_void_p), ("a_stride", ctypes.c_int64),
+                ("lda", ctypes.c_int64), ("B", ctypes.c_void_p), ("b_stride", ctypes.c_int64), ("ldb", ctypes.c_int64), ("N", ctypes.c_int), ("R", ctypes.c_int),
+                ("n_adapters", ctypes.c_int), ("ranks", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("adapters", ctypes.c_void_p), ("base", ctypes.c_void_p),
+                ("ld_base", ctypes.c_int64), ("Y", ctypes.c_void_p), ("ldy", ctypes.c_int64)]
 
 
 _lib = None
@@ -154,6 +190,17 @@ def lib() -> ctypes.CDLL:
         L.rudder_block_cached_workspace_bytes.argtypes = [ctypes.POINTER(_BlockArgs), ctypes.POINTER(_AttentionArgs), i32]
         L.rudder_block_cached.argtypes = [ctypes.POINTER(_BlockArgs), ctypes.POINTER(_BlockGlue), ctypes.POINTER(_QkArgs), ctypes.POINTER(_AttentionArgs),
                                           i32, ctypes.POINTER(_Segments), i32, vp, sz, vp]
+        pcache = ctypes.POINTER(_PagedCache)
+        L.rudder_page_fork.argtypes = [ctypes.POINTER(_PageForkArgs), pcache, i32, vp]
+        L.rudder_page_copy.argtypes = [ctypes.POINTER(_PageCopyArgs), pcache, i32, vp]
+        L.rudder_page_release.argtypes = [ctypes.POINTER(_PageReleaseArgs), vp]
+        L.rudder_page_compact.argtypes = [ctypes.POINTER(_PageCompactArgs), pcache, i32, vp]
+        L.rudder_attention_shared_workspace_bytes.restype = sz
+        L.rudder_attention_shared_workspace_bytes.argtypes = [ctypes.POINTER(_SharedAttentionArgs)]
+        L.rudder_attention_shared.argtypes = [ctypes.POINTER(_SharedAttentionArgs), vp, sz, vp]
+        L.rudder_lora_workspace_bytes.restype = sz
+        L.rudder_lora_workspace_bytes.argtypes = [ctypes.POINTER(_LoraArgs)]
+        L.rudder_lora.argtypes = [ctypes.POINTER(_LoraArgs), vp, sz, vp]
         _lib = L
     return _lib
 
@@ -600,6 +647,192 @@ def rudder_attention_paged(args: AttentionArgs, workspace: torch.Tensor | None =
     p = workspace.data_ptr()
     off = -p % 256
     _check(lib().rudder_attention_paged(args.ref, p + off, workspace.numel() - off, st), "rudder_attention_paged")
+
+
+# ---- many requests that continue one context ---------------------------------------------------------------------------------
+
+class PagedCaches:
+    """The caches of the layers that one page table serves: ``PagedCache`` objects of the same type, shape and strides."""
+
+    def __init__(self, caches):
+        self.keep = tuple(caches)
+        self.device = _on_one_device(*(t for c in self.keep for t in c.keep))
+        self.n = len(self.keep)
+        self.c = (_PagedCache * self.n)(*(c.c for c in self.keep))
+
+
+def _table(t, B=None):
+    """(rows, pitch, columns) of a page table."""
+    assert t.dtype == torch.int32 and t.dim() == 2 and t.stride(1) == 1 and (B is None or t.shape[0] == B)
+    return t.shape[0], t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1]), t.shape[1]
+
+
+def _layers(args, caches):
+    if caches is None:
+        return None, 0
+    if caches.device != args.device:
+        raise RudderError(ERR_ARG, f"caches on device {caches.device}, arguments on device {args.device}")
+    return caches.c, caches.n
+
+
+class PageForkArgs:
+    """Arguments of rudder_page_fork: int32 device tensors.  ``page_table`` [B, columns] and ``lens`` [B] are updated in place; child i is row
+    ``dst[i]``, a copy of row ``src[i]`` up to ``fork_lens[i]`` tokens (None: all); pages come from ``free_pages`` behind the first ``taken[0]``
+    (None: 0); ``used`` [1] and ``copies`` [n, 3] (or None) are outputs."""
+
+    def __init__(self, page_table, lens, page_size: int, src, dst, free_pages, used, fork_lens=None, taken=None, copies=None):
+        n = src.numel()
+        B, ld, cols = _table(page_table, lens.numel())
+        _int32(lens), _int32(src), _int32(dst, (n,)), _int32(free_pages), _int32(used, (1,))
+        if fork_lens is not None:
+            _int32(fork_lens, (n,))
+        if taken is not None:
+            _int32(taken, (1,))
+        if copies is not None:
+            _int32(copies, (n, 3))
+        self.keep = (page_table, lens, src, dst, free_pages, used, fork_lens, taken, copies)
+        self.device = _on_one_device(*self.keep)
+        p = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
+        self.c = _PageForkArgs(p(page_table), ld, cols, p(lens), B, int(page_size), p(src), p(dst), p(fork_lens), n, p(free_pages) if free_pages.numel() else None,
+                               free_pages.numel(), p(taken), p(copies), p(used))
+        self.ref = ctypes.byref(self.c)
+
+
+def rudder_page_fork(args: PageForkArgs, caches: PagedCaches | None = None, stream=None):
+    """Requests become copies of others: full pages shared, the rest of a page copied in every layer of ``caches``."""
+    c, n = _layers(args, caches)
+    _check(lib().rudder_page_fork(args.ref, c, n, _launch_stream(args.device, stream)), "rudder_page_fork")
+
+
+class PageCopyArgs:
+    """Arguments of rudder_page_copy: ``copies`` int32 [n, 3] (from, to, tokens), of which the first ``count[0]`` (None: all) are in use."""
+
+    def __init__(self, copies, count=None):
+        _int32(copies, (copies.shape[0], 3))
+        if count is not None:
+            _int32(count, (1,))
+        self.keep = (copies, count)
+        self.device = _on_one_device(*self.keep)
+        self.c = _PageCopyArgs(copies.data_ptr(), count.data_ptr() if count is not None else None, copies.shape[0])
+        self.ref = ctypes.byref(self.c)
+
+
+def rudder_page_copy(args: PageCopyArgs, caches: PagedCaches, stream=None):
+    """Tokens of pages to other pages, in every layer of ``caches``."""
+    c, n = _layers(args, caches)
+    _check(lib().rudder_page_copy(args.ref, c, n, _launch_stream(args.device, stream)), "rudder_page_copy")
+
+
+class PageReleaseArgs:
+    """Arguments of rudder_page_release: int32 device tensors.  ``lens`` [B] of the requests ``drop`` (or None) become 0; ``refs`` and ``free_pages``
+    [pages] and ``n_free`` [1] are outputs."""
+
+    def __init__(self, page_table, lens, page_size: int, refs, free_pages, n_free, drop=None):
+        B, ld, cols = _table(page_table, lens.numel())
+        _int32(lens), _int32(refs), _int32(free_pages, (refs.numel(),)), _int32(n_free, (1,))
+        if drop is not None:
+            _int32(drop)
+        self.keep = (page_table, lens, refs, free_pages, n_free, drop)
+        self.device = _on_one_device(*self.keep)
+        n_drop = drop.numel() if drop is not None else 0
+        self.c = _PageReleaseArgs(page_table.data_ptr(), ld, cols, lens.data_ptr(), B, int(page_size), drop.data_ptr() if n_drop else None, n_drop, refs.numel(),
+                                  refs.data_ptr(), free_pages.data_ptr(), n_free.data_ptr())
+        self.ref = ctypes.byref(self.c)
+
+
+def rudder_page_release(args: PageReleaseArgs, stream=None):
+    """Requests end; every page's references and the list of pages without any, from the tables."""
+    _check(lib().rudder_page_release(args.ref, _launch_stream(args.device, stream)), "rudder_page_release")
+
+
+class PageCompactArgs:
+    """Arguments of rudder_page_compact: int32 device tensors.  Outputs: ``new_table`` [B, columns] (may be ``page_table``), ``remap`` [pages], ``copies``
+    [pages // 2, 3], ``n_copies`` [1], ``n_live`` [1]."""
+
+    def __init__(self, page_table, lens, page_size: int, new_table, remap, copies, n_copies, n_live):
+        B, ld, cols = _table(page_table, lens.numel())
+        _, ld_new, cols_new = _table(new_table, B)
+        assert cols_new == cols
+        _int32(lens), _int32(remap), _int32(copies, (remap.numel() // 2, 3)), _int32(n_copies, (1,)), _int32(n_live, (1,))
+        self.keep = (page_table, lens, new_table, remap, copies, n_copies, n_live)
+        self.device = _on_one_device(*self.keep)
+        self.c = _PageCompactArgs(page_table.data_ptr(), ld, cols, lens.data_ptr(), B, int(page_size), remap.numel(), new_table.data_ptr(), ld_new, remap.data_ptr(),
+                                  copies.data_ptr() if copies.numel() else None, n_copies.data_ptr(), n_live.data_ptr())
+        self.ref = ctypes.byref(self.c)
+
+
+def rudder_page_compact(args: PageCompactArgs, caches: PagedCaches | None = None, stream=None):
+    """The pages that requests hold move to the lowest ids: plan, renamed table, and the copies in every layer of ``caches``."""
+    c, n = _layers(args, caches)
+    _check(lib().rudder_page_compact(args.ref, c, n, _launch_stream(args.device, stream)), "rudder_page_compact")
+
+
+class SharedAttentionArgs:
+    """Arguments of rudder_attention_shared: those of rudder_attention_paged and the groups.  Requests ``group_starts[g]`` .. ``group_starts[g + 1]`` - 1
+    share their first ``prefix_lens[g]`` tokens, read through row ``prefix_rows[g]`` of ``page_table`` (None: attn's own; one with more rows may be given,
+    of which attn's is the first part); ``group_q``: the most new tokens of a group."""
+
+    def __init__(self, attn: AttentionArgs, group_starts, prefix_lens, prefix_rows, group_q: int, page_table=None):
+        G = prefix_lens.numel()
+        _int32(group_starts, (G + 1,)), _int32(prefix_lens), _int32(prefix_rows, (G,))
+        rows = attn.c.B
+        if page_table is not None:
+            assert page_table.dtype == torch.int32 and page_table.data_ptr() == attn.c.page_table and page_table.shape[0] >= rows
+            assert page_table.shape[1] == attn.c.max_pages and page_table.stride(1) == 1 and (page_table.shape[0] == 1 or page_table.stride(0) == attn.c.ld_table)
+            rows = page_table.shape[0]
+        self.attn = attn
+        self.keep = (group_starts, prefix_lens, prefix_rows, page_table)
+        self.device = _on_one_device(*self.keep, *attn.keep)
+        self.c = _SharedAttentionArgs(attn.c, group_starts.data_ptr(), prefix_lens.data_ptr(), prefix_rows.data_ptr(), G, rows, int(group_q))
+        self.ref = ctypes.byref(self.c)
+
+
+def rudder_attention_shared_workspace_bytes(args: SharedAttentionArgs) -> int:
+    return int(lib().rudder_attention_shared_workspace_bytes(args.ref))
+
+
+def rudder_attention_shared(args: SharedAttentionArgs, workspace: torch.Tensor | None = None, stream=None):
+    """rudder_attention_paged for groups of requests with common prefixes, each read once, written into ``O`` (and ``lse``) of ``args.attn``."""
+    st = _launch_stream(args.device, stream)
+    if workspace is None:
+        workspace = _workspace(rudder_attention_shared_workspace_bytes(args), args.keep[0].device, stream)
+    p = workspace.data_ptr()
+    off = -p % 256
+    _check(lib().rudder_attention_shared(args.ref, p + off, workspace.numel() - off, st), "rudder_attention_shared")
+
+
+class LoraArgs:
+    """Arguments of rudder_lora.  bf16: ``X`` [M, K], ``A`` [adapters, R, K], ``B`` [adapters, N, R], ``base`` [M, N] or None, ``Y`` [M, N] (may be
+    ``base``); ``ranks`` int32 and ``scales`` fp32 [adapters]; ``adapters`` int32 [M], -1 for a row without one."""
+
+    def __init__(self, X, A, B, ranks, scales, adapters, base, Y):
+        (M, K), (n, R, _), N = X.shape, A.shape, B.shape[1]
+        assert all(t.dtype == torch.bfloat16 for t in (X, A, B, Y)) and A.shape[2] == K and tuple(B.shape) == (n, N, R) and tuple(Y.shape) == (M, N)
+        assert A.stride(2) == 1 and B.stride(2) == 1
+        _int32(ranks, (n,)), _int32(adapters, (M,))
+        assert scales.dtype == torch.float32 and scales.is_contiguous() and scales.numel() == n
+        assert base is None or (base.dtype == torch.bfloat16 and base.shape == Y.shape)
+        self.keep = (X, A, B, ranks, scales, adapters, base, Y)
+        self.device = _on_one_device(*self.keep)
+        one = lambda t: t.stride(0) if n > 1 else 0  # noqa: E731
+        self.c = _LoraArgs(X.data_ptr(), _rows(X), M, K, A.data_ptr(), one(A), A.stride(1), B.data_ptr(), one(B), B.stride(1), N, R, n, ranks.data_ptr(),
+                           scales.data_ptr(), adapters.data_ptr(), base.data_ptr() if base is not None else None, _rows(base) if base is not None else 0,
+                           Y.data_ptr(), _rows(Y))
+        self.ref = ctypes.byref(self.c)
+
+
+def rudder_lora_workspace_bytes(args: LoraArgs) -> int:
+    return int(lib().rudder_lora_workspace_bytes(args.ref))
+
+
+def rudder_lora(args: LoraArgs, workspace: torch.Tensor | None = None, stream=None):
+    """Each row's low-rank adapter added to ``base``, written into ``Y`` of ``args``."""
+    st = _launch_stream(args.device, stream)
+    if workspace is None:
+        workspace = _workspace(rudder_lora_workspace_bytes(args), args.keep[0].device, stream)
+    p = workspace.data_ptr()
+    off = -p % 256
+    _check(lib().rudder_lora(args.ref, p + off, workspace.numel() - off, st), "rudder_lora")
 
 
 def rudder_linear_a16(w: Weight, X: torch.Tensor, bias=None, Y=None, stream=None) -> torch.Tensor:

@@ -134,9 +134,9 @@ rudder_status check_attention(const rudder_attention_args* a, AttnArgs* out)
 }
 
 // Where the kernel that the call runs takes the cache by TMA: the tensor maps (without them it copies row by row).
-void add_maps(const rudder_paged_cache* c, AttnArgs* a)
+void add_maps(const rudder_paged_cache* c, int max_rows, AttnArgs* a)
 {
-    if (attention_uses_maps(a->max_q * (a->heads / a->kv_heads), a->head_dim, a->e4m3, c->page_size, static_cast<long long>(a->max_pages) * c->page_size)) a->tma = make_tmap_cache(&a->tm_k, c->k, c) && make_tmap_cache(&a->tm_v, c->v, c);
+    if (attention_uses_maps(max_rows, a->head_dim, a->e4m3, c->page_size, static_cast<long long>(a->max_pages) * c->page_size)) a->tma = make_tmap_cache(&a->tm_k, c->k, c) && make_tmap_cache(&a->tm_v, c->v, c);
 }
 
 }  // namespace
@@ -182,7 +182,7 @@ rudder_status rudder_attention_paged(const rudder_attention_args* args, void* wo
     if (!workspace || !aligned(workspace, 256) || workspace_bytes < rudder_attention_workspace_bytes(args)) return RUDDER_ERR_WORKSPACE;
     s = ensure_paged_init();
     if (s != RUDDER_OK) return s;
-    add_maps(args->cache, &a);
+    add_maps(args->cache, a.max_q * (a.heads / a.kv_heads), &a);
     return launch_attention_paged(a, workspace, sm_count(), static_cast<cudaStream_t>(stream)) == cudaSuccess ? RUDDER_OK : RUDDER_ERR_CUDA;
 }
 
@@ -254,7 +254,7 @@ rudder_status rudder_block_cached(const rudder_block_args* args, const rudder_bl
     AttnArgs tp;
     if ((s = check_qk(&qa, &qp)) != RUDDER_OK || (s = check_attention(&ta, &tp)) != RUDDER_OK) return s;
     if ((s = ensure_init()) != RUDDER_OK || (s = ensure_paged_init()) != RUDDER_OK) return s;
-    add_maps(ta.cache, &tp);
+    add_maps(ta.cache, tp.max_q * (tp.heads / tp.kv_heads), &tp);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     const int sms = sm_count();
     auto lin = [&](int l, const uint16_t* x, int64_t ldx, bool gelu_first) {

@@ -4,6 +4,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "internal.cuh"
 #include "paged.cuh"
 
@@ -12,6 +14,18 @@ namespace rudder {
 namespace {
 
 constexpr float kLn2 = 0.6931471805599453f;
+
+// Requests in groups that share a prefix: the prefixes are a pass in which a GROUP stands in a request's place (its rows are those of all its requests, its
+// keys the prefix) and whose rows end as parts in `base`; what stands behind the prefixes is a second pass that joins these parts to its own.
+struct SharedPass {
+    const int32_t* group_starts; const int32_t* prefix_lens; const int32_t* prefix_rows;
+    int n_groups, table_rows, requests;
+    int key_mask;                       // a prefix is cut down to a multiple of 64 where the second pass takes its tiles by TMA
+    int prefixes;                       // this pass is the first
+    int causal;                         // of the call (the first pass has no causal limits of its own)
+    float* base_o;                      // [M x heads][D], relative to ...
+    float2* base_ml;                    // [M x heads]: reference and sum
+};
 
 struct AttnParams {
     const uint16_t* Q; int64_t ldq;
@@ -31,6 +45,11 @@ struct AttnParams {
     int G;                              // CTAs
     int tma;                            // many rows: tensor maps over the cache are there
 };
+struct SharedParams : AttnParams {
+    SharedPass sh;
+};
+template <bool SHARED>
+using ParamsOf = std::conditional_t<SHARED, SharedParams, AttnParams>;
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool valid) {
     const int n = valid ? 16 : 0;
@@ -94,7 +113,7 @@ __device__ __forceinline__ bool drop_nonfinite(uint32_t addr) {
     if (any) asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
     return any != 0;
 }
-// What was dropped of keys [k0, k1) of request b, channels d .. d + 3, summed.  (A handful of new tokens at most, and only when there was something.)
+// What was dropped of keys [k0, k1) of row b of the page table, channels d .. d + 3, summed.  (A handful of new tokens at most, and only when there was something.)
 template <bool E4M3>
 __device__ __forceinline__ float4 nonfinite_values(const AttnParams& p, int b, int h, int k0, int k1, int d) {
     float z[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -134,23 +153,83 @@ __device__ __forceinline__ Req load_request(const AttnParams& p, int b) {
     return r;
 }
 
+// With shared prefixes: its keys begin at key0 (behind the prefix that is joined to it, or 0), and its pages stand in row `trow` of the table.
+struct SharedReq : Req { int key0, trow; };
+// The group of a request: requests [begin, end) and the part of the prefix that is read for all of them; begin .. begin + 1 and 0 for a request of no group.
+struct Group { int begin, end, prefix; };
+
+__device__ __forceinline__ int prefix_of(const SharedParams& p, int g) {
+    const long long cap = static_cast<long long>(p.max_pages) << p.cache.page_shift;
+    const int len = p.sh.prefix_lens[g], row = p.sh.prefix_rows[g];
+    const int n = static_cast<int>(len < 0 ? 0 : (len > cap ? cap : len));
+    if (n != len || row < 0 || row >= p.sh.table_rows) record_bad_data(kBadLength);
+    return row < 0 || row >= p.sh.table_rows ? 0 : n & p.sh.key_mask;
+}
+__device__ __forceinline__ Group find_group(const SharedParams& p, int b) {
+    int lo = -1, hi = p.sh.n_groups;                       // last group that starts at or before b
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (p.sh.group_starts[mid] <= b) lo = mid; else hi = mid;
+    }
+    if (lo < 0) return Group{b, b + 1, 0};
+    const int end = p.sh.group_starts[lo + 1];
+    if (b >= end) return Group{b, b + 1, 0};
+    return Group{p.sh.group_starts[lo], end, prefix_of(p, lo)};
+}
+// Group g in a request's place.
+__device__ __forceinline__ SharedReq load_group(const SharedParams& p, int g) {
+    SharedReq r;
+    r.len = prefix_of(p, g);
+    r.key0 = 0;
+    r.trow = p.sh.prefix_rows[g];                          // (a bad one has no keys)
+    const int s0 = p.sh.group_starts[g], s1 = p.sh.group_starts[g + 1];
+    const int b0 = min(max(s0, 0), p.sh.requests), b1 = min(max(s1, b0), p.sh.requests);
+    if (b0 != s0 || b1 != s1) record_bad_data(kBadLength);
+    r.row0 = min(max(p.q_starts != nullptr ? p.q_starts[b0] : b0 * p.max_q, 0), p.M);
+    const int end = min(max(p.q_starts != nullptr ? p.q_starts[b1] : b1 * p.max_q, r.row0), p.M);
+    r.qlen = r.len > 0 ? end - r.row0 : 0;                 // without a prefix there is nothing to join
+    return r;
+}
+// Request b of a group with this prefix: it reads what stands behind the prefix if each of its rows sees all of that.
+__device__ __forceinline__ SharedReq load_member(const SharedParams& p, int b, int prefix) {
+    SharedReq r;
+    static_cast<Req&>(r) = load_request(p, b);
+    r.trow = b;
+    r.key0 = r.len - (p.sh.causal ? r.qlen - 1 : 0) >= prefix ? prefix : 0;
+    r.len -= r.key0;
+    return r;
+}
+
 // A place in the sequence of units: request, kv head, row tile, unit inside the item, and what is left of the run from there on.
 // What starting and ending an item costs, in units (queries, merge of the warp groups, output): an item counts as its units + kItemCost,
 // the cost in front.  A cut inside the cost leaves the item whole to the run behind.
 constexpr int kItemCost = 2;                               // 48 requests of up to 16384 keys 56 us, without a cost 172 us, with 6 59 us
 
-template <int ROWS, int UK>
+template <int ROWS, int UK, bool SHARED = false>
 struct Cursor {
     int b, h, rt, j, nt, n_rt;
     long long left;
-    Req rq;
-    __device__ __forceinline__ void set_request(const AttnParams& p, int bb) {
+    std::conditional_t<SHARED, SharedReq, Req> rq;
+    Group grp;                                             // SHARED, second pass: of request b
+    __device__ __forceinline__ void set_request(const ParamsOf<SHARED>& p, int bb) {
         b = bb;
-        rq = load_request(p, bb);
+        if constexpr (SHARED) {
+            if (p.sh.prefixes) {
+                rq = load_group(p, bb);
+            } else {
+                if (bb < grp.begin || bb >= grp.end) grp = find_group(p, bb);
+                rq = load_member(p, bb, grp.prefix);
+            }
+        } else {
+            rq = load_request(p, bb);
+        }
         nt = max(1, (rq.len + UK - 1) / UK);
         n_rt = (rq.qlen * p.group + ROWS - 1) / ROWS;
     }
-    __device__ __forceinline__ void next_item(const AttnParams& p) {
+    // the item's row of the page table, and what its first key is in the request's count
+    __device__ __forceinline__ int table_row() const { if constexpr (SHARED) return rq.trow; else return b; }
+    __device__ __forceinline__ int first_key() const { if constexpr (SHARED) return rq.key0; else return 0; }
+    __device__ __forceinline__ void next_item(const ParamsOf<SHARED>& p) {
         j = 0;
         if (++rt < n_rt) return;
         rt = 0;
@@ -163,13 +242,34 @@ struct Cursor {
             ++bb;
         }
     }
-    __device__ __forceinline__ void advance(const AttnParams& p) {
+    __device__ __forceinline__ void advance(const ParamsOf<SHARED>& p) {
         ++j;
         if (--left <= 0 || j < nt) return;
         left -= kItemCost;
         if (left > 0) next_item(p);
     }
 };
+
+// Row `r` of an item whose rows begin at row0: its place in base_o and base_ml.
+__device__ __forceinline__ bool shared_prefixes(const AttnParams&) { return false; }
+__device__ __forceinline__ bool shared_prefixes(const SharedParams& p) { return p.sh.prefixes != 0; }
+__device__ __forceinline__ size_t prefix_row(const AttnParams& p, int row0, int h, int r) {
+    const RowOf at = row_of(p, r);
+    return static_cast<size_t>(row0 + at.token) * p.heads + h * p.group + at.head;
+}
+__device__ __forceinline__ void store_prefix_ml(const AttnParams&, int, int, int, float, float) {}
+__device__ __forceinline__ void store_prefix_ml(const SharedParams& p, int row0, int h, int r, float m, float l) { p.sh.base_ml[prefix_row(p, row0, h, r)] = make_float2(m, l); }
+// A row's own (reference, sum) and those of its prefix: both together, and the factors of the two weighted sums of values.
+struct JoinWeights { float m, l, own, prefix; };
+__device__ __forceinline__ JoinWeights join_weights(float2 own, float2 pre) {
+    JoinWeights j;
+    j.m = fmaxf(own.x, pre.x);
+    const float u = j.m == -INFINITY ? 0.0f : j.m;
+    j.own = exp2_approx(own.x - u);
+    j.prefix = exp2_approx(pre.x - u);
+    j.l = own.y * j.own + pre.y * j.prefix;
+    return j;
+}
 
 // Quotient of non-negative numbers, in 32 bits where they fit (they nearly always do; a 64-bit division is a hundred instructions of latency).
 __device__ __forceinline__ long long quotient(long long a, long long b) {
@@ -179,9 +279,11 @@ __device__ __forceinline__ long long quotient(long long a, long long b) {
 
 // This CTA's run of units: sums over the requests (threads over consecutive requests), the place of its first unit, and the descriptor that
 // the join reads.  All threads call it; false = nothing to do.
-template <int ROWS, int UK, int THREADS>
-__device__ __forceinline__ bool start_of_run(const AttnParams& p, Cursor<ROWS, UK>& cur)
+template <int ROWS, int UK, int THREADS, bool SHARED>
+__device__ __forceinline__ bool start_of_run(const ParamsOf<SHARED>& p, Cursor<ROWS, UK, SHARED>& cur)
 {
+    using R = decltype(cur.rq);
+    if constexpr (SHARED) cur.grp = Group{0, 0, 0};
     __shared__ long long s_units[THREADS / 32];
     __shared__ int s_items[THREADS / 32];
     __shared__ int s_max[THREADS / 32];
@@ -192,8 +294,29 @@ __device__ __forceinline__ bool start_of_run(const AttnParams& p, Cursor<ROWS, U
     int place;
     if (p.B <= 32) {
         // a request per lane, every warp for itself: no barrier, nothing loaded twice (one request of 333 keys: 3200 -> 1900 clocks)
-        Req r = {0, 0, 0};
-        if (lane < p.B) r = load_request(p, lane);
+        R r = {};
+        Group grp = {0, 0, 0};
+        if constexpr (SHARED) {
+            if (p.sh.prefixes) {
+                if (lane < p.B) r = load_group(p, lane);
+            } else {
+                if (p.sh.n_groups <= 32) {
+                    // a group per lane: no search, its loads beside those of the requests
+                    const bool is = lane < p.sh.n_groups;
+                    const int s0 = is ? p.sh.group_starts[lane] : 0x7fffffff, s1 = is ? p.sh.group_starts[lane + 1] : 0, pre = is ? prefix_of(p, lane) : 0;
+                    int at = -1;
+                    for (int i = 0; i < p.sh.n_groups; ++i) at = __shfl_sync(0xffffffffu, s0, i) <= lane ? i : at;
+                    const int from = max(at, 0);
+                    grp = Group{__shfl_sync(0xffffffffu, s0, from), __shfl_sync(0xffffffffu, s1, from), __shfl_sync(0xffffffffu, pre, from)};
+                    if (at < 0 || lane >= grp.end) grp = Group{lane, lane + 1, 0};
+                } else if (lane < p.B) {
+                    grp = find_group(p, lane);
+                }
+                if (lane < p.B) r = load_member(p, lane, grp.prefix);
+            }
+        } else {
+            if (lane < p.B) r = load_request(p, lane);
+        }
         const int n_rt = (r.qlen * p.group + ROWS - 1) / ROWS, nt = max(1, (r.len + UK - 1) / UK);
         const long long t_units = static_cast<long long>(n_rt) * p.kv_heads * (nt + kItemCost);
         const int t_items = n_rt * p.kv_heads;
@@ -222,6 +345,11 @@ __device__ __forceinline__ bool start_of_run(const AttnParams& p, Cursor<ROWS, U
         cur.rq.len = __shfl_sync(0xffffffffu, r.len, b);
         cur.rq.row0 = __shfl_sync(0xffffffffu, r.row0, b);
         cur.rq.qlen = __shfl_sync(0xffffffffu, r.qlen, b);
+        if constexpr (SHARED) {
+            cur.rq.key0 = __shfl_sync(0xffffffffu, r.key0, b);
+            cur.rq.trow = __shfl_sync(0xffffffffu, r.trow, b);
+            cur.grp = Group{__shfl_sync(0xffffffffu, grp.begin, b), __shfl_sync(0xffffffffu, grp.end, b), __shfl_sync(0xffffffffu, grp.prefix, b)};
+        }
         cur.nt = __shfl_sync(0xffffffffu, nt, b);
         cur.n_rt = __shfl_sync(0xffffffffu, n_rt, b);
         const long long off = u_begin - __shfl_sync(0xffffffffu, before, b);
@@ -235,8 +363,12 @@ __device__ __forceinline__ bool start_of_run(const AttnParams& p, Cursor<ROWS, U
     const int rb0 = min(p.B, tid * per), rb1 = min(p.B, rb0 + per);
     long long t_units = 0;
     int t_items = 0, t_max = 0;
+    auto request = [&](int b) {
+        if constexpr (SHARED) { cur.set_request(p, b); return cur.rq; }        // (the cursor remembers the group)
+        else return load_request(p, b);
+    };
     for (int b = rb0; b < rb1; ++b) {
-        const Req r = load_request(p, b);
+        const R r = request(b);
         const int n_rt = (r.qlen * p.group + ROWS - 1) / ROWS, nt = max(1, (r.len + UK - 1) / UK);
         t_units += static_cast<long long>(n_rt) * p.kv_heads * (nt + kItemCost);
         t_items += n_rt * p.kv_heads;
@@ -276,7 +408,7 @@ __device__ __forceinline__ bool start_of_run(const AttnParams& p, Cursor<ROWS, U
         if (u_begin >= mine0 && u_begin < mine1) {         // exactly one thread
             long long at = mine0;
             for (int b = rb0; b < rb1; ++b) {
-                const Req r = load_request(p, b);
+                const R r = request(b);
                 const int n_rt = (r.qlen * p.group + ROWS - 1) / ROWS, nt = whole ? 1 : max(1, (r.len + UK - 1) / UK) + kItemCost;
                 const long long here = static_cast<long long>(n_rt) * p.kv_heads * nt;
                 if (u_begin < at + here) {
@@ -313,6 +445,7 @@ __device__ __forceinline__ bool start_of_run(const AttnParams& p, Cursor<ROWS, U
         d[5] = static_cast<int>(quotient(unit0 + cur.nt - 1, share));            // last owner
         d[6] = unit0 <= before + kItemCost ? 0 : 1;        // slot of the first owner's part: its run starts with this item (or inside its cost)
         d[0] = first_cut ? 1 : 0;
+        if constexpr (SHARED) d[7] = cur.rq.key0 > 0;       // the join adds the prefix's part
     }
     return true;
 }

@@ -96,9 +96,9 @@ struct AttnCfg {
     static_assert(SMEM <= 226 * 1024, "shared memory of an SM");
 };
 
-// CAUSAL: the rows of an item may see different numbers of keys.
-template <class C, bool CAUSAL>
-__global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const AttnParams p)
+// CAUSAL: the rows of an item may see different numbers of keys.  SHARED: see SharedPass.
+template <class C, bool CAUSAL, bool SHARED>
+__global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const ParamsOf<SHARED> p)
 {
     constexpr int D = C::D, NB = C::NB, RW = C::RW, KW = C::KW, KT = C::KT, NST = C::NST, LO = C::LO, RB = C::RB, UK = C::UK, ROWS = C::ROWS, DC = C::DC;
     constexpr bool E4M3 = C::E4M3;
@@ -112,6 +112,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
     static_assert(GT % CH == 0 || CH % GT == 0, "rows are copied by whole groups of lanes");
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ uint32_t s_dropped[RW * KW];                // per warp: see drop_nonfinite
+    __shared__ float s_prefix[SHARED ? ROWS : 1];          // weight of the prefix's part
     pdl_launch_dependents();
     pdl_wait();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -119,22 +120,23 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
     const int kg = warp / RW, rw = warp % RW;
     const int gt = tid - kg * GT;                          // thread inside the warp group
 
-    Cursor<ROWS, UK> cur;
-    if (!start_of_run<ROWS, UK, C::THREADS>(p, cur)) return;
+    using Cur = Cursor<ROWS, UK, SHARED>;
+    Cur cur;
+    if (!start_of_run<ROWS, UK, C::THREADS, SHARED>(p, cur)) return;
 
     // ---- the ring of this warp group
     const uint32_t ring = smem_u32(smem) + kg * (NST * C::STAGE);
-    Cursor<ROWS, UK> ld = cur;
+    Cur ld = cur;
     // page ids of the tile `at` is about to load: lane i holds the one of key i (KT <= 32)
-    auto page_of_lane = [&](const Cursor<ROWS, UK>& at) -> int {
+    auto page_of_lane = [&](const Cur& at) -> int {
         const int key = at.j * UK + kg * KT + lane;
-        return (lane < KT && key < at.rq.len) ? p.table[static_cast<size_t>(at.b) * p.ld_table + (key >> p.cache.page_shift)] : -2;
+        return (lane < KT && key < at.rq.len) ? p.table[static_cast<size_t>(at.table_row()) * p.ld_table + ((key + at.first_key()) >> p.cache.page_shift)] : -2;
     };
-    auto issue = [&](const Cursor<ROWS, UK>& at, int page, int stage) {
+    auto issue = [&](const Cur& at, int page, int stage) {
         const int key0 = at.j * UK + kg * KT;
         if (key0 < at.rq.len) {
             if (page != -2 && (page < 0 || page >= p.cache.n_pages)) { record_bad_data(kBadPage); page = -2; }
-            const int key = key0 + lane;
+            const int key = key0 + at.first_key() + lane;
             // a key without a page gets an offset that no valid one has
             const long long off = page < 0 ? -1 : page * p.cache.page_stride + static_cast<long long>(at.h) * p.cache.head_stride +
                                                   static_cast<long long>(key & ((1 << p.cache.page_shift) - 1)) * p.cache.token_stride;
@@ -152,7 +154,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
     };
     int pages[NST - 1];                                    // of the first tiles: one wait for all of them
     {
-        Cursor<ROWS, UK> ahead = cur;
+        Cur ahead = cur;
 #pragma unroll
         for (int s = 0; s < NST - 1; ++s) {
             pages[s] = ahead.left > 0 ? page_of_lane(ahead) : -2;
@@ -402,6 +404,8 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
             float* box = reinterpret_cast<float*>(smem + C::RING);
             float2* ml = reinterpret_cast<float2*>(smem + C::RING + C::BOX);
             const bool entire = item_end && part_j == 0;
+            const bool prefix_pass = SHARED && shared_prefixes(p), joins = SHARED && entire && !prefix_pass && cur.first_key() > 0;
+            const bool final = entire && !prefix_pass;                           // O and lse, not a part of them
             const int slot = 2 * blockIdx.x + (first_part ? 0 : 1);              // part at the start of the run, or at its end
             const int R = cur.rq.qlen * p.group;
             const float vs = E4M3 ? (p.cache.v_scale != nullptr ? p.cache.v_scale[cur.h] : 1.0f) : 1.0f;
@@ -436,11 +440,24 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
                         const float2 o = ml[w * ROWS + rl];
                         l += o.y * exp2_approx(o.x - u);
                     }
-                    wgt[n][e] = exp2_approx(mx[n][e] - u) * vs * (entire ? (l == 0.0f ? 0.0f : 1.0f / l) : 1.0f);
+                    float w = exp2_approx(mx[n][e] - u) * vs;
+                    if constexpr (SHARED) {
+                        const int r = cur.rt * ROWS + (LO == 1 ? rl & 3 : rl);       // (the low parts of a row are weighted as the row)
+                        if (joins) {
+                            float2 pre = make_float2(-INFINITY, 0.0f);
+                            if (r < R) pre = __ldcg(p.sh.base_ml + prefix_row(p, cur.rq.row0, cur.h, r));
+                            const JoinWeights j = join_weights(make_float2(m, l), pre);
+                            m = j.m; l = j.l;
+                            w *= j.own;
+                            if (kg == 0 && g == 0) s_prefix[rl] = l == 0.0f ? 0.0f : j.prefix / l;
+                        }
+                    }
+                    wgt[n][e] = w * (final ? (l == 0.0f ? 0.0f : 1.0f / l) : 1.0f);
                     if (kg == 0 && g == 0) {
                         const int r = cur.rt * ROWS + rl;
                         if (r < R) {
                             if (!entire) p.part_ml[static_cast<size_t>(slot) * ROWS + rl] = make_float2(m, l);
+                            else if (prefix_pass) store_prefix_ml(p, cur.rq.row0, cur.h, r, m, l);
                             else if (p.lse != nullptr) {
                                 const RowOf at = row_of(p, r);
                                 p.lse[static_cast<size_t>(cur.rq.row0 + at.token) * p.heads + cur.h * p.group + at.head] = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
@@ -482,6 +499,17 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
                         }
                     }
                     const RowOf at = row_of(p, cur.rt * ROWS + rl);
+                    if constexpr (SHARED) {
+                        float* pre = p.sh.base_o + prefix_row(p, cur.rq.row0, cur.h, cur.rt * ROWS + rl) * D + round * DC + d;
+                        if (joins) {
+                            const float4 x = __ldcg(reinterpret_cast<const float4*>(pre));
+                            const float w = s_prefix[rl];
+                            o.x = fmaf(x.x, w, o.x); o.y = fmaf(x.y, w, o.y); o.z = fmaf(x.z, w, o.z); o.w = fmaf(x.w, w, o.w);
+                        } else if (entire && prefix_pass) {
+                            *reinterpret_cast<float4*>(pre) = o;
+                            continue;
+                        }
+                    }
                     if (entire)
                         *reinterpret_cast<uint2*>(p.O + static_cast<size_t>(cur.rq.row0 + at.token) * p.ldo + static_cast<size_t>(cur.h * p.group + at.head) * D +
                                                   round * DC + d) = make_uint2(bf16x2(o.x, o.y), bf16x2(o.z, o.w));
@@ -495,7 +523,8 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
                     for (int i = tid; i < rows_here * (DC / 4); i += C::THREADS) {
                         const int rl = i / (DC / 4), d = round * DC + 4 * (i % (DC / 4));
                         const RowOf at = row_of(p, cur.rt * ROWS + rl);
-                        const float4 z = nonfinite_values<E4M3>(p, cur.b, cur.h, max(tail, part_j * UK), min(cur.rq.len - cur.rq.qlen + at.token + 1, (cur.j + 1) * UK), d);
+                        const float4 z = nonfinite_values<E4M3>(p, cur.table_row(), cur.h, cur.first_key() + max(tail, part_j * UK),
+                                                                    cur.first_key() + min(cur.rq.len - cur.rq.qlen + at.token + 1, (cur.j + 1) * UK), d);
                         if (entire) {
                             uint2* o = reinterpret_cast<uint2*>(p.O + static_cast<size_t>(cur.rq.row0 + at.token) * p.ldo + static_cast<size_t>(cur.h * p.group + at.head) * D + d);
                             const uint2 v = *o;
@@ -521,15 +550,15 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const At
 constexpr int JOIN_THREADS = 256, JOIN_ROWS = 2, JOIN_SPLIT = JOIN_THREADS / 32 / JOIN_ROWS;
 
 // The item that run c starts inside; false if its join is another CTA's or there is none.
-struct Cut { int h, rt, row0, qlen, first, n, slot_first; };
+struct Cut { int h, rt, row0, qlen, first, n, slot_first, joins; };
 __device__ __forceinline__ bool load_cut(const AttnParams& p, int c, Cut& x) {
     const int4 a = __ldcg(reinterpret_cast<const int4*>(p.desc + 8 * c)), b = __ldcg(reinterpret_cast<const int4*>(p.desc + 8 * c + 4));
-    x.h = a.y; x.rt = a.z; x.row0 = a.w; x.qlen = b.x; x.first = c - 1; x.n = b.y - (c - 1) + 1; x.slot_first = b.z;
+    x.h = a.y; x.rt = a.z; x.row0 = a.w; x.qlen = b.x; x.first = c - 1; x.n = b.y - (c - 1) + 1; x.slot_first = b.z; x.joins = b.w;
     return a.x != 0;
 }
 
-template <int D>
-__global__ void __launch_bounds__(JOIN_THREADS) attention_join_kernel(const AttnParams p, int rows_of_tile)
+template <int D, bool SHARED>
+__global__ void __launch_bounds__(JOIN_THREADS) attention_join_kernel(const ParamsOf<SHARED> p, int rows_of_tile)
 {
     __shared__ float s_o[JOIN_ROWS][JOIN_SPLIT][D];
     __shared__ float2 s_ml[JOIN_ROWS][JOIN_SPLIT];
@@ -582,6 +611,31 @@ __global__ void __launch_bounds__(JOIN_THREADS) attention_join_kernel(const Attn
         w[s] = exp2_approx(s_ml[ry][s].x - u);
         ll += s_ml[ry][s].y * w[s];
     }
+    const float* pre = nullptr;                            // the prefix's part
+    float wp = 0.0f;
+    if constexpr (SHARED) {
+        const size_t row = prefix_row(p, x.row0, x.h, r);
+        if (shared_prefixes(p)) {
+            // (cut items of the first pass end as parts of their rows)
+            float* out = p.sh.base_o + row * D + lane * V;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+                float a = 0.0f;
+#pragma unroll
+                for (int s = 0; s < JOIN_SPLIT; ++s) a += s_o[ry][s][lane * V + i] * w[s];
+                out[i] = a;
+            }
+            if (lane == 0) p.sh.base_ml[row] = make_float2(mm, ll);
+            return;
+        }
+        if (x.joins) {
+            const JoinWeights j = join_weights(make_float2(mm, ll), __ldcg(p.sh.base_ml + row));
+            mm = j.m; ll = j.l; wp = j.prefix;
+#pragma unroll
+            for (int s = 0; s < JOIN_SPLIT; ++s) w[s] *= j.own;
+            pre = p.sh.base_o + row * D + lane * V;
+        }
+    }
     const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
     const RowOf at = row_of(p, r);
     const int hh = x.h * p.group + at.head;
@@ -594,14 +648,18 @@ __global__ void __launch_bounds__(JOIN_THREADS) attention_join_kernel(const Attn
             a += s_o[ry][s][lane * V + i] * w[s];
             b += s_o[ry][s][lane * V + i + 1] * w[s];
         }
+        if (SHARED && pre != nullptr) {
+            a = fmaf(__ldcg(pre + i), wp, a);
+            b = fmaf(__ldcg(pre + i + 1), wp, b);
+        }
         *reinterpret_cast<uint32_t*>(orow + i) = bf16x2(a * inv, b * inv);
     }
     if (lane == 0 && p.lse != nullptr) p.lse[static_cast<size_t>(x.row0 + at.token) * p.heads + hh] = ll == 0.0f ? -INFINITY : (mm + log2f(ll)) * kLn2;
 }
 
 // The same for many rows: a lane per row, as the parts lie; a warp has 32 rows x 8 channels, a CTA 64 channels, y = row block x channel block.
-template <int D>
-__global__ void __launch_bounds__(JOIN_THREADS) attention_join_rows_kernel(const AttnParams p, int rows_of_tile)
+template <int D, bool SHARED>
+__global__ void __launch_bounds__(JOIN_THREADS) attention_join_rows_kernel(const ParamsOf<SHARED> p, int rows_of_tile)
 {
     pdl_launch_dependents();
     pdl_wait();
@@ -627,6 +685,24 @@ __global__ void __launch_bounds__(JOIN_THREADS) attention_join_rows_kernel(const
         l = l * a + ml.y * b;
         o[0] = o[0] * a + v0.x * b; o[1] = o[1] * a + v0.y * b; o[2] = o[2] * a + v0.z * b; o[3] = o[3] * a + v0.w * b;
         o[4] = o[4] * a + v1.x * b; o[5] = o[5] * a + v1.y * b; o[6] = o[6] * a + v1.z * b; o[7] = o[7] * a + v1.w * b;
+    }
+    if constexpr (SHARED) {
+        const size_t row = prefix_row(p, x.row0, x.h, r);
+        float* pre = p.sh.base_o + row * D + ch;
+        if (shared_prefixes(p)) {
+            *reinterpret_cast<float4*>(pre) = make_float4(o[0], o[1], o[2], o[3]);
+            *reinterpret_cast<float4*>(pre + 4) = make_float4(o[4], o[5], o[6], o[7]);
+            if (ch == 0) p.sh.base_ml[row] = make_float2(m, l);
+            return;
+        }
+        if (x.joins) {
+            const JoinWeights j = join_weights(make_float2(m, l), __ldcg(p.sh.base_ml + row));
+            const float4 v0 = __ldcg(reinterpret_cast<const float4*>(pre)), v1 = __ldcg(reinterpret_cast<const float4*>(pre + 4));
+            const float v[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
+            m = j.m; l = j.l;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) o[i] = fmaf(v[i], j.prefix, o[i] * j.own);
+        }
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     const RowOf at = row_of(p, r);
@@ -663,30 +739,34 @@ int rows_class(int max_rows) { return max_rows <= 4 ? 0 : (max_rows <= 8 ? 1 : (
 //   E4M3, D = 128: 20 x 1000 12.1 / 15.9, 32 x 8000 25 / 36, 32 x 60k 96 / 144, 32 x 126k 189 / 282, 64 x 126k 353 / 295; D = 64: 20 x 8000 18.3 / 25.5, 32 x 126k 143 / 227,
 //   64 x 126k 269 / 227; D = 256: 32 x 1500 19.1 / 21.4, 32 x 60k 219 / 244.
 bool many_rows(int max_rows, int head_dim, bool e4m3, long long max_kv) { return max_rows > 32 || (max_rows > 16 && head_dim == 128 && !e4m3 && max_kv >= 4096); }
+bool shared_prefixes_host(const AttnParams&) { return false; }
+bool shared_prefixes_host(const SharedParams& p) { return p.sh.prefixes != 0; }
 // Rows of a part in the workspace (whichever kernel runs: the size depends on the shapes alone)
 int tile_rows(int max_rows) { return max_rows <= 8 ? 8 : (max_rows <= 16 ? 16 : 128); }
 
-template <int D, bool E4M3>
-cudaError_t launch_main(const AttnParams& p, const AttnArgs& a, cudaStream_t st, RowsCfg<D, E4M3>) { return launch_rows<RowsCfg<D, E4M3>>(p, &a.tm_k, &a.tm_v, st); }
-template <class C>
-cudaError_t launch_main(const AttnParams& p, const AttnArgs&, cudaStream_t st, C)
+template <bool SHARED, class C>
+cudaError_t launch_main(const ParamsOf<SHARED>& p, const AttnArgs& a, cudaStream_t st)
 {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(p.G), 1, 1);
-    cfg.blockDim = dim3(C::THREADS, 1, 1);
-    cfg.dynamicSmemBytes = C::SMEM;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, p.causal ? attention_paged_kernel<C, true> : attention_paged_kernel<C, false>, p);
+    if constexpr (C::ROWS == 128) {
+        return launch_rows<C, SHARED>(p, &a.tm_k, &a.tm_v, st);
+    } else {
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3(static_cast<unsigned>(p.G), 1, 1);
+        cfg.blockDim = dim3(C::THREADS, 1, 1);
+        cfg.dynamicSmemBytes = C::SMEM;
+        cfg.stream = st;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        return cudaLaunchKernelEx(&cfg, p.causal ? attention_paged_kernel<C, true, SHARED> : attention_paged_kernel<C, false, SHARED>, p);
+    }
 }
-template <int D>
-cudaError_t launch_join(const AttnParams& p, int rows_of_tile, int max_rows, cudaStream_t st)
+template <bool SHARED, int D>
+cudaError_t launch_join(const ParamsOf<SHARED>& p, int rows_of_tile, long long max_rows, cudaStream_t st)
 {
-    const int rows = max_rows < rows_of_tile ? max_rows : rows_of_tile;
+    const int rows = max_rows < rows_of_tile ? static_cast<int>(max_rows) : rows_of_tile;
     const bool many = rows_of_tile == 128;                 // the parts of attention_rows.cu
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(p.G), static_cast<unsigned>(many ? (rows + 31) / 32 * (D / 64) : (rows + JOIN_ROWS - 1) / JOIN_ROWS), 1);
@@ -697,43 +777,52 @@ cudaError_t launch_join(const AttnParams& p, int rows_of_tile, int max_rows, cud
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return many ? cudaLaunchKernelEx(&cfg, attention_join_rows_kernel<D>, p, rows_of_tile) : cudaLaunchKernelEx(&cfg, attention_join_kernel<D>, p, rows_of_tile);
+    return many ? cudaLaunchKernelEx(&cfg, attention_join_rows_kernel<D, SHARED>, p, rows_of_tile) : cudaLaunchKernelEx(&cfg, attention_join_kernel<D, SHARED>, p, rows_of_tile);
 }
-template <class C>
-cudaError_t run_one(AttnParams p, const AttnArgs& a, int max_rows, long long max_kv, cudaStream_t st)
+template <bool SHARED, class C>
+cudaError_t run_one(ParamsOf<SHARED> p, const AttnArgs& a, int max_rows, long long max_kv, cudaStream_t st)
 {
-    const long long items = static_cast<long long>(p.B) * p.kv_heads * ((max_rows + C::ROWS - 1) / C::ROWS);
+    // (the rows of a group are as many as the device's data says: all rows of the call at most)
+    const long long join_rows = SHARED ? static_cast<long long>(p.M) * p.group : max_rows;
+    const long long items = SHARED && shared_prefixes_host(p) ? p.kv_heads * (p.B + join_rows / C::ROWS) : static_cast<long long>(p.B) * p.kv_heads * ((max_rows + C::ROWS - 1) / C::ROWS);
     // Short items are handed out whole: a join costs about 1.2 us, a unit of 128 keys in one CTA as much.  Measured, whole / cut: 16 items of 200 keys
     // 6.2 / 7.4 us, 333 7.4 / 7.4, 500 8.7 / 7.5; 64 items of 333 7.6 / 9.7, 500 9.0 / 10.1, 1000 14.0 / 12.6.
     p.whole_units = (4 * items > p.G ? 512 : 384) / C::UK;
-    cudaError_t e = launch_main(p, a, st, C());
+    cudaError_t e = launch_main<SHARED, C>(p, a, st);
     if (e != cudaSuccess) return e;
     // no item can be cut: there is a CTA for each and the table has no room for a longer one
     if (items <= p.G && (max_kv + C::UK - 1) / C::UK <= p.whole_units) return cudaSuccess;
-    return launch_join<C::D>(p, C::ROWS, max_rows, st);
+    return launch_join<SHARED, C::D>(p, C::ROWS, join_rows, st);
 }
-template <int D, bool E4M3>
-cudaError_t run_df(const AttnParams& p, const AttnArgs& a, int max_rows, long long max_kv, cudaStream_t st)
+template <bool SHARED, int D, bool E4M3>
+cudaError_t run_df(const ParamsOf<SHARED>& p, const AttnArgs& a, int max_rows, long long max_kv, cudaStream_t st)
 {
     static_assert(Pick<D, E4M3, 0>::C::ROWS == 8 && Pick<D, E4M3, 2>::C::ROWS == 16 && RowsCfg<D, E4M3>::ROWS == 128, "tile_rows()");
     switch (rows_class(max_rows)) {
-        case 0: return run_one<typename Pick<D, E4M3, E4M3 ? 1 : 0>::C>(p, a, max_rows, max_kv, st);
-        case 1: return run_one<typename Pick<D, E4M3, 1>::C>(p, a, max_rows, max_kv, st);
-        case 2: return run_one<typename Pick<D, E4M3, 2>::C>(p, a, max_rows, max_kv, st);
-        case 3: if (!many_rows(max_rows, D, E4M3, max_kv)) return run_one<typename Pick<D, E4M3, 3>::C>(p, a, max_rows, max_kv, st); [[fallthrough]];
-        default: return run_one<RowsCfg<D, E4M3>>(p, a, max_rows, max_kv, st);
+        case 0: return run_one<SHARED, typename Pick<D, E4M3, E4M3 ? 1 : 0>::C>(p, a, max_rows, max_kv, st);
+        case 1: return run_one<SHARED, typename Pick<D, E4M3, 1>::C>(p, a, max_rows, max_kv, st);
+        case 2: return run_one<SHARED, typename Pick<D, E4M3, 2>::C>(p, a, max_rows, max_kv, st);
+        case 3: if (!many_rows(max_rows, D, E4M3, max_kv)) return run_one<SHARED, typename Pick<D, E4M3, 3>::C>(p, a, max_rows, max_kv, st); [[fallthrough]];
+        default: return run_one<SHARED, RowsCfg<D, E4M3>>(p, a, max_rows, max_kv, st);
     }
 }
-template <int D>
-cudaError_t run_d(const AttnParams& p, const AttnArgs& a, bool e4m3, int max_rows, long long max_kv, cudaStream_t st)
+template <bool SHARED>
+cudaError_t run_any(const ParamsOf<SHARED>& p, const AttnArgs& a, int max_rows, long long max_kv, cudaStream_t st)
 {
-    return e4m3 ? run_df<D, true>(p, a, max_rows, max_kv, st) : run_df<D, false>(p, a, max_rows, max_kv, st);
+    if (a.head_dim == 64) return a.e4m3 ? run_df<SHARED, 64, true>(p, a, max_rows, max_kv, st) : run_df<SHARED, 64, false>(p, a, max_rows, max_kv, st);
+    if (a.head_dim == 128) return a.e4m3 ? run_df<SHARED, 128, true>(p, a, max_rows, max_kv, st) : run_df<SHARED, 128, false>(p, a, max_rows, max_kv, st);
+    return a.e4m3 ? run_df<SHARED, 256, true>(p, a, max_rows, max_kv, st) : run_df<SHARED, 256, false>(p, a, max_rows, max_kv, st);
 }
 template <class C>
 cudaError_t init_one_attn()
 {
-    const cudaError_t e = cudaFuncSetAttribute(attention_paged_kernel<C, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
-    return e == cudaSuccess ? cudaFuncSetAttribute(attention_paged_kernel<C, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) : e;
+    cudaError_t e = cudaSuccess;
+    auto allow = [&](auto* kernel) { if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM); };
+    allow(attention_paged_kernel<C, false, false>);
+    allow(attention_paged_kernel<C, true, false>);
+    allow(attention_paged_kernel<C, false, true>);
+    allow(attention_paged_kernel<C, true, true>);
+    return e;
 }
 template <int D, bool E4M3>
 cudaError_t init_df()
@@ -768,14 +857,14 @@ bool attention_uses_maps(int max_rows, int head_dim, bool e4m3, int page_size, l
     return many_rows(max_rows, head_dim, e4m3, max_kv) && page_size >= 8;
 }
 
-size_t attention_workspace_bytes(int max_rows, int head_dim, int sm_count)
-{
-    const size_t rows = 2 * static_cast<size_t>(sm_count) * tile_rows(max_rows);
-    const size_t desc = (static_cast<size_t>(sm_count) * 32 + 255) / 256 * 256;
-    return desc + (rows * sizeof(float2) + 255) / 256 * 256 + rows * head_dim * sizeof(float);
-}
+namespace {
 
-cudaError_t launch_attention_paged(const AttnArgs& a, void* workspace, int sm_count, cudaStream_t st)
+constexpr size_t up256(size_t n) { return (n + 255) / 256 * 256; }
+size_t ml_bytes(int max_rows, int sm_count) { return up256(2 * static_cast<size_t>(sm_count) * tile_rows(max_rows) * sizeof(float2)); }
+size_t desc_bytes(int sm_count) { return up256(static_cast<size_t>(sm_count) * 32); }
+
+// What a pass over the cache needs but its requests; the workspace as attention_workspace_bytes counts it.
+AttnParams attn_params(const AttnArgs& a, int max_rows, uint8_t* ws, int sm_count)
 {
     AttnParams p;
     const int elt = a.e4m3 ? 1 : 2;
@@ -789,18 +878,59 @@ cudaError_t launch_attention_paged(const AttnArgs& a, void* workspace, int sm_co
     p.group_inv = p.group == 1 ? 0u : static_cast<uint32_t>(((1ull << 32) + p.group - 1) / p.group);
     p.G = sm_count;
     p.tma = a.tma;
-    const int max_rows = a.max_q * p.group;
-    const size_t rows = 2 * static_cast<size_t>(sm_count) * tile_rows(max_rows);
-    uint8_t* ws = static_cast<uint8_t*>(workspace);
     p.desc = reinterpret_cast<int*>(ws);
-    ws += (static_cast<size_t>(sm_count) * 32 + 255) / 256 * 256;
-    p.part_ml = reinterpret_cast<float2*>(ws);
-    ws += (rows * sizeof(float2) + 255) / 256 * 256;
-    p.part_o = reinterpret_cast<float*>(ws);
+    p.part_ml = reinterpret_cast<float2*>(ws + desc_bytes(sm_count));
+    p.part_o = reinterpret_cast<float*>(ws + desc_bytes(sm_count) + ml_bytes(max_rows, sm_count));
+    return p;
+}
+
+}  // namespace
+
+size_t attention_workspace_bytes(int max_rows, int head_dim, int sm_count)
+{
+    return desc_bytes(sm_count) + ml_bytes(max_rows, sm_count) + 2 * static_cast<size_t>(sm_count) * tile_rows(max_rows) * head_dim * sizeof(float);
+}
+
+cudaError_t launch_attention_paged(const AttnArgs& a, void* workspace, int sm_count, cudaStream_t st)
+{
+    const int max_rows = a.max_q * (a.heads / a.kv_heads);
     const long long max_kv = static_cast<long long>(a.max_pages) << a.cache.page_shift;
-    if (a.head_dim == 64) return run_d<64>(p, a, a.e4m3, max_rows, max_kv, st);
-    if (a.head_dim == 128) return run_d<128>(p, a, a.e4m3, max_rows, max_kv, st);
-    return run_d<256>(p, a, a.e4m3, max_rows, max_kv, st);
+    return run_any<false>(attn_params(a, max_rows, static_cast<uint8_t*>(workspace), sm_count), a, max_rows, max_kv, st);
+}
+
+// Shared prefixes.  Each pass has its workspace as above, behind them lie the prefixes' parts of all rows.
+size_t attention_shared_workspace_bytes(int group_rows, int max_rows, int M, int heads, int head_dim, int sm_count)
+{
+    const size_t rows = static_cast<size_t>(M) * heads;
+    return up256(attention_workspace_bytes(group_rows, head_dim, sm_count)) + up256(attention_workspace_bytes(max_rows, head_dim, sm_count)) + up256(rows * sizeof(float2)) +
+           rows * head_dim * sizeof(float);
+}
+
+cudaError_t launch_attention_shared(const AttnArgs& prefixes, const AttnArgs& rest, const SharedGroups& g, void* workspace, int sm_count, cudaStream_t st)
+{
+    const int group = rest.heads / rest.kv_heads, max_rows = rest.max_q * group;
+    const int group_rows = shared_group_rows(g.group_q, rest.M, group);
+    const long long max_kv = static_cast<long long>(rest.max_pages) << rest.cache.page_shift;
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    SharedParams p1, p2;
+    static_cast<AttnParams&>(p1) = attn_params(prefixes, group_rows, ws, sm_count);
+    ws += up256(attention_workspace_bytes(group_rows, rest.head_dim, sm_count));
+    static_cast<AttnParams&>(p2) = attn_params(rest, max_rows, ws, sm_count);
+    ws += up256(attention_workspace_bytes(max_rows, rest.head_dim, sm_count));
+    SharedPass& sh = p2.sh;
+    sh.group_starts = g.starts; sh.prefix_lens = g.lens; sh.prefix_rows = g.rows;
+    sh.n_groups = g.n; sh.table_rows = g.table_rows; sh.requests = rest.B;
+    sh.key_mask = many_rows(max_rows, rest.head_dim, rest.e4m3, max_kv) ? ~63 : ~0;
+    sh.prefixes = 0;
+    sh.causal = p2.causal;
+    sh.base_ml = reinterpret_cast<float2*>(ws);
+    sh.base_o = reinterpret_cast<float*>(ws + up256(static_cast<size_t>(rest.M) * rest.heads * sizeof(float2)));
+    p1.sh = sh;
+    p1.sh.prefixes = 1;
+    p1.B = g.n;
+    p1.causal = 0;
+    const cudaError_t e = run_any<true>(p1, prefixes, group_rows, max_kv, st);
+    return e == cudaSuccess ? run_any<true>(p2, rest, max_rows, max_kv, st) : e;
 }
 
 }  // namespace rudder

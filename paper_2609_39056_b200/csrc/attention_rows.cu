@@ -120,8 +120,8 @@ __device__ __forceinline__ void store_f16(uint32_t at0, uint32_t at1, uint4 v) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at1), "r"(h[4]), "r"(h[5]), "r"(h[6]), "r"(h[7]) : "memory");
 }
 
-template <class C>
-__global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const AttnParams p, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v)
+template <class C, bool SHARED>
+__global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const ParamsOf<SHARED> p, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v)
 {
     constexpr int D = C::D, KT = C::KT, ST = C::ST, RU = C::RU, LW = C::LW, ROWS = C::ROWS, SETS = C::SETS, HALF = C::HALF, MMA_WARP = C::MMA_WARP;
     constexpr bool E4M3 = C::E4M3;
@@ -136,8 +136,9 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
     pdl_launch_dependents();
     pdl_wait();
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    Cursor<ROWS, KT> cur;
-    if (!start_of_run<ROWS, KT, C::THREADS>(p, cur)) return;
+    using Cur = Cursor<ROWS, KT, SHARED>;
+    Cur cur;
+    if (!start_of_run<ROWS, KT, C::THREADS, SHARED>(p, cur)) return;
 
     const uint32_t base = (smem_u32(smem_raw_rows) + 1023u) & ~1023u;
     const uint32_t q_s = base, k_s = base + C::QBYTES, v_s = k_s + ST * C::TILE;
@@ -382,8 +383,24 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                         }
                         tcgen05_fence_after_sync();
                         const bool entire = item_end && part_j == 0;
+                        const bool prefix_pass = SHARED && shared_prefixes(p), final = entire && !prefix_pass;      // final: O and lse, not a part of them
                         const float vs = E4M3 && p.cache.v_scale != nullptr ? p.cache.v_scale[cur.h] : 1.0f;
-                        const float w = entire ? (ll == 0.0f ? 0.0f : vs / ll) : vs;
+                        float* pre = nullptr;              // the prefix's part of the row: written, or added with weight wp
+                        float wp = 0.0f;
+                        if constexpr (SHARED) {
+                            if (entire && r < R && (prefix_pass || cur.first_key() > 0)) {
+                                const size_t at_row = prefix_row(p, cur.rq.row0, cur.h, r);
+                                pre = p.sh.base_o + at_row * D;
+                                if (!prefix_pass) {
+                                    const JoinWeights j = join_weights(make_float2(mm, ll), __ldcg(p.sh.base_ml + at_row));
+                                    mm = j.m; ll = j.l;
+                                    w0 *= j.own; w1 *= j.own;
+                                    wp = ll == 0.0f ? 0.0f : j.prefix / ll;
+                                }
+                            }
+                            __syncwarp();
+                        }
+                        const float w = final ? (ll == 0.0f ? 0.0f : vs / ll) : vs;
                         w0 *= w;
                         w1 *= w;
                         const int slot = 2 * blockIdx.x + (first_part ? 0 : 1);
@@ -404,7 +421,23 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                                 if (SETS == 2) v[i] = fmaf(__uint_as_float(o2[i]), w1, v[i]);
                             }
                             if (r < R) {
-                                if (entire) {
+                                if constexpr (SHARED) {
+                                    if (pre != nullptr) {
+#pragma unroll
+                                        for (int i = 0; i < 32; i += 4) {
+                                            float4* at4 = reinterpret_cast<float4*>(pre + 32 * c + i);
+                                            if (prefix_pass) {
+                                                *at4 = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                                            } else {
+                                                const float4 x = __ldcg(at4);
+                                                v[i] = fmaf(x.x, wp, v[i]); v[i + 1] = fmaf(x.y, wp, v[i + 1]); v[i + 2] = fmaf(x.z, wp, v[i + 2]); v[i + 3] = fmaf(x.w, wp, v[i + 3]);
+                                            }
+                                        }
+                                    }
+                                }
+                                if (SHARED && entire && prefix_pass) {
+                                    // (written)
+                                } else if (entire) {
 #pragma unroll
                                     for (int i = 0; i < 32; i += 8)
                                         *reinterpret_cast<uint4*>(orow + 32 * c + i) = make_uint4(bf16x2(v[i], v[i + 1]), bf16x2(v[i + 2], v[i + 3]),
@@ -419,7 +452,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                         if (*const_cast<volatile int*>(&s_dropped[item & 1]) == item && r < R) {
 #pragma unroll 1
                             for (int d = 0; d < D; d += 4) {
-                                const float4 z = nonfinite_values<E4M3>(p, cur.b, cur.h, max(tail, part_j * KT), min(lim, (cur.j + 1) * KT), d);
+                                const float4 z = nonfinite_values<E4M3>(p, cur.table_row(), cur.h, cur.first_key() + max(tail, part_j * KT), cur.first_key() + min(lim, (cur.j + 1) * KT), d);
                                 const float zz[4] = {z.x, z.y, z.z, z.w};
                                 for (int e = 0; e < 4; ++e) {
                                     if (entire) orow[d + e] = static_cast<uint16_t>(bf16x2(__uint_as_float(static_cast<uint32_t>(orow[d + e]) << 16) + zz[e], 0.0f) & 0xFFFFu);
@@ -429,6 +462,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                         }
                         if (r < R) {
                             if (!entire) p.part_ml[static_cast<size_t>(slot) * ROWS + row] = make_float2(mm, ll);
+                            else if (prefix_pass) store_prefix_ml(p, cur.rq.row0, cur.h, r, mm, ll);
                             else if (p.lse != nullptr)
                                 p.lse[static_cast<size_t>(cur.rq.row0 + tok) * p.heads + hh] = ll == 0.0f ? -INFINITY : (mm + log2f(ll)) * kLn2;
                         }
@@ -444,8 +478,9 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
             cur.advance(p);
         }
     } else {
-    auto page_at = [&](const Cursor<ROWS, KT>& at, int key) -> int {
-        return key < at.rq.len ? p.table[static_cast<size_t>(at.b) * p.ld_table + (key >> p.cache.page_shift)] : -1;
+    // (keys of an item count from its first one; their places in pages and pages in the table from the request's first)
+    auto page_at = [&](const Cur& at, int key) -> int {
+        return key < at.rq.len ? p.table[static_cast<size_t>(at.table_row()) * p.ld_table + ((key + at.first_key()) >> p.cache.page_shift)] : -1;
     };
     const int box_rows = min(64, 1 << p.cache.page_shift), boxes = KT / box_rows;
     if (E4M3 && warp > MMA_WARP + LW) {
@@ -456,7 +491,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
             if (cur.j * KT + KT <= cur.rq.len) {
                 int page = lane < boxes ? page_at(cur, cur.j * KT + box_rows * lane) : 0;
                 if (page < 0 || page >= p.cache.n_pages) { record_bad_data(kBadPage); page = p.cache.n_pages; }                // out of range: zeros
-                const int tok = (cur.j * KT + box_rows * lane) & ((1 << p.cache.page_shift) - 1);
+                const int tok = (cur.first_key() + cur.j * KT + box_rows * lane) & ((1 << p.cache.page_shift) - 1);
 #pragma unroll
                 for (int half = 0; half < 2; ++half, ++issued) {
                     const int at = issued % max(RU, 1);
@@ -561,7 +596,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
         auto page_of = [&](int key) -> int { return page_at(cur, key); };
         auto place = [&](int page, int key) -> long long {
             return page * p.cache.page_stride + static_cast<long long>(cur.h) * p.cache.head_stride +
-                   static_cast<long long>(key & ((1 << p.cache.page_shift) - 1)) * p.cache.token_stride;
+                   static_cast<long long>((key + cur.first_key()) & ((1 << p.cache.page_shift) - 1)) * p.cache.token_stride;
         };
         auto run_pages = [&]() -> int {
             const int run = w + lane * LW;
@@ -623,7 +658,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
                     if (lane < boxes) {
                         int page = box_page;
                         if (page < 0 || page >= p.cache.n_pages) { record_bad_data(kBadPage); page = p.cache.n_pages; }      // out of range: zeros
-                        const int tok = (tile0 + box_rows * lane) & ((1 << p.cache.page_shift) - 1);
+                        const int tok = (cur.first_key() + tile0 + box_rows * lane) & ((1 << p.cache.page_shift) - 1);
 #pragma unroll
                         for (int blk = 0; blk < D / 64; ++blk) {
                             tma_load_4d(k_dst + blk * C::BLK + box_rows * lane * 128, &tm_k, 64 * blk, tok, cur.h, page, kv_full(slot));
@@ -729,8 +764,8 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Att
     }
 }
 
-template <class C>
-cudaError_t launch_rows(const AttnParams& p, const CUtensorMap* tm_k, const CUtensorMap* tm_v, cudaStream_t st)
+template <class C, bool SHARED>
+cudaError_t launch_rows(const ParamsOf<SHARED>& p, const CUtensorMap* tm_k, const CUtensorMap* tm_v, cudaStream_t st)
 {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(p.G), 1, 1);
@@ -742,10 +777,14 @@ cudaError_t launch_rows(const AttnParams& p, const CUtensorMap* tm_k, const CUte
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, attention_rows_kernel<C>, p, *tm_k, *tm_v);
+    return cudaLaunchKernelEx(&cfg, attention_rows_kernel<C, SHARED>, p, *tm_k, *tm_v);
 }
 template <class C>
-cudaError_t init_rows() { return cudaFuncSetAttribute(attention_rows_kernel<C>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM); }
+cudaError_t init_rows()
+{
+    const cudaError_t e = cudaFuncSetAttribute(attention_rows_kernel<C, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+    return e == cudaSuccess ? cudaFuncSetAttribute(attention_rows_kernel<C, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) : e;
+}
 
 }  // namespace
 

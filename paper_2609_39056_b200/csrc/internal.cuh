@@ -185,7 +185,30 @@ cudaError_t attention_paged_init();
 bool attention_uses_maps(int max_rows, int head_dim, bool e4m3, int page_size, long long max_kv);
 size_t attention_workspace_bytes(int max_rows, int head_dim, int sm_count);
 cudaError_t launch_attention_paged(const AttnArgs& a, void* workspace, int sm_count, cudaStream_t st);
+struct SharedGroups {                      // groups of requests with a common prefix, see rudder_attention_shared
+    const int32_t* starts; const int32_t* lens; const int32_t* rows;
+    int n, table_rows, group_q;
+};
+// Rows of a group that choose the kernel of the prefixes' pass.  group_q is what the caller expects: the kernel for up to 4 rows, which takes no more than
+// one tile of them, only where the call has no more.
+inline int shared_group_rows(int group_q, int M, int group)
+{
+    const int rows = (group_q < M ? group_q : M) * group;
+    return rows <= 4 && static_cast<long long>(M) * group > 4 ? 5 : rows;
+}
+size_t attention_shared_workspace_bytes(int group_rows, int max_rows, int M, int heads, int head_dim, int sm_count);
+// `prefixes`, `rest`: the same call, each with the tensor maps that its pass takes
+cudaError_t launch_attention_shared(const AttnArgs& prefixes, const AttnArgs& rest, const SharedGroups& g, void* workspace, int sm_count, cudaStream_t st);
 cudaError_t launch_padding_rows(const AttnArgs& a, const int32_t* positions, cudaStream_t st);
+struct PageForkArgs; struct PageCopyArgs; struct PagePoolArgs; struct LoraArgs;
+cudaError_t page_pool_init();
+cudaError_t launch_page_fork(const PageForkArgs& a, const rudder_paged_cache* caches, int sm_count, cudaStream_t st);
+cudaError_t launch_page_copy(const PageCopyArgs& a, const rudder_paged_cache* caches, int sm_count, cudaStream_t st);
+cudaError_t launch_page_pool(const PagePoolArgs& a, bool compact, cudaStream_t st);
+constexpr int kMaxRank = 256, kMaxAdapters = 4096;
+cudaError_t lora_init();
+size_t lora_workspace_bytes(int M, int K, int R, int n_adapters, int sm_count);
+cudaError_t launch_lora(const LoraArgs& a, void* workspace, int sm_count, cudaStream_t st);
 cudaError_t linear_a16_init();
 bool linear_a16_fits(int K);              // the widest layer whose rows fit in shared memory
 cudaError_t launch_linear_a16(const rudder_weight* w, const uint16_t* X, int64_t ldx, int M, const float* bias, uint16_t* Y, int64_t ldy, int sm_count,

@@ -61,6 +61,45 @@ struct AttnArgs {
     CUtensorMap tm_k, tm_v;               // [pages][heads][tokens][channels], box of min(64, page size) tokens: bf16 64 channels, 128-byte swizzle; E4M3 whole rows as they lie
 };
 
+// The caches of several layers in the same geometry, their strides in BYTES (page_pool.cu; the bases come beside it).
+constexpr int kMaxLayers = 128;
+struct PoolCache {
+    int64_t page_stride, head_stride, token_stride;
+    int heads, chunk_shift;               // 16-byte pieces of a head's token: 1 << chunk_shift
+};
+struct PageForkArgs {
+    int32_t* table; int64_t ld_table; int max_pages, B;
+    int32_t* lens;
+    int page_shift, n_pages;
+    const int32_t* src; const int32_t* dst; const int32_t* fork_lens; int n;
+    const int32_t* free_pages; int n_free; const int32_t* taken;
+    int32_t* copies;                      // or nullptr
+    int32_t* used;
+    PoolCache cache; int layers;
+};
+struct PageCopyArgs {
+    const int32_t* copies; const int32_t* count; int n;
+    int page_shift, n_pages;
+    PoolCache cache; int layers;
+};
+struct PagePoolArgs {
+    const int32_t* table; int64_t ld_table; int max_pages, B;
+    int32_t* lens;                        // written by a release only
+    int page_shift, n_pages;
+    const int32_t* drop; int n_drop;      // release
+    int32_t* refs; int32_t* free_pages; int32_t* n_free;
+    int32_t* new_table; int64_t ld_new;   // compaction
+    int32_t* remap; int32_t* copies; int32_t* n_copies; int32_t* n_live;
+};
+struct LoraArgs {
+    const uint16_t* X; int64_t ldx; int M, K;
+    const uint16_t* A; int64_t a_stride, lda;
+    const uint16_t* B; int64_t b_stride, ldb; int N, R, n_adapters;
+    const int32_t* ranks; const float* scales; const int32_t* adapters;
+    const uint16_t* base; int64_t ld_base;
+    uint16_t* Y; int64_t ldy;
+};
+
 // A kernel that is launched early lives while the kernels in front of it still write.  Behind pdl_wait it sees what they wrote, but only by ordinary
 // loads: what a caller may write on the stream (tables, lengths, scales, biases, angles) is not read through __ldg, which asks for memory that nobody
 // writes while the kernel lives.  (Packed weights are complete when rudder_pack_weights returns.)
