@@ -496,7 +496,8 @@ rudder_status rudder_page_compact(const rudder_page_compact_args* args, const ru
  * has of its own under `causal`) reads all of its tokens through its own row of the table, as does a request of no group.  prefix_lens need not be a
  * multiple of the page size, and 0 is allowed; the requests' own rows of the table name the prefix's pages, too, or pages with the same tokens.
  * Groups do not overlap.  group_q, the most new tokens that a group has, chooses the kernel; a group with more is computed all the same.
- * M x heads / cache heads up to 2^20.  workspace: rudder_attention_shared_workspace_bytes(args) bytes, rules as in rudder_attention_paged. */
+ * M x heads / cache heads up to 2^20.  workspace: rudder_attention_shared_workspace_bytes(args) bytes (from M, heads, max_q, group_q, max_pages and the
+ * cache's shape alone), 256-byte aligned, contents irrelevant; calls that may overlap on the GPU need one each.  Results do not depend on timing. */
 typedef struct {
     rudder_attention_args attn;
     const int32_t* group_starts; /* [n_groups + 1], not descending */

@@ -137,7 +137,8 @@ size_t rudder_attention_shared_workspace_bytes(const rudder_attention_shared_arg
     if (check_shared_shape(args) != RUDDER_OK) return 0;
     const rudder_attention_args& a = args->attn;
     const int group = a.heads / a.cache->heads;
-    return attention_shared_workspace_bytes(shared_group_rows(args->group_q, a.M, group), a.max_q * group, a.M, a.heads, a.cache->head_dim, sm_count());
+    return attention_shared_workspace_bytes(shared_group_rows(args->group_q, a.M, group), a.max_q * group, a.M, a.heads, a.cache->head_dim, a.cache->format == RUDDER_CACHE_E4M3,
+                                            static_cast<long long>(a.max_pages) * a.cache->page_size, sm_count());
 }
 
 rudder_status rudder_attention_shared(const rudder_attention_shared_args* args, void* workspace, size_t workspace_bytes, void* stream)

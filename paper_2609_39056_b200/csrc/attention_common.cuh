@@ -203,7 +203,9 @@ __device__ __forceinline__ SharedReq load_member(const SharedParams& p, int b, i
 // A place in the sequence of units: request, kv head, row tile, unit inside the item, and what is left of the run from there on.
 // What starting and ending an item costs, in units (queries, merge of the warp groups, output): an item counts as its units + kItemCost,
 // the cost in front.  A cut inside the cost leaves the item whole to the run behind.
-constexpr int kItemCost = 2;                               // 48 requests of up to 16384 keys 56 us, without a cost 172 us, with 6 59 us
+// 48 requests of up to 16384 keys 56 us, without a cost 172 us, with 6 59 us.  (Units of 16 or 32 keys, a warp's: see PickSolo.)
+template <int UNIT_KEYS>
+constexpr int kItemCost = UNIT_KEYS >= 64 ? 2 : 4;
 
 template <int ROWS, int UK, bool SHARED = false>
 struct Cursor {
@@ -245,7 +247,7 @@ struct Cursor {
     __device__ __forceinline__ void advance(const ParamsOf<SHARED>& p) {
         ++j;
         if (--left <= 0 || j < nt) return;
-        left -= kItemCost;
+        left -= kItemCost<UK>;
         if (left > 0) next_item(p);
     }
 };
@@ -253,6 +255,16 @@ struct Cursor {
 // Row `r` of an item whose rows begin at row0: its place in base_o and base_ml.
 __device__ __forceinline__ bool shared_prefixes(const AttnParams&) { return false; }
 __device__ __forceinline__ bool shared_prefixes(const SharedParams& p) { return p.sh.prefixes != 0; }
+// The start of a pass in a chain of early launches.  The prefixes' pass lets the next launch begin only when everything in front of the call is complete; so the
+// pass behind it (and what may come between them) begins while prefixes are still read, and waits for them in front of its first output.
+__device__ __forceinline__ void start_pass(const AttnParams&) {
+    pdl_launch_dependents();
+    pdl_wait();
+}
+__device__ __forceinline__ void start_pass(const SharedParams& p) {
+    if (p.sh.prefixes) pdl_wait();
+    pdl_launch_dependents();
+}
 __device__ __forceinline__ size_t prefix_row(const AttnParams& p, int row0, int h, int r) {
     const RowOf at = row_of(p, r);
     return static_cast<size_t>(row0 + at.token) * p.heads + h * p.group + at.head;
@@ -318,7 +330,7 @@ __device__ __forceinline__ bool start_of_run(const ParamsOf<SHARED>& p, Cursor<R
             if (lane < p.B) r = load_request(p, lane);
         }
         const int n_rt = (r.qlen * p.group + ROWS - 1) / ROWS, nt = max(1, (r.len + UK - 1) / UK);
-        const long long t_units = static_cast<long long>(n_rt) * p.kv_heads * (nt + kItemCost);
+        const long long t_units = static_cast<long long>(n_rt) * p.kv_heads * (nt + kItemCost<UK>);
         const int t_items = n_rt * p.kv_heads;
         long long i_units = t_units;
         int i_items = t_items;
@@ -353,11 +365,11 @@ __device__ __forceinline__ bool start_of_run(const ParamsOf<SHARED>& p, Cursor<R
         cur.nt = __shfl_sync(0xffffffffu, nt, b);
         cur.n_rt = __shfl_sync(0xffffffffu, n_rt, b);
         const long long off = u_begin - __shfl_sync(0xffffffffu, before, b);
-        const int size = whole ? 1 : cur.nt + kItemCost;
+        const int size = whole ? 1 : cur.nt + kItemCost<UK>;
         const uint32_t item = static_cast<uint32_t>(quotient(off, size));
         cur.h = static_cast<int>(item / static_cast<uint32_t>(cur.n_rt));
         cur.rt = static_cast<int>(item % static_cast<uint32_t>(cur.n_rt));
-        place = whole ? kItemCost : static_cast<int>(off - static_cast<long long>(item) * size);
+        place = whole ? kItemCost<UK> : static_cast<int>(off - static_cast<long long>(item) * size);
     } else {
     const int per = (p.B + THREADS - 1) / THREADS;
     const int rb0 = min(p.B, tid * per), rb1 = min(p.B, rb0 + per);
@@ -370,7 +382,7 @@ __device__ __forceinline__ bool start_of_run(const ParamsOf<SHARED>& p, Cursor<R
     for (int b = rb0; b < rb1; ++b) {
         const R r = request(b);
         const int n_rt = (r.qlen * p.group + ROWS - 1) / ROWS, nt = max(1, (r.len + UK - 1) / UK);
-        t_units += static_cast<long long>(n_rt) * p.kv_heads * (nt + kItemCost);
+        t_units += static_cast<long long>(n_rt) * p.kv_heads * (nt + kItemCost<UK>);
         t_items += n_rt * p.kv_heads;
         if (n_rt > 0) t_max = max(t_max, nt);
     }
@@ -409,7 +421,7 @@ __device__ __forceinline__ bool start_of_run(const ParamsOf<SHARED>& p, Cursor<R
             long long at = mine0;
             for (int b = rb0; b < rb1; ++b) {
                 const R r = request(b);
-                const int n_rt = (r.qlen * p.group + ROWS - 1) / ROWS, nt = whole ? 1 : max(1, (r.len + UK - 1) / UK) + kItemCost;
+                const int n_rt = (r.qlen * p.group + ROWS - 1) / ROWS, nt = whole ? 1 : max(1, (r.len + UK - 1) / UK) + kItemCost<UK>;
                 const long long here = static_cast<long long>(n_rt) * p.kv_heads * nt;
                 if (u_begin < at + here) {
                     const long long off = u_begin - at;
@@ -427,10 +439,10 @@ __device__ __forceinline__ bool start_of_run(const ParamsOf<SHARED>& p, Cursor<R
     __syncthreads();
     cur.set_request(p, s_place[0]);
     cur.h = s_place[1]; cur.rt = s_place[2];
-    place = whole ? kItemCost : s_place[3];
+    place = whole ? kItemCost<UK> : s_place[3];
     }
-    cur.j = max(0, place - kItemCost);
-    cur.left = whole ? cur.nt : (u_end - u_begin) - max(0, kItemCost - place);      // of this run, from unit cur.j on
+    cur.j = max(0, place - kItemCost<UK>);
+    cur.left = whole ? cur.nt : (u_end - u_begin) - max(0, kItemCost<UK> - place);      // of this run, from unit cur.j on
     if (cur.left <= 0) {                                       // nothing but a part of an item's cost
         if (tid == 0) p.desc[8 * blockIdx.x] = 0;
         return false;
@@ -443,7 +455,7 @@ __device__ __forceinline__ bool start_of_run(const ParamsOf<SHARED>& p, Cursor<R
         const bool first_cut = !whole && cur.j > 0 && unit0 >= before;
         d[1] = cur.h; d[2] = cur.rt; d[3] = cur.rq.row0; d[4] = cur.rq.qlen;
         d[5] = static_cast<int>(quotient(unit0 + cur.nt - 1, share));            // last owner
-        d[6] = unit0 <= before + kItemCost ? 0 : 1;        // slot of the first owner's part: its run starts with this item (or inside its cost)
+        d[6] = unit0 <= before + kItemCost<UK> ? 0 : 1;        // slot of the first owner's part: its run starts with this item (or inside its cost)
         d[0] = first_cut ? 1 : 0;
         if constexpr (SHARED) d[7] = cur.rq.key0 > 0;       // the join adds the prefix's part
     }

@@ -113,8 +113,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const Pa
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ uint32_t s_dropped[RW * KW];                // per warp: see drop_nonfinite
     __shared__ float s_prefix[SHARED ? ROWS : 1];          // weight of the prefix's part
-    pdl_launch_dependents();
-    pdl_wait();
+    start_pass(p);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int g = lane >> 2, q = lane & 3;
     const int kg = warp / RW, rw = warp % RW;
@@ -122,7 +121,10 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const Pa
 
     using Cur = Cursor<ROWS, UK, SHARED>;
     Cur cur;
-    if (!start_of_run<ROWS, UK, C::THREADS, SHARED>(p, cur)) return;
+    if (!start_of_run<ROWS, UK, C::THREADS, SHARED>(p, cur)) {
+        if (SHARED) pdl_wait();                            // (what follows this launch follows the prefixes' pass, too)
+        return;
+    }
 
     // ---- the ring of this warp group
     const uint32_t ring = smem_u32(smem) + kg * (NST * C::STAGE);
@@ -403,6 +405,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const Pa
             // ---- end of an item or of this run: add the warp groups, write the rows or the part
             float* box = reinterpret_cast<float*>(smem + C::RING);
             float2* ml = reinterpret_cast<float2*>(smem + C::RING + C::BOX);
+            if (SHARED) pdl_wait();                        // the prefixes' parts are there, and their pass has read its queries
             const bool entire = item_end && part_j == 0;
             const bool prefix_pass = SHARED && shared_prefixes(p), joins = SHARED && entire && !prefix_pass && cur.first_key() > 0;
             const bool final = entire && !prefix_pass;                           // O and lse, not a part of them
@@ -486,7 +489,25 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const Pa
                         }
                     }
                 __syncthreads();
-                for (int i = tid; i < rows_here * (DC / 4); i += C::THREADS) {
+                // (the prefix's part of several pieces is requested together: a thread of a small CTA has up to sixteen)
+                constexpr int PIECES = ROWS * (DC / 4) / C::THREADS, AHEAD = !SHARED || PIECES < 1 ? 1 : (PIECES < 8 ? PIECES : 8);
+                for (int i0 = tid; i0 < rows_here * (DC / 4); i0 += AHEAD * C::THREADS) {
+                    float4 pre[AHEAD];
+                    if constexpr (SHARED) {
+                        if (joins) {
+#pragma unroll
+                            for (int a = 0; a < AHEAD; ++a) {
+                                const int i = i0 + a * C::THREADS;
+                                pre[a] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                                if (i < rows_here * (DC / 4))
+                                    pre[a] = __ldcg(reinterpret_cast<const float4*>(p.sh.base_o + prefix_row(p, cur.rq.row0, cur.h, cur.rt * ROWS + i / (DC / 4)) * D + round * DC + 4 * (i % (DC / 4))));
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int a = 0; a < AHEAD; ++a) {
+                    const int i = i0 + a * C::THREADS;
+                    if (SHARED && i >= rows_here * (DC / 4)) break;
                     const int rl = i / (DC / 4), d = 4 * (i % (DC / 4));
                     float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
@@ -500,13 +521,12 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const Pa
                     }
                     const RowOf at = row_of(p, cur.rt * ROWS + rl);
                     if constexpr (SHARED) {
-                        float* pre = p.sh.base_o + prefix_row(p, cur.rq.row0, cur.h, cur.rt * ROWS + rl) * D + round * DC + d;
                         if (joins) {
-                            const float4 x = __ldcg(reinterpret_cast<const float4*>(pre));
+                            const float4 x = pre[a];
                             const float w = s_prefix[rl];
                             o.x = fmaf(x.x, w, o.x); o.y = fmaf(x.y, w, o.y); o.z = fmaf(x.z, w, o.z); o.w = fmaf(x.w, w, o.w);
                         } else if (entire && prefix_pass) {
-                            *reinterpret_cast<float4*>(pre) = o;
+                            *reinterpret_cast<float4*>(p.sh.base_o + prefix_row(p, cur.rq.row0, cur.h, cur.rt * ROWS + rl) * D + round * DC + d) = o;
                             continue;
                         }
                     }
@@ -515,6 +535,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const Pa
                                                   round * DC + d) = make_uint2(bf16x2(o.x, o.y), bf16x2(o.z, o.w));
                     else
                         *reinterpret_cast<float4*>(p.part_o + (static_cast<size_t>(slot) * ROWS + rl) * D + round * DC + d) = o;
+                    }
                 }
             }
             if (CAUSAL && dropped) {
@@ -568,7 +589,11 @@ __global__ void __launch_bounds__(JOIN_THREADS) attention_join_kernel(const Para
     if (!load_cut(p, blockIdx.x, x)) return;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int ry = warp / JOIN_SPLIT, part = warp % JOIN_SPLIT;
-    const int rl = blockIdx.y * JOIN_ROWS + ry, r = x.rt * rows_of_tile + rl;
+    // (SHARED: there are many runs and few of them start inside an item; one CTA takes all rows of its tile)
+    for (int y = blockIdx.y * JOIN_ROWS; y == static_cast<int>(blockIdx.y) * JOIN_ROWS || (SHARED && y < rows_of_tile); y += gridDim.y * JOIN_ROWS) {
+    if (SHARED && x.rt * rows_of_tile + y >= x.qlen * p.group) return;
+    if (SHARED && y != static_cast<int>(blockIdx.y) * JOIN_ROWS) __syncthreads();
+    const int rl = y + ry, r = x.rt * rows_of_tile + rl;
     const bool live = r < x.qlen * p.group;
     constexpr int V = D / 32;                              // channels of a lane
     float o[V];
@@ -601,7 +626,10 @@ __global__ void __launch_bounds__(JOIN_THREADS) attention_join_kernel(const Para
     for (int i = 0; i < V; ++i) s_o[ry][part][lane * V + i] = o[i];
     if (lane == 0) s_ml[ry][part] = make_float2(m, l);
     __syncthreads();
-    if (part != 0 || !live) return;
+    if (part != 0 || !live) {
+        if (SHARED) continue;
+        return;
+    }
     float mm = -INFINITY, ll = 0.0f, w[JOIN_SPLIT];
 #pragma unroll
     for (int s = 0; s < JOIN_SPLIT; ++s) mm = fmaxf(mm, s_ml[ry][s].x);
@@ -626,7 +654,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) attention_join_kernel(const Para
                 out[i] = a;
             }
             if (lane == 0) p.sh.base_ml[row] = make_float2(mm, ll);
-            return;
+            continue;
         }
         if (x.joins) {
             const JoinWeights j = join_weights(make_float2(mm, ll), __ldcg(p.sh.base_ml + row));
@@ -655,6 +683,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) attention_join_kernel(const Para
         *reinterpret_cast<uint32_t*>(orow + i) = bf16x2(a * inv, b * inv);
     }
     if (lane == 0 && p.lse != nullptr) p.lse[static_cast<size_t>(x.row0 + at.token) * p.heads + hh] = ll == 0.0f ? -INFINITY : (mm + log2f(ll)) * kLn2;
+    }
 }
 
 // The same for many rows: a lane per row, as the parts lie; a warp has 32 rows x 8 channels, a CTA 64 channels, y = row block x channel block.
@@ -731,6 +760,17 @@ template <> struct Pick<128, true, 3> { using C = AttnCfg<128, true, 2, 2, 4, 32
 template <> struct Pick<256, false, 3> { using C = AttnCfg<256, false, 2, 2, 4, 16, 3, 2>; };
 template <> struct Pick<256, true, 3> { using C = AttnCfg<256, true, 2, 2, 4, 16, 5, 0>; };
 
+// What stands behind shared prefixes: many short items (16 candidates x 8 heads of 64 keys each), where adding up eight warps' parts at an item's end costs more than
+// its keys.  One warp (up to 16 rows) or two (32) are a CTA of their own, several to an SM, with an item each: as many bytes in flight, nothing to add up.
+// 512 items of 16 rows x 16 to 80 keys 38 -> SOLO_US us; 512 items of 12 rows x up to 1024 keys in E4M3 67 -> SOLO2_US us.
+template <int D, bool E4M3, int CLS>
+struct PickSolo {
+    static constexpr int KT = D == 64 || (D == 128 && E4M3) ? 32 : 16;
+    using C = AttnCfg<D, E4M3, CLS <= 1 ? 1 : 2, CLS == 3 ? 2 : 1, 1, KT, 3, E4M3 ? 0 : kLo<CLS>>;
+};
+template <class C>
+constexpr int solo_ctas() { return 224 * 1024 / (C::SMEM + 2048); }              // to an SM; 2 KB for its static shared memory and what the system takes
+
 int rows_class(int max_rows) { return max_rows <= 4 ? 0 : (max_rows <= 8 ? 1 : (max_rows <= 16 ? 2 : (max_rows <= 32 ? 3 : 4))); }
 // The tcgen05 kernel (attention_rows.cu): above 32 rows always; 17 to 32 rows in bf16 with D = 128 and a table of 4096 tokens or more (the lengths
 // themselves are device data).  Measured, this kernel / that one, 4 requests x 4 key-value heads unless said:
@@ -760,13 +800,14 @@ cudaError_t launch_main(const ParamsOf<SHARED>& p, const AttnArgs& a, cudaStream
         attr[0].val.programmaticStreamSerializationAllowed = 1;
         cfg.attrs = attr;
         cfg.numAttrs = 1;
-        return cudaLaunchKernelEx(&cfg, p.causal ? attention_paged_kernel<C, true, SHARED> : attention_paged_kernel<C, false, SHARED>, p);
+        if constexpr (SHARED && C::KW > 1) return cudaLaunchKernelEx(&cfg, attention_paged_kernel<C, false, true>, p);       // prefixes
+        else return cudaLaunchKernelEx(&cfg, p.causal ? attention_paged_kernel<C, true, SHARED> : attention_paged_kernel<C, false, SHARED>, p);
     }
 }
 template <bool SHARED, int D>
 cudaError_t launch_join(const ParamsOf<SHARED>& p, int rows_of_tile, long long max_rows, cudaStream_t st)
 {
-    const int rows = max_rows < rows_of_tile ? static_cast<int>(max_rows) : rows_of_tile;
+    const int rows = SHARED && rows_of_tile <= 32 ? JOIN_ROWS : (max_rows < rows_of_tile ? static_cast<int>(max_rows) : rows_of_tile);
     const bool many = rows_of_tile == 128;                 // the parts of attention_rows.cu
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(p.G), static_cast<unsigned>(many ? (rows + 31) / 32 * (D / 64) : (rows + JOIN_ROWS - 1) / JOIN_ROWS), 1);
@@ -787,7 +828,7 @@ cudaError_t run_one(ParamsOf<SHARED> p, const AttnArgs& a, int max_rows, long lo
     const long long items = SHARED && shared_prefixes_host(p) ? p.kv_heads * (p.B + join_rows / C::ROWS) : static_cast<long long>(p.B) * p.kv_heads * ((max_rows + C::ROWS - 1) / C::ROWS);
     // Short items are handed out whole: a join costs about 1.2 us, a unit of 128 keys in one CTA as much.  Measured, whole / cut: 16 items of 200 keys
     // 6.2 / 7.4 us, 333 7.4 / 7.4, 500 8.7 / 7.5; 64 items of 333 7.6 / 9.7, 500 9.0 / 10.1, 1000 14.0 / 12.6.
-    p.whole_units = (4 * items > p.G ? 512 : 384) / C::UK;
+    p.whole_units = C::UK < 64 ? 192 / C::UK : (4 * items > p.G ? 512 : 384) / C::UK;
     cudaError_t e = launch_main<SHARED, C>(p, a, st);
     if (e != cudaSuccess) return e;
     // no item can be cut: there is a CTA for each and the table has no room for a longer one
@@ -798,6 +839,15 @@ template <bool SHARED, int D, bool E4M3>
 cudaError_t run_df(const ParamsOf<SHARED>& p, const AttnArgs& a, int max_rows, long long max_kv, cudaStream_t st)
 {
     static_assert(Pick<D, E4M3, 0>::C::ROWS == 8 && Pick<D, E4M3, 2>::C::ROWS == 16 && RowsCfg<D, E4M3>::ROWS == 128, "tile_rows()");
+    if constexpr (SHARED) {
+        // (the grid and the workspace go by the same rule: rest_grid)
+        if (!p.sh.prefixes && !many_rows(max_rows, D, E4M3, max_kv)) switch (rows_class(max_rows)) {
+            case 0: return run_one<true, typename PickSolo<D, E4M3, E4M3 ? 1 : 0>::C>(p, a, max_rows, max_kv, st);
+            case 1: return run_one<true, typename PickSolo<D, E4M3, 1>::C>(p, a, max_rows, max_kv, st);
+            case 2: return run_one<true, typename PickSolo<D, E4M3, 2>::C>(p, a, max_rows, max_kv, st);
+            default: return run_one<true, typename PickSolo<D, E4M3, 3>::C>(p, a, max_rows, max_kv, st);
+        }
+    }
     switch (rows_class(max_rows)) {
         case 0: return run_one<SHARED, typename Pick<D, E4M3, E4M3 ? 1 : 0>::C>(p, a, max_rows, max_kv, st);
         case 1: return run_one<SHARED, typename Pick<D, E4M3, 1>::C>(p, a, max_rows, max_kv, st);
@@ -820,9 +870,14 @@ cudaError_t init_one_attn()
     auto allow = [&](auto* kernel) { if (e == cudaSuccess) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM); };
     allow(attention_paged_kernel<C, false, false>);
     allow(attention_paged_kernel<C, true, false>);
-    allow(attention_paged_kernel<C, false, true>);
-    allow(attention_paged_kernel<C, true, true>);
+    allow(attention_paged_kernel<C, false, true>);         // (prefixes: their pass has no causal limits)
     return e;
+}
+template <class C>
+cudaError_t init_solo()
+{
+    const cudaError_t e = cudaFuncSetAttribute(attention_paged_kernel<C, false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+    return e == cudaSuccess ? cudaFuncSetAttribute(attention_paged_kernel<C, true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) : e;
 }
 template <int D, bool E4M3>
 cudaError_t init_df()
@@ -832,7 +887,32 @@ cudaError_t init_df()
     if (e == cudaSuccess) e = init_one_attn<typename Pick<D, E4M3, 2>::C>();
     if (e == cudaSuccess) e = init_one_attn<typename Pick<D, E4M3, 3>::C>();
     if (e == cudaSuccess) e = init_rows<RowsCfg<D, E4M3>>();
+    if (e == cudaSuccess) e = init_solo<typename PickSolo<D, E4M3, E4M3 ? 1 : 0>::C>();
+    if (e == cudaSuccess) e = init_solo<typename PickSolo<D, E4M3, 1>::C>();
+    if (e == cudaSuccess) e = init_solo<typename PickSolo<D, E4M3, 2>::C>();
+    if (e == cudaSuccess) e = init_solo<typename PickSolo<D, E4M3, 3>::C>();
     return e;
+}
+// CTAs of the pass behind the prefixes, and rows of its parts
+struct RestGrid { int ctas, part_rows; };
+template <class C>
+RestGrid solo_grid(int sm_count) { return RestGrid{sm_count * solo_ctas<C>(), C::ROWS}; }
+template <int D, bool E4M3>
+RestGrid solo_grid_df(int max_rows, int sm_count)
+{
+    switch (rows_class(max_rows)) {
+        case 0: return solo_grid<typename PickSolo<D, E4M3, E4M3 ? 1 : 0>::C>(sm_count);
+        case 1: return solo_grid<typename PickSolo<D, E4M3, 1>::C>(sm_count);
+        case 2: return solo_grid<typename PickSolo<D, E4M3, 2>::C>(sm_count);
+        default: return solo_grid<typename PickSolo<D, E4M3, 3>::C>(sm_count);
+    }
+}
+RestGrid rest_grid(int max_rows, int head_dim, bool e4m3, long long max_kv, int sm_count)
+{
+    if (many_rows(max_rows, head_dim, e4m3, max_kv)) return RestGrid{sm_count, 128};
+    if (head_dim == 64) return e4m3 ? solo_grid_df<64, true>(max_rows, sm_count) : solo_grid_df<64, false>(max_rows, sm_count);
+    if (head_dim == 128) return e4m3 ? solo_grid_df<128, true>(max_rows, sm_count) : solo_grid_df<128, false>(max_rows, sm_count);
+    return e4m3 ? solo_grid_df<256, true>(max_rows, sm_count) : solo_grid_df<256, false>(max_rows, sm_count);
 }
 template <int D>
 cudaError_t init_d()
@@ -860,11 +940,12 @@ bool attention_uses_maps(int max_rows, int head_dim, bool e4m3, int page_size, l
 namespace {
 
 constexpr size_t up256(size_t n) { return (n + 255) / 256 * 256; }
-size_t ml_bytes(int max_rows, int sm_count) { return up256(2 * static_cast<size_t>(sm_count) * tile_rows(max_rows) * sizeof(float2)); }
-size_t desc_bytes(int sm_count) { return up256(static_cast<size_t>(sm_count) * 32); }
+size_t desc_bytes(int ctas) { return up256(static_cast<size_t>(ctas) * 32); }
+size_t ml_bytes(int part_rows, int ctas) { return up256(2 * static_cast<size_t>(ctas) * part_rows * sizeof(float2)); }
+size_t pass_bytes(int part_rows, int head_dim, int ctas) { return desc_bytes(ctas) + ml_bytes(part_rows, ctas) + 2 * static_cast<size_t>(ctas) * part_rows * head_dim * sizeof(float); }
 
-// What a pass over the cache needs but its requests; the workspace as attention_workspace_bytes counts it.
-AttnParams attn_params(const AttnArgs& a, int max_rows, uint8_t* ws, int sm_count)
+// What a pass over the cache needs but its requests, with parts of `part_rows` rows in its workspace.
+AttnParams attn_params(const AttnArgs& a, int part_rows, uint8_t* ws, int ctas)
 {
     AttnParams p;
     const int elt = a.e4m3 ? 1 : 2;
@@ -876,34 +957,31 @@ AttnParams attn_params(const AttnArgs& a, int max_rows, uint8_t* ws, int sm_coun
     p.max_pages = a.max_pages; p.B = a.B; p.max_q = a.max_q; p.M = a.M; p.heads = a.heads; p.kv_heads = a.kv_heads;
     p.group = a.heads / a.kv_heads; p.causal = a.causal && a.max_q > 1;
     p.group_inv = p.group == 1 ? 0u : static_cast<uint32_t>(((1ull << 32) + p.group - 1) / p.group);
-    p.G = sm_count;
+    p.G = ctas;
     p.tma = a.tma;
     p.desc = reinterpret_cast<int*>(ws);
-    p.part_ml = reinterpret_cast<float2*>(ws + desc_bytes(sm_count));
-    p.part_o = reinterpret_cast<float*>(ws + desc_bytes(sm_count) + ml_bytes(max_rows, sm_count));
+    p.part_ml = reinterpret_cast<float2*>(ws + desc_bytes(ctas));
+    p.part_o = reinterpret_cast<float*>(ws + desc_bytes(ctas) + ml_bytes(part_rows, ctas));
     return p;
 }
 
 }  // namespace
 
-size_t attention_workspace_bytes(int max_rows, int head_dim, int sm_count)
-{
-    return desc_bytes(sm_count) + ml_bytes(max_rows, sm_count) + 2 * static_cast<size_t>(sm_count) * tile_rows(max_rows) * head_dim * sizeof(float);
-}
+size_t attention_workspace_bytes(int max_rows, int head_dim, int sm_count) { return pass_bytes(tile_rows(max_rows), head_dim, sm_count); }
 
 cudaError_t launch_attention_paged(const AttnArgs& a, void* workspace, int sm_count, cudaStream_t st)
 {
     const int max_rows = a.max_q * (a.heads / a.kv_heads);
     const long long max_kv = static_cast<long long>(a.max_pages) << a.cache.page_shift;
-    return run_any<false>(attn_params(a, max_rows, static_cast<uint8_t*>(workspace), sm_count), a, max_rows, max_kv, st);
+    return run_any<false>(attn_params(a, tile_rows(max_rows), static_cast<uint8_t*>(workspace), sm_count), a, max_rows, max_kv, st);
 }
 
 // Shared prefixes.  Each pass has its workspace as above, behind them lie the prefixes' parts of all rows.
-size_t attention_shared_workspace_bytes(int group_rows, int max_rows, int M, int heads, int head_dim, int sm_count)
+size_t attention_shared_workspace_bytes(int group_rows, int max_rows, int M, int heads, int head_dim, bool e4m3, long long max_kv, int sm_count)
 {
     const size_t rows = static_cast<size_t>(M) * heads;
-    return up256(attention_workspace_bytes(group_rows, head_dim, sm_count)) + up256(attention_workspace_bytes(max_rows, head_dim, sm_count)) + up256(rows * sizeof(float2)) +
-           rows * head_dim * sizeof(float);
+    const RestGrid r = rest_grid(max_rows, head_dim, e4m3, max_kv, sm_count);
+    return up256(pass_bytes(tile_rows(group_rows), head_dim, sm_count)) + up256(pass_bytes(r.part_rows, head_dim, r.ctas)) + up256(rows * sizeof(float2)) + rows * head_dim * sizeof(float);
 }
 
 cudaError_t launch_attention_shared(const AttnArgs& prefixes, const AttnArgs& rest, const SharedGroups& g, void* workspace, int sm_count, cudaStream_t st)
@@ -913,10 +991,11 @@ cudaError_t launch_attention_shared(const AttnArgs& prefixes, const AttnArgs& re
     const long long max_kv = static_cast<long long>(rest.max_pages) << rest.cache.page_shift;
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     SharedParams p1, p2;
-    static_cast<AttnParams&>(p1) = attn_params(prefixes, group_rows, ws, sm_count);
-    ws += up256(attention_workspace_bytes(group_rows, rest.head_dim, sm_count));
-    static_cast<AttnParams&>(p2) = attn_params(rest, max_rows, ws, sm_count);
-    ws += up256(attention_workspace_bytes(max_rows, rest.head_dim, sm_count));
+    static_cast<AttnParams&>(p1) = attn_params(prefixes, tile_rows(group_rows), ws, sm_count);
+    ws += up256(pass_bytes(tile_rows(group_rows), rest.head_dim, sm_count));
+    const RestGrid r = rest_grid(max_rows, rest.head_dim, rest.e4m3, max_kv, sm_count);
+    static_cast<AttnParams&>(p2) = attn_params(rest, r.part_rows, ws, r.ctas);
+    ws += up256(pass_bytes(r.part_rows, rest.head_dim, r.ctas));
     SharedPass& sh = p2.sh;
     sh.group_starts = g.starts; sh.prefix_lens = g.lens; sh.prefix_rows = g.rows;
     sh.n_groups = g.n; sh.table_rows = g.table_rows; sh.requests = rest.B;

@@ -120,6 +120,50 @@ __device__ __forceinline__ void store_f16(uint32_t at0, uint32_t at1, uint4 v) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at1), "r"(h[4]), "r"(h[5]), "r"(h[6]), "r"(h[7]) : "memory");
 }
 
+// Two 32-bit numbers in one register pair: arithmetic on both at the price of one instruction, each rounded on its own.
+__device__ __forceinline__ uint64_t pair(uint32_t a, uint32_t b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t pair(float a, float b) { return pair(__float_as_uint(a), __float_as_uint(b)); }
+__device__ __forceinline__ float2 unpair(uint64_t x) {
+    uint32_t a, b;
+    asm("mov.b64 {%0, %1}, %2;" : "=r"(a), "=r"(b) : "l"(x));
+    return make_float2(__uint_as_float(a), __uint_as_float(b));
+}
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t exp2_pair(uint64_t x) {
+    const float2 v = unpair(x);
+    return pair(exp2_approx(v.x), exp2_approx(v.y));
+}
+// Two probabilities as bf16 hi + lo without a conversion instruction: those share a pipe of a sixteenth of a warp per clock with the exponentials, and that pipe bounded
+// this pass (64 probabilities a thread 2300 -> SPLIT_CLK clocks).  x (2^16 + 1) - (x (2^16 + 1) - x) is x rounded to 8 bits (Dekker's splitting, Numer. Math. 18, 1971), what is
+// left is exact, and its upper half is its bf16 number cut off: |x - hi - lo| < 2^-15 x.
+__device__ __forceinline__ void split_bf16(uint64_t x, uint32_t& hi, uint32_t& lo) {
+    const uint64_t neg = pair(-1.0f, -1.0f);
+    const uint64_t c = mul2(x, pair(65537.0f, 65537.0f));
+    const uint64_t d = fma2(x, neg, c);                    // c - x
+    const uint64_t h = fma2(d, neg, c), l = fma2(h, neg, x);
+    const float2 hv = unpair(h), lv = unpair(l);
+    hi = __byte_perm(__float_as_uint(hv.x), __float_as_uint(hv.y), 0x7632);
+    lo = __byte_perm(__float_as_uint(lv.x), __float_as_uint(lv.y), 0x7632);
+}
+
 template <class C, bool SHARED>
 __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const ParamsOf<SHARED> p, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v)
 {
@@ -133,12 +177,14 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Par
     __shared__ int abort_word;
     __shared__ int s_dropped[2];                           // [item & 1]: the item, if values were dropped (see drop_nonfinite)
 
-    pdl_launch_dependents();
-    pdl_wait();
+    start_pass(p);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     using Cur = Cursor<ROWS, KT, SHARED>;
     Cur cur;
-    if (!start_of_run<ROWS, KT, C::THREADS, SHARED>(p, cur)) return;
+    if (!start_of_run<ROWS, KT, C::THREADS, SHARED>(p, cur)) {
+        if (SHARED) pdl_wait();
+        return;
+    }
 
     const uint32_t base = (smem_u32(smem_raw_rows) + 1023u) & ~1023u;
     const uint32_t q_s = base, k_s = base + C::QBYTES, v_s = k_s + ST * C::TILE;
@@ -253,12 +299,15 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Par
 #pragma unroll
                     for (int c = 0; c < HALF / 32; ++c) tmem_ld_32x32b_x32(s_t + 32 * c, x[c]);
                     tmem_wait_ld();
+                    float fs = f;
                     if (edge) {
                         const uint32_t gone = __float_as_uint(f < 0.0f ? INFINITY : -INFINITY);
 #pragma unroll
                         for (int c = 0; c < HALF / 32; ++c)
 #pragma unroll
-                            for (int i = 0; i < 32; ++i) x[c][i] = key0 + 32 * c + i < lim ? x[c][i] : gone;
+                            for (int i = 0; i < 32; ++i) x[c][i] = key0 + 32 * c + i < lim ? (SHARED && f == 0.0f ? 0u : x[c][i]) : gone;
+                        // (a factor of zero, which makes no -infinity of a key that is not seen: scores of zero instead, with a factor of one)
+                        if (SHARED && f == 0.0f) fs = 1.0f;
                     }
                     float mx;
                     {
@@ -303,13 +352,22 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Par
                     // pass 2: probabilities over the scores they come from
                     const float u = m == -INFINITY ? 0.0f : m;
                     float l0 = 0.0f, l1 = 0.0f;
+                    uint64_t l01 = 0;                      // two zeros
 #pragma unroll
                     for (int c = 0; c < HALF / 32; ++c) {
                         uint32_t w[32];                    // hi (or f16) in the first half, lo in the second
+                        if constexpr (SHARED && !E4M3) {
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                const uint64_t e = exp2_pair(fma2(pair(x[c][2 * i], x[c][2 * i + 1]), pair(fs, fs), pair(-u, -u)));
+                                l01 = add2(l01, e);
+                                split_bf16(e, w[i], w[16 + i]);
+                            }
+                        } else {
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            float a = exp2_approx(fmaf(__uint_as_float(x[c][2 * i]), f, -u)), b = exp2_approx(fmaf(__uint_as_float(x[c][2 * i + 1]), f, -u));
-                            if (edge && f == 0.0f) {       // (0 x infinity)
+                            float a = exp2_approx(fmaf(__uint_as_float(x[c][2 * i]), fs, -u)), b = exp2_approx(fmaf(__uint_as_float(x[c][2 * i + 1]), fs, -u));
+                            if (!SHARED && edge && f == 0.0f) {       // (0 x infinity)
                                 if (key0 + 32 * c + 2 * i >= lim) a = 0.0f;
                                 if (key0 + 32 * c + 2 * i + 1 >= lim) b = 0.0f;
                             }
@@ -322,9 +380,14 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Par
                                 w[16 + i] = bf16x2(a - bf16_lo(w[i]), b - bf16_hi(w[i]));
                             }
                         }
+                        }
                         __syncwarp();
                         if (E4M3) tmem_st_x16(s_t + 32 * c, reinterpret_cast<const uint32_t (&)[16]>(w));
                         else tmem_st_x32(s_t + 32 * c, w);
+                    }
+                    if constexpr (SHARED && !E4M3) {
+                        const float2 z = unpair(l01);
+                        l0 = z.x; l1 = z.y;
                     }
                     l += l0 + l1;
                     tmem_wait_st();
@@ -371,6 +434,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Par
                     ok = wait_all(pv_done(0), t & 1, W_R_PV_DONE) &&
                          (SETS == 1 || (wait_all(ml_full, (item - 1) & 1, W_R_ML_FULL) && wait_all(pv_done(1), t & 1, W_R_PV_DONE)));
                     if (!ok) break;
+                    if (SHARED) pdl_wait();
                     if (live_warp) {
                         float w0 = 1.0f, w1 = 0.0f, mm = m, ll = l;
                         if (SETS == 2) {

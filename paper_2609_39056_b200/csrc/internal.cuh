@@ -183,7 +183,7 @@ cudaError_t launch_qk_norm_rope(const QkArgs& a, int head_dim, bool e4m3, int sm
 struct AttnArgs;
 cudaError_t attention_paged_init();
 bool attention_uses_maps(int max_rows, int head_dim, bool e4m3, int page_size, long long max_kv);
-size_t attention_workspace_bytes(int max_rows, int head_dim, int sm_count);
+size_t attention_workspace_bytes(int max_rows, int head_dim, int ctas);
 cudaError_t launch_attention_paged(const AttnArgs& a, void* workspace, int sm_count, cudaStream_t st);
 struct SharedGroups {                      // groups of requests with a common prefix, see rudder_attention_shared
     const int32_t* starts; const int32_t* lens; const int32_t* rows;
@@ -196,7 +196,7 @@ inline int shared_group_rows(int group_q, int M, int group)
     const int rows = (group_q < M ? group_q : M) * group;
     return rows <= 4 && static_cast<long long>(M) * group > 4 ? 5 : rows;
 }
-size_t attention_shared_workspace_bytes(int group_rows, int max_rows, int M, int heads, int head_dim, int sm_count);
+size_t attention_shared_workspace_bytes(int group_rows, int max_rows, int M, int heads, int head_dim, bool e4m3, long long max_kv, int sm_count);
 // `prefixes`, `rest`: the same call, each with the tensor maps that its pass takes
 cudaError_t launch_attention_shared(const AttnArgs& prefixes, const AttnArgs& rest, const SharedGroups& g, void* workspace, int sm_count, cudaStream_t st);
 cudaError_t launch_padding_rows(const AttnArgs& a, const int32_t* positions, cudaStream_t st);
