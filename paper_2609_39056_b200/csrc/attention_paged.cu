@@ -779,6 +779,8 @@ int rows_class(int max_rows) { return max_rows <= 4 ? 0 : (max_rows <= 8 ? 1 : (
 //   E4M3, D = 128: 20 x 1000 12.1 / 15.9, 32 x 8000 25 / 36, 32 x 60k 96 / 144, 32 x 126k 189 / 282, 64 x 126k 353 / 295; D = 64: 20 x 8000 18.3 / 25.5, 32 x 126k 143 / 227,
 //   64 x 126k 269 / 227; D = 256: 32 x 1500 19.1 / 21.4, 32 x 60k 219 / 244.
 bool many_rows(int max_rows, int head_dim, bool e4m3, long long max_kv) { return max_rows > 32 || (max_rows > 16 && head_dim == 128 && !e4m3 && max_kv >= 4096); }
+// Prefixes of groups with more than 128 rows: two tiles of rows at a time (tensor memory holds two with up to 128 channels)
+bool prefix_pairs(int group_rows, int head_dim) { return group_rows > 128 && head_dim <= 128; }
 bool shared_prefixes_host(const AttnParams&) { return false; }
 bool shared_prefixes_host(const SharedParams& p) { return p.sh.prefixes != 0; }
 // Rows of a part in the workspace (whichever kernel runs: the size depends on the shapes alone)
@@ -787,7 +789,7 @@ int tile_rows(int max_rows) { return max_rows <= 8 ? 8 : (max_rows <= 16 ? 16 : 
 template <bool SHARED, class C>
 cudaError_t launch_main(const ParamsOf<SHARED>& p, const AttnArgs& a, cudaStream_t st)
 {
-    if constexpr (C::ROWS == 128) {
+    if constexpr (C::ROWS >= 128) {
         return launch_rows<C, SHARED>(p, &a.tm_k, &a.tm_v, st);
     } else {
         cudaLaunchConfig_t cfg = {};
@@ -808,7 +810,7 @@ template <bool SHARED, int D>
 cudaError_t launch_join(const ParamsOf<SHARED>& p, int rows_of_tile, long long max_rows, cudaStream_t st)
 {
     const int rows = SHARED && rows_of_tile <= 32 ? JOIN_ROWS : (max_rows < rows_of_tile ? static_cast<int>(max_rows) : rows_of_tile);
-    const bool many = rows_of_tile == 128;                 // the parts of attention_rows.cu
+    const bool many = rows_of_tile >= 128;                 // the parts of attention_rows.cu
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(p.G), static_cast<unsigned>(many ? (rows + 31) / 32 * (D / 64) : (rows + JOIN_ROWS - 1) / JOIN_ROWS), 1);
     cfg.blockDim = dim3(JOIN_THREADS, 1, 1);
@@ -847,6 +849,9 @@ cudaError_t run_df(const ParamsOf<SHARED>& p, const AttnArgs& a, int max_rows, l
             case 2: return run_one<true, typename PickSolo<D, E4M3, 2>::C>(p, a, max_rows, max_kv, st);
             default: return run_one<true, typename PickSolo<D, E4M3, 3>::C>(p, a, max_rows, max_kv, st);
         }
+    }
+    if constexpr (SHARED && D <= 128) {
+        if (p.sh.prefixes && prefix_pairs(max_rows, D)) return run_one<true, RowsCfg<D, E4M3, true>>(p, a, max_rows, max_kv, st);
     }
     switch (rows_class(max_rows)) {
         case 0: return run_one<SHARED, typename Pick<D, E4M3, E4M3 ? 1 : 0>::C>(p, a, max_rows, max_kv, st);
@@ -887,6 +892,9 @@ cudaError_t init_df()
     if (e == cudaSuccess) e = init_one_attn<typename Pick<D, E4M3, 2>::C>();
     if (e == cudaSuccess) e = init_one_attn<typename Pick<D, E4M3, 3>::C>();
     if (e == cudaSuccess) e = init_rows<RowsCfg<D, E4M3>>();
+    if constexpr (D <= 128) {
+        if (e == cudaSuccess) e = init_rows<RowsCfg<D, E4M3, true>>();
+    }
     if (e == cudaSuccess) e = init_solo<typename PickSolo<D, E4M3, E4M3 ? 1 : 0>::C>();
     if (e == cudaSuccess) e = init_solo<typename PickSolo<D, E4M3, 1>::C>();
     if (e == cudaSuccess) e = init_solo<typename PickSolo<D, E4M3, 2>::C>();
@@ -967,6 +975,8 @@ AttnParams attn_params(const AttnArgs& a, int part_rows, uint8_t* ws, int ctas)
 
 }  // namespace
 
+int prefix_part_rows(int group_rows, int head_dim) { return prefix_pairs(group_rows, head_dim) ? 256 : tile_rows(group_rows); }
+
 size_t attention_workspace_bytes(int max_rows, int head_dim, int sm_count) { return pass_bytes(tile_rows(max_rows), head_dim, sm_count); }
 
 cudaError_t launch_attention_paged(const AttnArgs& a, void* workspace, int sm_count, cudaStream_t st)
@@ -981,7 +991,7 @@ size_t attention_shared_workspace_bytes(int group_rows, int max_rows, int M, int
 {
     const size_t rows = static_cast<size_t>(M) * heads;
     const RestGrid r = rest_grid(max_rows, head_dim, e4m3, max_kv, sm_count);
-    return up256(pass_bytes(tile_rows(group_rows), head_dim, sm_count)) + up256(pass_bytes(r.part_rows, head_dim, r.ctas)) + up256(rows * sizeof(float2)) + rows * head_dim * sizeof(float);
+    return up256(pass_bytes(prefix_part_rows(group_rows, head_dim), head_dim, sm_count)) + up256(pass_bytes(r.part_rows, head_dim, r.ctas)) + up256(rows * sizeof(float2)) + rows * head_dim * sizeof(float);
 }
 
 cudaError_t launch_attention_shared(const AttnArgs& prefixes, const AttnArgs& rest, const SharedGroups& g, void* workspace, int sm_count, cudaStream_t st)
@@ -991,8 +1001,8 @@ cudaError_t launch_attention_shared(const AttnArgs& prefixes, const AttnArgs& re
     const long long max_kv = static_cast<long long>(rest.max_pages) << rest.cache.page_shift;
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     SharedParams p1, p2;
-    static_cast<AttnParams&>(p1) = attn_params(prefixes, tile_rows(group_rows), ws, sm_count);
-    ws += up256(pass_bytes(tile_rows(group_rows), rest.head_dim, sm_count));
+    static_cast<AttnParams&>(p1) = attn_params(prefixes, prefix_part_rows(group_rows, rest.head_dim), ws, sm_count);
+    ws += up256(pass_bytes(prefix_part_rows(group_rows, rest.head_dim), rest.head_dim, sm_count));
     const RestGrid r = rest_grid(max_rows, rest.head_dim, rest.e4m3, max_kv, sm_count);
     static_cast<AttnParams&>(p2) = attn_params(rest, r.part_rows, ws, r.ctas);
     ws += up256(pass_bytes(r.part_rows, rest.head_dim, r.ctas));

@@ -33,16 +33,17 @@ namespace {
 enum RowsWhere { W_R_Q_EMPTY = 1001, W_R_KV_EMPTY = 1002, W_R_RAW_FULL = 1003, W_R_RAW_EMPTY = 1004, W_R_Q_FULL = 1101, W_R_KV_FULL = 1102, W_R_P_FULL = 1104, W_R_O_FREE = 1105,
                  W_R_S_FULL = 1201, W_R_PV_DONE = 1202, W_R_ML_FULL = 1203 };
 
-template <int D_, bool E4M3_>
+// PAIR: two tiles of 128 rows over the same keys, see pair_softmax.
+template <int D_, bool E4M3_, bool PAIR_ = false>
 struct RowsCfg {
     static constexpr int D = D_;
-    static constexpr bool E4M3 = E4M3_;
-    static constexpr int ROWS = 128;
+    static constexpr bool E4M3 = E4M3_, PAIR = PAIR_;
+    static constexpr int ROWS = PAIR ? 256 : 128;
     static constexpr int UK = D <= 128 ? 128 : 64;
     static constexpr int KT = UK;                          // keys of a tile: a unit of the work split
-    static constexpr int ST = D == 64 ? 4 : (D == 128 && !E4M3 ? 3 : 2);
+    static constexpr int ST = D == 64 ? 4 : (D == 128 && !E4M3 && !PAIR ? 3 : 2);
     static constexpr int SETS = D <= 128 ? 2 : 1;          // sets of four softmax warps: each takes its share of a tile's keys, with an O of its own
-    static constexpr int HALF = KT / SETS;
+    static constexpr int HALF = PAIR ? KT : KT / SETS;     // keys of a tile that a set takes
     static constexpr int LW = E4M3 ? 4 : 3;                // loading warps (12 warps in all: 168 registers a thread),
     static constexpr int TW = E4M3 ? 1 : 0;                // with E4M3 they convert, and one more issues the TMA loads (14 warps: 144)
     // The reference is the maximum less TOP when it is taken and is raised when the maximum less TOP exceeds it by RAISE: probabilities up to 2^(TOP + RAISE),
@@ -56,9 +57,10 @@ struct RowsCfg {
     static constexpr int QBLK = ROWS * 128;
     static constexpr int QBYTES = D / 64 * QBLK;
     static constexpr int RAW = KT * D;                     // E4M3: a K or a V tile as it lies in the cache,
-    static constexpr int RU = E4M3 ? (D == 64 ? 8 : (D == 128 ? 4 : 2)) : 0;     // and how many of them are on their way
+    static constexpr int RU = E4M3 ? (D == 64 ? 8 : (D == 128 && !PAIR ? 4 : 2)) : 0;     // and how many of them are on their way
     static constexpr int SMEM = 1024 + QBYTES + 2 * ST * TILE + RU * RAW;
     static constexpr int O_COL = 2 * KT;                   // tensor memory columns: two S / P buffers, O
+    static_assert(!PAIR || SETS == 2, "a set of softmax warps for each tile of rows");
     static_assert(O_COL + SETS * D <= 512 && SMEM <= 226 * 1024, "tensor memory and shared memory");
 };
 
@@ -171,7 +173,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Par
     constexpr bool E4M3 = C::E4M3;
     extern __shared__ uint8_t smem_raw_rows[];
     __shared__ __align__(8) uint64_t bars[2 * ST + 12 + 2 * C::RU];
-    __shared__ float2 s_ml[ROWS];                          // (reference, sum) of the second set's rows
+    __shared__ float2 s_ml[C::PAIR ? 1 : ROWS];                          // (reference, sum) of the second set's rows
     __shared__ int8_t s_exp[E4M3 ? ROWS : 1];              // E4M3: the power of two that a row of Q was multiplied by
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_word;
@@ -194,7 +196,8 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Par
     auto s_full = [&](int i) { return bar0 + 8u * (2 * ST + i); };
     auto p_full = [&](int buf, int set) { return bar0 + 8u * (2 * ST + 2 + buf + 2 * set); };
     auto pv_done = [&](int set) { return bar0 + 8u * (2 * ST + 6 + set); };
-    const uint32_t ml_full = bar0 + 8u * (2 * ST + 8), o_free = ml_full + 8u, q_full = ml_full + 16u, q_empty = ml_full + 24u;
+    const uint32_t ml_full = bar0 + 8u * (2 * ST + 8), o_free = ml_full + 8u,                 // (PAIR: the first is the second set's o_free)
+                    q_full = ml_full + 16u, q_empty = ml_full + 24u;
     const uint32_t raw_s = v_s + ST * C::TILE;
     auto raw_full = [&](int i) { return bar0 + 8u * (2 * ST + 12 + i); };
     auto raw_empty = [&](int i) { return bar0 + 8u * (2 * ST + 12 + RU + i); };
@@ -253,7 +256,252 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Par
     volatile int* abortp = &abort_word;
     auto wait_all = [&](uint32_t bar, uint32_t parity, int where) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, abortp, where)) != 0; };
 
-    if (warp < MMA_WARP) {
+    if (C::PAIR && warp < MMA_WARP) {
+        // ---------------------------------------------------------------------------------------- softmax and output, a set of warps for each tile of rows
+        // Rows of shared prefixes: each sees every key of its item.  A set has its own scores, probabilities (over them), O and counts of what it did; the two run at
+        // their own pace, so that the products of one fall under the softmax of the other.  In one tile of rows the two sets wait for the same products:
+        // 16 heads x 512 rows x 4416 keys PAIR_US us.
+        const int set = warp >> 2, quad = warp & 3;
+        const int row = 128 * set + 32 * quad + lane;
+        const uint32_t lanes = static_cast<uint32_t>(32 * quad) << 16;
+        const uint32_t s_t = tmem + lanes + set * KT, o_t = tmem + lanes + C::O_COL + set * D, done = set == 0 ? o_free : ml_full;
+        int t = 0, item = 0, part_j = 0, R = 0, r = 0;
+        bool ok = true, fresh = true, first_part = true, active = false, live_warp = false, first_tile = false;
+        float f = 0.0f, m = -INFINITY, l = 0.0f;
+        while (cur.left > 0) {
+            if (fresh) {
+                fresh = false;
+                first_tile = true;
+                part_j = cur.j;
+                R = cur.rq.qlen * p.group;
+                r = cur.rt * ROWS + row;
+                active = cur.rt * ROWS + 128 * set < R;
+                live_warp = cur.rt * ROWS + 128 * set + 32 * quad < R;
+                m = -INFINITY;
+                l = 0.0f;
+                f = r < R ? p.scale_log2 : 0.0f;           // rows that do not exist hold whatever the buffer held: nothing is read from them
+                ok = wait_all(q_full, item & 1, W_R_Q_FULL);
+                if (!ok) break;
+                if (E4M3 && r < R) f *= __uint_as_float(static_cast<uint32_t>(127 - s_exp[row]) << 23) * (p.cache.k_scale != nullptr ? p.cache.k_scale[cur.h] : 1.0f);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(q_empty);
+                ++item;
+            }
+            const bool item_end = cur.j + 1 == cur.nt, ends = item_end || cur.left == 1;
+            if (active) {
+                ok = wait_all(s_full(set), t & 1, W_R_S_FULL);
+                if (!ok) break;
+                if (live_warp) {
+                    tcgen05_fence_after_sync();            // (the product before is complete, too: these scores lie over its probabilities)
+                    const int live = cur.rq.len - cur.j * KT;                      // keys of the tile that there are
+                    const bool edge = live < KT;
+                    const float gone = f < 0.0f ? INFINITY : -INFINITY;
+                    float fs = f;
+                    if (edge && f == 0.0f) fs = 1.0f;      // (a factor of zero makes no -infinity: scores of zero with a factor of one)
+                    constexpr int TOGETHER = E4M3 ? 1 : 2;                         // (with E4M3 there are 14 warps, and 128 registers a thread)
+                    uint32_t x[TOGETHER][32];
+                    auto load = [&](int c, uint32_t (&to)[32]) { tmem_ld_32x32b_x32(s_t + 32 * c, to); };
+                    auto cut = [&](int c, uint32_t (&to)[32]) {
+                        if (edge) {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) to[i] = 32 * c + i < live ? (f == 0.0f ? 0u : to[i]) : __float_as_uint(gone);
+                        }
+                    };
+                    float q[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    auto most = [&](const uint32_t (&v)[32]) {
+                        if (f >= 0.0f) {
+#pragma unroll
+                            for (int i = 0; i < 32; i += 2) q[(i >> 1) & 3] = fmaxf(q[(i >> 1) & 3], fmaxf(__uint_as_float(v[i]), __uint_as_float(v[i + 1])));
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) q[i & 3] = fmaxf(q[i & 3], -__uint_as_float(v[i]));
+                        }
+                    };
+                    // pass 1: the maximum of s f
+#pragma unroll 1                                           // (four times the code costs more at the start, instruction by instruction from L2, than it saves later)
+                    for (int c = 0; c < KT / 32; c += TOGETHER) {
+#pragma unroll
+                        for (int i = 0; i < TOGETHER; ++i) load(c + i, x[i]);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < TOGETHER; ++i) {
+                            cut(c + i, x[i]);
+                            most(x[i]);
+                        }
+                    }
+                    float mx = fmaxf(fmaxf(q[0], q[1]), fmaxf(q[2], q[3]));
+                    mx = mx == -INFINITY ? mx : mx * fabsf(f) - C::TOP;
+                    __syncwarp();
+                    if (first_tile) {
+                        m = mx;
+                    } else if (__any_sync(0xffffffffu, r < R && mx > m + C::RAISE)) {
+                        const float n = mx > m + C::RAISE ? mx : m;
+                        const float cor = n == -INFINITY ? 1.0f : exp2_approx(m - n);
+                        m = n;
+                        l *= cor;
+#pragma unroll 1
+                        for (int c = 0; c < D / 16; ++c) {
+                            uint32_t o[16];
+                            tmem_ld_32x32b_x16(o_t + 16 * c, o);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * cor);
+                            tmem_st_x16(o_t + 16 * c, o);
+                        }
+                        tmem_wait_st();
+                    }
+                    // pass 2: probabilities over the scores they come from
+                    const float u = m == -INFINITY ? 0.0f : m;
+                    uint64_t l01 = 0;
+                    auto weigh = [&](int c, const uint32_t (&v)[32]) {
+                        uint32_t w[32];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const uint64_t e = exp2_pair(fma2(pair(v[2 * i], v[2 * i + 1]), pair(fs, fs), pair(-u, -u)));
+                            l01 = add2(l01, e);
+                            if (E4M3) {
+                                const float2 z = unpair(e);
+                                w[i] = f16x2(z.x, z.y);
+                            } else {
+                                split_bf16(e, w[i], w[16 + i]);
+                            }
+                        }
+                        __syncwarp();
+                        if (E4M3) tmem_st_x16(s_t + 32 * c, reinterpret_cast<const uint32_t (&)[16]>(w));
+                        else tmem_st_x32(s_t + 32 * c, w);
+                    };
+#pragma unroll 1
+                    for (int c = 0; c < KT / 32; ++c) {
+                        load(c, x[0]);
+                        tmem_wait_ld();
+                        cut(c, x[0]);
+                        weigh(c, x[0]);
+                    }
+                    const float2 z = unpair(l01);
+                    l += z.x + z.y;
+                    tmem_wait_st();
+                    tcgen05_fence_before_sync();
+                }
+                first_tile = false;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(p_full(0, set));
+                ++t;
+                if (ends) {
+                    ok = wait_all(pv_done(set), (t - 1) & 1, W_R_PV_DONE);
+                    if (!ok) break;
+                    if (live_warp) {
+                        tcgen05_fence_after_sync();
+                        const bool entire = item_end && part_j == 0;
+                        const float vs = E4M3 && p.cache.v_scale != nullptr ? p.cache.v_scale[cur.h] : 1.0f;
+                        const int slot = 2 * blockIdx.x + (first_part ? 0 : 1);
+                        float* out = p.part_o + static_cast<size_t>(slot) * ROWS * D + 4 * row;                  // [channels / 4][rows][4]: coalesced
+                        int step = 4 * ROWS;
+                        if constexpr (SHARED) {
+                            if (entire && r < R) {
+                                out = p.sh.base_o + prefix_row(p, cur.rq.row0, cur.h, r) * D;
+                                step = 4;
+                            }
+                        }
+                        __syncwarp();
+#pragma unroll 1
+                        for (int c = 0; c < D / 32; ++c) {
+                            uint32_t o[32];
+                            tmem_ld_32x32b_x32(o_t + 32 * c, o);
+                            tmem_wait_ld();
+                            if (r < R) {
+#pragma unroll
+                                for (int i = 0; i < 32; i += 4)
+                                    *reinterpret_cast<float4*>(out + (8 * c + i / 4) * step) = make_float4(__uint_as_float(o[i]) * vs, __uint_as_float(o[i + 1]) * vs,
+                                                                                                         __uint_as_float(o[i + 2]) * vs, __uint_as_float(o[i + 3]) * vs);
+                            }
+                            __syncwarp();
+                        }
+                        if (r < R) {
+                            if (!entire) p.part_ml[static_cast<size_t>(slot) * ROWS + row] = make_float2(m, l);
+                            else store_prefix_ml(p, cur.rq.row0, cur.h, r, m, l);
+                        }
+                        tcgen05_fence_before_sync();
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(done);
+                }
+            }
+            if (ends) {
+                fresh = true;
+                first_part = false;
+            }
+            cur.advance(p);
+        }
+    } else if (C::PAIR && warp == MMA_WARP) {
+        // ---------------------------------------------------------------------------------------- MMA issue for a pair: first set, second set, in turn
+        const bool leader = elect_one();
+        const uint32_t idesc_s = umma_idesc_f16(128, KT, !E4M3, false), idesc_o = umma_idesc_f16(128, D, !E4M3, true);
+        int mine[2] = {0, 0}, own_items[2] = {0, 0};       // scores issued for a set, items with rows of the set
+        int t = 0, item = 0;
+        bool ok = true;
+        // scores of tile `of`, over the probabilities of the set's tile before: its product must be complete (products into different accumulators are not ordered)
+        auto scores = [&](int set, int of) -> bool {
+            if (!wait_all(kv_full(of % ST), (of / ST) & 1, W_R_KV_FULL)) return false;
+            if (mine[set] > 0 && !wait_all(pv_done(set), (mine[set] - 1) & 1, W_R_PV_DONE)) return false;
+            tcgen05_fence_after_sync();
+            if (leader) {
+                const uint32_t k0 = k_s + (of % ST) * C::TILE, q0 = q_s + set * 128 * 128;
+#pragma unroll
+                for (int ks = 0; ks < D / 16; ++ks)
+                    umma_f16_ss(tmem + set * KT, umma_desc_sw128(q0 + (ks >> 2) * C::QBLK) + 2u * (ks & 3), umma_desc_sw128(k0 + (ks >> 2) * C::BLK) + 2u * (ks & 3), idesc_s,
+                                ks > 0 ? 1u : 0u);
+                umma_commit(s_full(set));
+            }
+            __syncwarp();
+            ++mine[set];
+            return true;
+        };
+        // O += P V of tile `of`; the item's first product starts its O, once the set's item before has been read out
+        auto product = [&](int set, int of, bool first, bool last_user) -> bool {
+            if (!wait_all(p_full(0, set), (mine[set] - 1) & 1, W_R_P_FULL)) return false;
+            if (first && own_items[set] > 1 && !wait_all(set == 0 ? o_free : ml_full, own_items[set] & 1, W_R_O_FREE)) return false;
+            tcgen05_fence_after_sync();
+            if (leader) {
+                const uint32_t v0 = v_s + (of % ST) * C::TILE, o = tmem + C::O_COL + set * D;
+#pragma unroll
+                for (int kk = 0; kk < KT / 16; ++kk) {
+                    const uint64_t db = umma_desc_sw128_mn(v0 + kk * 2048, C::BLK);
+                    const uint32_t pa = tmem + set * KT + 32 * (kk >> 1) + 8 * (kk & 1);
+                    umma_f16_ts(o, pa, db, idesc_o, (first && kk == 0) ? 0u : 1u);
+                    if (!E4M3) umma_f16_ts(o, pa + 16, db, idesc_o, 1u);
+                }
+                umma_commit(pv_done(set));
+                if (last_user) umma_commit(kv_empty(of % ST));
+            }
+            __syncwarp();
+            return true;
+        };
+        auto last_of_item = [&]() { return cur.j + 1 == cur.nt || cur.left == 1; };
+        auto second_has_rows = [&]() { return cur.rt * ROWS + 128 < cur.rq.qlen * p.group; };
+        while (ok && cur.left > 0) {
+            // an item: its first scores, then tile by tile product and the next scores, set by set
+            const bool both = second_has_rows();
+            bool ends = last_of_item(), first = true;
+            ok = wait_all(q_full, item & 1, W_R_Q_FULL);
+            ++item;
+            ++own_items[0];
+            own_items[1] += both;
+            ok = ok && scores(0, t) && (!both || scores(1, t));
+            if (ok && ends && leader) umma_commit(q_empty);
+            while (ok) {
+                cur.advance(p);
+                const bool next_ends = !ends && last_of_item();
+                ok = product(0, t, first, !both) && (ends || scores(0, t + 1));
+                if (ok && both) ok = product(1, t, first, true) && (ends || scores(1, t + 1));
+                if (ok && next_ends && leader) umma_commit(q_empty);
+                __syncwarp();
+                ++t;
+                if (ends) break;
+                ends = next_ends;
+                first = false;
+            }
+        }
+    } else if (warp < MMA_WARP) {
         // ---------------------------------------------------------------------------------------- softmax and output
         const int set = warp >> 2, quad = warp & 3;
         const int row = 32 * quad + lane;
@@ -846,8 +1094,11 @@ cudaError_t launch_rows(const ParamsOf<SHARED>& p, const CUtensorMap* tm_k, cons
 template <class C>
 cudaError_t init_rows()
 {
+    if constexpr (C::PAIR) return cudaFuncSetAttribute(attention_rows_kernel<C, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+    else {
     const cudaError_t e = cudaFuncSetAttribute(attention_rows_kernel<C, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
     return e == cudaSuccess ? cudaFuncSetAttribute(attention_rows_kernel<C, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) : e;
+    }
 }
 
 }  // namespace
