@@ -200,6 +200,27 @@ __device__ __forceinline__ SharedReq load_member(const SharedParams& p, int b, i
     return r;
 }
 
+// Request (or group) b by this lane, the whole warp together; b at or beyond the last one has no rows.
+__device__ __forceinline__ void load_by_lane(const SharedParams& p, int b, int lane, SharedReq& r, Group& grp) {
+    if (p.sh.prefixes) {
+        if (b < p.B) r = load_group(p, b);
+        return;
+    }
+    if (p.sh.n_groups <= 32) {
+        // a group per lane: no search, its loads beside those of the requests
+        const bool is = lane < p.sh.n_groups;
+        const int s0 = is ? p.sh.group_starts[lane] : 0x7fffffff, s1 = is ? p.sh.group_starts[lane + 1] : 0, pre = is ? prefix_of(p, lane) : 0;
+        int at = -1;
+        for (int i = 0; i < p.sh.n_groups; ++i) at = __shfl_sync(0xffffffffu, s0, i) <= b ? i : at;
+        const int from = max(at, 0);
+        grp = Group{__shfl_sync(0xffffffffu, s0, from), __shfl_sync(0xffffffffu, s1, from), __shfl_sync(0xffffffffu, pre, from)};
+        if (at < 0 || b >= grp.end) grp = Group{b, b + 1, 0};
+    } else if (b < p.B) {
+        grp = find_group(p, b);
+    }
+    if (b < p.B) r = load_member(p, b, grp.prefix);
+}
+
 // A place in the sequence of units: request, kv head, row tile, unit inside the item, and what is left of the run from there on.
 // What starting and ending an item costs, in units (queries, merge of the warp groups, output): an item counts as its units + kItemCost,
 // the cost in front.  A cut inside the cost leaves the item whole to the run behind.
@@ -271,6 +292,12 @@ __device__ __forceinline__ size_t prefix_row(const AttnParams& p, int row0, int 
 }
 __device__ __forceinline__ void store_prefix_ml(const AttnParams&, int, int, int, float, float) {}
 __device__ __forceinline__ void store_prefix_ml(const SharedParams& p, int row0, int h, int r, float m, float l) { p.sh.base_ml[prefix_row(p, row0, h, r)] = make_float2(m, l); }
+template <int D>
+__device__ __forceinline__ void store_prefix_o(const AttnParams&, int, int, int, int, float4) {}
+template <int D>
+__device__ __forceinline__ void store_prefix_o(const SharedParams& p, int row0, int h, int r, int d, float4 o) {
+    *reinterpret_cast<float4*>(p.sh.base_o + prefix_row(p, row0, h, r) * D + d) = o;
+}
 // A row's own (reference, sum) and those of its prefix: both together, and the factors of the two weighted sums of values.
 struct JoinWeights { float m, l, own, prefix; };
 __device__ __forceinline__ JoinWeights join_weights(float2 own, float2 pre) {
@@ -304,31 +331,82 @@ __device__ __forceinline__ bool start_of_run(const ParamsOf<SHARED>& p, Cursor<R
     long long total, share, u_begin, u_end;
     bool whole;
     int place;
-    if (p.B <= 32) {
+    if constexpr (SHARED && UK < 64) {
+        // CTAs of a warp or two: every warp for itself, 32 requests at a time (a thread after another's requests, as below, would be a chain of loads for each)
+        const int chunks = (p.B + 31) / 32;
+        R r = {};
+        Group grp = {0, 0, 0};
+        int n_rt = 0, nt = 0;
+        auto load = [&](int c) {
+            r = {};
+            load_by_lane(p, 32 * c + lane, lane, r, grp);
+            n_rt = (r.qlen * p.group + ROWS - 1) / ROWS;
+            nt = max(1, (r.len + UK - 1) / UK);
+        };
+        long long units = 0, n_items = 0;
+        int most = 0;
+#pragma unroll 2
+        for (int c = 0; c < chunks; ++c) {
+            load(c);
+            units += static_cast<long long>(n_rt) * p.kv_heads * (nt + kItemCost<UK>);
+            n_items += static_cast<long long>(n_rt) * p.kv_heads;
+            if (n_rt > 0) most = max(most, nt);
+        }
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) {
+            units += __shfl_xor_sync(0xffffffffu, units, d);
+            n_items += __shfl_xor_sync(0xffffffffu, n_items, d);
+        }
+        total = units;
+        whole = n_items <= p.G && __reduce_max_sync(0xffffffffu, most) <= p.whole_units;
+        share = whole ? 1 : quotient(total + p.G - 1, p.G);
+        const long long all = whole ? n_items : total;
+        u_begin = min(all, share * blockIdx.x);
+        u_end = min(all, u_begin + share);
+        if (u_begin >= u_end) {
+            if (tid == 0) p.desc[8 * blockIdx.x] = 0;
+            return false;
+        }
+        long long carry = 0, before = 0;
+        int at = -1;
+        for (int c = 0;; ++c) {
+            if (chunks > 1) load(c);
+            const long long mine = static_cast<long long>(n_rt) * p.kv_heads * (whole ? 1 : nt + kItemCost<UK>);
+            long long inc = mine;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const long long u = __shfl_up_sync(0xffffffffu, inc, d);
+                if (lane >= d) inc += u;
+            }
+            before = carry + inc - mine;
+            const uint32_t hit = __ballot_sync(0xffffffffu, u_begin >= before && u_begin < before + mine);          // at most one lane
+            if (hit != 0 || c + 1 >= chunks) {
+                at = max(0, __ffs(hit) - 1);
+                cur.b = 32 * c + at;
+                break;
+            }
+            carry += __shfl_sync(0xffffffffu, inc, 31);
+        }
+        cur.rq.len = __shfl_sync(0xffffffffu, r.len, at);
+        cur.rq.row0 = __shfl_sync(0xffffffffu, r.row0, at);
+        cur.rq.qlen = __shfl_sync(0xffffffffu, r.qlen, at);
+        cur.rq.key0 = __shfl_sync(0xffffffffu, r.key0, at);
+        cur.rq.trow = __shfl_sync(0xffffffffu, r.trow, at);
+        cur.grp = Group{__shfl_sync(0xffffffffu, grp.begin, at), __shfl_sync(0xffffffffu, grp.end, at), __shfl_sync(0xffffffffu, grp.prefix, at)};
+        cur.nt = __shfl_sync(0xffffffffu, nt, at);
+        cur.n_rt = __shfl_sync(0xffffffffu, n_rt, at);
+        const long long off = u_begin - __shfl_sync(0xffffffffu, before, at);
+        const int size = whole ? 1 : cur.nt + kItemCost<UK>;
+        const uint32_t item = static_cast<uint32_t>(quotient(off, size));
+        cur.h = static_cast<int>(item / static_cast<uint32_t>(cur.n_rt));
+        cur.rt = static_cast<int>(item % static_cast<uint32_t>(cur.n_rt));
+        place = whole ? kItemCost<UK> : static_cast<int>(off - static_cast<long long>(item) * size);
+    } else if (p.B <= 32) {
         // a request per lane, every warp for itself: no barrier, nothing loaded twice (one request of 333 keys: 3200 -> 1900 clocks)
         R r = {};
         Group grp = {0, 0, 0};
-        if constexpr (SHARED) {
-            if (p.sh.prefixes) {
-                if (lane < p.B) r = load_group(p, lane);
-            } else {
-                if (p.sh.n_groups <= 32) {
-                    // a group per lane: no search, its loads beside those of the requests
-                    const bool is = lane < p.sh.n_groups;
-                    const int s0 = is ? p.sh.group_starts[lane] : 0x7fffffff, s1 = is ? p.sh.group_starts[lane + 1] : 0, pre = is ? prefix_of(p, lane) : 0;
-                    int at = -1;
-                    for (int i = 0; i < p.sh.n_groups; ++i) at = __shfl_sync(0xffffffffu, s0, i) <= lane ? i : at;
-                    const int from = max(at, 0);
-                    grp = Group{__shfl_sync(0xffffffffu, s0, from), __shfl_sync(0xffffffffu, s1, from), __shfl_sync(0xffffffffu, pre, from)};
-                    if (at < 0 || lane >= grp.end) grp = Group{lane, lane + 1, 0};
-                } else if (lane < p.B) {
-                    grp = find_group(p, lane);
-                }
-                if (lane < p.B) r = load_member(p, lane, grp.prefix);
-            }
-        } else {
-            if (lane < p.B) r = load_request(p, lane);
-        }
+        if constexpr (SHARED) load_by_lane(p, lane, lane, r, grp);
+        else if (lane < p.B) r = load_request(p, lane);
         const int n_rt = (r.qlen * p.group + ROWS - 1) / ROWS, nt = max(1, (r.len + UK - 1) / UK);
         const long long t_units = static_cast<long long>(n_rt) * p.kv_heads * (nt + kItemCost<UK>);
         const int t_items = n_rt * p.kv_heads;

@@ -81,8 +81,8 @@ struct AttnCfg {
     static constexpr int STAGE = 2 * KT * RB;              // K tile, V tile
     static constexpr int RING = KW * NST * STAGE;
     // the box in which the warp groups' outputs are added, [KW][ROWS][channels of a round + 4]: as many rounds as make it fit behind the ring
-    static constexpr int ML = KW * ROWS * 8;
-    static constexpr int box_bytes(int rounds) { return KW * ROWS * (D / rounds + 4) * 4; }
+    static constexpr int ML = KW == 1 ? 0 : KW * ROWS * 8;                       // (one group: nothing to add)
+    static constexpr int box_bytes(int rounds) { return KW == 1 ? 0 : KW * ROWS * (D / rounds + 4) * 4; }
     static constexpr int rounds() {
         int r = 1;
         while (r < D / 32 && (RING + ML + box_bytes(r) > 226 * 1024 || box_bytes(r) > 36 * 1024)) r *= 2;
@@ -95,6 +95,109 @@ struct AttnCfg {
     static_assert(DC % 16 == 0 && DC >= 32, "a round is whole channel tiles");
     static_assert(SMEM <= 226 * 1024, "shared memory of an SM");
 };
+
+// The end of an item, or of a run inside one, of a CTA of one warp group (what stands behind shared prefixes): rows joined to the prefix's part and written, or a
+// part.  Everything stays in the lanes that have it; the code is short because a CTA comes here once or twice, and code that runs for the first time comes from L2
+// (through shared memory, sixteen pieces a lane, this end cost half of what the whole pass does).
+template <class C, class Cur>
+__device__ __forceinline__ void end_of_item(const SharedParams& p, const Cur& cur, const float (&acc)[C::D / 16][C::NB][4], const float (&mx)[C::NB][2], const float (&sum)[C::NB][2],
+                                            bool entire, int slot, int rw)
+{
+    constexpr int D = C::D, NB = C::NB, ROWS = C::ROWS, LO = C::LO, DT = D / 16;
+    constexpr bool E4M3 = C::E4M3;
+    const int lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
+    const int R = cur.rq.qlen * p.group, first = cur.rt * ROWS + rw * 8 * NB;
+    const float vs = E4M3 && p.cache.v_scale != nullptr ? p.cache.v_scale[cur.h] : 1.0f;
+    const bool joins = entire && cur.first_key() > 0;
+    pdl_wait();                                            // the prefixes' parts are there, and their pass has read its queries
+#pragma unroll
+    for (int n = 0; n < NB; ++n) {
+        float w[2], wp[2] = {0.0f, 0.0f};
+        bool live[2];
+        const float* pre[2] = {nullptr, nullptr};
+        float* part[2];
+        uint16_t* out[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int rl = 8 * n + 2 * q + e, r = first + (LO == 1 ? rl & 3 : rl);       // (columns 4..7 of LO = 1 carry the low parts of rows 0..3)
+            live[e] = r < R && (LO != 1 || rl < 4);
+            float m = mx[n][e], l = sum[n][e];
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+            const RowOf at = row_of(p, r);
+            const size_t row = static_cast<size_t>(cur.rq.row0 + at.token) * p.heads + cur.h * p.group + at.head;
+            w[e] = vs;
+            if (joins) {
+                float2 x = make_float2(-INFINITY, 0.0f);
+                if (r < R) {
+                    x = __ldcg(p.sh.base_ml + row);
+                    pre[e] = p.sh.base_o + row * D;
+                }
+                const JoinWeights j = join_weights(make_float2(m, l), x);
+                m = j.m; l = j.l;
+                w[e] *= j.own;
+                wp[e] = l == 0.0f ? 0.0f : j.prefix / l;
+            }
+            if (entire) w[e] *= l == 0.0f ? 0.0f : 1.0f / l;
+            const size_t at_part = static_cast<size_t>(slot) * ROWS + rw * 8 * NB + rl;
+            part[e] = p.part_o + at_part * D;
+            // the row that this lane writes: bf16 numbers change places first, so that a lane has neighbouring channels of row g of the eight
+            const RowOf to = E4M3 ? at : row_of(p, first + 8 * n + g);
+            out[e] = p.O + static_cast<size_t>(cur.rq.row0 + to.token) * p.ldo + static_cast<size_t>(cur.h * p.group + to.head) * D;
+            if (g == 0 && live[e]) {
+                if (!entire) p.part_ml[at_part] = make_float2(m, l);
+                else if (p.lse != nullptr) p.lse[row] = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
+            }
+        }
+        // channels of acc[t][n]: E4M3 16 t + 2 g (rows 2 q, 2 q + 1), then 16 t + 2 g + 1; else 16 t + g, then 16 t + 8 + g
+        float b[DT][4];
+#pragma unroll
+        for (int t = 0; t < DT; ++t) {
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                b[t][e] = b[t][2 + e] = 0.0f;
+                if (joins && pre[e] != nullptr) {
+                    if (E4M3) {
+                        const float2 x = __ldcg(reinterpret_cast<const float2*>(pre[e] + 16 * t + 2 * g));
+                        b[t][e] = x.x; b[t][2 + e] = x.y;
+                    } else {
+                        b[t][e] = __ldcg(pre[e] + 16 * t + g);
+                        b[t][2 + e] = __ldcg(pre[e] + 16 * t + 8 + g);
+                    }
+                }
+            }
+        }
+        const bool writes = first + 8 * n + g < R && (LO != 1 || g < 4);
+#pragma unroll
+        for (int t = 0; t < DT; ++t) {
+            float v[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[i] = acc[t][n][i] * w[i & 1];
+                if (LO == 1) v[i] += __shfl_xor_sync(0xffffffffu, v[i], 2);
+                v[i] = fmaf(b[t][i], wp[i & 1], v[i]);
+            }
+            if (!entire) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    if (!live[e]) continue;
+                    if (E4M3) *reinterpret_cast<float2*>(part[e] + 16 * t + 2 * g) = make_float2(v[e], v[2 + e]);
+                    else { part[e][16 * t + g] = v[e]; part[e][16 * t + 8 + g] = v[2 + e]; }
+                }
+            } else if (E4M3) {
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                    if (live[e]) *reinterpret_cast<uint32_t*>(out[e] + 16 * t + 2 * g) = bf16x2(v[e], v[2 + e]);
+            } else {
+                const uint32_t x0 = transpose8x8(bf16x2(v[0], v[1])), x1 = transpose8x8(bf16x2(v[2], v[3]));
+                if (writes) {
+                    *reinterpret_cast<uint32_t*>(out[0] + 16 * t + 2 * q) = x0;
+                    *reinterpret_cast<uint32_t*>(out[0] + 16 * t + 8 + 2 * q) = x1;
+                }
+            }
+        }
+    }
+}
 
 // CAUSAL: the rows of an item may see different numbers of keys.  SHARED: see SharedPass.
 template <class C, bool CAUSAL, bool SHARED>
@@ -112,7 +215,6 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const Pa
     static_assert(GT % CH == 0 || CH % GT == 0, "rows are copied by whole groups of lanes");
     extern __shared__ __align__(128) uint8_t smem[];
     __shared__ uint32_t s_dropped[RW * KW];                // per warp: see drop_nonfinite
-    __shared__ float s_prefix[SHARED ? ROWS : 1];          // weight of the prefix's part
     start_pass(p);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int g = lane >> 2, q = lane & 3;
@@ -402,13 +504,44 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const Pa
 
         const bool item_end = cur.j + 1 == cur.nt;
         if (item_end || cur.left == 1) {
+            if constexpr (SHARED && KW == 1) {
+                if (CAUSAL && tail < cur.rq.len) {
+                    dropped = __any_sync(0xffffffffu, dropped);
+                    if (RW > 1) {
+                        if (lane == 0) s_dropped[warp] = dropped;
+                        asm volatile("bar.sync 1, %0;" ::"n"(GT) : "memory");
+                        for (int w = 0; w < RW; ++w) dropped |= s_dropped[w] != 0;
+                    }
+                }
+                const bool entire = item_end && part_j == 0;
+                const int slot = 2 * blockIdx.x + (first_part ? 0 : 1);
+                end_of_item<C>(p, cur, acc, mx, sum, entire, slot, rw);
+                if (CAUSAL && dropped) {
+                    // (each thread reads what others have written; and s_dropped is free again)
+                    if (RW == 1) __syncwarp();
+                    else asm volatile("bar.sync 1, %0;" ::"n"(GT) : "memory");
+                    const int rows_here = min(ROWS, cur.rq.qlen * p.group - cur.rt * ROWS);
+                    for (int i = tid; i < rows_here * (D / 4); i += C::THREADS) {
+                        const int rl = i / (D / 4), d = 4 * (i % (D / 4));
+                        const RowOf at = row_of(p, cur.rt * ROWS + rl);
+                        const float4 z = nonfinite_values<E4M3>(p, cur.table_row(), cur.h, cur.first_key() + max(tail, part_j * UK),
+                                                                cur.first_key() + min(cur.rq.len - cur.rq.qlen + at.token + 1, (cur.j + 1) * UK), d);
+                        if (entire) {
+                            uint2* o = reinterpret_cast<uint2*>(p.O + static_cast<size_t>(cur.rq.row0 + at.token) * p.ldo + static_cast<size_t>(cur.h * p.group + at.head) * D + d);
+                            const uint2 v = *o;
+                            *o = make_uint2(bf16x2(bf16_lo(v.x) + z.x, bf16_hi(v.x) + z.y), bf16x2(bf16_lo(v.y) + z.z, bf16_hi(v.y) + z.w));
+                        } else {
+                            float4* o = reinterpret_cast<float4*>(p.part_o + (static_cast<size_t>(slot) * ROWS + rl) * D + d);
+                            const float4 v = *o;
+                            *o = make_float4(v.x + z.x, v.y + z.y, v.z + z.z, v.w + z.w);
+                        }
+                    }
+                }
+            } else {
             // ---- end of an item or of this run: add the warp groups, write the rows or the part
             float* box = reinterpret_cast<float*>(smem + C::RING);
             float2* ml = reinterpret_cast<float2*>(smem + C::RING + C::BOX);
-            if (SHARED) pdl_wait();                        // the prefixes' parts are there, and their pass has read its queries
-            const bool entire = item_end && part_j == 0;
-            const bool prefix_pass = SHARED && shared_prefixes(p), joins = SHARED && entire && !prefix_pass && cur.first_key() > 0;
-            const bool final = entire && !prefix_pass;                           // O and lse, not a part of them
+            const bool entire = item_end && part_j == 0;                         // (SHARED: of a prefix, which ends as a part of its row)
             const int slot = 2 * blockIdx.x + (first_part ? 0 : 1);              // part at the start of the run, or at its end
             const int R = cur.rq.qlen * p.group;
             const float vs = E4M3 ? (p.cache.v_scale != nullptr ? p.cache.v_scale[cur.h] : 1.0f) : 1.0f;
@@ -443,24 +576,12 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const Pa
                         const float2 o = ml[w * ROWS + rl];
                         l += o.y * exp2_approx(o.x - u);
                     }
-                    float w = exp2_approx(mx[n][e] - u) * vs;
-                    if constexpr (SHARED) {
-                        const int r = cur.rt * ROWS + (LO == 1 ? rl & 3 : rl);       // (the low parts of a row are weighted as the row)
-                        if (joins) {
-                            float2 pre = make_float2(-INFINITY, 0.0f);
-                            if (r < R) pre = __ldcg(p.sh.base_ml + prefix_row(p, cur.rq.row0, cur.h, r));
-                            const JoinWeights j = join_weights(make_float2(m, l), pre);
-                            m = j.m; l = j.l;
-                            w *= j.own;
-                            if (kg == 0 && g == 0) s_prefix[rl] = l == 0.0f ? 0.0f : j.prefix / l;
-                        }
-                    }
-                    wgt[n][e] = w * (final ? (l == 0.0f ? 0.0f : 1.0f / l) : 1.0f);
+                    wgt[n][e] = exp2_approx(mx[n][e] - u) * vs * (entire && !SHARED ? (l == 0.0f ? 0.0f : 1.0f / l) : 1.0f);
                     if (kg == 0 && g == 0) {
                         const int r = cur.rt * ROWS + rl;
                         if (r < R) {
                             if (!entire) p.part_ml[static_cast<size_t>(slot) * ROWS + rl] = make_float2(m, l);
-                            else if (prefix_pass) store_prefix_ml(p, cur.rq.row0, cur.h, r, m, l);
+                            else if (SHARED) store_prefix_ml(p, cur.rq.row0, cur.h, r, m, l);
                             else if (p.lse != nullptr) {
                                 const RowOf at = row_of(p, r);
                                 p.lse[static_cast<size_t>(cur.rq.row0 + at.token) * p.heads + cur.h * p.group + at.head] = l == 0.0f ? -INFINITY : (m + log2f(l)) * kLn2;
@@ -489,25 +610,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const Pa
                         }
                     }
                 __syncthreads();
-                // (the prefix's part of several pieces is requested together: a thread of a small CTA has up to sixteen)
-                constexpr int PIECES = ROWS * (DC / 4) / C::THREADS, AHEAD = !SHARED || PIECES < 1 ? 1 : (PIECES < 8 ? PIECES : 8);
-                for (int i0 = tid; i0 < rows_here * (DC / 4); i0 += AHEAD * C::THREADS) {
-                    float4 pre[AHEAD];
-                    if constexpr (SHARED) {
-                        if (joins) {
-#pragma unroll
-                            for (int a = 0; a < AHEAD; ++a) {
-                                const int i = i0 + a * C::THREADS;
-                                pre[a] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                                if (i < rows_here * (DC / 4))
-                                    pre[a] = __ldcg(reinterpret_cast<const float4*>(p.sh.base_o + prefix_row(p, cur.rq.row0, cur.h, cur.rt * ROWS + i / (DC / 4)) * D + round * DC + 4 * (i % (DC / 4))));
-                            }
-                        }
-                    }
-#pragma unroll
-                    for (int a = 0; a < AHEAD; ++a) {
-                    const int i = i0 + a * C::THREADS;
-                    if (SHARED && i >= rows_here * (DC / 4)) break;
+                for (int i = tid; i < rows_here * (DC / 4); i += C::THREADS) {
                     const int rl = i / (DC / 4), d = 4 * (i % (DC / 4));
                     float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
@@ -520,22 +623,15 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const Pa
                         }
                     }
                     const RowOf at = row_of(p, cur.rt * ROWS + rl);
-                    if constexpr (SHARED) {
-                        if (joins) {
-                            const float4 x = pre[a];
-                            const float w = s_prefix[rl];
-                            o.x = fmaf(x.x, w, o.x); o.y = fmaf(x.y, w, o.y); o.z = fmaf(x.z, w, o.z); o.w = fmaf(x.w, w, o.w);
-                        } else if (entire && prefix_pass) {
-                            *reinterpret_cast<float4*>(p.sh.base_o + prefix_row(p, cur.rq.row0, cur.h, cur.rt * ROWS + rl) * D + round * DC + d) = o;
-                            continue;
-                        }
+                    if (SHARED && entire) {
+                        store_prefix_o<D>(p, cur.rq.row0, cur.h, cur.rt * ROWS + rl, round * DC + d, o);
+                        continue;
                     }
                     if (entire)
                         *reinterpret_cast<uint2*>(p.O + static_cast<size_t>(cur.rq.row0 + at.token) * p.ldo + static_cast<size_t>(cur.h * p.group + at.head) * D +
                                                   round * DC + d) = make_uint2(bf16x2(o.x, o.y), bf16x2(o.z, o.w));
                     else
                         *reinterpret_cast<float4*>(p.part_o + (static_cast<size_t>(slot) * ROWS + rl) * D + round * DC + d) = o;
-                    }
                 }
             }
             if (CAUSAL && dropped) {
@@ -556,6 +652,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_paged_kernel(const Pa
                             *o = make_float4(v.x + z.x, v.y + z.y, v.z + z.z, v.w + z.w);
                         }
                     }
+            }
             }
             fresh = true;
             first_part = false;
@@ -589,11 +686,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) attention_join_kernel(const Para
     if (!load_cut(p, blockIdx.x, x)) return;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int ry = warp / JOIN_SPLIT, part = warp % JOIN_SPLIT;
-    // (SHARED: there are many runs and few of them start inside an item; one CTA takes all rows of its tile)
-    for (int y = blockIdx.y * JOIN_ROWS; y == static_cast<int>(blockIdx.y) * JOIN_ROWS || (SHARED && y < rows_of_tile); y += gridDim.y * JOIN_ROWS) {
-    if (SHARED && x.rt * rows_of_tile + y >= x.qlen * p.group) return;
-    if (SHARED && y != static_cast<int>(blockIdx.y) * JOIN_ROWS) __syncthreads();
-    const int rl = y + ry, r = x.rt * rows_of_tile + rl;
+    const int rl = blockIdx.y * JOIN_ROWS + ry, r = x.rt * rows_of_tile + rl;
     const bool live = r < x.qlen * p.group;
     constexpr int V = D / 32;                              // channels of a lane
     float o[V];
@@ -626,10 +719,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) attention_join_kernel(const Para
     for (int i = 0; i < V; ++i) s_o[ry][part][lane * V + i] = o[i];
     if (lane == 0) s_ml[ry][part] = make_float2(m, l);
     __syncthreads();
-    if (part != 0 || !live) {
-        if (SHARED) continue;
-        return;
-    }
+    if (part != 0 || !live) return;
     float mm = -INFINITY, ll = 0.0f, w[JOIN_SPLIT];
 #pragma unroll
     for (int s = 0; s < JOIN_SPLIT; ++s) mm = fmaxf(mm, s_ml[ry][s].x);
@@ -639,30 +729,19 @@ __global__ void __launch_bounds__(JOIN_THREADS) attention_join_kernel(const Para
         w[s] = exp2_approx(s_ml[ry][s].x - u);
         ll += s_ml[ry][s].y * w[s];
     }
-    const float* pre = nullptr;                            // the prefix's part
-    float wp = 0.0f;
     if constexpr (SHARED) {
+        // a cut item of the prefixes ends as a part of its row
         const size_t row = prefix_row(p, x.row0, x.h, r);
-        if (shared_prefixes(p)) {
-            // (cut items of the first pass end as parts of their rows)
-            float* out = p.sh.base_o + row * D + lane * V;
+        float* out = p.sh.base_o + row * D + lane * V;
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                float a = 0.0f;
+        for (int i = 0; i < V; ++i) {
+            float a = 0.0f;
 #pragma unroll
-                for (int s = 0; s < JOIN_SPLIT; ++s) a += s_o[ry][s][lane * V + i] * w[s];
-                out[i] = a;
-            }
-            if (lane == 0) p.sh.base_ml[row] = make_float2(mm, ll);
-            continue;
+            for (int s = 0; s < JOIN_SPLIT; ++s) a += s_o[ry][s][lane * V + i] * w[s];
+            out[i] = a;
         }
-        if (x.joins) {
-            const JoinWeights j = join_weights(make_float2(mm, ll), __ldcg(p.sh.base_ml + row));
-            mm = j.m; ll = j.l; wp = j.prefix;
-#pragma unroll
-            for (int s = 0; s < JOIN_SPLIT; ++s) w[s] *= j.own;
-            pre = p.sh.base_o + row * D + lane * V;
-        }
+        if (lane == 0) p.sh.base_ml[row] = make_float2(mm, ll);
+        return;
     }
     const float inv = ll == 0.0f ? 0.0f : 1.0f / ll;
     const RowOf at = row_of(p, r);
@@ -676,13 +755,75 @@ __global__ void __launch_bounds__(JOIN_THREADS) attention_join_kernel(const Para
             a += s_o[ry][s][lane * V + i] * w[s];
             b += s_o[ry][s][lane * V + i + 1] * w[s];
         }
-        if (SHARED && pre != nullptr) {
-            a = fmaf(__ldcg(pre + i), wp, a);
-            b = fmaf(__ldcg(pre + i + 1), wp, b);
-        }
         *reinterpret_cast<uint32_t*>(orow + i) = bf16x2(a * inv, b * inv);
     }
     if (lane == 0 && p.lse != nullptr) p.lse[static_cast<size_t>(x.row0 + at.token) * p.heads + hh] = ll == 0.0f ? -INFINITY : (mm + log2f(ll)) * kLn2;
+}
+
+// What the pass behind the prefixes has cut (into two or three parts, mostly): a warp per row takes them in order, then the prefix's part.
+template <int D>
+__global__ void __launch_bounds__(JOIN_THREADS) attention_join_rest_kernel(const SharedParams p, int rows_of_tile)
+{
+    constexpr int V = D / 32;                              // channels of a lane
+    pdl_launch_dependents();
+    pdl_wait();
+    Cut x;
+    if (!load_cut(p, blockIdx.x, x)) return;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    auto load = [&](const float* src, float (&v)[V]) {
+        if (V == 2) {
+            const float2 t = __ldcg(reinterpret_cast<const float2*>(src));
+            v[0] = t.x; v[1] = t.y;
+        } else {
+#pragma unroll
+            for (int i = 0; i < V; i += 4) {
+                const float4 t = __ldcg(reinterpret_cast<const float4*>(src + i));
+                v[i] = t.x; v[i + 1] = t.y; v[i + 2] = t.z; v[i + 3] = t.w;
+            }
+        }
+    };
+#pragma unroll 2
+    for (int rl = warp; rl < rows_of_tile; rl += JOIN_THREADS / 32) {
+        const int r = x.rt * rows_of_tile + rl;
+        if (r >= x.qlen * p.group) break;
+        const size_t row = prefix_row(p, x.row0, x.h, r);
+        float o[V];
+        float2 ml = make_float2(-INFINITY, 0.0f);
+#pragma unroll
+        for (int i = 0; i < V; ++i) o[i] = 0.0f;
+        constexpr int AHEAD = 4;
+        const int n = x.n + (x.joins ? 1 : 0);
+        for (int s0 = 0; s0 < n; s0 += AHEAD) {
+            float2 part_ml[AHEAD];
+            float part[AHEAD][V];
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a) {
+                const int s = s0 + a;
+                if (s < x.n) {
+                    const size_t at = (2 * static_cast<size_t>(x.first + s) + (s == 0 ? x.slot_first : 0)) * rows_of_tile + rl;
+                    part_ml[a] = __ldcg(p.part_ml + at);
+                    load(p.part_o + at * D + lane * V, part[a]);
+                } else if (s < n) {
+                    part_ml[a] = __ldcg(p.sh.base_ml + row);
+                    load(p.sh.base_o + row * D + lane * V, part[a]);
+                }
+            }
+#pragma unroll
+            for (int a = 0; a < AHEAD; ++a) {
+                if (s0 + a >= n) break;
+                const JoinWeights j = join_weights(ml, part_ml[a]);
+                ml = make_float2(j.m, j.l);
+#pragma unroll
+                for (int i = 0; i < V; ++i) o[i] = o[i] * j.own + part[a][i] * j.prefix;
+            }
+        }
+        const float inv = ml.y == 0.0f ? 0.0f : 1.0f / ml.y;
+        const RowOf at = row_of(p, r);
+        const int hh = x.h * p.group + at.head;
+        uint16_t* out = p.O + static_cast<size_t>(x.row0 + at.token) * p.ldo + static_cast<size_t>(hh) * D + lane * V;
+#pragma unroll
+        for (int i = 0; i < V; i += 2) *reinterpret_cast<uint32_t*>(out + i) = bf16x2(o[i] * inv, o[i + 1] * inv);
+        if (lane == 0 && p.lse != nullptr) p.lse[static_cast<size_t>(x.row0 + at.token) * p.heads + hh] = ml.y == 0.0f ? -INFINITY : (ml.x + log2f(ml.y)) * kLn2;
     }
 }
 
@@ -769,7 +910,7 @@ struct PickSolo {
     using C = AttnCfg<D, E4M3, CLS <= 1 ? 1 : 2, CLS == 3 ? 2 : 1, 1, KT, 3, E4M3 ? 0 : kLo<CLS>>;
 };
 template <class C>
-constexpr int solo_ctas() { return 224 * 1024 / (C::SMEM + 2048); }              // to an SM; 2 KB for its static shared memory and what the system takes
+constexpr int solo_ctas() { return 224 * 1024 / (C::SMEM + 2048) < 8 / C::RW ? 224 * 1024 / (C::SMEM + 2048) : 8 / C::RW; }     // to an SM: eight warps with 255 registers a thread; 2 KB for static shared memory and what the system takes
 
 int rows_class(int max_rows) { return max_rows <= 4 ? 0 : (max_rows <= 8 ? 1 : (max_rows <= 16 ? 2 : (max_rows <= 32 ? 3 : 4))); }
 // The tcgen05 kernel (attention_rows.cu): above 32 rows always; 17 to 32 rows in bf16 with D = 128 and a table of 4096 tokens or more (the lengths
@@ -809,7 +950,7 @@ cudaError_t launch_main(const ParamsOf<SHARED>& p, const AttnArgs& a, cudaStream
 template <bool SHARED, int D>
 cudaError_t launch_join(const ParamsOf<SHARED>& p, int rows_of_tile, long long max_rows, cudaStream_t st)
 {
-    const int rows = SHARED && rows_of_tile <= 32 ? JOIN_ROWS : (max_rows < rows_of_tile ? static_cast<int>(max_rows) : rows_of_tile);
+    const int rows = max_rows < rows_of_tile ? static_cast<int>(max_rows) : rows_of_tile;
     const bool many = rows_of_tile >= 128;                 // the parts of attention_rows.cu
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(p.G), static_cast<unsigned>(many ? (rows + 31) / 32 * (D / 64) : (rows + JOIN_ROWS - 1) / JOIN_ROWS), 1);
@@ -820,6 +961,12 @@ cudaError_t launch_join(const ParamsOf<SHARED>& p, int rows_of_tile, long long m
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
+    if constexpr (SHARED) {
+        if (!many && !p.sh.prefixes) {
+            cfg.gridDim.y = 1;
+            return cudaLaunchKernelEx(&cfg, attention_join_rest_kernel<D>, p, rows_of_tile);
+        }
+    }
     return many ? cudaLaunchKernelEx(&cfg, attention_join_rows_kernel<D, SHARED>, p, rows_of_tile) : cudaLaunchKernelEx(&cfg, attention_join_kernel<D, SHARED>, p, rows_of_tile);
 }
 template <bool SHARED, class C>

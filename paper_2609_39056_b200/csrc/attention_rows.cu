@@ -436,13 +436,15 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Par
         // ---------------------------------------------------------------------------------------- MMA issue for a pair: first set, second set, in turn
         const bool leader = elect_one();
         const uint32_t idesc_s = umma_idesc_f16(128, KT, !E4M3, false), idesc_o = umma_idesc_f16(128, D, !E4M3, true);
-        int mine[2] = {0, 0}, own_items[2] = {0, 0};       // scores issued for a set, items with rows of the set
+        // Bit `set` of each: whether scores were issued for the set, and whether an odd number of them; the same of its items.  (Not arrays: both products stand in a
+        // loop over the sets, once each, because code that runs for the first time comes instruction by instruction from L2.)
+        uint32_t scored = 0, scored_odd = 0, begun = 0, begun_odd = 0, read_out = 0;
         int t = 0, item = 0;
         bool ok = true;
         // scores of tile `of`, over the probabilities of the set's tile before: its product must be complete (products into different accumulators are not ordered)
         auto scores = [&](int set, int of) -> bool {
             if (!wait_all(kv_full(of % ST), (of / ST) & 1, W_R_KV_FULL)) return false;
-            if (mine[set] > 0 && !wait_all(pv_done(set), (mine[set] - 1) & 1, W_R_PV_DONE)) return false;
+            if ((scored >> set & 1) && !wait_all(pv_done(set), scored_odd >> set & 1 ^ 1, W_R_PV_DONE)) return false;
             tcgen05_fence_after_sync();
             if (leader) {
                 const uint32_t k0 = k_s + (of % ST) * C::TILE, q0 = q_s + set * 128 * 128;
@@ -453,13 +455,14 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Par
                 umma_commit(s_full(set));
             }
             __syncwarp();
-            ++mine[set];
+            scored |= 1u << set;
+            scored_odd ^= 1u << set;
             return true;
         };
         // O += P V of tile `of`; the item's first product starts its O, once the set's item before has been read out
         auto product = [&](int set, int of, bool first, bool last_user) -> bool {
-            if (!wait_all(p_full(0, set), (mine[set] - 1) & 1, W_R_P_FULL)) return false;
-            if (first && own_items[set] > 1 && !wait_all(set == 0 ? o_free : ml_full, own_items[set] & 1, W_R_O_FREE)) return false;
+            if (!wait_all(p_full(0, set), scored_odd >> set & 1 ^ 1, W_R_P_FULL)) return false;
+            if (first && (read_out >> set & 1) && !wait_all(set == 0 ? o_free : ml_full, begun_odd >> set & 1, W_R_O_FREE)) return false;
             tcgen05_fence_after_sync();
             if (leader) {
                 const uint32_t v0 = v_s + (of % ST) * C::TILE, o = tmem + C::O_COL + set * D;
@@ -480,25 +483,28 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Par
         auto second_has_rows = [&]() { return cur.rt * ROWS + 128 < cur.rq.qlen * p.group; };
         while (ok && cur.left > 0) {
             // an item: its first scores, then tile by tile product and the next scores, set by set
-            const bool both = second_has_rows();
-            bool ends = last_of_item(), first = true;
+            const uint32_t sets = second_has_rows() ? 3 : 1;
             ok = wait_all(q_full, item & 1, W_R_Q_FULL);
             ++item;
-            ++own_items[0];
-            own_items[1] += both;
-            ok = ok && scores(0, t) && (!both || scores(1, t));
-            if (ok && ends && leader) umma_commit(q_empty);
-            while (ok) {
-                cur.advance(p);
-                const bool next_ends = !ends && last_of_item();
-                ok = product(0, t, first, !both) && (ends || scores(0, t + 1));
-                if (ok && both) ok = product(1, t, first, true) && (ends || scores(1, t + 1));
+            read_out = begun;                              // (of an earlier item)
+            begun |= sets;
+            begun_odd ^= sets;
+            bool ends = false;
+            for (int k = -1; ok; ++k) {
+                const bool next = k < 0 || !ends, next_ends = next && last_of_item();
+#pragma unroll 1
+                for (int set = 0; ok && (sets >> set) != 0; ++set) {
+                    if (k >= 0) ok = product(set, t, k == 0, (sets >> set) == 1);
+                    if (ok && next) ok = scores(set, k < 0 ? t : t + 1);
+                }
                 if (ok && next_ends && leader) umma_commit(q_empty);
                 __syncwarp();
-                ++t;
-                if (ends) break;
+                if (k >= 0) {
+                    ++t;
+                    if (ends) break;
+                }
                 ends = next_ends;
-                first = false;
+                cur.advance(p);
             }
         }
     } else if (warp < MMA_WARP) {
