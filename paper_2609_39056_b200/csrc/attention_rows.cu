@@ -201,12 +201,12 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Par
     const uint32_t raw_s = v_s + ST * C::TILE;
     auto raw_full = [&](int i) { return bar0 + 8u * (2 * ST + 12 + i); };
     auto raw_empty = [&](int i) { return bar0 + 8u * (2 * ST + 12 + RU + i); };
-    // an item's queries, two warps their share each of the rows that exist (the others never matter)
-    auto load_queries = [&](int part) {
+    // an item's queries, two warps (PAIR: for the first item all warps) their share each of the rows that exist (the others never matter)
+    auto load_queries = [&](int part, int parts) {
                         const int rows_here = min(ROWS, cur.rq.qlen * p.group - cur.rt * ROWS);
                         constexpr int QCH = D / 8, QSTEP = 32 / QCH;
 #pragma unroll 4
-                        for (int i = part * QSTEP; i < rows_here; i += C::QW * QSTEP) {
+                        for (int i = part * QSTEP; i < rows_here; i += parts * QSTEP) {
                             const int rl = i + lane / QCH, qc = lane % QCH, r = cur.rt * ROWS + rl;
                             const bool live = rl < rows_here;
                             const uint16_t* src = p.Q + 8 * qc;
@@ -234,7 +234,8 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Par
                             }
                         }
     };
-    if (warp > MMA_WARP + LW - C::QW && warp <= MMA_WARP + LW) load_queries(warp - 1 - MMA_WARP - (LW - C::QW));
+    if (C::PAIR) load_queries(warp, C::THREADS / 32);      // (256 rows by two warps take 3 us)
+    else if (warp > MMA_WARP + LW - C::QW && warp <= MMA_WARP + LW) load_queries(warp - 1 - MMA_WARP - (LW - C::QW), C::QW);
     if (tid == 0) {
         abort_word = 0;
         s_dropped[0] = s_dropped[1] = -1;
@@ -248,6 +249,12 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Par
     if (warp == MMA_WARP) {
         tmem_alloc(smem_u32(&tmem_slot), 512);
         tmem_relinquish();
+    }
+    if (C::PAIR) {
+        // the first item's queries, visible to the tensor core (the loading warps say so below)
+        if (!E4M3) asm volatile("cp.async.wait_all;" ::: "memory");
+        fence_proxy_async_smem();
+        __syncwarp();
     }
     tcgen05_fence_before_sync();
     __syncthreads();
@@ -1054,7 +1061,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Par
                 if (item > 0) {
                     ok = wait_all(q_empty, (item - 1) & 1, W_R_Q_EMPTY);
                     if (!ok) break;
-                    load_queries(w - (LW - C::QW));
+                    load_queries(w - (LW - C::QW), C::QW);
                 }
                 ++item;
                 signal(q_full);
