@@ -160,7 +160,7 @@ rudder_status rudder_attention_shared(const rudder_attention_shared_args* args, 
 size_t rudder_lora_workspace_bytes(const rudder_lora_args* a)
 {
     if (check_lora_shape(a) != RUDDER_OK) return 0;
-    return lora_workspace_bytes(a->M, a->K, a->R, a->n_adapters, sm_count());
+    return lora_workspace_bytes(a->M, a->K, a->N, a->R, a->n_adapters, sm_count());
 }
 
 rudder_status rudder_lora(const rudder_lora_args* a, void* workspace, size_t workspace_bytes, void* stream)

@@ -207,7 +207,7 @@ cudaError_t launch_page_copy(const PageCopyArgs& a, const rudder_paged_cache* ca
 cudaError_t launch_page_pool(const PagePoolArgs& a, bool compact, cudaStream_t st);
 constexpr int kMaxRank = 256, kMaxAdapters = 4096;
 cudaError_t lora_init();
-size_t lora_workspace_bytes(int M, int K, int R, int n_adapters, int sm_count);
+size_t lora_workspace_bytes(int M, int K, int N, int R, int n_adapters, int sm_count);
 cudaError_t launch_lora(const LoraArgs& a, void* workspace, int sm_count, cudaStream_t st);
 cudaError_t linear_a16_init();
 bool linear_a16_fits(int K);              // the widest layer whose rows fit in shared memory

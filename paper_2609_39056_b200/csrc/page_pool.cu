@@ -23,7 +23,9 @@ namespace rudder {
 
 namespace {
 
-constexpr int PF_THREADS = 512;            // fork, copy
+// Fork, copy: CTAs of 256 threads, eight for each SM although three fit at a time (the hardware hands out the rest as they end).  64 children x 12 layers 46 us, with CTAs of
+// 512 threads that stay 52; four CTAs at a time with 64 registers a thread 55, the eight pieces no longer in flight together.
+constexpr int PF_THREADS = 256, PF_PER_SM = 8;
 constexpr int PP_THREADS = 1024;           // release, compact: CTAs of one cluster
 constexpr int PP_MAX_CTAS = 8;
 
@@ -96,7 +98,7 @@ __device__ __forceinline__ int fork_length(const PageForkArgs& a, int i, int s) 
 }
 
 template <int CAP>
-__global__ void __launch_bounds__(PF_THREADS) page_fork_kernel(const PageForkArgs a, const __grid_constant__ Layers<CAP> layers)
+__global__ void __launch_bounds__(PF_THREADS, 2) page_fork_kernel(const PageForkArgs a, const __grid_constant__ Layers<CAP> layers)
 {
     extern __shared__ int s_fork[];
     int* owner = s_fork;                                           // [B] first child that goes to the row
@@ -182,7 +184,7 @@ __global__ void __launch_bounds__(PF_THREADS) page_fork_kernel(const PageForkArg
 
 // ------------------------------------------------------------------------------------------------------------------- copies by a list
 template <int CAP>
-__global__ void __launch_bounds__(PF_THREADS) page_copy_kernel(const PageCopyArgs a, const __grid_constant__ Layers<CAP> layers)
+__global__ void __launch_bounds__(PF_THREADS, 2) page_copy_kernel(const PageCopyArgs a, const __grid_constant__ Layers<CAP> layers)
 {
     pdl_launch_dependents();
     pdl_wait();
@@ -204,7 +206,12 @@ __global__ void __launch_bounds__(PF_THREADS) page_copy_kernel(const PageCopyArg
 }
 
 // ------------------------------------------------------------------------------------------------------------------- release, compact
+// All CTAs of the cluster have written what they have written.  (One CTA alone: a cluster's barrier costs it a microsecond more.)
 __device__ __forceinline__ void pool_sync() {
+    if (gridDim.x == 1) {
+        __syncthreads();
+        return;
+    }
     __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
@@ -242,6 +249,7 @@ __device__ __forceinline__ void held_entries(const PagePoolArgs& a, F f) {
 
 constexpr int PP_EACH = 4;                 // neighbouring pages of a thread
 constexpr int PP_TILE = PP_THREADS * PP_EACH;
+constexpr int PP_WORK = 4096;              // pages or table entries of a CTA: 48 requests x 512 columns 19 us, with 16384 23
 
 template <bool COMPACT>
 __global__ void __launch_bounds__(PP_THREADS) page_pool_kernel(const PagePoolArgs a)
@@ -383,11 +391,11 @@ constexpr int kFewLayers = 8;              // 128 instead of 2048 bytes of argum
 
 size_t fork_smem(int B, int n) { return sizeof(int) * (static_cast<size_t>(B) + 2 * static_cast<size_t>(n) + (static_cast<size_t>(B) + 31) / 32); }
 
-// CTAs for `units` warp-sized pieces of copying: four CTAs of 512 threads fill an SM
+// CTAs for `units` warp-sized pieces of copying
 int copy_ctas(long long units, int sm_count)
 {
     const long long ctas = (units + PF_THREADS / 32 - 1) / (PF_THREADS / 32);
-    return static_cast<int>(ctas < 1 ? 1 : (ctas > 4 * sm_count ? 4 * sm_count : ctas));
+    return static_cast<int>(ctas < 1 ? 1 : (ctas > PF_PER_SM * sm_count ? PF_PER_SM * sm_count : ctas));
 }
 
 }  // namespace
@@ -417,10 +425,10 @@ cudaError_t launch_page_copy(const PageCopyArgs& a, const rudder_paged_cache* ca
 
 cudaError_t launch_page_pool(const PagePoolArgs& a, bool compact, cudaStream_t st)
 {
-    // a CTA per 4096 pages or table entries, at most a portable cluster
+    // a CTA per PP_WORK pages or table entries, at most a portable cluster
     const long long work = std::max<long long>(a.n_pages, static_cast<long long>(a.B) * a.max_pages);
     int ctas = 1;
-    while (ctas < PP_MAX_CTAS && static_cast<long long>(ctas) * PP_TILE < work) ctas *= 2;
+    while (ctas < PP_MAX_CTAS && static_cast<long long>(ctas) * PP_WORK < work) ctas *= 2;
     return launch_pdl(compact ? page_pool_kernel<true> : page_pool_kernel<false>, dim3(static_cast<unsigned>(ctas), 1, 1), PP_THREADS, 0, ctas, st, a);
 }
 
