@@ -28,7 +28,7 @@ def build(force: bool = False, verbose: bool = False) -> Path:
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     tmp = LIB.with_suffix(f".{os.getpid()}.tmp")
-    cmd = [nvcc, "--split-compile=0", "-std=c++17", "-O3", "-lineinfo", "-gencode", "arch=compute_100a,code=sm_100a",
+    cmd = [nvcc, "-std=c++17", "-O3", "-lineinfo", "-gencode", "arch=compute_100a,code=sm_100a",
            "-Xcompiler", "-fPIC", "-shared", "-cudart", "static", "-I", str(INCLUDE),
            "-o", str(tmp), str(CSRC / "rudder_lib.cu")]
     if verbose:

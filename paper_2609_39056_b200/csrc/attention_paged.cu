@@ -903,7 +903,7 @@ template <> struct Pick<256, true, 3> { using C = AttnCfg<256, true, 2, 2, 4, 16
 
 // What stands behind shared prefixes: many short items (16 candidates x 8 heads of 64 keys each), where adding up eight warps' parts at an item's end costs more than
 // its keys.  One warp (up to 16 rows) or two (32) are a CTA of their own, several to an SM, with an item each: as many bytes in flight, nothing to add up.
-// 512 items of 16 rows x 16 to 80 keys 38 -> SOLO_US us; 512 items of 12 rows x up to 1024 keys in E4M3 67 -> SOLO2_US us.
+// 512 items of 16 rows x 16 to 80 keys 38 -> 17 us; 512 items of 12 rows x up to 1024 keys in E4M3 67 -> 33 us.  (Four stages instead of three, so fewer CTAs: 26 and 63.)
 template <int D, bool E4M3, int CLS>
 struct PickSolo {
     static constexpr int KT = D == 64 || (D == 128 && E4M3) ? 32 : 16;

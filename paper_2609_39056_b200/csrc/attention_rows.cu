@@ -154,7 +154,7 @@ __device__ __forceinline__ uint64_t exp2_pair(uint64_t x) {
     return pair(exp2_approx(v.x), exp2_approx(v.y));
 }
 // Two probabilities as bf16 hi + lo without a conversion instruction: those share a pipe of a sixteenth of a warp per clock with the exponentials, and that pipe bounded
-// this pass (64 probabilities a thread 2300 -> SPLIT_CLK clocks).  x (2^16 + 1) - (x (2^16 + 1) - x) is x rounded to 8 bits (Dekker's splitting, Numer. Math. 18, 1971), what is
+// this pass (64 probabilities a thread 2300 -> 1500 clocks).  x (2^16 + 1) - (x (2^16 + 1) - x) is x rounded to 8 bits (Dekker's splitting, Numer. Math. 18, 1971), what is
 // left is exact, and its upper half is its bf16 number cut off: |x - hi - lo| < 2^-15 x.
 __device__ __forceinline__ void split_bf16(uint64_t x, uint32_t& hi, uint32_t& lo) {
     const uint64_t neg = pair(-1.0f, -1.0f);
@@ -267,7 +267,9 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Par
         // ---------------------------------------------------------------------------------------- softmax and output, a set of warps for each tile of rows
         // Rows of shared prefixes: each sees every key of its item.  A set has its own scores, probabilities (over them), O and counts of what it did; the two run at
         // their own pace, so that the products of one fall under the softmax of the other.  In one tile of rows the two sets wait for the same products:
-        // 16 heads x 512 rows x 4416 keys PAIR_US us.
+        // 16 heads x 512 rows x 4416 keys 56 -> 48 us (a tile of 256 rows x 128 keys
+        // 5700 clocks, one of 128 rows 3600; of the 48 us 14 are the start: place of the run, queries, and code that comes from L2 for the first time).  Tried without gain:
+        // issuing whatever product is ready by polling (8200 clocks a tile); one pass with the maximum checked 32 keys at a time (52 us).
         const int set = warp >> 2, quad = warp & 3;
         const int row = 128 * set + 32 * quad + lane;
         const uint32_t lanes = static_cast<uint32_t>(32 * quad) << 16;
@@ -305,8 +307,7 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Par
                     const float gone = f < 0.0f ? INFINITY : -INFINITY;
                     float fs = f;
                     if (edge && f == 0.0f) fs = 1.0f;      // (a factor of zero makes no -infinity: scores of zero with a factor of one)
-                    constexpr int TOGETHER = E4M3 ? 1 : 2;                         // (with E4M3 there are 14 warps, and 128 registers a thread)
-                    uint32_t x[TOGETHER][32];
+                    uint32_t x[32];
                     auto load = [&](int c, uint32_t (&to)[32]) { tmem_ld_32x32b_x32(s_t + 32 * c, to); };
                     auto cut = [&](int c, uint32_t (&to)[32]) {
                         if (edge) {
@@ -326,15 +327,11 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Par
                     };
                     // pass 1: the maximum of s f
 #pragma unroll 1                                           // (four times the code costs more at the start, instruction by instruction from L2, than it saves later)
-                    for (int c = 0; c < KT / 32; c += TOGETHER) {
-#pragma unroll
-                        for (int i = 0; i < TOGETHER; ++i) load(c + i, x[i]);
+                    for (int c = 0; c < KT / 32; ++c) {
+                        load(c, x);
                         tmem_wait_ld();
-#pragma unroll
-                        for (int i = 0; i < TOGETHER; ++i) {
-                            cut(c + i, x[i]);
-                            most(x[i]);
-                        }
+                        cut(c, x);
+                        most(x);
                     }
                     float mx = fmaxf(fmaxf(q[0], q[1]), fmaxf(q[2], q[3]));
                     mx = mx == -INFINITY ? mx : mx * fabsf(f) - C::TOP;
@@ -379,10 +376,10 @@ __global__ void __launch_bounds__(C::THREADS, 1) attention_rows_kernel(const Par
                     };
 #pragma unroll 1
                     for (int c = 0; c < KT / 32; ++c) {
-                        load(c, x[0]);
+                        load(c, x);
                         tmem_wait_ld();
-                        cut(c, x[0]);
-                        weigh(c, x[0]);
+                        cut(c, x);
+                        weigh(c, x);
                     }
                     const float2 z = unpair(l01);
                     l += z.x + z.y;

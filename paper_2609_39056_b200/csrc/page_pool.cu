@@ -278,8 +278,17 @@ __global__ void __launch_bounds__(PP_THREADS) page_pool_kernel(const PagePoolArg
     const int p0 = static_cast<int>(min(static_cast<long long>(a.n_pages), static_cast<long long>(rank) * slice)), p1 = min(a.n_pages, p0 + min(slice, a.n_pages - p0));
     auto counts = [&](int x) { return COMPACT ? x >= 0 : x == 0; };
     int mine = 0, total;
-    for (int p = p0 + tid; p < p1; p += PP_THREADS) mine += counts(__ldcg(mark + p));
-    block_prefix<PP_THREADS>(mine, total);
+    // (a slice of one tile stays in registers, in the order in which it is written below)
+    const bool one = slice == PP_TILE;
+    bool kept[PP_EACH];
+#pragma unroll
+    for (int e = 0; e < PP_EACH; ++e) {
+        const int p = p0 + tid * PP_EACH + e;
+        kept[e] = one && p < p1 && counts(__ldcg(mark + p));
+        mine += kept[e];
+    }
+    for (int p = one ? p1 : p0 + tid; p < p1; p += PP_THREADS) mine += counts(__ldcg(mark + p));
+    const int in_front = block_prefix<PP_THREADS>(mine, total);    // (of this thread's pages, in a slice of one tile)
     if (tid < ctas) store_remote(s_sums, rank, tid, total);
     pool_sync();
     int before = 0, all = 0;
@@ -302,11 +311,11 @@ __global__ void __launch_bounds__(PP_THREADS) page_pool_kernel(const PagePoolArg
         int n = 0;
 #pragma unroll
         for (int e = 0; e < PP_EACH; ++e) {
-            hit[e] = first + e < p1 && counts(__ldcg(mark + first + e));
+            hit[e] = one ? kept[e] : first + e < p1 && counts(__ldcg(mark + first + e));
             n += hit[e];
         }
-        int in_tile;
-        int at = before + block_prefix<PP_THREADS>(n, in_tile);    // those in front of page `first`
+        int in_tile = 0;
+        int at = before + (one ? in_front : block_prefix<PP_THREADS>(n, in_tile));                 // those in front of page `first`
         before += in_tile;
 #pragma unroll
         for (int e = 0; e < PP_EACH; ++e) {
