@@ -456,7 +456,7 @@ rudder_status rudder_page_copy(const rudder_page_copy_args* args, const rudder_p
 typedef struct {
     const int32_t* page_table;   /* [B, ld_table] */
     int64_t ld_table;
-    int max_pages;
+    int max_pages;               /* columns, <= ld_table, up to 2^30 */
     int32_t* lens;               /* [B], in and out */
     int B;                       /* 1..2^20 */
     int page_size;
@@ -476,7 +476,7 @@ rudder_status rudder_page_release(const rudder_page_release_args* args, void* st
 typedef struct {
     const int32_t* page_table;   /* [B, ld_table] */
     int64_t ld_table;
-    int max_pages;
+    int max_pages;               /* columns, <= ld_table, up to 2^30 */
     const int32_t* lens;         /* [B] */
     int B;                       /* 1..2^20 */
     int page_size;

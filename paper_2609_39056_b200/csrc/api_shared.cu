@@ -103,7 +103,9 @@ rudder_status rudder_page_release(const rudder_page_release_args* a, void* strea
 {
     if (!a || !a->page_table || !a->lens || !a->refs || !a->free_pages || !a->n_free || a->n_drop < 0 || (a->n_drop > 0 && !a->drop)) return RUDDER_ERR_ARG;
     const int shift = page_shift_of(a->page_size);
-    if (shift < 0 || a->B < 1 || a->B > kMaxRows || a->max_pages < 1 || a->ld_table < a->max_pages || a->n_pages < 1 || a->n_pages > kMaxPages) return RUDDER_ERR_SHAPE;
+    if (shift < 0 || a->B < 1 || a->B > kMaxRows || a->max_pages < 1 || a->max_pages > kMaxPages || a->ld_table < a->max_pages || a->n_pages < 1 ||
+        a->n_pages > kMaxPages)
+        return RUDDER_ERR_SHAPE;
     PagePoolArgs p = {};
     p.table = a->page_table; p.ld_table = a->ld_table; p.max_pages = a->max_pages; p.B = a->B; p.lens = a->lens; p.page_shift = shift; p.n_pages = a->n_pages;
     p.drop = a->drop; p.n_drop = a->n_drop; p.refs = a->refs; p.free_pages = a->free_pages; p.n_free = a->n_free;
@@ -114,7 +116,7 @@ rudder_status rudder_page_compact(const rudder_page_compact_args* a, const rudde
 {
     if (!a || !a->page_table || !a->lens || !a->new_table || !a->remap || !a->n_copies || !a->n_live || (a->n_pages > 1 && !a->copies)) return RUDDER_ERR_ARG;
     const int shift = page_shift_of(a->page_size);
-    if (shift < 0 || a->B < 1 || a->B > kMaxRows || a->max_pages < 1 || a->ld_table < a->max_pages || a->ld_new < a->max_pages || a->n_pages < 1 || a->n_pages > kMaxPages ||
+    if (shift < 0 || a->B < 1 || a->B > kMaxRows || a->max_pages < 1 || a->max_pages > kMaxPages || a->ld_table < a->max_pages || a->ld_new < a->max_pages || a->n_pages < 1 || a->n_pages > kMaxPages ||
         (a->new_table == a->page_table && a->ld_new != a->ld_table))
         return RUDDER_ERR_SHAPE;
     PageCopyArgs c = {};

@@ -313,6 +313,20 @@ class Shared(Attention):
         return glue.bf16_to_f32(bf16_to_np(O[:M, :width])).astype(np.float64).reshape(M, self.heads, self.D), lse[:M].cpu().numpy().astype(np.float64)
 
 
+    def check_far_apart(self, o, lse, causal):
+        """check() for scores far apart.  An E4M3 cache's probabilities are f16 numbers: below 2^-25 of the row's largest (which is at most 1) they are off by up to
+        2^-36 of it each, so a channel in which every larger one meets a value of zero may be off by (number of keys) 2^-36 max |v|."""
+        q = glue.bf16_to_f32(self.qb).astype(np.float64).reshape(-1, self.heads, self.D)
+        ep, at = (2.0 ** -15 if self.fmt == "bf16" else 2.0 ** -10), 0
+        for b, n in enumerate(self.q_lens):
+            wo, wl_, a, ds = paged.attention(q[at:at + n], self.k[b], self.v[b], self.scale, causal)
+            es = ds * (self.D + 4) * 2 * U
+            floor = 0.0 if self.fmt == "bf16" or not self.lens[b] else self.lens[b] * 2.0 ** -36 * np.abs(self.v[b]).max()
+            assert (np.abs(o[at:at + n] - wo) <= 2.0 ** -8 * np.abs(wo) + a * (2 * es[..., None] + ep + 2.0 ** -18) + floor + 1e-38).all(), b
+            assert (np.abs(lse[at:at + n] - wl_) <= es + 2.0 ** -20 * (1 + np.abs(wl_)) + self.lens[b] * U).all(), b
+            at += n
+
+
 def same(n, own, q):
     return [(own, q)] * n
 
@@ -447,6 +461,42 @@ def test_shared_captured_follows_the_lengths(rd, heads, kv, T, fmt):
                 a.check(got, l1, True)
             if p == [700, 333]:
                 assert torch.equal(O, want)
+    status_clean(rd)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("scale", [3.0, -3.0, 0.0, -0.05])
+@pytest.mark.parametrize("heads,kv,D,n,T,prefix", [(2, 2, 128, 20, 16, 900), (4, 1, 64, 9, 20, 700), (4, 2, 128, 9, 1, 900), (2, 1, 256, 7, 20, 300), (16, 1, 64, 6, 1, 500), (2, 2, 128, 3, 40, 400)])
+def test_shared_scales_of_any_sign(rd, heads, kv, D, n, T, prefix, scale, fmt):
+    """Large scores, whose running maximum is raised again and again, and factors below and at zero, on every kernel of either pass."""
+    rng = np.random.default_rng(n)
+    a = Shared(rd, [(prefix, [(int(rng.integers(T, T + 90)), T) for _ in range(n)]), (prefix // 3, same(2, T + 3, T))], heads, kv, D, 16, fmt, seed=n)
+    a.scale = scale
+    o, lse = a.run_shared(True)
+    a.check_far_apart(o, lse, True)
+    status_clean(rd)
+
+
+@pytest.mark.parametrize("T", [1, 40])
+def test_shared_far_pages(rd, T):
+    """Pages behind 2^31 elements and 2^32 bytes: attention, and a copy between them."""
+    page, kv, D = 64, 8, 128
+    n_pages = int(2.8e9) // (page * kv * D) + 1
+    a = Attention(rd, [333, 320, 330], [T, T, T], 8, kv, D, page, "bf16", seed=4, far=n_pages)
+    for b in (1, 2):
+        a.table[b, :3] = a.table[0, :3]
+        for store in (a.k, a.v):
+            store[b][:192] = store[0][:192]
+    a.run(True)
+    attn = a.args
+    a.O.fill_(7.0)
+    rd.rudder_attention_shared(rd.SharedAttentionArgs(attn, i32([0, 3]), i32([192]), i32([2]), 3 * T))
+    a.check(glue.bf16_to_f32(bf16_to_np(a.O)).astype(np.float64).reshape(3 * T, 8, D), a.lse.cpu().numpy().astype(np.float64), True)
+    src, dst = n_pages - 1, n_pages - 9
+    a.vc[src] = torch.randn((kv, page, D), device="cuda").to(torch.bfloat16)
+    a.vc[dst] = 1.0
+    rd.rudder_page_copy(rd.PageCopyArgs(i32([[src, dst, 50]])), rd.PagedCaches([a.cache]))
+    assert torch.equal(a.vc[dst, :, :50], a.vc[src, :, :50]) and (a.vc[dst, :, 50:] == 1.0).all().item()
     status_clean(rd)
 
 

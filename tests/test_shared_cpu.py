@@ -65,14 +65,14 @@ def test_fork_refusals(rd, kw, want):
 
 @pytest.mark.parametrize("kw,want", COMMON + [
     (dict(refs=None), "ARG"), (dict(free_pages=None), "ARG"), (dict(n_free=None), "ARG"), (dict(drop=None), "ARG"), (dict(n_drop=-1), "ARG"), (dict(n_pages=0), "SHAPE"),
-    (dict(n_pages=(1 << 30) + 1), "SHAPE"), (dict(B=(1 << 20) + 1), "SHAPE")])
+    (dict(n_pages=(1 << 30) + 1), "SHAPE"), (dict(B=(1 << 20) + 1), "SHAPE"), (dict(max_pages=(1 << 30) + 1, ld_table=1 << 31), "SHAPE")])
 def test_release_refusals(rd, kw, want):
     assert rd.lib().rudder_page_release(ctypes.byref(release_c(rd, **kw)), None) == want_of(rd, want)
 
 
 @pytest.mark.parametrize("kw,want", COMMON + [
     (dict(new_table=None), "ARG"), (dict(remap=None), "ARG"), (dict(copies=None), "ARG"), (dict(n_copies=None), "ARG"), (dict(n_live=None), "ARG"), (dict(n_pages=0), "SHAPE"),
-    (dict(ld_new=7), "SHAPE"), (dict(new_table=FAKE, ld_new=9), "SHAPE")])
+    (dict(ld_new=7), "SHAPE"), (dict(new_table=FAKE, ld_new=9), "SHAPE"), (dict(max_pages=(1 << 30) + 1, ld_table=1 << 31, ld_new=1 << 31), "SHAPE")])
 def test_compact_refusals(rd, kw, want):
     assert rd.lib().rudder_page_compact(ctypes.byref(compact_c(rd, **kw)), None, 0, None) == want_of(rd, want)
 
