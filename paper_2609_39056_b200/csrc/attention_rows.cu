@@ -33,7 +33,7 @@ namespace {
 enum RowsWhere { W_R_Q_EMPTY = 1001, W_R_KV_EMPTY = 1002, W_R_RAW_FULL = 1003, W_R_RAW_EMPTY = 1004, W_R_Q_FULL = 1101, W_R_KV_FULL = 1102, W_R_P_FULL = 1104, W_R_O_FREE = 1105,
                  W_R_S_FULL = 1201, W_R_PV_DONE = 1202, W_R_ML_FULL = 1203 };
 
-// PAIR: two tiles of 128 rows over the same keys, see pair_softmax.
+// PAIR: two tiles of 128 rows over the same keys, a set of softmax warps for each (prefixes that many rows share).
 template <int D_, bool E4M3_, bool PAIR_ = false>
 struct RowsCfg {
     static constexpr int D = D_;

