@@ -452,7 +452,8 @@ typedef struct {
 rudder_status rudder_page_copy(const rudder_page_copy_args* args, const rudder_paged_cache* caches, int n_caches, void* stream);
 
 /* rudder_page_release -- lens[drop[i]] = 0, then refs[p] = entries of page p that requests hold, free_pages = the pages with none in ascending
- * order, -1 behind the last, n_free = their number.  One launch; nothing is kept between calls, so it also makes the first free list. */
+ * order, -1 behind the last, n_free = their number.  One launch; nothing is kept between calls, so it also makes the first free list.  (A caller that does not read n_free may
+ * give all n_pages entries to the next call: rudder_page_fork takes a -1 for no page, with rudder_page_tables a token that meets one has slot -1.) */
 typedef struct {
     const int32_t* page_table;   /* [B, ld_table] */
     int64_t ld_table;
