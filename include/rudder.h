@@ -422,7 +422,7 @@ rudder_status rudder_block_cached(const rudder_block_args* args, const rudder_bl
  *     page_table[dst][j] = page_table[src][j], j < l / page_size,   page_table[dst][l / page_size] = free_pages[taken + children with such tokens before i]
  * and lens[dst] = l.  Left out (row and length as they were): a child whose dst is a source of the call or the dst of a child before it, whose rows or
  * lengths do not exist, or for which the free list has no page (an entry below 0 is none).  used = pages asked for.  Calling again with
- * the same inputs writes the same. */
+ * the same inputs writes the same.  lens, copies and used have no word in common with one another or with the arrays that are read (refused: RUDDER_ERR_ARG). */
 typedef struct {
     int32_t* page_table;         /* [B, ld_table], in and out */
     int64_t ld_table;

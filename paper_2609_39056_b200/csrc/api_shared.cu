@@ -48,6 +48,30 @@ rudder_status check_layers(const rudder_paged_cache* c, int n, int page_size, in
     return RUDDER_OK;
 }
 
+// What a kernel writes while other CTAs of it still read: no word in common.
+struct Words {
+    const int32_t* at;
+    size_t n;
+    bool meets(const Words& o) const
+    {
+        const uintptr_t a = reinterpret_cast<uintptr_t>(at), b = reinterpret_cast<uintptr_t>(o.at);
+        return at != nullptr && o.at != nullptr && a < b + o.n * sizeof(int32_t) && b < a + n * sizeof(int32_t);
+    }
+};
+bool fork_arrays_apart(const rudder_page_fork_args* a)
+{
+    const size_t n = static_cast<size_t>(a->n);
+    const Words out[] = {{a->lens, static_cast<size_t>(a->B)}, {a->copies, 3 * n}, {a->used, 1}};
+    const Words in[] = {{a->src, n}, {a->dst, n}, {a->fork_lens, n}, {a->free_pages, static_cast<size_t>(a->n_free)}, {a->taken, 1}};
+    for (int i = 0; i < 3; ++i) {
+        for (const Words& r : in)
+            if (out[i].meets(r)) return false;
+        for (int j = 0; j < i; ++j)
+            if (out[i].meets(out[j])) return false;
+    }
+    return true;
+}
+
 rudder_status ok_or_cuda(cudaError_t e) { return e == cudaSuccess ? RUDDER_OK : RUDDER_ERR_CUDA; }
 
 rudder_status check_shared_shape(const rudder_attention_shared_args* a)
@@ -80,7 +104,9 @@ rudder_status rudder_page_fork(const rudder_page_fork_args* a, const rudder_page
     PageForkArgs p = {};
     p.n_pages = 0x7fffffff;                                    // (without caches any page id is taken for one)
     rudder_status s = check_layers(caches, n_caches, a->page_size, a->n, &p.cache, &p.n_pages);
-    if (s != RUDDER_OK || (s = ensure_pool_init()) != RUDDER_OK) return s;
+    if (s != RUDDER_OK) return s;
+    if (!fork_arrays_apart(a)) return RUDDER_ERR_ARG;
+    if ((s = ensure_pool_init()) != RUDDER_OK) return s;
     p.table = a->page_table; p.ld_table = a->ld_table; p.max_pages = a->max_pages; p.B = a->B; p.lens = a->lens; p.page_shift = shift;
     p.src = a->src; p.dst = a->dst; p.fork_lens = a->fork_lens; p.n = a->n;
     p.free_pages = a->free_pages; p.n_free = a->n_free; p.taken = a->taken; p.copies = a->copies; p.used = a->used;
