@@ -426,7 +426,7 @@ rudder_status rudder_block_cached(const rudder_block_args* args, const rudder_bl
 typedef struct {
     int32_t* page_table;         /* [B, ld_table], in and out */
     int64_t ld_table;
-    int max_pages;               /* columns, <= ld_table */
+    int max_pages;               /* columns, <= ld_table, up to 2^30 */
     int32_t* lens;               /* [B], in and out */
     int B;                       /* 1..8192 */
     int page_size;

@@ -100,7 +100,7 @@ rudder_status rudder_page_fork(const rudder_page_fork_args* a, const rudder_page
 {
     if (!a || !a->page_table || !a->lens || !a->src || !a->dst || !a->used || a->n_free < 0 || (a->n_free > 0 && !a->free_pages)) return RUDDER_ERR_ARG;
     const int shift = page_shift_of(a->page_size);
-    if (shift < 0 || a->B < 1 || a->B > kMaxRequests || a->n < 1 || a->n > kMaxRequests || a->max_pages < 1 || a->ld_table < a->max_pages) return RUDDER_ERR_SHAPE;
+    if (shift < 0 || a->B < 1 || a->B > kMaxRequests || a->n < 1 || a->n > kMaxRequests || a->max_pages < 1 || a->max_pages > kMaxPages || a->ld_table < a->max_pages) return RUDDER_ERR_SHAPE;
     PageForkArgs p = {};
     p.n_pages = 0x7fffffff;                                    // (without caches any page id is taken for one)
     rudder_status s = check_layers(caches, n_caches, a->page_size, a->n, &p.cache, &p.n_pages);
