@@ -519,7 +519,7 @@ rudder_status rudder_attention_shared(const rudder_attention_shared_args* args, 
 typedef struct {
     const uint16_t* X;           /* bf16 [M, ldx] */
     int64_t ldx;
-    int M, K;                    /* K % 8 == 0 */
+    int M, K;                    /* K % 8 == 0; M, K and N up to 2^30 */
     const uint16_t* A;           /* bf16 [n_adapters][R][lda], adapters a_stride elements apart */
     int64_t a_stride, lda;
     const uint16_t* B;           /* bf16 [n_adapters][N][ldb] */

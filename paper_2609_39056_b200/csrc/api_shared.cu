@@ -7,7 +7,7 @@ using namespace rudder;
 
 namespace {
 
-constexpr int kMaxPages = 1 << 30, kMaxRows = 1 << 20;
+constexpr int kMaxPages = 1 << 30, kMaxRows = 1 << 20, kMaxSize = 1 << 30;
 
 bool g_pool_ready[64] = {false};
 
@@ -87,7 +87,8 @@ rudder_status check_shared_shape(const rudder_attention_shared_args* a)
 rudder_status check_lora_shape(const rudder_lora_args* a)
 {
     if (!a) return RUDDER_ERR_ARG;
-    if (a->M < 1 || a->K < 8 || a->K % 8 != 0 || a->N < 8 || a->N % 8 != 0 || a->R < 8 || a->R > kMaxRank || a->R % 8 != 0 || a->n_adapters < 1 || a->n_adapters > kMaxAdapters)
+    // (2^30: the kernels step over rows, inputs and columns in 32 bits)
+    if (a->M < 1 || a->M > kMaxSize || a->K < 8 || a->K > kMaxSize || a->K % 8 != 0 || a->N < 8 || a->N > kMaxSize || a->N % 8 != 0 || a->R < 8 || a->R > kMaxRank || a->R % 8 != 0 || a->n_adapters < 1 || a->n_adapters > kMaxAdapters)
         return RUDDER_ERR_SHAPE;
     return RUDDER_OK;
 }
