@@ -514,7 +514,8 @@ rudder_status rudder_attention_shared(const rudder_attention_shared_args* args, 
 /* rudder_lora -- low-rank adapters beside a shared projection (whose output is `base`), a = adapters[m] for every row m:
  *     Y_m = bf16( base_m + scales[a] sum_{r < ranks[a]} (sum_k x_mk A_a[r][k]) B_a[.][r] ),    Y_m = base_m where a is -1
  * Sums fp32, the inner sum enters the outer one with 16 significant bits, one rounding at the end.  What A and B hold at and behind ranks[a] is never used, and
- * another row's numbers have no part in a row.  Y may be base (same leading dimension).  workspace: rudder_lora_workspace_bytes(args) bytes (from M, K, N, R and
+ * another row's numbers have no part in a row.  Infinite weights and inner sums give the infinities, or what is no number, of the formula (an inner sum below
+ * 2^-133 counts as zero).  Y may be base (same leading dimension).  workspace: rudder_lora_workspace_bytes(args) bytes (from M, K, N, R and
  * n_adapters alone), 256-byte aligned; calls that may overlap on the GPU need one each. */
 typedef struct {
     const uint16_t* X;           /* bf16 [M, ldx] */
