@@ -303,8 +303,8 @@ typedef struct {
  * free_pages in order:  need_b = pages(old + new) - pages(old),  first_b = sum_{i<b} need_i,
  *     page_table[b][pages(old_b) + j] = free_pages[first_b + j]            for j < need_b
  * starts[b] = sum_{i<b} new_i (starts[B] = all new tokens); token starts[b] + i has position old_b + i and its slot; the
- * capacity - starts[B] rows behind the last token get position and slot -1.  used = sum need_b (above n_free: exhausted -- the
- * tokens without a page get slot -1).  Other table entries are left as they were; calling again with the same inputs writes the same. */
+ * capacity - starts[B] rows behind the last token get position and slot -1.  used = sum need_b (above n_free, or an
+ * entry below 0 among those taken: exhausted -- the tokens without a page get slot -1).  Other table entries are left as they were; calling again with the same inputs writes the same. */
 typedef struct {
     const int32_t* old_lens;     /* [B] >= 0 */
     const int32_t* new_lens;     /* [B] >= 0 */
@@ -453,7 +453,7 @@ rudder_status rudder_page_copy(const rudder_page_copy_args* args, const rudder_p
 
 /* rudder_page_release -- lens[drop[i]] = 0, then refs[p] = entries of page p that requests hold, free_pages = the pages with none in ascending
  * order, -1 behind the last, n_free = their number.  One launch; nothing is kept between calls, so it also makes the first free list.  (A caller that does not read n_free may
- * give all n_pages entries to the next call: rudder_page_fork takes a -1 for no page, with rudder_page_tables a token that meets one has slot -1.) */
+ * give all n_pages entries to the next call: rudder_page_fork takes a -1 for no page, with rudder_page_tables a token that meets one has slot -1; both record 915.) */
 typedef struct {
     const int32_t* page_table;   /* [B, ld_table] */
     int64_t ld_table;

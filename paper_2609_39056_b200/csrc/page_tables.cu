@@ -93,8 +93,9 @@ __global__ void __launch_bounds__(PT_THREADS) page_tables_kernel(const PageTable
         const int b = owner(s_need, a.B, i);
         const int held = pages_of(min(max(a.old_lens[b], 0), kSumCap), a.page_shift);
         const long long col = static_cast<long long>(held) + (i - s_need[b]);
-        if (col < a.max_pages) a.table[static_cast<size_t>(b) * a.ld_table + col] = a.free_pages[i];
-        else record_bad_data(kNoPages);
+        const int page = a.free_pages[i];
+        if (col < a.max_pages) a.table[static_cast<size_t>(b) * a.ld_table + col] = page;
+        if (col >= a.max_pages || page < 0) record_bad_data(kNoPages);         // (below 0: behind the last free page of rudder_page_release's list)
     }
     // the tokens
     for (int t = gtid; t < a.capacity; t += gsize) {
