@@ -422,7 +422,8 @@ rudder_status rudder_block_cached(const rudder_block_args* args, const rudder_bl
  *     page_table[dst][j] = page_table[src][j], j < l / page_size,   page_table[dst][l / page_size] = free_pages[taken + children with such tokens before i]
  * and lens[dst] = l.  Left out (row and length as they were): a child whose dst is a source of the call or the dst of a child before it, whose rows or
  * lengths do not exist, or for which the free list has no page (an entry below 0 is none).  used = pages asked for.  Calling again with
- * the same inputs writes the same.  lens, copies and used have no word in common with one another or with the arrays that are read (refused: RUDDER_ERR_ARG). */
+ * the same inputs writes the same.  lens, copies and used have no word in common with one another or with the arrays that are read (refused: RUDDER_ERR_ARG).  rudder_page_tables
+ * takes pages from its list's first entry on: between a fork and it, make a new list (rudder_page_release). */
 typedef struct {
     int32_t* page_table;         /* [B, ld_table], in and out */
     int64_t ld_table;
@@ -436,9 +437,9 @@ typedef struct {
     int n;                       /* 1..8192 */
     const int32_t* free_pages;   /* [n_free]; may be NULL when n_free is 0 */
     int n_free;
-    const int32_t* taken;        /* [1] entries of the free list that are gone already (`used` of the call before), or NULL = 0 */
+    const int32_t* taken;        /* [1] entries of the free list that are gone already: the SUM of `used` of all calls since the list was made; or NULL = 0 */
     int32_t* copies;             /* [n, 3] out: page copied from, to (-1, -1 for none), tokens; or NULL */
-    int32_t* used;               /* [1] out */
+    int32_t* used;               /* [1] out: of this call alone */
 } rudder_page_fork_args;
 rudder_status rudder_page_fork(const rudder_page_fork_args* args, const rudder_paged_cache* caches, int n_caches, void* stream);
 

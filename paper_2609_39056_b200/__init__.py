@@ -678,7 +678,8 @@ def _layers(args, caches):
 class PageForkArgs:
     """Arguments of rudder_page_fork: int32 device tensors.  ``page_table`` [B, columns] and ``lens`` [B] are updated in place; child i is row
     ``dst[i]``, a copy of row ``src[i]`` up to ``fork_lens[i]`` tokens (None: all); pages come from ``free_pages`` behind the first ``taken[0]``
-    (None: 0); ``used`` [1] and ``copies`` [n, 3] (or None) are outputs."""
+    (None: 0), the sum of ``used`` of all calls since the list was made; ``used`` [1] (of this call alone) and ``copies`` [n, 3] (or None) are outputs, with memory of
+    their own."""
 
     def __init__(self, page_table, lens, page_size: int, src, dst, free_pages, used, fork_lens=None, taken=None, copies=None):
         n = src.numel()
