@@ -494,7 +494,7 @@ rudder_status rudder_page_compact(const rudder_page_compact_args* args, const ru
 
 /* rudder_attention_shared -- rudder_attention_paged for requests in groups whose first tokens lie in the same pages: requests group_starts[g] ..
  * group_starts[g + 1] - 1 share their first prefix_lens[g] tokens, which are read once for all of them, through row prefix_rows[g] of attn.page_table.  The
- * result is that of rudder_attention_paged to the rounding of fp32 sums (added in another order) and of probabilities (2^-15 here with a bf16 cache).  A request with a row that does not see the whole prefix (shorter, or more new tokens than it
+ * result is that of rudder_attention_paged to the rounding of fp32 sums (added in another order).  A request with a row that does not see the whole prefix (shorter, or more new tokens than it
  * has of its own under `causal`) reads all of its tokens through its own row of the table, as does a request of no group.  prefix_lens need not be a
  * multiple of the page size, and 0 is allowed; the requests' own rows of the table name the prefix's pages, too, or pages with the same tokens.
  * Groups do not overlap.  group_q, the most new tokens that a group has, chooses the kernel; a group with more is computed all the same.

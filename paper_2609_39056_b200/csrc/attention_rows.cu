@@ -155,7 +155,8 @@ __device__ __forceinline__ uint64_t exp2_pair(uint64_t x) {
 }
 // Two probabilities as bf16 hi + lo without a conversion instruction: those share a pipe of a sixteenth of a warp per clock with the exponentials, and that pipe bounded
 // this pass (64 probabilities a thread 2300 -> 1500 clocks).  x (2^16 + 1) - (x (2^16 + 1) - x) is x rounded to 8 bits (Dekker's splitting, Numer. Math. 18, 1971), what is
-// left is exact, and its upper half is its bf16 number cut off: |x - hi - lo| < 2^-15 x.
+// left is exact, and the upper half of its bits plus half a step is its bf16 number: |x - hi - lo| <= 2^-17 x.  (Cut off instead it is 2^-16: 32 requests of 16 rows x
+// 16 heads over 4416 shared tokens 68.0 instead of 68.3 us, D = 64 43.0 instead of 44.3.)
 __device__ __forceinline__ void split_bf16(uint64_t x, uint32_t& hi, uint32_t& lo) {
     const uint64_t neg = pair(-1.0f, -1.0f);
     const uint64_t c = mul2(x, pair(65537.0f, 65537.0f));
@@ -163,7 +164,7 @@ __device__ __forceinline__ void split_bf16(uint64_t x, uint32_t& hi, uint32_t& l
     const uint64_t h = fma2(d, neg, c), l = fma2(h, neg, x);
     const float2 hv = unpair(h), lv = unpair(l);
     hi = __byte_perm(__float_as_uint(hv.x), __float_as_uint(hv.y), 0x7632);
-    lo = __byte_perm(__float_as_uint(lv.x), __float_as_uint(lv.y), 0x7632);
+    lo = __byte_perm(__float_as_uint(lv.x) + 0x8000u, __float_as_uint(lv.y) + 0x8000u, 0x7632);
 }
 
 template <class C, bool SHARED>
