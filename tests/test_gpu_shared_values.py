@@ -1,4 +1,4 @@
-"""rudder_attention_shared, on the GPU: the precision of the probabilities."""
+"""rudder_attention_shared, on the GPU: values that are infinite or no numbers among the new tokens, and the precision of the probabilities."""
 import numpy as np
 import pytest
 import torch
@@ -6,9 +6,51 @@ import torch
 from helpers import bf16_to_np
 from oracle import glue
 from test_gpu_paged import rd, status_clean  # noqa: F401  (rd: the fixture)
-from test_gpu_shared import i32
+from test_gpu_shared import Shared, i32
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "e4m3"])
+@pytest.mark.parametrize("prefix,own,n,heads,kv,D", [
+    (320, [5, 40, 300], 3, 2, 2, 128), (1000, [9, 3000, 77], 9, 4, 2, 64), (129, [2500, 7, 20], 7, 6, 2, 256), (700, [20, 257, 64], 20, 1, 1, 64), (777, [70, 128, 1700], 70, 2, 2, 128),
+    (333, [9000, 41], 40, 1, 1, 128), (64, [131, 33, 5000], 33, 2, 1, 256), (500, [5, 6, 60] * 12, 5, 8, 1, 64), (17, [4, 4], 4, 1, 1, 128), (0, [30, 300], 6, 2, 1, 64)])
+def test_what_a_row_does_not_see_does_not_reach_it(rd, prefix, own, n, heads, kv, D, fmt):
+    """Not a number or infinite among the new tokens' own keys and values: rows in front of that token keep their bits, rows that see it get it in its channels alone."""
+    a = Shared(rd, [(prefix, [(t, n) for t in own])], heads, kv, D, 16, fmt, seed=n)
+    lens = a.lens
+    clean, lse = a.run_shared(True)
+    a.check(clean, lse, True)
+    clean, lse = clean.reshape(len(lens), n, heads, D), lse.reshape(len(lens), n, heads)
+    if fmt == "bf16":
+        bits, poison = torch.int16, [(float("nan"), 0x7FC0, "v"), (float("inf"), 0x7F80, "v"), (-float("inf"), 0xFF80 - 0x10000, "v"), (float("nan"), 0x7FC0, "k")]
+    else:
+        bits, poison = torch.uint8, [(float("nan"), 0x7F, "v"), (float("nan"), 0xFF, "k")]
+    for back, (value, code, which) in zip((2, 1, n // 2, 3), poison):          # the key `back` before the end
+        cache = (a.vc if which == "v" else a.kc).view(bits)
+        saved = []
+        for b, length in enumerate(lens):
+            key = length - back
+            pg, pl = int(a.table[b, key // 16]), key % 16
+            saved.append((pg, pl, cache[pg, :, pl].clone()))
+            cache[pg, :, pl, 0::2] = code
+        o, l = a.run_shared(True)
+        o, l = o.reshape(clean.shape), l.reshape(lse.shape)
+        for b, length in enumerate(lens):
+            for t in range(n):
+                if length - back > length - n + t:                 # not seen
+                    assert np.array_equal(o[b, t], clean[b, t]) and np.array_equal(l[b, t], lse[b, t]), (b, t, back)
+                elif which == "k":
+                    assert np.isnan(o[b, t]).all() and np.isnan(l[b, t]).all(), (b, t)
+                else:
+                    assert np.array_equal(o[b, t][:, 1::2], clean[b, t][:, 1::2]) and np.array_equal(l[b, t], lse[b, t]), (b, t)
+                    even = o[b, t][:, 0::2]
+                    assert (np.isnan(even) if np.isnan(value) else (even == value) | np.isnan(even)).all(), (b, t, back)
+        for pg, pl, x in saved:
+            cache[pg, :, pl] = x
+    again, _ = a.run_shared(True)
+    assert np.array_equal(again.reshape(clean.shape), clean)
+    status_clean(rd)
 
 
 def key_of(s):
