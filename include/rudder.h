@@ -497,7 +497,8 @@ rudder_status rudder_page_compact(const rudder_page_compact_args* args, const ru
  * result is that of rudder_attention_paged to the rounding of fp32 sums (added in another order).  A request with a row that does not see the whole prefix (shorter, or more new tokens than it
  * has of its own under `causal`) reads all of its tokens through its own row of the table, as does a request of no group.  prefix_lens need not be a
  * multiple of the page size, and 0 is allowed; the requests' own rows of the table name the prefix's pages, too, or pages with the same tokens.
- * Groups do not overlap.  group_q, the most new tokens that a group has, chooses the kernel; a group with more is computed all the same.
+ * Groups do not overlap.  (Rows of requests where q_starts or group_starts descend, recorded as 912, are not defined.)  It pays where much need not be read again, (requests - 1) x prefix of every key-value head: from 100 to 150 MB of a bf16 cache and 100 to 500 MB of an E4M3 one on; below
+ * that rudder_attention_paged is mostly faster.  group_q, the most new tokens that a group has, chooses the kernel; a group with more is computed all the same.
  * M x heads / cache heads up to 2^20.  workspace: rudder_attention_shared_workspace_bytes(args) bytes (from M, heads, max_q, group_q, max_pages and the
  * cache's shape alone), 256-byte aligned, contents irrelevant; calls that may overlap on the GPU need one each.  Results do not depend on timing. */
 typedef struct {

@@ -17,9 +17,10 @@ constexpr float kLn2 = 0.6931471805599453f;
 
 // Requests in groups that share a prefix: the prefixes are a pass in which a GROUP stands in a request's place (its rows are those of all its requests, its
 // keys the prefix) and whose rows end as parts in `base`; what stands behind the prefixes is a second pass that joins these parts to its own.  A prefix is read once for its
-// group this way, and its rows fill the tensor core's tiles.  Measured: 32 requests of 16 rows x 16 heads over 4416 shared and up to 80 own tokens 70 us (the prefixes 48, the join
-// of their parts 8, the second pass 17), 64 requests over four prefixes of 17k to 28k tokens in E4M3, 8 key-value heads, 175 us (132, 7, 33); one by one the requests of the
-// second would read 1.4 million keys instead of 88 thousand and those behind them.
+// group this way, and its rows fill the tensor core's tiles.  Measured: 32 requests of 16 rows x 16 heads over 4416 shared and up to 80 own tokens 69 us (the prefixes 47, the join
+// of their parts 8, the second pass 16), 64 requests over four prefixes of 17k to 28k tokens in E4M3, 8 key-value heads, 175 us (132, 7, 33); one by one, by
+// rudder_attention_paged, 198 and 553 us.  A few requests over a short prefix take longer this way (8 of one token over 320: 13.7 against 7.0 us): three launches, of which each waits for
+// the one in front.
 struct SharedPass {
     const int32_t* group_starts; const int32_t* prefix_lens; const int32_t* prefix_rows;
     int n_groups, table_rows, requests;
@@ -276,11 +277,11 @@ struct Cursor {
     }
 };
 
-// Row `r` of an item whose rows begin at row0: its place in base_o and base_ml.
 __device__ __forceinline__ bool shared_prefixes(const AttnParams&) { return false; }
 __device__ __forceinline__ bool shared_prefixes(const SharedParams& p) { return p.sh.prefixes != 0; }
 // The start of a pass in a chain of early launches.  The prefixes' pass lets the next launch begin only when everything in front of the call is complete; so the
-// pass behind it (and what may come between them) begins while prefixes are still read, and waits for them in front of its first output.
+// pass behind it (and what may come between them) may begin while prefixes are still read, and waits for them in front of its first output.  It begins where its CTAs find room: beside
+// those of the kernel for few rows.  The kernel for many rows takes all registers of an SM (12 x 32 threads x 168), so behind that one it begins beside the join, 3 us after the prefixes.
 __device__ __forceinline__ void start_pass(const AttnParams&) {
     pdl_launch_dependents();
     pdl_wait();
@@ -289,6 +290,7 @@ __device__ __forceinline__ void start_pass(const SharedParams& p) {
     if (p.sh.prefixes) pdl_wait();
     pdl_launch_dependents();
 }
+// Row `r` of an item whose rows begin at row0: its place in base_o and base_ml.
 __device__ __forceinline__ size_t prefix_row(const AttnParams& p, int row0, int h, int r) {
     const RowOf at = row_of(p, r);
     return static_cast<size_t>(row0 + at.token) * p.heads + h * p.group + at.head;

@@ -7,8 +7,8 @@
 // handed to the tensor core does not matter as long as both operands use the same one, so lane q takes 8 neighbours of each row: 16 bytes that the lane
 // itself copies to shared memory, as it will use them, several steps ahead (cp.async), without ldmatrix or a swizzle.
 //
-// Measured: 4416 rows, rank 64, 2048 -> 8192 50 us (floor 25: X, base and Y once), of which the sorting 8, shrink 12 and expand 30; 64 rows of 40 adapters of rank up to
-// 64, 2048 -> 6144 15.8 us (floor 4.5); one row of rank 16 4.7 us, two launches.  Expand issues in 44 % of its slots with 12 to 16 warps to an SM: the products (hi and lo, 16 us
+// Measured: 4416 rows, rank 64, 2048 -> 8192 49.4 us (floor 25: X, base and Y once), of which the sorting 8, shrink 13 and expand 29; 64 rows of 40 adapters of rank up to
+// 64, 2048 -> 6144 15.8 us (floor 4.5); one row of rank 16 4.9 us, two launches.  Expand issues in 51 % of its slots with 14 warps to an SM: the products (hi and lo, 16 us
 // at the rate of mma.sync) and some 200 instructions for every 16 x 64 numbers of base and Y.
 //
 // Two launches: shrink writes h (a few KB, fp32) and expand reads it; the second is launched early, fetches base and B meanwhile and waits only for
@@ -27,7 +27,11 @@ namespace rudder {
 namespace {
 
 constexpr int kBadAdapter = 917;           // adapter at or beyond n_adapters (or below -1), or a rank outside 0..R
-constexpr int kWindowRows = 64;            // rows up to which they are taken as they lie
+// Rows up to which they are taken as they lie.  Measured, windows / sorted, us, inputs -> outputs and rank 2048 -> 6144 64; 2048 -> 8192 16; 1024 -> 4096 32; 2048 -> 2048 128:
+//   four adapters in turn   64 rows 12.6 / 17.3; 11.2 / 14.5; 7.7 / 12.3; 11.5 / 20.2    128 rows 20.0 / 19.2; 18.0 / 15.3; 11.0 / 12.7; 17.1 / 23.5    256 rows 35.2 / 22.8; 31.3 / 17.0; 18.3 / 13.8; 25.9 / 29.2
+//   forty                   64 rows 15.4 / 35.2; 13.1 / 30.3; 8.6 / 22.8; 15.4 / 36.4    128 rows 26.2 / 39.3; 20.9 / 31.4; 12.7 / 21.7; 24.5 / 39.9    256 rows 47.7 / 40.8; 36.4 / 32.6; 22.3 / 22.2; 36.8 / 42.2
+// Up to 96 rows windows won every case; the two cross between there and some hundreds of rows, later the more adapters there are and the larger the rank.  The bound lies in front of the crossing.
+constexpr int kWindowRows = 64;
 constexpr int kTileRows = 64;              // rows of a sorted tile
 constexpr int kSortThreads = 1024;
 constexpr int kNoTile = -2;

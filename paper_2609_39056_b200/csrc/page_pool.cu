@@ -15,7 +15,7 @@
 // changes nothing.  Compaction needs no counts, only a mark, and renames the tables in the same launch; its copies are a second one that reads their
 // number from the device.
 //
-// Measured: a fork of 8 children 4.8 us, of 64 over 12 layers (184 MB written) 46 to 50 us; release of 512 requests 9.4 us, of 9 4.1; the plan of a compaction of 48
+// Measured: a fork of 8 children 4.8 us, of 64 over 12 layers (184 MB written) 49.5 us; release of 512 requests 9.3 us, of 9 4.1; the plan of a compaction of 48
 // requests 19 us and its 452 MB of copies 73 us (6.2 TB/s, 95 % of a plain copy's rate).
 #include <algorithm>
 
@@ -26,8 +26,8 @@ namespace rudder {
 
 namespace {
 
-// Fork, copy: CTAs of 256 threads, eight for each SM although three fit at a time (the hardware hands out the rest as they end).  64 children x 12 layers 46 us, with CTAs of
-// 512 threads that stay 52; four CTAs at a time with 64 registers a thread 55, the eight pieces no longer in flight together.
+// Fork, copy: CTAs of 256 threads, eight for each SM although two fit at a time (the hardware hands out the rest as they end).  64 children x 12 layers 49.5 us, 452 MB of
+// a compaction's copies with their plan 91.6; with one CTA of 512 threads to an SM that stays 52.9 and 97.5, with four CTAs of 64 registers a thread at a time 45.3 and 93.9.
 constexpr int PF_THREADS = 256, PF_PER_SM = 8;
 constexpr int PP_THREADS = 1024;           // release, compact: CTAs of one cluster
 constexpr int PP_MAX_CTAS = 8;
